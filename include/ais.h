@@ -77,6 +77,7 @@ typedef enum ais_error {
 #define AIS_STATUS_BAD_TOKEN 1   /* evaluated row with token id outside [0, vocab)     */
 #define AIS_STATUS_BAD_CU    2   /* cu_rows not a non-decreasing partition of the rows */
 #define AIS_STATUS_LIVE_OVERFLOW 4 /* ais_lm_head_grad: more rows with a gradient than n_live_max */
+#define AIS_STATUS_BAD_ROW   8   /* ais_sample_tokens: a row without a distribution             */
 
 /* Hyper-parameters.  ais_params_default() fills in the paper's values:
  * C, delta, gamma, eps_std from App. "AIS hyperparameters"; clip_eps from the
@@ -346,12 +347,107 @@ int ais_lm_head_grad(ais_ctx* ctx, const void* hidden, long long hidden_stride, 
                      const float* coeff, float inv_temperature, long long chunk_vocab, long long n_live_max,
                      float* dhidden_out, float* dweight_out);
 
+/* ---- a 4-bit rollout: quantisation, read-out product, sampling ------------------------------------ */
+
+/* Rows in microscaled 4-bit floating point (MXFP4): the symmetric scaling of Eq. 1 (Sec. 2.1) with a scale for every 32
+ * elements instead of one for a row, the E2M1 value grid {0, .5, 1, 1.5, 2, 3, 4, 6} and powers of two as scales.  For the
+ * block x of 32 consecutive elements (the last one of a row may be shorter, its missing elements are 0):
+ *   e = max(floor(log2(max |x|)) - 2, -127)  (-127 for a block of zeros),   q = e2m1(x / 2^e)
+ * rounded to nearest, ties to even, saturating at 6; x stands for q 2^e.  With nb = ceil(width / 32) blocks a row:
+ *   x           [n_rows, row_stride] of `dtype`
+ *   codes_out   [n_rows, codes_stride] bytes, 16 nb of each row written: two codes (sign, then the grid's index) to a byte, the
+ *               element of the lower index in the lower half; missing elements are 0
+ *   scales_out  [n_rows, scales_stride] bytes, nb of each row written: e + 127 (E8M0), or 255 (NaN) for a block that holds a
+ *               NaN or an infinity
+ *   values_out  [n_rows, values_stride] of `dtype`, or NULL: what the codes stand for (exact in either type; NaN in a block
+ *               of scale 255), the weights that a straight-through gradient is taken at.  May be x itself (in place) with
+ *               values_stride == row_stride.
+ * codes_stride is a multiple of 16 bytes and scales_stride of 4, and the two arrays are aligned to that, as ais_mxfp4_logits
+ * wants them.
+ * Errors: NULL x / codes_out / scales_out (with n_rows > 0), n_rows < 0, width < 1 or >= 2^31 - 64, unknown dtype,
+ * row_stride or values_stride < width, codes_stride < 16 nb, scales_stride < nb (AIS_ERR_STRIDE), x, values_out, codes_out or
+ * scales_out misaligned, a stride of codes or scales that is not such a multiple (AIS_ERR_ALIGN). */
+int ais_mxfp4_quantize_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, long long width,
+                            long long row_stride, unsigned char* codes_out, long long codes_stride,
+                            unsigned char* scales_out, long long scales_stride, void* values_out,
+                            long long values_stride);
+
+/* Logits of the 4-bit policy (the W4A4 counterpart of the W8A8 rollout model of Sec. 2.1): the product of hidden states and
+ * output embedding, both in the form that ais_mxfp4_quantize_rows writes,
+ *   out[n, v] = sum_d hidden[n, d] weight[v, d]     (products exact, sums in fp32 on the matrix cores)
+ *   hidden_codes, hidden_scales   [n_rows, ...] bytes with their strides;  weight_codes, weight_scales   [vocab, ...]
+ *   width       elements of a row; ceil(width / 32) blocks of either operand are read
+ *   out         [n_rows, out_stride] of `out_dtype`, the first `vocab` elements of each row are written (bf16: rounded to
+ *               nearest even)
+ * A block of scale 255 makes every logit that it enters NaN.  One row at a time is the same call as many.
+ * Errors: NULL arrays (with n_rows > 0), n_rows < 0, vocab < 1, width < 1 or >= 2^31 - 64, a stride that does not hold the
+ * row's blocks (or out_stride < vocab), misaligned codes, scales or out or a stride that is not a multiple (16 bytes for
+ * codes, 4 for scales), unknown dtype. */
+int ais_mxfp4_logits(ais_ctx* ctx, const unsigned char* hidden_codes, long long hidden_codes_stride,
+                     const unsigned char* hidden_scales, long long hidden_scales_stride, long long n_rows,
+                     const unsigned char* weight_codes, long long weight_codes_stride,
+                     const unsigned char* weight_scales, long long weight_scales_stride, long long vocab,
+                     long long width, void* out, ais_dtype out_dtype, long long out_stride);
+
+/* The next token of each row and its log-probability (Alg. 1, "sample a group of responses" and the log pi_roll of its
+ * ratio), from logits and given random numbers.  A row's tokens are ranked by their logits, equal ones by their index.  With
+ * t = z / temperature and p = softmax(t), the kept tokens are the longest prefix of the ranking in which
+ *   - fewer than top_k tokens rank before each,
+ *   - the tokens that rank before each hold less than top_p of the mass of the first top_k,
+ *   - p >= min_p max p;
+ * the first one always is.  The drawn token is the arg-max over the kept of  t - log(noise[n, v]),  the lowest index on
+ * ties: with independent Exp(1) noise that is a draw from p restricted to the kept tokens.
+ *   logits      [n_rows, row_stride] of `dtype`, read only on rows with valid != 0
+ *   noise       [n_rows, noise_stride] fp32, of kept tokens alone.  Numbers outside [2^-126, 3e38] count as the nearest of
+ *               these, NaN as the largest.
+ *   valid       [n_rows] or NULL; rows with valid == 0 get token -1 and log-probs 0
+ *   temperature [n_rows] fp32 or NULL (all 1): 0 takes the first ranked token (greedy), with log-probs 0
+ *   top_k       [n_rows] int32 or NULL; top_k <= 0 is no limit
+ *   top_p       [n_rows] fp32 or NULL; top_p >= 1 is no limit, top_p <= 0 keeps the first token
+ *   min_p       [n_rows] fp32 or NULL; min_p <= 0 is no limit, min_p > 1 keeps the first token
+ *   token_out   [n_rows] int32
+ *   logp_out    [n_rows] fp32   log-prob of the drawn token among the kept ones: that of the policy that drew it
+ *   logp_full_out [n_rows] fp32 or NULL   its log softmax(t) over the whole vocabulary
+ * A logit of -inf is a token that cannot be drawn and does not count.  A row without a distribution (a NaN or +inf among its
+ * logits, nothing but -inf, a largest z / temperature beyond 2e38, a temperature that is negative or not finite, a NaN limit) gets token -1 and log-probs 0, and
+ * AIS_STATUS_BAD_ROW is set in the status word.
+ * Errors: as ais_token_logprob for the logits, NULL noise / token_out / logp_out (with n_rows > 0), noise_stride < vocab. */
+int ais_sample_tokens(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
+                      long long row_stride, const float* noise, long long noise_stride, const unsigned char* valid,
+                      const float* temperature, const int* top_k, const float* top_p, const float* min_p,
+                      int* token_out, float* logp_out, float* logp_full_out);
+
+/* ---- distillation from a teacher's top logits --------------------------------------------------------- */
+
+/* Divergence of the policy from a teacher of which the n_top largest logits of each row are known, and its gradient: the
+ * KL term of Eq. 19 with the teacher in the place of the reference policy and its expectation taken over the listed tokens
+ * instead of estimated from the sampled one.  With q = softmax over the row's listed tokens of inv_temperature teacher and
+ * p = softmax over the vocabulary of inv_temperature z,
+ *   kl[n] = sum_j q_j (log q_j - log p[id_j]),     loss = sum_n weight[n] kl[n]
+ *   dlogits[n, v] = weight[n] inv_temperature (p[v] - sum_j q_j 1[id_j = v])
+ *   logits      [n_rows, row_stride] of `dtype`, read only on rows with valid != 0
+ *   teacher_ids, teacher_logits   [n_rows, n_top] int32 and fp32, contiguous; an id of -1 is no entry (rows may list fewer
+ *               tokens), any other id outside [0, vocab) is left out and sets AIS_STATUS_BAD_TOKEN; an id listed twice counts
+ *               with both its entries
+ *   weight      [n_rows] fp32, or NULL: 1 / n_rows each
+ *   kl_out      [n_rows] fp32;  0 where valid == 0 or no entry has a finite logit
+ *   loss_out    one fp32 (the sum is taken in fp64, in a fixed order)
+ *   dlogits     [n_rows, dlogits_stride] of `dtype`, or NULL (loss alone); the first `vocab` elements of each row are written, 0
+ *               where kl_out is 0 for one of these reasons.  May be `logits` itself with dlogits_stride == row_stride.
+ * Errors: as ais_token_logprob for the logits; n_top < 1 or > 1024 (AIS_ERR_SIZE); NULL teacher_ids / teacher_logits / kl_out
+ * (with n_rows > 0) or loss_out; dlogits_stride < vocab; dlogits misaligned; inv_temperature <= 0 or not finite. */
+int ais_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
+                     long long row_stride, const int* teacher_ids, const float* teacher_logits, int n_top,
+                     const unsigned char* valid, const float* weight, float inv_temperature, float* kl_out,
+                     float* loss_out, void* dlogits, long long dlogits_stride);
+
 /* ---- measurement helpers -------------------------------------------------------------------- */
 
 /* Kernels whose device time can be read back. */
 typedef enum ais_kernel {
   AIS_K_LOGPROB = 0, AIS_K_DLOGITS = 1, AIS_K_COPY = 2, AIS_K_FP8_QUANT = 3, AIS_K_FP8_DEQUANT = 4,
-  AIS_K_FP8_LOGPROB = 5, AIS_K_FUSED = 6, AIS_K_LM_HEAD = 7, AIS_K_LM_HEAD_GRAD = 8, AIS_K_COUNT_ = 9
+  AIS_K_FP8_LOGPROB = 5, AIS_K_FUSED = 6, AIS_K_LM_HEAD = 7, AIS_K_LM_HEAD_GRAD = 8,
+  AIS_K_MXFP4_QUANT = 9, AIS_K_MXFP4_LOGITS = 10, AIS_K_SAMPLE = 11, AIS_K_DISTILL = 12, AIS_K_COUNT_ = 13
 } ais_kernel;
 
 /* With `enable` != 0 every launch of the kernels above is bracketed by HIP events on the

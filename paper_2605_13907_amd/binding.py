@@ -27,8 +27,10 @@ AIS_K_LOGPROB, AIS_K_DLOGITS, AIS_K_COPY, AIS_K_FP8_QUANT, AIS_K_FP8_DEQUANT, AI
 AIS_K_FUSED = 6
 AIS_K_LM_HEAD = 7
 AIS_K_LM_HEAD_GRAD = 8
+AIS_K_MXFP4_QUANT, AIS_K_MXFP4_LOGITS, AIS_K_SAMPLE, AIS_K_DISTILL = range(9, 13)
 AIS_STATUS_LIVE_OVERFLOW = 4
-STATUS_BAD_TOKEN, STATUS_BAD_CU = 1, 2
+STATUS_BAD_TOKEN, STATUS_BAD_CU, STATUS_BAD_ROW = 1, 2, 8
+MXFP4_BLOCK = 32            # elements that share a scale
 
 ERRORS = {
     0: "AIS_OK", -1: "AIS_ERR_NULL", -2: "AIS_ERR_SIZE", -3: "AIS_ERR_STRIDE", -4: "AIS_ERR_ALIGN",
@@ -87,6 +89,10 @@ SYMBOLS = {
     "ais_fp8_rollout_logprob": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _P]),
     "ais_lm_head_logprob": (_I, [_P, _P, _LL, _P, _LL, _I, _LL, _LL, _LL, _P, _P, _F, _P, _P]),
     "ais_lm_head_grad": (_I, [_P, _P, _LL, _P, _LL, _I, _LL, _LL, _LL, _P, _P, _P, _P, _F, _LL, _LL, _P, _P]),
+    "ais_mxfp4_quantize_rows": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _LL, _P, _LL, _P, _LL]),
+    "ais_mxfp4_logits": (_I, [_P, _P, _LL, _P, _LL, _LL, _P, _LL, _P, _LL, _LL, _LL, _P, _I, _LL]),
+    "ais_sample_tokens": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _LL, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "ais_distill_topk": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _I, _P, _P, _F, _P, _P, _P, _LL]),
     "ais_profile": (_I, [_P, _I]),
     "ais_profile_read": (_I, [_P, _I, C.POINTER(_F), C.POINTER(_I)]),
     "ais_copy": (_I, [_P, _P, _P, _LL]),
@@ -157,12 +163,12 @@ def default_params(**overrides) -> AisParams:
     return p
 
 
-def _dtype_code(t: torch.Tensor) -> int:
+def _dtype_code(t: torch.Tensor, name: str = "logits") -> int:
     if t.dtype == torch.bfloat16:
         return AIS_BF16
     if t.dtype == torch.float32:
         return AIS_F32
-    raise TypeError(f"logits must be bfloat16 or float32, not {t.dtype}")
+    raise TypeError(f"{name} must be bfloat16 or float32, not {t.dtype}")
 
 
 def _ptr(t: Optional[torch.Tensor], dtype=None, numel=None, name="tensor", device=None):
@@ -201,6 +207,22 @@ def _logits_geometry(logits: torch.Tensor, device: Optional[torch.device] = None
     n_rows, vocab = logits.shape
     row_stride = logits.stride(0) if n_rows > 1 else max(vocab, logits.stride(0))
     return n_rows, vocab, row_stride
+
+
+def _mxfp4_rows(codes: torch.Tensor, scales: torch.Tensor, device: torch.device, name: str):
+    """(rows, blocks, codes pointer and stride, scales pointer and stride) of an MXFP4 matrix."""
+    for what, t in ((f"{name}_codes", codes), (f"{name}_scales", scales)):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{what} must be a torch.Tensor")
+        if t.dtype != torch.uint8:
+            raise TypeError(f"{what}: expected torch.uint8, got {t.dtype}")
+        if t.dim() != 2 or t.stride(1) != 1 and t.shape[1] > 1:
+            raise ValueError(f"{what} must be 2-D with unit stride along its rows")
+    rows, blocks = scales.shape
+    if codes.shape != (rows, 16 * blocks):
+        raise ValueError(f"{name}_codes: expected {(rows, 16 * blocks)} bytes for the scales' blocks, got {tuple(codes.shape)}")
+    return (rows, blocks, _dev_ptr(codes, device, f"{name}_codes"), codes.stride(0) if rows > 1 else 16 * blocks,
+            _dev_ptr(scales, device, f"{name}_scales"), scales.stride(0) if rows > 1 else -(-blocks // 4) * 4)
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # not part of torch's public interface
@@ -480,6 +502,109 @@ class AisContext:
         if rc != 0:
             raise AisError(rc, "ais_fp8_rollout_logprob")
         return out
+
+    # ------------------------------------------------------------------ a 4-bit rollout
+    def mxfp4_quantize_rows(self, x, want_values: bool = False):
+        """x [R, D] bf16 or fp32 -> (codes [R, 16 nb], scales [R, nb]) uint8, nb = ceil(D / 32); with want_values also what
+        the codes stand for, [R, D] of x's dtype.  See ais_mxfp4_quantize_rows in include/ais.h."""
+        dev = self.device
+        n_rows, width, row_stride = _logits_geometry(x, dev, "x")
+        dtype = _dtype_code(x, "x")
+        blocks = -(-width // MXFP4_BLOCK)
+        codes = torch.empty((n_rows, 16 * blocks), dtype=torch.uint8, device=dev)
+        # rows of scales padded to whole groups of 16 blocks: every row begins at a whole word
+        scales = torch.empty((n_rows, -(-blocks // 16) * 16), dtype=torch.uint8, device=dev)
+        values = torch.empty((n_rows, width), dtype=x.dtype, device=dev) if want_values else None
+        self._sync_stream()
+        rc = self._lib.ais_mxfp4_quantize_rows(self._h, x.data_ptr(), dtype, n_rows, width, row_stride, _ptr(codes),
+                                               16 * blocks, _ptr(scales), scales.shape[1], _ptr(values), width)
+        if rc != 0:
+            raise AisError(rc, "ais_mxfp4_quantize_rows")
+        return (codes, scales[:, :blocks], values) if want_values else (codes, scales[:, :blocks])
+
+    def mxfp4_logits(self, hidden_codes, hidden_scales, weight_codes, weight_scales, dtype=torch.bfloat16):
+        """-> logits [R, V] of `dtype` (bfloat16 or float32): hidden states times output embedding, both as
+        mxfp4_quantize_rows returns them.  See ais_mxfp4_logits in include/ais.h."""
+        dev = self.device
+        n_rows, blocks, *hidden = _mxfp4_rows(hidden_codes, hidden_scales, dev, "hidden")
+        vocab, weight_blocks, *weight = _mxfp4_rows(weight_codes, weight_scales, dev, "weight")
+        if weight_blocks != blocks:
+            raise ValueError("hidden and weight disagree on the number of blocks")
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(f"logits must be bfloat16 or float32, not {dtype}")
+        out = torch.empty((n_rows, vocab), dtype=dtype, device=dev)
+        self._sync_stream()
+        rc = self._lib.ais_mxfp4_logits(self._h, *hidden, n_rows, *weight, vocab, MXFP4_BLOCK * blocks, _ptr(out),
+                                        _dtype_code(out), vocab)
+        if rc != 0:
+            raise AisError(rc, "ais_mxfp4_logits")
+        return out
+
+    def sample_tokens(self, logits, noise, valid=None, temperature=None, top_k=None, top_p=None, min_p=None):
+        """-> (tokens [R] int32, logp [R] fp32 of the policy that drew them, logp_full [R] fp32 over the whole vocabulary).
+        noise [R, V] fp32: independent Exp(1) numbers (torch's exponential_).  The limits are tensors of one value a row
+        (fp32, top_k int32), numbers for all rows, or None.  See ais_sample_tokens in include/ais.h."""
+        dev = self.device
+        n_rows, vocab, row_stride = _logits_geometry(logits, dev)
+        dtype = _dtype_code(logits)
+        noise_rows, noise_width, noise_stride = _logits_geometry(noise, dev, "noise")
+        if noise.dtype != torch.float32:
+            raise TypeError(f"noise: expected torch.float32, got {noise.dtype}")
+        if (noise_rows, noise_width) != (n_rows, vocab):
+            raise ValueError(f"noise: expected {(n_rows, vocab)}, got {(noise_rows, noise_width)}")
+
+        def each_row(value, kind, name):
+            if value is not None and not isinstance(value, torch.Tensor):
+                value = torch.full((n_rows,), value, dtype=kind, device=dev)
+            return value, _ptr(value, kind, n_rows, name, dev)
+
+        valid_ptr = _ptr(valid, torch.uint8, n_rows, "valid", dev)
+        limits = [each_row(temperature, torch.float32, "temperature"), each_row(top_k, torch.int32, "top_k"),
+                  each_row(top_p, torch.float32, "top_p"), each_row(min_p, torch.float32, "min_p")]
+        tokens = torch.empty(n_rows, dtype=torch.int32, device=dev)
+        logp = torch.empty(n_rows, dtype=torch.float32, device=dev)
+        full = torch.empty(n_rows, dtype=torch.float32, device=dev)
+        self._sync_stream()
+        rc = self._lib.ais_sample_tokens(self._h, logits.data_ptr(), dtype, n_rows, vocab, row_stride, noise.data_ptr(),
+                                         noise_stride, valid_ptr, *[p for _, p in limits], _ptr(tokens), _ptr(logp), _ptr(full))
+        if rc != 0:
+            raise AisError(rc, "ais_sample_tokens")
+        return tokens, logp, full
+
+    # ------------------------------------------------------------------ distillation
+    def distill_topk(self, logits, teacher_ids, teacher_logits, weight=None, valid=None, inv_temperature: float = 1.0,
+                     want_grad: bool = True, dlogits=None):
+        """-> (loss [1] fp32, kl [R] fp32, dlogits like logits or None): divergence of each row's policy from the teacher's
+        distribution over the listed tokens (teacher_ids [R, K] int32, -1 for no entry; teacher_logits [R, K] fp32), and the
+        gradient of sum_n weight[n] kl[n] (weight None: the mean).  Pass dlogits=logits to overwrite the logits in place.
+        See ais_distill_topk in include/ais.h."""
+        dev = self.device
+        n_rows, vocab, row_stride = _logits_geometry(logits, dev)
+        dtype = _dtype_code(logits)
+        if not isinstance(teacher_ids, torch.Tensor) or teacher_ids.dim() != 2 or teacher_ids.shape[0] != n_rows:
+            raise ValueError(f"teacher_ids must be a [{n_rows}, K] tensor")
+        n_top = teacher_ids.shape[1]
+        if not isinstance(teacher_logits, torch.Tensor) or teacher_logits.shape != teacher_ids.shape:
+            raise ValueError("teacher_logits must have the shape of teacher_ids")
+        ptrs = [_ptr(teacher_ids, torch.int32, n_rows * n_top, "teacher_ids", dev),
+                _ptr(teacher_logits, torch.float32, n_rows * n_top, "teacher_logits", dev)]
+        tail = [_ptr(valid, torch.uint8, n_rows, "valid", dev), _ptr(weight, torch.float32, n_rows, "weight", dev)]
+        if dlogits is not None:
+            if not isinstance(dlogits, torch.Tensor) or dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or \
+                    dlogits.stride() != logits.stride():
+                raise ValueError("dlogits must have the dtype, shape and strides of logits")
+            _dev_ptr(dlogits, dev, "dlogits")
+        elif want_grad:
+            dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=dev)
+        kl = torch.empty(n_rows, dtype=torch.float32, device=dev)
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        self._sync_stream()
+        rc = self._lib.ais_distill_topk(self._h, logits.data_ptr(), dtype, n_rows, vocab, row_stride, *ptrs, n_top, *tail,
+                                        float(inv_temperature), _ptr(kl), _ptr(loss),
+                                        None if dlogits is None else dlogits.data_ptr(), row_stride)
+        if rc != 0:
+            raise AisError(rc, "ais_distill_topk")
+        return loss, kl, dlogits
 
     # ------------------------------------------------------------------ log-probs without materialised logits
     def lm_head_logprob(self, hidden, weight, token_ids, valid=None, inv_temperature: float = 1.0):

@@ -215,6 +215,32 @@ int launch_fp8_rollout_logprob(ais_ctx* ctx, const void* logits, ais_dtype dtype
                                long long row_stride, const int* token_ids, const unsigned char* valid,
                                float* logp_out);
 
+int launch_mxfp4_quantize(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, int width, long long row_stride,
+                          unsigned char* codes, long long codes_stride, unsigned char* scales, long long scales_stride,
+                          void* values, long long values_stride);
+// The two operands of the 4-bit product.
+struct Mxfp4Rows {
+  const unsigned char* codes;
+  long long codes_stride;
+  const unsigned char* scales;
+  long long scales_stride;
+};
+int launch_mxfp4_logits(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks,
+                        void* out, ais_dtype out_dtype, long long out_stride);
+// The limits of each row that a token is drawn under (null: none for any row).
+struct SampleLimits {
+  const float* temperature;
+  const int* top_k;
+  const float* top_p;
+  const float* min_p;
+};
+int launch_sample_tokens(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, int vocab, long long row_stride,
+                         const float* noise, long long noise_stride, const unsigned char* valid, const SampleLimits& limits,
+                         int* token_out, float* logp_out, float* logp_full_out);
+int launch_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, int vocab, long long row_stride,
+                        const int* ids, const float* teacher, int n_top, const unsigned char* valid, const float* weight,
+                        float inv_temperature, float* kl_out, float* loss_out, void* dlogits, long long dlogits_stride);
+
 int launch_lm_head_grad_setup(ais_ctx* ctx, const unsigned char* live_mask, long long n_rows, int n_cap, int width,
                               int width_last, int* row_index, int* row_pos, void* dev_plan);
 int launch_lm_head_dlogits_chunk(ais_ctx* ctx, const void* hidden, long long ld_h, const void* weight,

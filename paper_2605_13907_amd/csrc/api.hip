@@ -132,6 +132,19 @@ int check_logits(const void* logits, ais_dtype dtype, long long n_rows, long lon
   return AIS_OK;
 }
 
+// Rows of MXFP4 codes and their scales: 16 bytes and one byte a block, read and written in words of 16 and 4 bytes.
+int check_mxfp4_rows(const unsigned char* codes, long long codes_stride, const unsigned char* scales,
+                     long long scales_stride, long long n_rows, long long width) {
+  if (width < 1 || width > 0x7fffffffLL - 64) return AIS_ERR_SIZE;
+  const long long blocks = (width + 31) / 32;
+  if (codes_stride < 16 * blocks || scales_stride < blocks) return AIS_ERR_STRIDE;
+  if (n_rows > 0 && (codes == nullptr || scales == nullptr)) return AIS_ERR_NULL;
+  if (codes_stride % 16 != 0 || scales_stride % 4 != 0 || reinterpret_cast<uintptr_t>(codes) % 16 != 0 ||
+      reinterpret_cast<uintptr_t>(scales) % 4 != 0)
+    return AIS_ERR_ALIGN;
+  return AIS_OK;
+}
+
 int check_params(const ais_params* p) {
   if (p == nullptr) return AIS_ERR_NULL;
   auto fin = [](float v) { return std::isfinite(v); };
@@ -646,6 +659,78 @@ int ais_lm_head_grad(ais_ctx* ctx, const void* hidden, long long hidden_stride, 
   if (elsewhere)
     return launch_lm_add_parts(ctx, dh_gathered, h_stride, parts.h, row_pos, n_rows, (int)d_model, dhidden_out);
   return AIS_OK;
+}
+
+int ais_mxfp4_quantize_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, long long width,
+                            long long row_stride, unsigned char* codes_out, long long codes_stride,
+                            unsigned char* scales_out, long long scales_stride, void* values_out,
+                            long long values_stride) {
+  int rc = check_logits(x, dtype, n_rows, width, row_stride);
+  if (rc != AIS_OK) return rc;
+  rc = check_mxfp4_rows(codes_out, codes_stride, scales_out, scales_stride, n_rows, width);
+  if (rc != AIS_OK) return rc;
+  if (values_out != nullptr) {
+    if (values_stride < width) return AIS_ERR_STRIDE;
+    if (reinterpret_cast<uintptr_t>(values_out) % (dtype == AIS_BF16 ? 2 : 4) != 0) return AIS_ERR_ALIGN;
+  }
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  return launch_mxfp4_quantize(ctx, x, dtype, n_rows, (int)width, row_stride, codes_out, codes_stride, scales_out,
+                               scales_stride, values_out, values_stride);
+}
+
+int ais_mxfp4_logits(ais_ctx* ctx, const unsigned char* hidden_codes, long long hidden_codes_stride,
+                     const unsigned char* hidden_scales, long long hidden_scales_stride, long long n_rows,
+                     const unsigned char* weight_codes, long long weight_codes_stride,
+                     const unsigned char* weight_scales, long long weight_scales_stride, long long vocab,
+                     long long width, void* out, ais_dtype out_dtype, long long out_stride) {
+  int rc = check_logits(out, out_dtype, n_rows, vocab, out_stride);
+  if (rc != AIS_OK) return rc;
+  rc = check_mxfp4_rows(hidden_codes, hidden_codes_stride, hidden_scales, hidden_scales_stride, n_rows, width);
+  if (rc != AIS_OK) return rc;
+  // an empty batch needs no embedding either
+  rc = check_mxfp4_rows(weight_codes, weight_codes_stride, weight_scales, weight_scales_stride, n_rows > 0 ? vocab : 0, width);
+  if (rc != AIS_OK) return rc;
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  return launch_mxfp4_logits(ctx, {hidden_codes, hidden_codes_stride, hidden_scales, hidden_scales_stride}, (int)n_rows,
+                             {weight_codes, weight_codes_stride, weight_scales, weight_scales_stride}, (int)vocab,
+                             (int)((width + 31) / 32), out, out_dtype, out_stride);
+}
+
+int ais_sample_tokens(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
+                      long long row_stride, const float* noise, long long noise_stride, const unsigned char* valid,
+                      const float* temperature, const int* top_k, const float* top_p, const float* min_p,
+                      int* token_out, float* logp_out, float* logp_full_out) {
+  int rc = check_logits(logits, dtype, n_rows, vocab, row_stride);
+  if (rc != AIS_OK) return rc;
+  if (noise_stride < vocab) return AIS_ERR_STRIDE;
+  if (n_rows > 0 && (noise == nullptr || token_out == nullptr || logp_out == nullptr)) return AIS_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(noise) % 4 != 0) return AIS_ERR_ALIGN;
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  return launch_sample_tokens(ctx, logits, dtype, n_rows, (int)vocab, row_stride, noise, noise_stride, valid,
+                              {temperature, top_k, top_p, min_p}, token_out, logp_out, logp_full_out);
+}
+
+int ais_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
+                     long long row_stride, const int* teacher_ids, const float* teacher_logits, int n_top,
+                     const unsigned char* valid, const float* weight, float inv_temperature, float* kl_out,
+                     float* loss_out, void* dlogits, long long dlogits_stride) {
+  int rc = check_logits(logits, dtype, n_rows, vocab, row_stride);
+  if (rc != AIS_OK) return rc;
+  if (n_top < 1 || n_top > 1024) return AIS_ERR_SIZE;
+  if (loss_out == nullptr) return AIS_ERR_NULL;
+  if (n_rows > 0 && (teacher_ids == nullptr || teacher_logits == nullptr || kl_out == nullptr)) return AIS_ERR_NULL;
+  if (dlogits != nullptr) {
+    if (dlogits_stride < vocab) return AIS_ERR_STRIDE;
+    if (reinterpret_cast<uintptr_t>(dlogits) % (dtype == AIS_BF16 ? 2 : 4) != 0) return AIS_ERR_ALIGN;
+  }
+  if (!std::isfinite(inv_temperature) || inv_temperature <= 0.f) return AIS_ERR_PARAM;
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  return launch_distill_topk(ctx, logits, dtype, n_rows, (int)vocab, row_stride, teacher_ids, teacher_logits, n_top, valid,
+                             weight, inv_temperature, kl_out, loss_out, dlogits, dlogits_stride);
 }
 
 int ais_profile(ais_ctx* ctx, int enable) {

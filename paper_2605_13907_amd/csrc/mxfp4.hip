@@ -1,0 +1,219 @@
+// Microscaled 4-bit floating point (MXFP4): rows of blocks of 32 E2M1 elements under one E8M0 scale, and the product of two
+// such matrices, which is the read-out of a 4-bit rollout policy.
+#include "ais_internal.h"
+#include "device_utils.h"
+
+namespace ais {
+namespace {
+
+using namespace dev;
+
+constexpr int kBlock = 32;             // elements under one scale
+constexpr int kUnit = 8;               // elements of a lane: four lanes share a block
+constexpr int kQuantThreads = 256;
+constexpr int kQuantUnits = 4;         // units that a lane works on
+
+// ---- quantisation ---------------------------------------------------------------------------------------------------
+// e = floor(log2 max|x|) - 2 comes from the exponent bits of the largest magnitude, compared as bit patterns: that order has
+// infinities and NaN at its top.  x 2^-e is exact, and so is q 2^e in either type, so the only rounding is the one to E2M1.
+// A lane holds 8 consecutive elements, and two exchanges inside a quad of lanes find the block's largest.
+// Bound by HBM: e R D bytes in, 17 bytes a block out, and e R D bytes where the values are asked for.
+
+template <typename T>
+__device__ __forceinline__ void load_unit(const T* p, int left, bool aligned, float* x) {
+  if (aligned && left >= kUnit) {
+    constexpr int N = Vec<T>::N;
+#pragma unroll
+    for (int k = 0; k < kUnit / N; ++k) Vec<T>::unpack(load_stream(reinterpret_cast<const u32x4*>(p) + k), x + k * N);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) x[k] = k < left ? Vec<T>::load1(p + k) : 0.f;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_unit(T* p, int left, bool aligned, const float* x) {
+  if (aligned && left >= kUnit) {
+    constexpr int N = Vec<T>::N;
+#pragma unroll
+    for (int k = 0; k < kUnit / N; ++k) store_stream(reinterpret_cast<u32x4*>(p) + k, Vec<T>::pack(x + k * N));
+  } else {
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k)
+      if (k < left) Vec<T>::store1(p + k, x[k]);
+  }
+}
+
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDppQuadXor1, 0xf, 0xf, true));
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDppQuadXor2, 0xf, 0xf, true));
+}
+
+template <typename T>
+__global__ __launch_bounds__(kQuantThreads) void mxfp4_quantize_kernel(
+    const T* x, long long row_stride, int width, int row_units, long long n_units, unsigned char* __restrict__ codes,
+    long long codes_stride, unsigned char* __restrict__ scales, long long scales_stride, T* values, long long values_stride,
+    int x_aligned, int values_aligned) {
+  const long long first = (long long)blockIdx.x * (kQuantThreads * kQuantUnits);
+  const long long row0 = first / row_units;
+  const uint32_t off0 = (uint32_t)(first - row0 * row_units);
+#pragma unroll
+  for (int k = 0; k < kQuantUnits; ++k) {
+    const uint32_t step = k * kQuantThreads + threadIdx.x;
+    if (first + step >= n_units) return;               // units come in fours: a quad of lanes leaves together
+    const uint32_t off = off0 + step;
+    const uint32_t down = off / (uint32_t)row_units;
+    const long long row = row0 + down;
+    const int unit = (int)(off - down * (uint32_t)row_units);
+    const int left = width - unit * kUnit;             // may be <= 0 in the last block
+    float v[kUnit];
+    load_unit(x + row * row_stride + (long long)unit * kUnit, left, x_aligned, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+    top = quad_max(top);
+    const bool finite = top < 0x7f800000u;
+    const int e = max((int)(top >> 23) - 2, 0);        // the scale's byte, exponent + 127
+    const float down_scale = __uint_as_float((uint32_t)(254 - e) << 23);
+    uint32_t word = 0;
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) v[j] *= down_scale;
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[0], v[1], 1.f, 0);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[2], v[3], 1.f, 1);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[4], v[5], 1.f, 2);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[6], v[7], 1.f, 3);
+    if (!finite) word = 0;
+    *reinterpret_cast<uint32_t*>(codes + row * codes_stride + (long long)unit * (kUnit / 2)) = word;
+    if ((unit & 3) == 0) scales[row * scales_stride + (unit >> 2)] = finite ? (unsigned char)e : (unsigned char)255;
+    if (values != nullptr) {
+      const float up = e > 0 ? __uint_as_float((uint32_t)e << 23) : __uint_as_float(1u << 22);   // 2^-127 is subnormal
+      const float scale = finite ? up : __builtin_nanf("");
+      const f32x2 q0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 0);
+      const f32x2 q1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 1);
+      const f32x2 q2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 2);
+      const f32x2 q3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.f, 3);
+      const float out[kUnit] = {q0[0] * scale, q0[1] * scale, q1[0] * scale, q1[1] * scale,
+                                q2[0] * scale, q2[1] * scale, q3[0] * scale, q3[1] * scale};
+      store_unit(values + row * values_stride + (long long)unit * kUnit, left, values_aligned, out);
+    }
+  }
+}
+
+// ---- product --------------------------------------------------------------------------------------------------------
+// out[t, v] = sum over blocks of 2^(ea + ew) sum_i a_i w_i: v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 rows of the
+// embedding with 16 tokens over four blocks and applies both scales.  A lane holds one block of one row: lane l that of row
+// l % 16, and which four blocks go together is free as long as both operands agree, so a lane takes blocks 4 (l / 16) + s of a
+// group of 16 in step s: 64 consecutive bytes of codes and one word of scales, whose byte s the instruction picks.
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kGroup = 16;             // blocks that four steps cover
+constexpr int kFp4 = 4;                // the instruction's code of the E2M1 format
+
+// A lane's share of a group of blocks: block b's codes at codes[b], its scale in byte b of `scale`; zeros beyond the row's end.
+struct Fragment {
+  i32x4 codes[4];
+  uint32_t scale;
+  __device__ __forceinline__ void load(const unsigned char* code_row, const unsigned char* scale_row, int block, int blocks) {
+    const int left = blocks - block;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      codes[s] = s < left ? *reinterpret_cast<const i32x4*>(code_row + 16LL * (block + s)) : i32x4{0, 0, 0, 0};
+    scale = 0;
+    if (left >= 4) {
+      scale = *reinterpret_cast<const uint32_t*>(scale_row + block);
+    } else {
+#pragma unroll
+      for (int s = 0; s < 3; ++s)
+        if (s < left) scale |= (uint32_t)scale_row[block + s] << (8 * s);
+    }
+  }
+};
+
+template <int S>
+__device__ __forceinline__ void multiply(f32x4& c, const Fragment& a, const Fragment& b) {
+  const i32x8 x = {a.codes[S][0], a.codes[S][1], a.codes[S][2], a.codes[S][3], 0, 0, 0, 0};
+  const i32x8 y = {b.codes[S][0], b.codes[S][1], b.codes[S][2], b.codes[S][3], 0, 0, 0, 0};
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, kFp4, kFp4, S, (int)a.scale, S, (int)b.scale);
+}
+
+constexpr int kLogitsThreads = 256;
+
+template <typename O>
+__global__ __launch_bounds__(kLogitsThreads) void mxfp4_logits_kernel(Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab,
+                                                                      int blocks, O* __restrict__ out, long long out_stride) {
+  const int lane = threadIdx.x & 63;
+  const int v0 = (blockIdx.x * (kLogitsThreads / 64) + (threadIdx.x >> 6)) * 16;
+  const int t0 = blockIdx.y * 16;
+  const long long w_row = min(v0 + (lane & 15), vocab - 1), h_row = min(t0 + (lane & 15), n_rows - 1);
+  const unsigned char* w_codes = weight.codes + w_row * weight.codes_stride;
+  const unsigned char* w_scales = weight.scales + w_row * weight.scales_stride;
+  const unsigned char* h_codes = hidden.codes + h_row * hidden.codes_stride;
+  const unsigned char* h_scales = hidden.scales + h_row * hidden.scales_stride;
+  f32x4 c = {0.f, 0.f, 0.f, 0.f};
+  for (int g = 0; g < blocks; g += kGroup) {
+    const int block = g + 4 * (lane >> 4);
+    Fragment w, h;
+    w.load(w_codes, w_scales, block, blocks);
+    h.load(h_codes, h_scales, block, blocks);
+    multiply<0>(c, w, h);
+    multiply<1>(c, w, h);
+    multiply<2>(c, w, h);
+    multiply<3>(c, w, h);
+  }
+  // four consecutive vocabulary entries of one token
+  const int t = t0 + (lane & 15), v = v0 + 4 * (lane >> 4);
+  if (t >= n_rows) return;
+  O* o = out + (long long)t * out_stride + v;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (v + k < vocab) Vec<O>::store1(o + k, c[k]);
+}
+
+bool rows_of_vectors(const void* p, long long stride, int esize) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * esize % 16 == 0;
+}
+
+}  // namespace
+
+int launch_mxfp4_quantize(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, int width, long long row_stride,
+                          unsigned char* codes, long long codes_stride, unsigned char* scales, long long scales_stride,
+                          void* values, long long values_stride) {
+  if (n_rows == 0) return AIS_OK;
+  ScopedTimer timer(ctx, AIS_K_MXFP4_QUANT);
+  const int row_units = (width + kBlock - 1) / kBlock * (kBlock / kUnit);
+  const long long n_units = n_rows * row_units;
+  const long long per_group = kQuantThreads * kQuantUnits;
+  const long long groups = (n_units + per_group - 1) / per_group;
+  if (groups > 0x7fffffffLL) return AIS_ERR_SIZE;
+  auto run = [&](auto type) {
+    typedef decltype(type) T;
+    mxfp4_quantize_kernel<T><<<dim3((unsigned)groups), dim3(kQuantThreads), 0, ctx->stream>>>(
+        static_cast<const T*>(x), row_stride, width, row_units, n_units, codes, codes_stride, scales, scales_stride,
+        static_cast<T*>(values), values_stride, rows_of_vectors(x, row_stride, sizeof(T)),
+        rows_of_vectors(values, values_stride, sizeof(T)));
+  };
+  if (dtype == AIS_BF16) run(bf16_t{});
+  else run(float{});
+  return hip_fail(ctx, hipGetLastError());
+}
+
+int launch_mxfp4_logits(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks,
+                        void* out, ais_dtype out_dtype, long long out_stride) {
+  if (n_rows == 0) return AIS_OK;
+  ScopedTimer timer(ctx, AIS_K_MXFP4_LOGITS);
+  const long long t_blocks = ((long long)n_rows + 15) / 16;
+  if (t_blocks > 65535) return AIS_ERR_SIZE;
+  const dim3 grid((unsigned)((vocab + 63LL) / 64), (unsigned)t_blocks);
+  if (out_dtype == AIS_BF16)
+    mxfp4_logits_kernel<bf16_t><<<grid, dim3(kLogitsThreads), 0, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks,
+                                                                               static_cast<bf16_t*>(out), out_stride);
+  else
+    mxfp4_logits_kernel<float><<<grid, dim3(kLogitsThreads), 0, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks,
+                                                                              static_cast<float*>(out), out_stride);
+  return hip_fail(ctx, hipGetLastError());
+}
+
+}  // namespace ais
