@@ -1,5 +1,4 @@
-// Microscaled 4-bit floating point (MXFP4): rows of blocks of 32 E2M1 elements under one E8M0 scale, and the product of two
-// such matrices, which is the read-out of a 4-bit rollout policy.
+// Microscaled 4-bit floating point (MXFP4): rows of blocks of 32 E2M1 elements under one E8M0 scale.
 #include "ais_internal.h"
 #include "device_utils.h"
 
@@ -99,79 +98,6 @@ __global__ __launch_bounds__(kQuantThreads) void mxfp4_quantize_kernel(
   }
 }
 
-// ---- product --------------------------------------------------------------------------------------------------------
-// out[t, v] = sum over blocks of 2^(ea + ew) sum_i a_i w_i: v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 rows of the
-// embedding with 16 tokens over four blocks and applies both scales.  A lane holds one block of one row: lane l that of row
-// l % 16, and which four blocks go together is free as long as both operands agree, so a lane takes blocks 4 (l / 16) + s of a
-// group of 16 in step s: 64 consecutive bytes of codes and one word of scales, whose byte s the instruction picks.
-
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kGroup = 16;             // blocks that four steps cover
-constexpr int kFp4 = 4;                // the instruction's code of the E2M1 format
-
-// A lane's share of a group of blocks: block b's codes at codes[b], its scale in byte b of `scale`; zeros beyond the row's end.
-struct Fragment {
-  i32x4 codes[4];
-  uint32_t scale;
-  __device__ __forceinline__ void load(const unsigned char* code_row, const unsigned char* scale_row, int block, int blocks) {
-    const int left = blocks - block;
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-      codes[s] = s < left ? *reinterpret_cast<const i32x4*>(code_row + 16LL * (block + s)) : i32x4{0, 0, 0, 0};
-    scale = 0;
-    if (left >= 4) {
-      scale = *reinterpret_cast<const uint32_t*>(scale_row + block);
-    } else {
-#pragma unroll
-      for (int s = 0; s < 3; ++s)
-        if (s < left) scale |= (uint32_t)scale_row[block + s] << (8 * s);
-    }
-  }
-};
-
-template <int S>
-__device__ __forceinline__ void multiply(f32x4& c, const Fragment& a, const Fragment& b) {
-  const i32x8 x = {a.codes[S][0], a.codes[S][1], a.codes[S][2], a.codes[S][3], 0, 0, 0, 0};
-  const i32x8 y = {b.codes[S][0], b.codes[S][1], b.codes[S][2], b.codes[S][3], 0, 0, 0, 0};
-  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, kFp4, kFp4, S, (int)a.scale, S, (int)b.scale);
-}
-
-constexpr int kLogitsThreads = 256;
-
-template <typename O>
-__global__ __launch_bounds__(kLogitsThreads) void mxfp4_logits_kernel(Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab,
-                                                                      int blocks, O* __restrict__ out, long long out_stride) {
-  const int lane = threadIdx.x & 63;
-  const int v0 = (blockIdx.x * (kLogitsThreads / 64) + (threadIdx.x >> 6)) * 16;
-  const int t0 = blockIdx.y * 16;
-  const long long w_row = min(v0 + (lane & 15), vocab - 1), h_row = min(t0 + (lane & 15), n_rows - 1);
-  const unsigned char* w_codes = weight.codes + w_row * weight.codes_stride;
-  const unsigned char* w_scales = weight.scales + w_row * weight.scales_stride;
-  const unsigned char* h_codes = hidden.codes + h_row * hidden.codes_stride;
-  const unsigned char* h_scales = hidden.scales + h_row * hidden.scales_stride;
-  f32x4 c = {0.f, 0.f, 0.f, 0.f};
-  for (int g = 0; g < blocks; g += kGroup) {
-    const int block = g + 4 * (lane >> 4);
-    Fragment w, h;
-    w.load(w_codes, w_scales, block, blocks);
-    h.load(h_codes, h_scales, block, blocks);
-    multiply<0>(c, w, h);
-    multiply<1>(c, w, h);
-    multiply<2>(c, w, h);
-    multiply<3>(c, w, h);
-  }
-  // four consecutive vocabulary entries of one token
-  const int t = t0 + (lane & 15), v = v0 + 4 * (lane >> 4);
-  if (t >= n_rows) return;
-  O* o = out + (long long)t * out_stride + v;
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (v + k < vocab) Vec<O>::store1(o + k, c[k]);
-}
-
 bool rows_of_vectors(const void* p, long long stride, int esize) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * esize % 16 == 0;
 }
@@ -197,22 +123,6 @@ int launch_mxfp4_quantize(ais_ctx* ctx, const void* x, ais_dtype dtype, long lon
   };
   if (dtype == AIS_BF16) run(bf16_t{});
   else run(float{});
-  return hip_fail(ctx, hipGetLastError());
-}
-
-int launch_mxfp4_logits(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks,
-                        void* out, ais_dtype out_dtype, long long out_stride) {
-  if (n_rows == 0) return AIS_OK;
-  ScopedTimer timer(ctx, AIS_K_MXFP4_LOGITS);
-  const long long t_blocks = ((long long)n_rows + 15) / 16;
-  if (t_blocks > 65535) return AIS_ERR_SIZE;
-  const dim3 grid((unsigned)((vocab + 63LL) / 64), (unsigned)t_blocks);
-  if (out_dtype == AIS_BF16)
-    mxfp4_logits_kernel<bf16_t><<<grid, dim3(kLogitsThreads), 0, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks,
-                                                                               static_cast<bf16_t*>(out), out_stride);
-  else
-    mxfp4_logits_kernel<float><<<grid, dim3(kLogitsThreads), 0, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks,
-                                                                              static_cast<float*>(out), out_stride);
   return hip_fail(ctx, hipGetLastError());
 }
 

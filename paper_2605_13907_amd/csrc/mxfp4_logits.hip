@@ -1,0 +1,468 @@
+// The read-out of a 4-bit rollout policy: logits from hidden states and output embedding that are both MXFP4 rows,
+//   out[t, v] = sum over blocks b of 2^(e_t,b + e_v,b) sum_i h[t, b, i] w[v, b, i].
+//
+// v_mfma_scale_f32_16x16x128_f8f6f4 multiplies 16 rows of the embedding with 16 tokens over four blocks of 32 elements and
+// applies both scales: a lane holds one block (16 bytes) of row lane % 16 and the byte of its scale.  Which four blocks go
+// together is free as long as both operands agree.  The embedding is the first operand: a lane of the result then has four
+// consecutive logits of one token.
+#include "ais_internal.h"
+#include "device_utils.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace ais {
+namespace {
+
+using namespace dev;
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef const __attribute__((address_space(1))) void* glb_ptr;
+
+constexpr int kFp4 = 4;                // the instruction's code of the E2M1 format
+constexpr int kGroup = 16;             // blocks whose scales are one 16-byte vector
+
+// c += w h over four blocks, the scales in byte S of the words.
+template <int S>
+__device__ __forceinline__ void multiply(f32x4& c, i32x4 w, uint32_t w_scale, i32x4 h, uint32_t h_scale) {
+  const i32x8 x = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, y = {h[0], h[1], h[2], h[3], 0, 0, 0, 0};
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, kFp4, kFp4, S, (int)w_scale, S, (int)h_scale);
+}
+
+// ---- few rows ---------------------------------------------------------------------------------------------------------
+// A decode step reads the whole embedding for a few tokens: 17 bytes a block from HBM, and next to nothing else.  A workgroup
+// takes MV * 16 entries of the vocabulary and NT * 16 tokens, its four wavefronts a quarter of the contraction each, so that a
+// wavefront is short and has all of its loads on their way at once.  In step s of a group of 16 blocks lane l takes block
+// 4 s + l / 16: an instruction reads 64 consecutive bytes of 16 rows.
+constexpr int kFewThreads = 256;
+constexpr int kFewWaves = kFewThreads / 64;
+
+// A lane's share of a group: the blocks of its quarter in the four steps, and their scales.
+struct Few {
+  i32x4 codes[4];
+  uint32_t scale[4];
+  __device__ __forceinline__ void load(const unsigned char* code_row, const unsigned char* scale_row, int group, int quarter,
+                                       int blocks) {
+    const int block = group * kGroup;
+    if (block + kGroup <= blocks) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) codes[s] = *reinterpret_cast<const i32x4*>(code_row + 16LL * (block + 4 * s + quarter));
+#pragma unroll
+      for (int s = 0; s < 4; ++s) scale[s] = *reinterpret_cast<const uint32_t*>(scale_row + block + 4 * s);
+    } else {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int b = block + 4 * s + quarter;
+        codes[s] = i32x4{0, 0, 0, 0};
+        scale[s] = 0;
+        if (b < blocks) {
+          codes[s] = *reinterpret_cast<const i32x4*>(code_row + 16LL * b);
+          scale[s] = (uint32_t)scale_row[b] << (8 * quarter);
+        }
+      }
+    }
+    // byte `quarter` of a word is the block's
+#pragma unroll
+    for (int s = 0; s < 4; ++s) scale[s] >>= 8 * quarter;
+  }
+};
+
+template <typename O, int MV, int NT>
+__global__ __launch_bounds__(kFewThreads) void mxfp4_few_rows_kernel(Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab,
+                                                                     int blocks, O* __restrict__ out, long long out_stride) {
+  __shared__ f32x4 part[kFewWaves][MV][NT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
+  const int v0 = blockIdx.x * (16 * MV), t0 = blockIdx.y * (16 * NT);
+  const unsigned char *w_codes[MV], *w_scales[MV], *h_codes[NT], *h_scales[NT];
+#pragma unroll
+  for (int i = 0; i < MV; ++i) {
+    const long long row = min(v0 + 16 * i + (lane & 15), vocab - 1);
+    w_codes[i] = weight.codes + row * weight.codes_stride;
+    w_scales[i] = weight.scales + row * weight.scales_stride;
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const long long row = min(t0 + 16 * j + (lane & 15), n_rows - 1);
+    h_codes[j] = hidden.codes + row * hidden.codes_stride;
+    h_scales[j] = hidden.scales + row * hidden.scales_stride;
+  }
+  f32x4 c[MV][NT];
+#pragma unroll
+  for (int i = 0; i < MV; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) c[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int groups = (blocks + kGroup - 1) / kGroup;
+  for (int g = wave; g < groups; g += kFewWaves) {
+    Few w[MV], h[NT];
+#pragma unroll
+    for (int i = 0; i < MV; ++i) w[i].load(w_codes[i], w_scales[i], g, quarter, blocks);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) h[j].load(h_codes[j], h_scales[j], g, quarter, blocks);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int i = 0; i < MV; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) multiply<0>(c[i][j], w[i].codes[s], w[i].scale[s], h[j].codes[s], h[j].scale[s]);
+  }
+#pragma unroll
+  for (int i = 0; i < MV; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) part[wave][i][j][lane] = c[i][j];
+  __syncthreads();
+  // a wavefront adds up and writes its share of the MV * NT tiles of 16 x 16
+  for (int k = wave; k < MV * NT; k += kFewWaves) {
+    const int i = k / NT, j = k % NT;
+    f32x4 z = part[0][i][j][lane];
+#pragma unroll
+    for (int p = 1; p < kFewWaves; ++p) z += part[p][i][j][lane];
+    const int t = t0 + 16 * j + (lane & 15), v = v0 + 16 * i + 4 * quarter;
+    if (t < n_rows) {
+      O* o = out + (long long)t * out_stride + v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v + e < vocab) Vec<O>::store1(o + e, z[e]);
+    }
+  }
+}
+
+// ---- many rows ----------------------------------------------------------------------------------------------------------
+// Tiles of 256 entries of the vocabulary x 64 NJ tokens, eight wavefronts, two along the vocabulary x four along the tokens,
+// 128 x 16 NJ logits each.  A step covers eight blocks: 128 bytes, a whole line, of every row, copied straight from global
+// memory into one of two LDS buffers; the copies of the next step are on their way while a step is multiplied.  Scales come
+// for two steps at a time.  A workgroup walks through its tiles without a pause: the first step of the next tile is copied during
+// the last of this one.
+//
+// The products are written as instructions: the compiler's own form of one may be moved past the barriers, and a step's worth
+// of fragments and accumulators with it.  It does not know what such a statement is, so what it would wait for is waited for
+// here: wait() stands between an ordinary instruction that writes scales or accumulators and the products, and settle()
+// between the products and the first look at their sums.  Fragments come from LDS reads, whose arrival it does wait for.
+template <int S>
+__device__ __forceinline__ void product(f32x4& c, i32x4 w, uint32_t w_scale, i32x4 h, uint32_t h_scale) {
+  if constexpr (S == 0)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+                 : "+a"(c) : "v"(w), "v"(h), "v"(w_scale), "v"(h_scale));
+  if constexpr (S == 1)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0] cbsz:4 blgp:4"
+                 : "+a"(c) : "v"(w), "v"(h), "v"(w_scale), "v"(h_scale));
+  if constexpr (S == 2)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[0,0,0] op_sel_hi:[1,1,0] cbsz:4 blgp:4"
+                 : "+a"(c) : "v"(w), "v"(h), "v"(w_scale), "v"(h_scale));
+  if constexpr (S == 3)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[1,1,0] cbsz:4 blgp:4"
+                 : "+a"(c) : "v"(w), "v"(h), "v"(w_scale), "v"(h_scale));
+}
+__device__ __forceinline__ void wait() { asm volatile("s_nop 7"); }
+__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 3"); }
+
+constexpr int kTileThreads = 512;
+constexpr int kTileV = 256;
+constexpr int kNI = 8;                                        // MFMA tiles of a wavefront along the vocabulary
+constexpr int kAhead = 2;
+constexpr int kStepBlocks = 8;
+constexpr int kRowBytes = 16 * kStepBlocks;                   // of a step's slice
+
+// Chunk c of a slice's row lies at position c ^ swizzle(row): the 16 rows that a fragment read touches lie in different 16-byte
+// bank groups.  The rows of a fragment are consecutive ones of the hidden states; of the embedding they are four fours, eight
+// apart (see tile_entry).
+__device__ __forceinline__ int swizzle_h(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int swizzle_w(int row) { return (row >> 1 & 1) | (row >> 2 & 6); }
+// First of the four entries, inside the wavefront's 128, that MFMA tile i leaves in a lane of this quarter: two tiles are 32
+// entries, eight consecutive ones to a lane.
+__device__ __forceinline__ int tile_entry(int i, int quarter) { return 32 * (i >> 1) + 8 * quarter + 4 * (i & 1); }
+
+struct TilePlan {
+  int n_vtiles, n_ttiles, group, per_xcd, n_items;            // tiles of tokens that walk the vocabulary together; items of an XCD
+};
+
+template <int NJ>
+struct TileLds {
+  static constexpr int kTileT = 64 * NJ;
+  static constexpr int kW = 0, kH = 2 * kTileV * kRowBytes;                     // two slices of each
+  static constexpr int kScales = kH + 2 * kTileT * kRowBytes;                   // two groups of 16 bytes for each row
+  static constexpr int kScaleCopies = (kTileV + kTileT + 127) / 128;            // instructions of each wavefront, 128 rows in all
+  static constexpr int kScaleBytes = 128 * kScaleCopies * kGroup;
+  static constexpr int kBytes = kScales + 2 * kScaleBytes;
+};
+
+template <typename O, int NJ, bool RAGGED>
+__global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void mxfp4_tile_kernel(
+    Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab, int blocks, TilePlan plan, O* __restrict__ out,
+    long long out_stride, int out_vectors) {
+  typedef TileLds<NJ> L;
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
+  const int wv = wave & 1, wt = wave >> 1;
+  // workgroups are dealt to the XCDs in turns; each XCD has a range of items of its own, which its workgroups take in turns
+  const int xcd = blockIdx.x & 7, local = blockIdx.x >> 3, locals = gridDim.x >> 3;
+  const int item0 = xcd * plan.per_xcd + local, item_end = min((xcd + 1) * plan.per_xcd, plan.n_items);
+  if (item0 >= item_end) return;
+  auto place = [&](int item, int& v0, int& t0) {
+    const int per_group = plan.group * plan.n_vtiles;
+    const int g = item / per_group, j = item - g * per_group;
+    const int size = min(plan.group, plan.n_ttiles - g * plan.group);
+    const int v = j / size;
+    v0 = v * kTileV;
+    t0 = (g * plan.group + (j - v * size)) * L::kTileT;
+  };
+
+  // ---- copies: a wavefront moves rows 8 wave .. 8 wave + 7 (+ 64 q) of a slice, a lane the chunk that lies at lane % 8.
+  // Scales: 16 rows of four words to an instruction, the rows of both operands numbered in one go.  Offsets are from the tile's
+  // first row, 32 bits.  Blocks beyond a row's end are its last one again: a code is always a finite number, and two scales of
+  // 2^-127 leave nothing of it.
+  const int crow = 8 * wave + (lane >> 3);
+  const int w_chunk = (lane & 7) ^ swizzle_w(crow), h_chunk = (lane & 7) ^ swizzle_h(crow);
+  constexpr int kScaleCopies = L::kScaleCopies;
+  const unsigned char *w_base, *h_base, *ws_base, *hs_base;
+  uint32_t w_off[4], h_off[NJ], s_off[kScaleCopies];
+  auto point = [&](int item) {
+    int v0, t0;
+    place(item, v0, t0);
+    w_base = weight.codes + (long long)v0 * weight.codes_stride;
+    h_base = hidden.codes + (long long)t0 * hidden.codes_stride;
+    ws_base = weight.scales + (long long)v0 * weight.scales_stride;
+    hs_base = hidden.scales + (long long)t0 * hidden.scales_stride;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) w_off[q] = (uint32_t)min(crow + 64 * q, vocab - 1 - v0) * (uint32_t)weight.codes_stride;
+#pragma unroll
+    for (int q = 0; q < NJ; ++q) h_off[q] = (uint32_t)min(crow + 64 * q, n_rows - 1 - t0) * (uint32_t)hidden.codes_stride;
+#pragma unroll
+    for (int q = 0; q < kScaleCopies; ++q) {
+      const int row = 16 * wave + 128 * q, r = row + (lane >> 2);              // row: the wavefront's first
+      s_off[q] = row < kTileV ? (uint32_t)min(r, vocab - 1 - v0) * (uint32_t)weight.scales_stride
+                              : (uint32_t)min(r - kTileV, n_rows - 1 - t0) * (uint32_t)hidden.scales_stride;
+    }
+  };
+  const int n_groups = (blocks + kGroup - 1) / kGroup;         // pairs of steps of a tile
+  // the cursor of the copies
+  int c_item = item0, c_group = 0;
+  point(item0);
+  auto copy_codes = [&](int half) {                             // of step 2 c_group + half, into buffer `half`
+    const int block = c_group * kGroup + half * kStepBlocks;
+    const uint32_t wb = 16u * (uint32_t)(RAGGED ? min(block + w_chunk, blocks - 1) : block + w_chunk);
+    const uint32_t hb = 16u * (uint32_t)(RAGGED ? min(block + h_chunk, blocks - 1) : block + h_chunk);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      __builtin_amdgcn_global_load_lds((glb_ptr)(w_base + (w_off[q] + wb)),
+                                       (lds_ptr)(lds + L::kW + half * kTileV * kRowBytes + (8 * wave + 64 * q) * kRowBytes), 16, 0, 0);
+#pragma unroll
+    for (int q = 0; q < NJ; ++q)
+      __builtin_amdgcn_global_load_lds((glb_ptr)(h_base + (h_off[q] + hb)),
+                                       (lds_ptr)(lds + L::kH + half * L::kTileT * kRowBytes + (8 * wave + 64 * q) * kRowBytes), 16, 0,
+                                       0);
+  };
+  auto copy_scales = [&](int buffer) {
+    const int word = c_group * kGroup + 4 * (lane & 3);
+    const uint32_t sb = (uint32_t)(RAGGED ? min(word, (blocks - 1) & ~3) : word);
+#pragma unroll
+    for (int q = 0; q < kScaleCopies; ++q) {
+      const unsigned char* base = 16 * wave + 128 * q < kTileV ? ws_base : hs_base;
+      __builtin_amdgcn_global_load_lds((glb_ptr)(base + (s_off[q] + sb)),
+                                       (lds_ptr)(lds + L::kScales + buffer * L::kScaleBytes + (16 * wave + 128 * q) * kGroup), 4, 0, 0);
+    }
+  };
+  // ---- fragments: in half step h lane takes chunk 2 quarter + h of its row, whose scale is byte 2 (quarter % 2) + h of word
+  // quarter / 2 of the step's eight bytes
+  const int a = lane & 15;
+  const int arow = wv * 128 + 8 * (a >> 2) + (a & 3);          // tile i: + tile_entry(i, 0)
+  const int brow = wt * 16 * NJ + a;
+  const uint32_t pick = (quarter & 1) ? 0x07060302u : 0x05040100u;
+  // swizzles do not depend on the MFMA tile: a fragment lies at a constant distance from the first one
+  const int w_at[2] = {arow * kRowBytes + ((2 * quarter ^ swizzle_w(arow)) << 4),
+                       arow * kRowBytes + (((2 * quarter + 1) ^ swizzle_w(arow)) << 4)};
+  const int h_at[2] = {brow * kRowBytes + ((2 * quarter ^ swizzle_h(brow)) << 4),
+                       brow * kRowBytes + (((2 * quarter + 1) ^ swizzle_h(brow)) << 4)};
+  const int ws_at = arow * kGroup + 4 * (quarter >> 1), hs_at = (kTileV + brow) * kGroup + 4 * (quarter >> 1);
+
+  f32x4 acc[kNI][NJ];
+  copy_scales(0);
+  copy_codes(0);
+  int scale_buffer = 0;
+  for (int item = item0; item < item_end; item += locals) {
+#pragma unroll
+    for (int i = 0; i < kNI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        asm volatile("" : "+a"(acc[i][j]));
+      }
+    wait();
+    // A group of blocks: two steps.  No branch inside: the compiler would move products across it, and accumulators with them.
+    auto two_steps = [&](int g, auto last) __attribute__((always_inline)) {
+      uint32_t ws[kNI], hs[NJ];
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        // this step's copies, the only ones in flight, have landed everywhere, and nobody reads the step before any more
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (half == 0) {
+          copy_codes(1);
+        } else {
+          if constexpr (decltype(last)::value) {                // on to the next tile; after the last one once more to its beginning
+            c_group = 0;
+            c_item = c_item + locals < item_end ? c_item + locals : c_item;
+            point(c_item);
+          } else {
+            ++c_group;
+          }
+          copy_scales(scale_buffer ^ 1);
+          copy_codes(0);
+        }
+        if (half == 0) {
+          const unsigned char* sl = lds + L::kScales + scale_buffer * L::kScaleBytes;
+          // scales beyond the row's end count as zero
+          uint32_t keep = ~0u;
+          if (RAGGED) {
+            const int left = blocks - g * kGroup - 2 * quarter;
+            keep = (left > 0 ? 0xffu : 0u) | (left > 1 ? 0xff00u : 0u) | (left > 8 ? 0xff0000u : 0u) | (left > 9 ? 0xff000000u : 0u);
+          }
+#pragma unroll
+          for (int i = 0; i < kNI; ++i) {
+            const uint32_t* r = reinterpret_cast<const uint32_t*>(sl + ws_at + tile_entry(i, 0) * kGroup);
+            ws[i] = __builtin_amdgcn_perm(r[2], r[0], pick) & keep;
+          }
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const uint32_t* r = reinterpret_cast<const uint32_t*>(sl + hs_at + 16 * j * kGroup);
+            hs[j] = __builtin_amdgcn_perm(r[2], r[0], pick) & keep;
+          }
+#pragma unroll
+          for (int i = 0; i < kNI; ++i) asm volatile("" : "+v"(ws[i]));
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(hs[j]));
+          wait();
+        }
+        const unsigned char* wl = lds + L::kW + half * kTileV * kRowBytes;
+        const unsigned char* hl = lds + L::kH + half * L::kTileT * kRowBytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          // the embedding's fragments are read two MFMA tiles ahead
+          i32x4 w[kAhead + 1], b[NJ];
+          auto read_w = [&](int i) {
+            w[i % (kAhead + 1)] = *reinterpret_cast<const i32x4*>(wl + w_at[h] + tile_entry(i, 0) * kRowBytes);
+          };
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) b[j] = *reinterpret_cast<const i32x4*>(hl + h_at[h] + 16 * j * kRowBytes);
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) read_w(i);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < kNI; ++i) {
+            if (i + kAhead < kNI) read_w(i + kAhead);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+              const i32x4 x = w[i % (kAhead + 1)];
+              if (half == 0 && h == 0) product<0>(acc[i][j], x, ws[i], b[j], hs[j]);
+              if (half == 0 && h == 1) product<1>(acc[i][j], x, ws[i], b[j], hs[j]);
+              if (half == 1 && h == 0) product<2>(acc[i][j], x, ws[i], b[j], hs[j]);
+              if (half == 1 && h == 1) product<3>(acc[i][j], x, ws[i], b[j], hs[j]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+      scale_buffer ^= 1;
+    };
+    for (int g = 0; g + 1 < n_groups; ++g) two_steps(g, std::false_type{});
+    two_steps(n_groups - 1, std::true_type{});
+    // ---- the finished tile: eight consecutive logits of a token from every two MFMA tiles
+    settle();
+#pragma unroll
+    for (int i = 0; i < kNI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
+    int v0, t0;
+    place(item, v0, t0);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int t = t0 + brow + 16 * j;
+      if (t >= n_rows) continue;
+      O* row = out + (long long)t * out_stride;
+#pragma unroll
+      for (int i = 0; i < kNI; i += 2) {
+        const int v = v0 + wv * 128 + tile_entry(i, quarter);
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = acc[i + (e >> 2)][j][e & 3];
+        if (out_vectors && v + 8 <= vocab) {
+          constexpr int N = Vec<O>::N;
+#pragma unroll
+          for (int e = 0; e < 8; e += N) *reinterpret_cast<u32x4*>(row + v + e) = Vec<O>::pack(z + e);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (v + e < vocab) Vec<O>::store1(row + v + e, z[e]);
+        }
+      }
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // copies for nobody land before the LDS is given back
+}
+
+template <typename O, int NJ, bool RAGGED>
+int launch_tiles(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks, O* out,
+                 long long out_stride) {
+  typedef TileLds<NJ> L;
+  auto kernel = mxfp4_tile_kernel<O, NJ, RAGGED>;
+  static std::once_flag once[kMaxDevices];
+  static bool ok[kMaxDevices];
+  if (!allow_dynamic_lds(ctx, reinterpret_cast<const void*>(kernel), L::kBytes, once, ok))
+    return hip_fail(ctx, hipErrorInvalidValue);
+  TilePlan plan;
+  plan.n_vtiles = (vocab + kTileV - 1) / kTileV;
+  plan.n_ttiles = (n_rows + L::kTileT - 1) / L::kTileT;
+  plan.group = plan.n_ttiles < 8 ? plan.n_ttiles : 8;
+  const long long items = (long long)plan.n_vtiles * plan.n_ttiles;
+  if (items > 0x7fffffffLL - 8) return AIS_ERR_SIZE;
+  plan.n_items = (int)items;
+  plan.per_xcd = (plan.n_items + 7) / 8;
+  const int locals = plan.per_xcd < (ctx->n_cus + 7) / 8 ? plan.per_xcd : (ctx->n_cus + 7) / 8;
+  const int vectors = reinterpret_cast<uintptr_t>(out) % 16 == 0 && out_stride * (long long)sizeof(O) % 16 == 0;
+  kernel<<<dim3((unsigned)(8 * locals)), dim3(kTileThreads), L::kBytes, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, plan,
+                                                                                      out, out_stride, vectors);
+  return hip_fail(ctx, hipGetLastError());
+}
+
+template <typename O, int MV, int NT>
+int launch_few(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks, O* out,
+               long long out_stride) {
+  const dim3 grid((unsigned)((vocab + 16LL * MV - 1) / (16 * MV)), (unsigned)((n_rows + 16 * NT - 1) / (16 * NT)));
+  mxfp4_few_rows_kernel<O, MV, NT><<<grid, dim3(kFewThreads), 0, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, out,
+                                                                               out_stride);
+  return hip_fail(ctx, hipGetLastError());
+}
+
+template <typename O>
+int launch_typed(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks, O* out,
+                 long long out_stride) {
+  if (n_rows <= 16) return launch_few<O, 1, 1>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+  if (n_rows <= 32) return launch_few<O, 2, 2>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+  const bool ragged = blocks % kGroup != 0;
+  // the tile kernel's offsets inside a tile are 32 bits wide
+  if (std::max(std::max(weight.codes_stride, hidden.codes_stride), std::max(weight.scales_stride, hidden.scales_stride)) >=
+      0xffffffffLL / kTileV)
+    return launch_few<O, 2, 2>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+  auto tiles = [&](auto nj) {
+    constexpr int NJ = decltype(nj)::value;
+    return ragged ? launch_tiles<O, NJ, true>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride)
+                  : launch_tiles<O, NJ, false>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+  };
+  if (n_rows <= 64) return tiles(std::integral_constant<int, 1>{});
+  if (n_rows <= 128) return tiles(std::integral_constant<int, 2>{});
+  return tiles(std::integral_constant<int, 4>{});
+}
+
+}  // namespace
+
+int launch_mxfp4_logits(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks,
+                        void* out, ais_dtype out_dtype, long long out_stride) {
+  if (n_rows == 0) return AIS_OK;
+  ScopedTimer timer(ctx, AIS_K_MXFP4_LOGITS);
+  if (out_dtype == AIS_BF16)
+    return launch_typed(ctx, hidden, n_rows, weight, vocab, blocks, static_cast<bf16_t*>(out), out_stride);
+  return launch_typed(ctx, hidden, n_rows, weight, vocab, blocks, static_cast<float*>(out), out_stride);
+}
+
+}  // namespace ais
