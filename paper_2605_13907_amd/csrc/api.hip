@@ -688,6 +688,9 @@ int ais_mxfp4_logits(ais_ctx* ctx, const unsigned char* hidden_codes, long long 
   if (rc != AIS_OK) return rc;
   rc = check_mxfp4_rows(hidden_codes, hidden_codes_stride, hidden_scales, hidden_scales_stride, n_rows, width);
   if (rc != AIS_OK) return rc;
+  // offsets inside a tile of 256 rows are 32 bits wide
+  if (std::max(std::max(hidden_codes_stride, hidden_scales_stride), std::max(weight_codes_stride, weight_scales_stride)) >= 1LL << 24)
+    return AIS_ERR_SIZE;
   // an empty batch needs no embedding either
   rc = check_mxfp4_rows(weight_codes, weight_codes_stride, weight_scales, weight_scales_stride, n_rows > 0 ? vocab : 0, width);
   if (rc != AIS_OK) return rc;

@@ -25,108 +25,172 @@ typedef const __attribute__((address_space(1))) void* glb_ptr;
 constexpr int kFp4 = 4;                // the instruction's code of the E2M1 format
 constexpr int kGroup = 16;             // blocks whose scales are one 16-byte vector
 
-// c += w h over four blocks, the scales in byte S of the words.
-template <int S>
+// c += w h over four blocks, the scales in the words' low bytes.
 __device__ __forceinline__ void multiply(f32x4& c, i32x4 w, uint32_t w_scale, i32x4 h, uint32_t h_scale) {
   const i32x8 x = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, y = {h[0], h[1], h[2], h[3], 0, 0, 0, 0};
-  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, kFp4, kFp4, S, (int)w_scale, S, (int)h_scale);
+  c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, kFp4, kFp4, 0, (int)w_scale, 0, (int)h_scale);
 }
 
-// ---- few rows ---------------------------------------------------------------------------------------------------------
-// A decode step reads the whole embedding for a few tokens: 17 bytes a block from HBM, and next to nothing else.  A workgroup
-// takes MV * 16 entries of the vocabulary and NT * 16 tokens, its four wavefronts a quarter of the contraction each, so that a
-// wavefront is short and has all of its loads on their way at once.  In step s of a group of 16 blocks lane l takes block
-// 4 s + l / 16: an instruction reads 64 consecutive bytes of 16 rows.
-constexpr int kFewThreads = 256;
-constexpr int kFewWaves = kFewThreads / 64;
+constexpr int kRowBytes = 128;         // of a slice of eight blocks
+// Chunk c (of 16 bytes) of a slice's row lies in LDS at position c ^ swizzle(row): the 16 rows that a fragment read touches lie in
+// different 16-byte bank groups.  The rows of a fragment are consecutive ones of the hidden states; in the tile kernel those of
+// the embedding are four fours, eight apart (see tile_entry).
+__device__ __forceinline__ int swizzle_h(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int swizzle_w(int row) { return (row >> 1 & 1) | (row >> 2 & 6); }
 
-// A lane's share of a group: the blocks of its quarter in the four steps, and their scales.
-struct Few {
-  i32x4 codes[4];
-  uint32_t scale[4];
-  __device__ __forceinline__ void load(const unsigned char* code_row, const unsigned char* scale_row, int group, int quarter,
-                                       int blocks) {
-    const int block = group * kGroup;
-    if (block + kGroup <= blocks) {
+// ---- few rows ---------------------------------------------------------------------------------------------------------
+// A decode step reads the whole embedding for a few tokens: 17 bytes a block from HBM, and next to nothing else.  One workgroup
+// on every compute unit walks through its share of the vocabulary, 16 entries at a time, with all of LDS as a ring of what is on
+// its way.  Its four wavefronts have a quarter of the contraction each, whose hidden states stay in registers.  A wavefront
+// copies and awaits its own share of the embedding, whole lines of 128 bytes, and nobody else's; the four sums of a tile meet
+// in LDS, and the wavefronts take turns in writing them out.
+constexpr int kStreamThreads = 256;
+constexpr int kStreamWaves = kStreamThreads / 64;
+
+// NT: tiles of 16 tokens; GPW: groups of 16 blocks of each wavefront.
+template <int NT, int GPW>
+struct StreamLds {
+  static constexpr int kCodes = GPW * 16 * 2 * kRowBytes;                       // of 16 rows: [group][half][row][128]
+  static constexpr int kSlot = kCodes + GPW * 16 * kGroup;                      // and their scales: [group][row][16]
+  static constexpr int kCopies = 5 * GPW;                                       // instructions that fill a slot
+  static constexpr int kSums = 2 * kStreamWaves * NT * 1024;
+  // as many slots as LDS holds; vmcnt counts to 63
+  static constexpr int kRoom = (160 * 1024 - kSums) / (kStreamWaves * kSlot), kCount = 63 / kCopies + 1;
+  static constexpr int kDepth = kRoom < 8 ? (kRoom < kCount ? kRoom : kCount) : (kCount < 8 ? kCount : 8);
+  static_assert(kDepth >= 2, "the next tile is on its way while one is multiplied");
+  static constexpr int kRing = kStreamWaves * kDepth * kSlot;
+  static constexpr int kBytes = kRing + kSums;
+};
+
+template <typename O, int NT, int GPW>
+__global__ __launch_bounds__(kStreamThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void mxfp4_stream_kernel(
+    Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab, int blocks, O* __restrict__ out, long long out_stride,
+    int out_fours) {
+  typedef StreamLds<NT, GPW> L;
+  extern __shared__ __align__(16) unsigned char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
+  const int n_tiles = (vocab + 15) / 16;
+  const int tile0 = (int)((long long)n_tiles * blockIdx.x / gridDim.x), tile1 = (int)((long long)n_tiles * (blockIdx.x + 1) / gridDim.x);
+  if (tile0 >= tile1) return;
+  const int block0 = wave * GPW * kGroup;                      // of the wavefront's quarter
+  unsigned char* ring = lds + wave * L::kDepth * L::kSlot;
+  f32x4* part = reinterpret_cast<f32x4*>(lds + L::kRing);      // [2][wave][NT][lane]
+
+  // ---- the hidden states: in step s of a group lane l has block 4 s + l / 16, whose scale is byte l / 16 of word s.  Blocks beyond
+  // a row's end are the last one again, on both sides: codes are finite numbers, and two scales of 2^-127 leave nothing of them.
+  i32x4 h[GPW][NT][4];
+  uint32_t hs[GPW][NT][4];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) codes[s] = *reinterpret_cast<const i32x4*>(code_row + 16LL * (block + 4 * s + quarter));
+  for (int g = 0; g < GPW; ++g)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) scale[s] = *reinterpret_cast<const uint32_t*>(scale_row + block + 4 * s);
-    } else {
+    for (int j = 0; j < NT; ++j) {
+      const long long row = min((int)(blockIdx.y * NT + j) * 16 + (lane & 15), n_rows - 1);
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const int b = block + 4 * s + quarter;
-        codes[s] = i32x4{0, 0, 0, 0};
-        scale[s] = 0;
-        if (b < blocks) {
-          codes[s] = *reinterpret_cast<const i32x4*>(code_row + 16LL * b);
-          scale[s] = (uint32_t)scale_row[b] << (8 * quarter);
+        const int b = block0 + g * kGroup + 4 * s + quarter;
+        h[g][j][s] = *reinterpret_cast<const i32x4*>(hidden.codes + row * hidden.codes_stride + 16LL * min(b, blocks - 1));
+        hs[g][j][s] = b < blocks ? hidden.scales[row * hidden.scales_stride + b] : 0u;
+      }
+    }
+  uint32_t keep[GPW][4];                                       // of a word of the embedding's scales
+#pragma unroll
+  for (int g = 0; g < GPW; ++g)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const int left = blocks - (block0 + g * kGroup + 4 * s);
+      keep[g][s] = left >= 4 ? ~0u : left > 0 ? (1u << 8 * left) - 1 : 0u;
+    }
+
+  // ---- copies: eight rows of a slice to an instruction, a lane the chunk that lies at its place
+  const int crow = lane >> 3;
+  auto copy = [&](int tile, int slot) {
+    unsigned char* to = ring + slot * L::kSlot;
+    const int v0 = tile * 16;
+#pragma unroll
+    for (int g = 0; g < GPW; ++g)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int row = 8 * q + crow;
+          const int b = block0 + g * kGroup + half * 8 + ((lane & 7) ^ swizzle_h(row));
+          const unsigned char* src =
+              weight.codes + (long long)min(v0 + row, vocab - 1) * weight.codes_stride + 16LL * min(b, blocks - 1);
+          __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(to + ((g * 2 + half) * 16 + 8 * q) * kRowBytes), 16, 0, 0);
+        }
+#pragma unroll
+    for (int g = 0; g < GPW; ++g) {
+      const int b = block0 + g * kGroup + 4 * (lane & 3);
+      const unsigned char* src = weight.scales + (long long)min(v0 + (lane >> 2), vocab - 1) * weight.scales_stride +
+                                 min(b, (blocks - 1) & ~3);
+      __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(to + L::kCodes + g * 16 * kGroup), 4, 0, 0);
+    }
+  };
+#pragma unroll
+  for (int d = 0; d < L::kDepth; ++d) copy(min(tile0 + d, tile1 - 1), d);
+  const int a = lane & 15;
+  int slot = 0, turn = 0;
+  for (int tile = tile0; tile < tile1; ++tile) {
+    // the copies into this slot are the oldest ones; stores on their way only make the wait longer
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((L::kDepth - 1) * L::kCopies) : "memory");
+    const unsigned char* from = ring + slot * L::kSlot;
+    f32x4 c[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) c[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    i32x4 w[GPW][4];
+    uint32_t ws[GPW][4];
+#pragma unroll
+    for (int g = 0; g < GPW; ++g) {
+      const u32x4 words = *reinterpret_cast<const u32x4*>(from + L::kCodes + (g * 16 + a) * kGroup);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        w[g][s] = *reinterpret_cast<const i32x4*>(from + ((g * 2 + (s >> 1)) * 16 + a) * kRowBytes +
+                                                  ((((s & 1) * 4 + quarter) ^ swizzle_h(a)) << 4));
+        ws[g][s] = (words[s] & keep[g][s]) >> (8 * quarter);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < GPW; ++g)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) multiply(c[j], w[g][s], ws[g][s], h[g][j][s], hs[g][j][s]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // the slot has been read
+    copy(min(tile + L::kDepth, tile1 - 1), slot);              // beyond the last tile: once more, for nobody
+    f32x4* mine = part + (turn & 1) * kStreamWaves * NT * 64;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) mine[(wave * NT + j) * 64 + lane] = c[j];
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // The buffer is written again two tiles on, behind the next barrier, which the wavefront that reads it now reaches afterwards.
+    if ((turn & (kStreamWaves - 1)) == wave) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        f32x4 z = mine[j * 64 + lane];
+#pragma unroll
+        for (int p = 1; p < kStreamWaves; ++p) z += mine[(p * NT + j) * 64 + lane];
+        const int t = (int)(blockIdx.y * NT + j) * 16 + a, v = tile * 16 + 4 * quarter;
+        if (t >= n_rows) continue;
+        O* o = out + (long long)t * out_stride + v;
+        if (out_fours && v + 4 <= vocab) {
+          if constexpr (sizeof(O) == 4) {
+            *reinterpret_cast<f32x4*>(o) = z;
+          } else {
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            const float x[8] = {z[0], z[1], z[2], z[3]};
+            const u32x4 q = Vec<O>::pack(x);
+            *reinterpret_cast<u32x2*>(o) = u32x2{q[0], q[1]};
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (v + e < vocab) Vec<O>::store1(o + e, z[e]);
         }
       }
     }
-    // byte `quarter` of a word is the block's
-#pragma unroll
-    for (int s = 0; s < 4; ++s) scale[s] >>= 8 * quarter;
+    slot = slot + 1 == L::kDepth ? 0 : slot + 1;
+    ++turn;
   }
-};
-
-template <typename O, int MV, int NT>
-__global__ __launch_bounds__(kFewThreads) void mxfp4_few_rows_kernel(Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab,
-                                                                     int blocks, O* __restrict__ out, long long out_stride) {
-  __shared__ f32x4 part[kFewWaves][MV][NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, quarter = lane >> 4;
-  const int v0 = blockIdx.x * (16 * MV), t0 = blockIdx.y * (16 * NT);
-  const unsigned char *w_codes[MV], *w_scales[MV], *h_codes[NT], *h_scales[NT];
-#pragma unroll
-  for (int i = 0; i < MV; ++i) {
-    const long long row = min(v0 + 16 * i + (lane & 15), vocab - 1);
-    w_codes[i] = weight.codes + row * weight.codes_stride;
-    w_scales[i] = weight.scales + row * weight.scales_stride;
-  }
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const long long row = min(t0 + 16 * j + (lane & 15), n_rows - 1);
-    h_codes[j] = hidden.codes + row * hidden.codes_stride;
-    h_scales[j] = hidden.scales + row * hidden.scales_stride;
-  }
-  f32x4 c[MV][NT];
-#pragma unroll
-  for (int i = 0; i < MV; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) c[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int groups = (blocks + kGroup - 1) / kGroup;
-  for (int g = wave; g < groups; g += kFewWaves) {
-    Few w[MV], h[NT];
-#pragma unroll
-    for (int i = 0; i < MV; ++i) w[i].load(w_codes[i], w_scales[i], g, quarter, blocks);
-#pragma unroll
-    for (int j = 0; j < NT; ++j) h[j].load(h_codes[j], h_scales[j], g, quarter, blocks);
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int i = 0; i < MV; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) multiply<0>(c[i][j], w[i].codes[s], w[i].scale[s], h[j].codes[s], h[j].scale[s]);
-  }
-#pragma unroll
-  for (int i = 0; i < MV; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) part[wave][i][j][lane] = c[i][j];
-  __syncthreads();
-  // a wavefront adds up and writes its share of the MV * NT tiles of 16 x 16
-  for (int k = wave; k < MV * NT; k += kFewWaves) {
-    const int i = k / NT, j = k % NT;
-    f32x4 z = part[0][i][j][lane];
-#pragma unroll
-    for (int p = 1; p < kFewWaves; ++p) z += part[p][i][j][lane];
-    const int t = t0 + 16 * j + (lane & 15), v = v0 + 16 * i + 4 * quarter;
-    if (t < n_rows) {
-      O* o = out + (long long)t * out_stride + v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (v + e < vocab) Vec<O>::store1(o + e, z[e]);
-    }
-  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // copies for nobody land before the LDS is given back
 }
 
 // ---- many rows ----------------------------------------------------------------------------------------------------------
@@ -136,10 +200,11 @@ __global__ __launch_bounds__(kFewThreads) void mxfp4_few_rows_kernel(Mxfp4Rows h
 // for two steps at a time.  A workgroup walks through its tiles without a pause: the first step of the next tile is copied during
 // the last of this one.
 //
-// The products are written as instructions: the compiler's own form of one may be moved past the barriers, and a step's worth
-// of fragments and accumulators with it.  It does not know what such a statement is, so what it would wait for is waited for
-// here: wait() stands between an ordinary instruction that writes scales or accumulators and the products, and settle()
+// The products are written as instructions: the compiler's own form of one may be moved past barriers and waits, and the
+// fragments and accumulators of a whole step with it.  It does not know what such a statement is, so what it would wait for is
+// waited for here: wait() stands between an ordinary instruction that writes an operand and the products, and settle()
 // between the products and the first look at their sums.  Fragments come from LDS reads, whose arrival it does wait for.
+// c += w h over four blocks, the scales in byte S of the words.
 template <int S>
 __device__ __forceinline__ void product(f32x4& c, i32x4 w, uint32_t w_scale, i32x4 h, uint32_t h_scale) {
   if constexpr (S == 0)
@@ -163,13 +228,7 @@ constexpr int kTileV = 256;
 constexpr int kNI = 8;                                        // MFMA tiles of a wavefront along the vocabulary
 constexpr int kAhead = 2;
 constexpr int kStepBlocks = 8;
-constexpr int kRowBytes = 16 * kStepBlocks;                   // of a step's slice
 
-// Chunk c of a slice's row lies at position c ^ swizzle(row): the 16 rows that a fragment read touches lie in different 16-byte
-// bank groups.  The rows of a fragment are consecutive ones of the hidden states; of the embedding they are four fours, eight
-// apart (see tile_entry).
-__device__ __forceinline__ int swizzle_h(int row) { return (row >> 1) & 7; }
-__device__ __forceinline__ int swizzle_w(int row) { return (row >> 1 & 1) | (row >> 2 & 6); }
 // First of the four entries, inside the wavefront's 128, that MFMA tile i leaves in a lane of this quarter: two tiles are 32
 // entries, eight consecutive ones to a lane.
 __device__ __forceinline__ int tile_entry(int i, int quarter) { return 32 * (i >> 1) + 8 * quarter + 4 * (i & 1); }
@@ -425,25 +484,42 @@ int launch_tiles(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4R
   return hip_fail(ctx, hipGetLastError());
 }
 
-template <typename O, int MV, int NT>
-int launch_few(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks, O* out,
-               long long out_stride) {
-  const dim3 grid((unsigned)((vocab + 16LL * MV - 1) / (16 * MV)), (unsigned)((n_rows + 16 * NT - 1) / (16 * NT)));
-  mxfp4_few_rows_kernel<O, MV, NT><<<grid, dim3(kFewThreads), 0, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, out,
-                                                                               out_stride);
+template <typename O, int NT, int GPW>
+int launch_stream(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks, O* out,
+                  long long out_stride) {
+  auto kernel = mxfp4_stream_kernel<O, NT, GPW>;
+  constexpr int kBytes = StreamLds<NT, GPW>::kBytes;
+  static std::once_flag once[kMaxDevices];
+  static bool ok[kMaxDevices];
+  if (!allow_dynamic_lds(ctx, reinterpret_cast<const void*>(kernel), kBytes, once, ok)) return hip_fail(ctx, hipErrorInvalidValue);
+  const int tiles = (vocab + 15) / 16;
+  const dim3 grid((unsigned)std::min(tiles, ctx->n_cus), (unsigned)((n_rows + 16 * NT - 1) / (16 * NT)));
+  const int fours = reinterpret_cast<uintptr_t>(out) % (4 * sizeof(O)) == 0 && out_stride % 4 == 0;
+  kernel<<<grid, dim3(kStreamThreads), kBytes, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, out, out_stride, fours);
   return hip_fail(ctx, hipGetLastError());
 }
 
 template <typename O>
 int launch_typed(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks, O* out,
                  long long out_stride) {
-  if (n_rows <= 16) return launch_few<O, 1, 1>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
-  if (n_rows <= 32) return launch_few<O, 2, 2>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+  const int groups = (blocks + kGroup - 1) / kGroup;
+#ifndef STREAM_ROWS
+#define STREAM_ROWS 64
+#endif
+  if (n_rows <= STREAM_ROWS && groups <= (n_rows <= 32 ? 4 : 2) * kStreamWaves) {
+    auto stream = [&](auto nt) {
+      constexpr int NT = decltype(nt)::value;
+      if (groups <= kStreamWaves) return launch_stream<O, NT, 1>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+      if constexpr (NT <= 2) {
+        if (groups > 2 * kStreamWaves) return launch_stream<O, NT, 4>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+      }
+      return launch_stream<O, NT, 2>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+    };
+    if (n_rows <= 16) return stream(std::integral_constant<int, 1>{});
+    if (n_rows <= 32) return stream(std::integral_constant<int, 2>{});
+    return stream(std::integral_constant<int, 4>{});
+  }
   const bool ragged = blocks % kGroup != 0;
-  // the tile kernel's offsets inside a tile are 32 bits wide
-  if (std::max(std::max(weight.codes_stride, hidden.codes_stride), std::max(weight.scales_stride, hidden.scales_stride)) >=
-      0xffffffffLL / kTileV)
-    return launch_few<O, 2, 2>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
   auto tiles = [&](auto nj) {
     constexpr int NJ = decltype(nj)::value;
     return ragged ? launch_tiles<O, NJ, true>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride)
