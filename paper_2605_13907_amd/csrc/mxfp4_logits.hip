@@ -107,17 +107,22 @@ __global__ __launch_bounds__(kStreamThreads) __attribute__((amdgpu_waves_per_eu(
     unsigned char* to = ring + slot * L::kSlot;
     const int v0 = tile * 16;
 #pragma unroll
-    for (int g = 0; g < GPW; ++g)
+    for (int g = 0; g < GPW; ++g) {
+      unsigned char* codes = to + g * 16 * 2 * kRowBytes;
+      if (block0 + g * kGroup < blocks) {
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const int row = 8 * q + crow;
-          const int b = block0 + g * kGroup + half * 8 + ((lane & 7) ^ swizzle_h(row));
+        for (int k = 0; k < 4; ++k) {
+          const int row = 8 * (k & 1) + crow, b = block0 + g * kGroup + 8 * (k >> 1) + ((lane & 7) ^ swizzle_h(row));
           const unsigned char* src =
               weight.codes + (long long)min(v0 + row, vocab - 1) * weight.codes_stride + 16LL * min(b, blocks - 1);
-          __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(to + ((g * 2 + half) * 16 + 8 * q) * kRowBytes), 16, 0, 0);
+          __builtin_amdgcn_global_load_lds((glb_ptr)src, (lds_ptr)(codes + k * 8 * kRowBytes), 16, 0, 2 /* non-temporal */);
         }
+      } else {                                                 // nothing there: as many instructions, of a line that is at hand
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          __builtin_amdgcn_global_load_lds((glb_ptr)hidden.codes, (lds_ptr)(codes + k * 8 * kRowBytes), 16, 0, 0);
+      }
+    }
 #pragma unroll
     for (int g = 0; g < GPW; ++g) {
       const int b = block0 + g * kGroup + 4 * (lane & 3);
@@ -511,7 +516,8 @@ int launch_typed(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4R
       constexpr int NT = decltype(nt)::value;
       if (groups <= kStreamWaves) return launch_stream<O, NT, 1>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
       if constexpr (NT <= 2) {
-        if (groups > 2 * kStreamWaves) return launch_stream<O, NT, 4>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+        if (groups > 3 * kStreamWaves) return launch_stream<O, NT, 4>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+        if (groups > 2 * kStreamWaves) return launch_stream<O, NT, 3>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
       }
       return launch_stream<O, NT, 2>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
     };
