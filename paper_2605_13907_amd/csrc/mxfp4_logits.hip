@@ -508,32 +508,34 @@ template <typename O>
 int launch_typed(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks, O* out,
                  long long out_stride) {
   const int groups = (blocks + kGroup - 1) / kGroup;
-#ifndef STREAM_ROWS
-#define STREAM_ROWS 64
-#endif
-  if (n_rows <= STREAM_ROWS && groups <= (n_rows <= 32 ? 4 : 2) * kStreamWaves) {
-    auto stream = [&](auto nt) {
-      constexpr int NT = decltype(nt)::value;
-      if (groups <= kStreamWaves) return launch_stream<O, NT, 1>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
-      if constexpr (NT <= 2) {
-        if (groups > 3 * kStreamWaves) return launch_stream<O, NT, 4>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
-        if (groups > 2 * kStreamWaves) return launch_stream<O, NT, 3>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
-      }
-      return launch_stream<O, NT, 2>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+  // Few rows of long contractions: the stream.  A tile of it costs the same however short its quarters are, and 64 rows want
+  // twice the registers of 32.  us, stream and tiles, with the quantisation of the hidden states: 16 rows x 151,936 x 512 25.2 and
+  // 17.0, x 1,024 27.2 and 23.7, x 4,096 65.0 and 87.4, 16 x 50,257 x 1,100 20.6 and 20.1; 4 x 32,000 x 2,048 14.8 and 16.7, x 4,096 (one
+  // row) 19.2 and 23.6; 32 x 151,936 x 1,024 34.0 and 25.6, x 2,048 41.9 and 49.9, x 4,096 70.8 and 91.5, x 8,192 125 and 179; 64 x
+  // 50,304 x 2,048 28.0 and 20.0, x 151,936 x 2,048 51.3 and 52.7, x 4,096 80.0 and 97.7, x 64,000 x 4,096 42.9 and 41.2.
+  auto stream = [&](auto nt, auto gpw) {
+    return launch_stream<O, decltype(nt)::value, decltype(gpw)::value>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+  };
+  typedef std::integral_constant<int, 1> One;
+  typedef std::integral_constant<int, 2> Two;
+  typedef std::integral_constant<int, 3> Three;
+  typedef std::integral_constant<int, 4> Four;
+  if (n_rows <= 32 && groups >= 4 && groups <= 16) {
+    auto rows = [&](auto nt) {
+      return groups <= 4 ? stream(nt, One{}) : groups <= 8 ? stream(nt, Two{}) : groups <= 12 ? stream(nt, Three{}) : stream(nt, Four{});
     };
-    if (n_rows <= 16) return stream(std::integral_constant<int, 1>{});
-    if (n_rows <= 32) return stream(std::integral_constant<int, 2>{});
-    return stream(std::integral_constant<int, 4>{});
+    return n_rows <= 16 ? rows(One{}) : rows(Two{});
   }
+  if (n_rows <= 64 && groups > 4 && groups <= 8) return stream(Four{}, Two{});
   const bool ragged = blocks % kGroup != 0;
   auto tiles = [&](auto nj) {
     constexpr int NJ = decltype(nj)::value;
     return ragged ? launch_tiles<O, NJ, true>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride)
                   : launch_tiles<O, NJ, false>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
   };
-  if (n_rows <= 64) return tiles(std::integral_constant<int, 1>{});
-  if (n_rows <= 128) return tiles(std::integral_constant<int, 2>{});
-  return tiles(std::integral_constant<int, 4>{});
+  if (n_rows <= 64) return tiles(One{});
+  if (n_rows <= 128) return tiles(Two{});
+  return tiles(Four{});
 }
 
 }  // namespace

@@ -5,16 +5,20 @@
 // numbers are read for the kept tokens alone.  The kept tokens are a prefix of the ranking by (logit, index), so what a limit
 // asks for is the place of a cut in that ranking: after k tokens, or where the mass before a token reaches its share.
 //
-// A workgroup owns a row.  One pass finds the largest logit and the sum of the exponentials.  A bound from it leaves a few
-// candidates of the ranking's head:
-//   top-k   the k-th largest of the threads' own maxima: at least k logits are no smaller;
-//   top-p   tokens of at most (1 - top_p) / vocab of the mass each hold no more than 1 - top_p together;
-//   min-p   its own condition.
-// A second pass collects them in LDS, where they are sorted and their masses summed.  If there are more than LDS holds, passes
-// that count tokens and mass in 2,048 ranges of the ranking narrow the cut down to one range until it does.
+// A workgroup owns a row.  A row without limits takes one pass over logits and random numbers.  Otherwise one pass finds the
+// largest logit, the sum of the exponentials, and each thread's own largest logit, of which a wavefront then makes a bound
+// that leaves little more than the kept tokens:
+//   top-k   the k-th largest of the threads' own: at least k logits are no smaller;
+//   top-p   where the masses of the threads' own alone reach the share;
+//   min-p   is a bound itself.
+// A second pass collects what is no smaller in LDS.  Up to 64 tokens are sorted, summed and drawn from by one wavefront in its
+// registers, up to 2,048 by the workgroup.  Where there is no such bound (flat rows, or more tokens than threads), tokens and
+// their masses are counted in 2,048 ranges of the exponent, and the range in which the cut lies is sorted.
 // Masses are summed as fixed-point numbers, so no result depends on the order in which threads arrive.
 #include "ais_internal.h"
 #include "device_utils.h"
+
+#include <type_traits>
 
 namespace ais {
 namespace {
@@ -50,18 +54,29 @@ struct SampleShared {
   u64 mass[kBins];
   u64 keys[kCap];
   uint32_t count[kBins];
+  float own_top[kThreads];
   u64 wave_mass[kWaves];
   uint32_t wave_count[kWaves];
   float wave_max[kWaves];
   MaxSum wave_sum[kWaves];
   Best wave_best[kWaves];
+  float least;
+  int bounded;
   uint32_t n;
   int bin;                             // the range that holds the cut, -1: none does
   uint32_t bin_count;                  // its tokens
   u64 above_mass;                      // of the tokens before it
   uint32_t above_count;
-  u64 total;
 };
+
+// Element j of a vector.
+template <typename T>
+__device__ __forceinline__ float element(u32x4 q, int j) {
+  const int w = j * (int)sizeof(T) / 4;
+  const uint32_t word = w < 2 ? (w == 0 ? q[0] : q[1]) : (w == 2 ? q[2] : q[3]);
+  if constexpr (sizeof(T) == 4) return __uint_as_float(word);
+  return __uint_as_float((j & 1) ? word & 0xffff0000u : word << 16);
+}
 
 // A row and how its tokens are ranked.
 template <typename T>
@@ -79,16 +94,20 @@ struct Row {
   __device__ __forceinline__ float value(u64 key) const { return from_ordered(~(uint32_t)(key >> index_bits)); }
   __device__ __forceinline__ int token(u64 key) const { return (int)(key & ((1ull << index_bits) - 1)); }
 
-  // f(logits, first index) of every vector and g(logit, index) of every element outside the vectors.
-  template <typename F, typename G>
-  __device__ __forceinline__ void visit(F f, G g) const {
+  // f(logits, first index) of every kUnroll vectors, their logits one after the other, and g(logit, index) of every element outside
+  // them.  In f the logits of vector u begin at u N and have the index v + u kThreads N.
+  template <int kUnroll, typename F, typename F1, typename G>
+  __device__ __forceinline__ void visit(F f, F1 f1, G g) const {
     constexpr int N = Vec<T>::N;
     const u32x4* zv = reinterpret_cast<const u32x4*>(z + head);
-    for (int i = threadIdx.x; i < nvec; i += kThreads) {
-      float x[N];
-      Vec<T>::unpack(zv[i], x);
-      f(x, head + i * N);
+    int i = threadIdx.x;
+    for (; i + (kUnroll - 1) * kThreads < nvec; i += kUnroll * kThreads) {
+      u32x4 q[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) q[u] = zv[i + u * kThreads];
+      f(q, head + i * N);
     }
+    for (; i < nvec; i += kThreads) f1(zv[i], head + i * N);
     const int r = threadIdx.x;
     if (r < rest) {
       const int v = r < head ? r : nvec * N + r;
@@ -99,17 +118,29 @@ struct Row {
   template <typename F>
   __device__ __forceinline__ void visit_from(float least, F f) const {
     constexpr int N = Vec<T>::N;
-    visit(
-        [&](const float* x, int v) {
-          float m = x[0];
+    auto one = [&](u32x4 q, int v) {
+      float x[N];
+      Vec<T>::unpack(q, x);
+      float m = x[0];
 #pragma unroll
-          for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
-          if (m >= least) {
+      for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
+      if (m >= least) {
+        uint32_t found = 0;
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-              if (x[j] >= least) f(x[j], v + j);
-          }
+        for (int j = 0; j < N; ++j) found |= (uint32_t)(x[j] >= least) << j;
+        while (found != 0) {                           // one copy of f, whatever the vector holds
+          const int j = __builtin_ctz(found);
+          found &= found - 1;
+          f(element<T>(q, j), v + j);
+        }
+      }
+    };
+    visit<4>(
+        [&](const u32x4* q, int v) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) one(q[u], v + u * kThreads * N);
         },
+        one,
         [&](float x, int v) {
           if (x >= least) f(x, v);
         });
@@ -118,9 +149,13 @@ struct Row {
 
 __device__ __forceinline__ float clamped_noise(float e) { return fmaxf(fminf(e, 3.0e38f), 1.17549435e-38f); }
 
-__device__ __forceinline__ Best block_best(Best b, SampleShared& sh) {
+__device__ __forceinline__ Best wave_best(Best b) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) b = better(b, Best{__shfl_xor(b.score, d), __shfl_xor(b.token, d)});
+  return b;
+}
+__device__ __forceinline__ Best block_best(Best b, SampleShared& sh) {
+  b = wave_best(b);
   if ((threadIdx.x & 63) == 0) sh.wave_best[threadIdx.x >> 6] = b;
   __syncthreads();
   b = sh.wave_best[0];
@@ -210,16 +245,20 @@ __device__ Cut cut_sorted(const Row<T>& row, uint32_t n, uint32_t above_count, u
   return cut;
 }
 
-// The cut among the tokens whose keys lie in [lo, hi) and whose logits are no smaller than `least`, before which none is
-// left out.
+// The cut of the whole row: the tokens no smaller than `least`, and of those that `depth` (in log2 of the mass) below the largest
+// or deeper only the last range knows.
 template <typename T>
-__device__ Cut cut_row(const Row<T>& row, float least, u64 lo, u64 hi, uint32_t limit_count, u64 limit_mass,
+__device__ Cut cut_row(const Row<T>& row, float least, float depth, uint32_t limit_count, u64 limit_mass, bool by_mass,
                        SampleShared& sh) {
+  const float per_range = (float)kBins / depth;
+  auto range_of = [&](float x) { return (int)fminf(-row.exponent(x) * per_range, (float)(kBins - 1)); };
+  int within = -1;                                     // the range that the ones below are parts of
   uint32_t above_count = 0;
-  u64 above_mass = 0;
+  u64 above_mass = 0, lo = 0, hi = kNoLimit;
   while (true) {
     int shift = 0;
-    while (((hi - lo - 1) >> shift) >= (u64)kBins) ++shift;
+    if (within >= 0)
+      while (((hi - lo - 1) >> shift) >= (u64)kBins) ++shift;
     __syncthreads();
     for (int b = threadIdx.x; b < kBins; b += kThreads) {
       sh.count[b] = 0;
@@ -230,14 +269,19 @@ __device__ Cut cut_row(const Row<T>& row, float least, u64 lo, u64 hi, uint32_t 
       sh.n = 0;
     }
     __syncthreads();
-    row.visit_from(least, [&](float x, int v) {
-      const u64 k = row.key(x, v);
-      if (k >= lo && k < hi) {
-        const uint32_t bin = (uint32_t)((k - lo) >> shift);
-        atomicAdd(&sh.count[bin], 1u);
-        atomicAdd(&sh.mass[bin], row.mass(x));
-      }
-    });
+    auto add = [&](uint32_t bin, float x) {
+      atomicAdd(&sh.count[bin], 1u);
+      if (by_mass) atomicAdd(&sh.mass[bin], row.mass(x));
+    };
+    if (within < 0) {
+      row.visit_from(least, [&](float x, int) { add((uint32_t)range_of(x), x); });
+    } else {
+      row.visit_from(least, [&](float x, int v) {
+        if (range_of(x) != within) return;
+        const u64 k = row.key(x, v);
+        if (k >= lo && k < hi) add((uint32_t)((k - lo) >> shift), x);
+      });
+    }
     __syncthreads();
     const int b0 = 2 * threadIdx.x;
     const uint32_t c0 = sh.count[b0], c1 = sh.count[b0 + 1];
@@ -257,16 +301,27 @@ __device__ Cut cut_row(const Row<T>& row, float least, u64 lo, u64 hi, uint32_t 
     look(b0, before.count, before.mass, c0, m0);
     look(b0 + 1, before.count + c0, before.mass + m0, c1, m1);
     __syncthreads();
-    if (sh.bin < 0) return Cut{hi, above_count + before.all_count, above_mass + before.all_mass};
-    const u64 width = 1ull << shift;
-    const u64 start = lo + ((u64)sh.bin << shift);
-    hi = hi - start < width ? hi : start + width;
-    lo = start;
+    const int bin = sh.bin;
+    if (bin < 0) return Cut{hi, above_count + before.all_count, above_mass + before.all_mass};
+    if (within < 0) {
+      // the keys of the range's logits, with room for the rounding of their exponents
+      within = bin;
+      const float upper = row.top - (float)bin / per_range / row.c, lower = row.top - (float)(bin + 1) / per_range / row.c;
+      const float room = 1e-5f * (fabsf(row.top) + fabsf(lower));
+      lo = row.key(fminf(upper + room, row.top), 0);
+      hi = row.key(bin == kBins - 1 ? -3.4028235e38f : fmaxf(lower - room, -3.4028235e38f), row.vocab - 1) + 1;
+    } else {
+      const u64 width = 1ull << shift;
+      const u64 start = lo + ((u64)bin << shift);
+      hi = hi - start < width ? hi : start + width;
+      lo = start;
+    }
     above_count = sh.above_count;
     above_mass = sh.above_mass;
     const uint32_t n = sh.bin_count;
     if (n > (uint32_t)kCap) continue;
     row.visit_from(least, [&](float x, int v) {
+      if (range_of(x) != within) return;
       const u64 k = row.key(x, v);
       if (k >= lo && k < hi) sh.keys[atomicAdd(&sh.n, 1u)] = k;
     });
@@ -274,6 +329,108 @@ __device__ Cut cut_row(const Row<T>& row, float least, u64 lo, u64 hi, uint32_t 
     sort_keys(n, sh);
     return cut_sorted(row, n, above_count, above_mass, limit_count, limit_mass, hi, sh);
   }
+}
+
+// What a row's limits ask for.
+struct Limits {
+  bool by_count, by_mass, by_share;
+  uint32_t count;
+  float top_p, share;                  // share: log2 of min-p
+  u64 mass;                            // that top-p without top-k ends at
+  __device__ __forceinline__ u64 part_of(double m) const { return (u64)fmax((double)top_p * m, 1.0); }
+};
+
+// A bound on the kept logits from the threads' own largest, by one wavefront; false if they allow none.
+template <typename T>
+__device__ bool bound(const Row<T>& row, const Limits& lim, float total, const float* own_top, float* least) {
+  constexpr int kOwn = kThreads / 64;
+  const int lane = threadIdx.x & 63;
+  float v[kOwn];
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) v[j] = own_top[j * 64 + lane];
+  if (lim.by_count) {
+    auto count = [&](float from) {
+      uint32_t c = 0;
+#pragma unroll
+      for (int j = 0; j < kOwn; ++j) c += (uint32_t)__builtin_popcountll(__ballot(v[j] >= from));
+      return c;
+    };
+    const float lowest = -3.4028235e38f;
+    if (count(lowest) < lim.count) return false;
+    uint32_t lo = ordered(lowest), hi = ordered(row.top);
+    const uint32_t enough = lim.count + (lim.count >> 3) + 2;
+    while (hi - lo > 1) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      const uint32_t c = count(from_ordered(mid));
+      if (c < lim.count) {
+        hi = mid;
+      } else {
+        lo = mid;
+        if (c <= enough) break;
+      }
+    }
+    *least = from_ordered(lo);
+    return true;
+  }
+  float p[kOwn];
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) p[j] = exp2_fast(row.exponent(v[j]));
+  auto mass = [&](float from) {
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j) m += v[j] >= from ? p[j] : 0.f;
+    return wave_sum(m);
+  };
+  // rounding of the sums must not cost a token that the fixed-point sums keep
+  const float wanted = lim.top_p * total * 1.00001f;
+  float hi = row.top, lo = row.top - 32.f / row.c;
+  if (!(mass(lo) >= wanted)) return false;
+  for (int k = 0; k < 13; ++k) {
+    const float mid = 0.5f * (lo + hi);
+    if (mass(mid) >= wanted) lo = mid;
+    else hi = mid;
+  }
+  *least = lo;
+  return true;
+}
+
+struct Drawn {
+  Best best;
+  u64 kept_mass;
+};
+
+// Up to 64 candidates, by one wavefront: sorted by exchanges between its lanes, lane i then has the i-th.
+template <typename T, typename S>
+__device__ Drawn draw_from_few(const Row<T>& row, const Limits& lim, uint32_t n, const u64* keys, S scored) {
+  const uint32_t i = threadIdx.x & 63;
+  u64 key = i < n ? keys[i] : kNoLimit;
+#pragma unroll
+  for (uint32_t run = 2; run <= 64; run <<= 1)
+#pragma unroll
+    for (uint32_t d = run >> 1; d > 0; d >>= 1) {
+      const u64 other = __shfl_xor(key, (int)d);
+      const bool keep_less = ((i & d) == 0) == ((i & run) == 0);
+      key = (other < key) == keep_less ? other : key;
+    }
+  const float x = i < n ? row.value(key) : row.top;
+  const u64 m = i < n ? row.mass(x) : 0;
+  auto sum_to = [&](u64 own) {
+    u64 s = own;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const u64 p = __shfl_up(s, d);
+      if ((int)i >= d) s += p;
+    }
+    return s;
+  };
+  const u64 upto = sum_to(m);
+  u64 limit = lim.mass;
+  if (lim.by_count && lim.by_mass) limit = lim.part_of((double)__shfl(upto, (int)min(n, lim.count) - 1));
+  const bool kept = i < n && i < lim.count && upto - m < limit && row.exponent(x) >= lim.share;
+  Drawn d{{-__builtin_inff(), row.vocab}, __shfl(sum_to(kept ? m : 0), 63)};
+  if (kept) d.best = scored(x, row.token(key));
+  d.best = wave_best(d.best);
+  return d;
 }
 
 template <typename T>
@@ -297,20 +454,26 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     return;
   }
   const float temperature = limits.temperature != nullptr ? limits.temperature[r] : 1.f;
-  const float top_p = limits.top_p != nullptr ? limits.top_p[r] : 1.f;
   const float min_p = limits.min_p != nullptr ? limits.min_p[r] : 0.f;
   int k = limits.top_k != nullptr ? limits.top_k[r] : 0;
+  Limits lim;
+  lim.top_p = limits.top_p != nullptr ? limits.top_p[r] : 1.f;
   auto refuse = [&] {
     if (tid == 0) atomicOr(status, AIS_STATUS_BAD_ROW);
     answer(-1, 0.f, 0.f);
   };
   const bool greedy = temperature == 0.f;
-  if (!(temperature >= 0.f) || temperature > 3.0e38f || top_p != top_p || min_p != min_p) {
+  if (!(temperature >= 0.f) || temperature > 3.0e38f || lim.top_p != lim.top_p || min_p != min_p) {
     refuse();
     return;
   }
-  if (greedy || top_p <= 0.f || min_p > 1.f) k = 1;
-  const bool by_count = k > 0 && k < vocab, by_mass = top_p < 1.f && k != 1, by_share = min_p > 0.f && k != 1;
+  if (greedy || lim.top_p <= 0.f || min_p > 1.f) k = 1;
+  lim.by_count = k > 0 && k < vocab;
+  lim.by_mass = lim.top_p < 1.f;
+  lim.by_share = min_p > 0.f;
+  lim.count = lim.by_count ? (uint32_t)k : 0xffffffffu;
+  lim.share = lim.by_share ? log2_fast(min_p) : -__builtin_inff();
+  lim.mass = kNoLimit;
 
   Row<T> row;
   row.z = logits + r * row_stride;
@@ -321,27 +484,79 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   row.index_bits = vocab > 1 ? 32 - __builtin_clz((unsigned)(vocab - 1)) : 1;
   row.mass_bits = min(40, 62 - row.index_bits);
   row.c = greedy ? kLog2e : kLog2e / temperature;
+  const float* e = noise + r * noise_stride;
+  const bool open = k != 1 && !lim.by_count && !lim.by_mass && !lim.by_share;
 
-  // ---- the largest logit and the sum of the exponentials ----
+  // ---- the largest logit and the sum of the exponentials; without limits the draw as well ----
   MaxSum st{kNegHuge, 0.f};
   float top = -__builtin_inff();
-  row.visit(
-      [&](const float* x, int) {
-        accumulate<N>(x, row.c, st);
+  Best best{-__builtin_inff(), vocab};
+  auto fold = [&](const float* x, auto count) {
+    constexpr int n = decltype(count)::value;
+    accumulate<n>(x, row.c, st);
 #pragma unroll
-        for (int j = 0; j < N; ++j) top = fmaxf(top, x[j]);
-      },
-      [&](float x, int) {
-        accumulate<1>(&x, row.c, st);
-        top = fmaxf(top, x);
-      });
-  const float own_top = top;
+    for (int j = 0; j < n; ++j) top = fmaxf(top, x[j]);
+  };
+  if (open) {
+    // indices rise, so that an equal score does not take a lower one's place; the threads' best are scored again below, relative
+    // to the largest logit
+    auto race = [&](float x, float noise_of, int v) {
+      const float score = __builtin_fmaf(x, row.c, -log2_fast(clamped_noise(noise_of)));
+      if (score > best.score) best = Best{score, v};
+    };
+    auto one = [&](u32x4 q, int v) {
+      float x[N], w[N];
+      Vec<T>::unpack(q, x);
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = __builtin_nontemporal_load(e + v + j);
+      fold(x, std::integral_constant<int, N>{});
+#pragma unroll
+      for (int j = 0; j < N; ++j) race(x[j], w[j], v + j);
+    };
+    row.template visit<2>(
+        [&](const u32x4* q, int v) {
+          float x[2 * N], w[2 * N];
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) w[u * N + j] = __builtin_nontemporal_load(e + v + u * kThreads * N + j);
+#pragma unroll
+          for (int u = 0; u < 2; ++u) Vec<T>::unpack(q[u], x + u * N);
+          fold(x, std::integral_constant<int, 2 * N>{});
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) race(x[u * N + j], w[u * N + j], v + u * kThreads * N + j);
+        },
+        one,
+        [&](float x, int v) {
+          fold(&x, std::integral_constant<int, 1>{});
+          const float score = __builtin_fmaf(x, row.c, -log2_fast(clamped_noise(e[v])));
+          best = better(best, Best{score, v});
+        });
+  } else {
+    row.template visit<4>(
+        [&](const u32x4* q, int) {
+          float x[4 * N];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) Vec<T>::unpack(q[u], x + u * N);
+          fold(x, std::integral_constant<int, 4 * N>{});
+        },
+        [&](u32x4 q, int) {
+          float x[N];
+          Vec<T>::unpack(q, x);
+          fold(x, std::integral_constant<int, N>{});
+        },
+        [&](float x, int) { fold(&x, std::integral_constant<int, 1>{}); });
+    sh.own_top[tid] = top;
+  }
   st = wave_merge(st);
   top = wave_max(top);
   if ((tid & 63) == 0) {
     sh.wave_sum[tid >> 6] = st;
     sh.wave_max[tid >> 6] = top;
   }
+  if (tid == 0) sh.n = 0;
   __syncthreads();
   st = sh.wave_sum[0];
   for (int w = 0; w < kWaves; ++w) {
@@ -356,84 +571,99 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   }
   // the sum relative to the largest logit's exponential: st.m is the rounded product top * c
   const float total = st.s * exp2_fast(-__builtin_fmaf(top, row.c, -st.m));
-  const float* e = noise + r * noise_stride;
   auto scored = [&](float x, int v) { return Best{row.exponent(x) - log2_fast(clamped_noise(e[v])), v}; };
-  Best best{-__builtin_inff(), vocab};
-  u64 kept_mass = 0;
+  auto finish = [&](int token, u64 kept_mass) {
+    if (tid != 0) return;
+    if (token >= vocab) {                              // not reached: the first ranked token is always kept
+      answer(-1, 0.f, 0.f);
+      return;
+    }
+    const double at = (double)row.exponent(Vec<T>::load1(row.z + token)) * 0.6931471805599453;
+    const double full = at - log((double)total);
+    answer(token, (float)(kept_mass > 0 ? at - log(ldexp((double)kept_mass, -row.mass_bits)) : full), (float)full);
+  };
   if (k == 1) {
-    row.visit_from(top, [&](float x, int v) { best = better(best, Best{0.f, v}); });
+    best = Best{-__builtin_inff(), vocab};
+    row.visit_from(top, [&](float, int v) { best = better(best, Best{0.f, v}); });
     best = block_best(best, sh);
     answer(best.token, 0.f, greedy ? 0.f : (float)-log((double)total));
     return;
   }
-  if (!by_count && !by_mass && !by_share) {
-    row.visit_from(-3.4028235e38f, [&](float x, int v) { best = better(best, scored(x, v)); });
-  } else {
-    // ---- a bound on the logits that can be kept ----
-    float least = -3.4028235e38f;
-    float share = -__builtin_inff();                   // log2 of the least mass, by min-p
-    if (by_share) share = log2_fast(min_p);
-    if (by_count && k <= kThreads) {
-      sh.keys[tid] = (u64)(~ordered(own_top));
-      sort_keys(kThreads, sh);
-      const float pivot = from_ordered(~(uint32_t)sh.keys[k - 1]);
-      least = fmaxf(least, pivot);
-      __syncthreads();
-    }
-    if (!by_count) {
-      float low = share;
-      if (by_mass) low = fmaxf(low, log2_fast((1.f - top_p) * total / (float)vocab) - 0.01f);
-      // (x - top) c >= low, with room for its rounding: the condition itself is looked at again
-      least = fmaxf(least, top + low / row.c - 1e-5f * (fabsf(top) + fabsf(low / row.c)));
-    }
-    if (tid == 0) sh.n = 0;
-    __syncthreads();
-    row.visit_from(least, [&](float x, int v) {
-      if (!by_count && row.exponent(x) < share) return;
-      const uint32_t at = atomicAdd(&sh.n, 1u);
-      if (at < (uint32_t)kCap) sh.keys[at] = row.key(x, v);
-    });
-    __syncthreads();
-    const uint32_t n = sh.n;
-    const uint32_t limit_count = by_count ? (uint32_t)k : 0xffffffffu;
-    const u64 end_key = kNoLimit;
-    auto share_of = [&](double mass) { return (u64)fmax((double)top_p * mass, 1.0); };
-    const u64 limit_mass = by_mass && !by_count ? share_of(ldexp((double)total, row.mass_bits)) : kNoLimit;
-    Cut cut;
-    const bool listed = n <= (uint32_t)kCap;
-    if (listed) {
-      sort_keys(n, sh);
-      cut = cut_sorted(row, n, 0, 0, limit_count, limit_mass, end_key, sh);
-      if (by_count && by_mass) cut = cut_sorted(row, n, 0, 0, limit_count, share_of((double)cut.mass), end_key, sh);
-    } else {
-      const u64 lo = row.key(top, 0), hi = row.key(least, vocab - 1) + 1;
-      cut = cut_row(row, least, lo, hi, limit_count, limit_mass, sh);
-      if (by_count && by_mass) cut = cut_row(row, least, lo, hi, limit_count, share_of((double)cut.mass), sh);
-    }
-    // ---- the draw ----
-    // min-p beside top-k, or beside a list that was not made by it, ends the prefix earlier; its tokens' mass is summed here
-    auto look = [&](float x, u64 key) {
-      if (key >= cut.key || row.exponent(x) < share) return;
-      kept_mass += row.mass(x);
-      best = better(best, scored(x, row.token(key)));
-    };
-    if (listed) {
-      for (uint32_t i = tid; i < n; i += kThreads) look(row.value(sh.keys[i]), sh.keys[i]);
-    } else {
-      row.visit_from(least, [&](float x, int v) { look(x, row.key(x, v)); });
-    }
-    const Before sum = scan(0, kept_mass, sh);
-    kept_mass = sum.all_mass;
-  }
-  best = block_best(best, sh);
-  if (tid != 0) return;
-  if (best.token >= vocab) {                           // not reached: the first ranked token is always kept
-    answer(-1, 0.f, 0.f);
+  if (open) {
+    if (best.token < vocab) best = scored(Vec<T>::load1(row.z + best.token), best.token);
+    finish(block_best(best, sh).token, 0);
     return;
   }
-  const double at = (double)row.exponent(Vec<T>::load1(row.z + best.token)) * 0.6931471805599453;
-  const double full = at - log((double)total);
-  answer(best.token, (float)(kept_mass > 0 ? at - log(ldexp((double)kept_mass, -row.mass_bits)) : full), (float)full);
+  if (lim.by_mass && !lim.by_count) lim.mass = lim.part_of(ldexp((double)total, row.mass_bits));
+  // (x - top) c >= the least exponent, with room for its rounding: the condition itself is looked at again
+  auto from_exponent = [&](float low) { return top + low / row.c - 1e-5f * (fabsf(top) + fabsf(low / row.c)); };
+  const float lowest = -3.4028235e38f;
+  float least = lim.by_share && !lim.by_count ? fmaxf(from_exponent(lim.share), lowest) : lowest;
+  u64 kept_mass = 0, end_key = kNoLimit;
+  auto look = [&](float x, u64 key) {
+    if (key >= end_key || row.exponent(x) < lim.share) return;
+    kept_mass += row.mass(x);
+    best = better(best, scored(x, row.token(key)));
+  };
+  if (lim.by_count || lim.by_mass) {
+    // ---- candidates ----
+    if (tid < 64) {
+      float bounded = lowest;
+      const bool some = bound(row, lim, total, sh.own_top, &bounded);
+      if (tid == 0) {
+        sh.bounded = some;
+        sh.least = bounded;
+      }
+    }
+    __syncthreads();
+    uint32_t n = 0xffffffffu;
+    if (sh.bounded) {
+      const float from = fmaxf(least, sh.least);
+      row.visit_from(from, [&](float x, int v) {
+        const uint32_t at = atomicAdd(&sh.n, 1u);
+        if (at < (uint32_t)kCap) sh.keys[at] = row.key(x, v);
+      });
+      __syncthreads();
+      n = sh.n;
+    }
+    if (n <= 64) {
+      if (tid >= 64) return;
+      const Drawn d = draw_from_few(row, lim, n, sh.keys, scored);
+      finish(d.best.token, d.kept_mass);
+      return;
+    }
+    Cut cut;
+    if (n <= (uint32_t)kCap) {
+      sort_keys(n, sh);
+      cut = cut_sorted(row, n, 0, 0, lim.count, lim.mass, kNoLimit, sh);
+      if (lim.by_count && lim.by_mass) cut = cut_sorted(row, n, 0, 0, lim.count, lim.part_of((double)cut.mass), kNoLimit, sh);
+      end_key = cut.key;
+      for (uint32_t i = tid; i < n; i += kThreads) look(row.value(sh.keys[i]), sh.keys[i]);
+      best = block_best(best, sh);
+      kept_mass = scan(0, kept_mass, sh).all_mass;
+      finish(best.token, kept_mass);
+      return;
+    }
+    // tokens of at most (1 - top_p) / vocab of the mass each hold no more than 1 - top_p together
+    float depth = 64.f;
+    if (!lim.by_count) {
+      const float low = fmaxf(lim.share, log2_fast((1.f - lim.top_p) * total / (float)vocab) - 0.01f);
+      least = fmaxf(least, from_exponent(low));
+      depth = fmaxf(-low, 1.f);
+    }
+    // with both limits the first cut, by count, tells the mass that top-p is a share of
+    u64 limit_mass = lim.mass;
+    for (int pass = lim.by_count && lim.by_mass ? 0 : 1; pass < 2; ++pass) {
+      cut = cut_row(row, least, depth, lim.count, limit_mass, lim.by_mass, sh);
+      limit_mass = lim.part_of((double)cut.mass);
+    }
+    end_key = cut.key;
+  }
+  // ---- the draw from the row itself ----
+  row.visit_from(least, [&](float x, int v) { look(x, row.key(x, v)); });
+  best = block_best(best, sh);
+  kept_mass = scan(0, kept_mass, sh).all_mass;
+  finish(best.token, kept_mass);
 }
 
 }  // namespace
