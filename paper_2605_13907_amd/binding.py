@@ -595,7 +595,10 @@ class AisContext:
                 raise ValueError("dlogits must have the dtype, shape and strides of logits")
             _dev_ptr(dlogits, dev, "dlogits")
         elif want_grad:
-            dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=dev)
+            # lies like the logits relative to 128-byte lines: rows that begin anywhere can then be held, too
+            shift = logits.data_ptr() % 128 // logits.element_size()
+            dlogits = torch.empty(shift + (n_rows - 1) * row_stride + vocab if n_rows else 0, dtype=logits.dtype, device=dev)
+            dlogits = dlogits.as_strided(logits.shape, logits.stride(), shift if n_rows else 0)
         kl = torch.empty(n_rows, dtype=torch.float32, device=dev)
         loss = torch.empty(1, dtype=torch.float32, device=dev)
         self._sync_stream()

@@ -5,9 +5,13 @@
 //   kl = sum_j q_j (log q_j - log p[id_j]),  dz = weight / T (p - sum_j q_j 1[id_j])
 //
 // A workgroup owns a row.  Beside the soft-max over the vocabulary, which is all of the traffic, there is little: the listed
-// tokens' logits are gathered, and their elements of the gradient are written again once the row is there.  A token that is
-// listed twice counts with both entries: a small hash table finds the entries of one token, their q added as fixed-point
-// numbers, whose sum does not depend on the order.
+// tokens' logits are gathered, and their elements of the gradient differ from the others'.  A token that is listed twice counts
+// with both entries: a small hash table finds the entries of one token, their q added as fixed-point numbers, whose sum does
+// not depend on the order.
+//
+// Rows that fit are held by one compute unit, in registers and, beyond 20 vectors a lane, in LDS: one read and one write of the
+// row.  The loads of a row are all on their way before the teacher's part begins, which they hide; the listed tokens' elements are
+// put into the registers of the threads that hold them, so that the row leaves in one burst of stores.
 #include "ais_internal.h"
 #include "device_utils.h"
 
@@ -18,29 +22,32 @@ using namespace dev;
 
 typedef unsigned long long u64;
 
-constexpr int kRowThreads = 256;
-constexpr int kRowWaves = kRowThreads / 64;
 constexpr int kQBits = 62;             // q as a fixed-point number
 
-// What a row's listed tokens need of LDS: dynamic, `slots` (a power of two >= 2 n_top) of the table and n_top entries.
+// What a row's listed tokens need of LDS: `slots` (a power of two >= 2 n_top) of the table and n_top entries.
 struct Listed {
   u64* mass;                           // [slots] sum of q of the token in the slot
   int* token;                          // [slots] or -1
-  float* z;                            // [n_top] logit
-  int* slot;                           // [n_top] slot of an entry that writes its token's element, or -1
-  static size_t bytes(int n_top, int slots) { return (size_t)slots * 12 + (size_t)n_top * 8; }
+  float* t;                            // [n_top] the teacher's logit in base 2; -inf where there is no entry
+  float* z;                            // [n_top] the policy's
+  int* next;                           // [n_top] next entry of the same thread's row elements, or -1
+  int* slot;                           // [n_top] of an entry that stands for its token, else -1
+  static size_t bytes(int n_top, int slots) { return (size_t)slots * 12 + (size_t)n_top * 16; }
   __device__ __forceinline__ Listed(unsigned char* lds, int n_top, int slots) {
     mass = reinterpret_cast<u64*>(lds);
     token = reinterpret_cast<int*>(mass + slots);
-    z = reinterpret_cast<float*>(token + slots);
-    slot = reinterpret_cast<int*>(z + n_top);
+    t = reinterpret_cast<float*>(token + slots);
+    z = t + n_top;
+    next = reinterpret_cast<int*>(z + n_top);
+    slot = next + n_top;
   }
 };
 
+template <int THREADS>
 struct RowShared {
-  float top[kRowWaves];
-  double sum[kRowWaves];
-  MaxSum soft[kRowWaves];
+  MaxSum teacher[THREADS / 64], policy[THREADS / 64];
+  double kl[THREADS / 64];
+  int first[THREADS];                  // first entry of each thread's row elements, or -1
 };
 
 __device__ __forceinline__ double wave_sum64(double v) {
@@ -48,146 +55,386 @@ __device__ __forceinline__ double wave_sum64(double v) {
   for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
   return v;
 }
-__device__ __forceinline__ float row_max(float v, RowShared& sh) {
-  v = wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.top[threadIdx.x >> 6] = v;
-  __syncthreads();
+template <int WAVES>
+__device__ __forceinline__ MaxSum merge_all(const MaxSum* part) {
+  MaxSum st = part[0];
 #pragma unroll
-  for (int w = 0; w < kRowWaves; ++w) v = fmaxf(v, sh.top[w]);
-  return v;
+  for (int w = 1; w < WAVES; ++w) st = merge(st, part[w]);
+  return st;
 }
-__device__ __forceinline__ double row_sum(double v, RowShared& sh) {
-  v = wave_sum64(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.sum[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = sh.sum[0];
+
+// The arguments of a row's kernels.
+template <typename T>
+struct DistillArgs {
+  const T* logits;
+  long long row_stride;
+  int vocab;
+  const int* ids;
+  const float* teacher;
+  int n_top, slots;
+  const unsigned char* valid;
+  const float* weight;
+  float inv_rows, inv_temperature;
+  double exact;                        // what the fp32 factor of the exponents is off by (see exact_exponents)
+  float* kl;
+  T* dlogits;
+  long long dlogits_stride;
+  int* status;
+};
+
+// The teacher's side of a row, in steps that its kernel places among its own.
+template <typename T, int THREADS>
+struct Teacher {
+  const Listed listed;
+  RowShared<THREADS>& sh;
+  const DistillArgs<T>& a;
+  const long long row;
+  const float c;
+  MaxSum all;
+  __device__ __forceinline__ Teacher(unsigned char* lds, RowShared<THREADS>& sh, const DistillArgs<T>& a, long long row)
+      : listed(lds, a.n_top, a.slots), sh(sh), a(a), row(row), c(a.inv_temperature * kLog2e) {}
+  __device__ __forceinline__ bool entry(int id) const { return id >= 0 && id < a.vocab; }
+
+  // Entries to LDS, their sum to the workgroup; empties the table.  No barrier.
+  __device__ __forceinline__ void read() {
+    const int tid = threadIdx.x;
+    MaxSum st{kNegHuge, 0.f};
+    if (a.valid == nullptr || a.valid[row] != 0) {
+      for (int j = tid; j < a.n_top; j += THREADS) {
+        const int id = a.ids[row * a.n_top + j];
+        float t = a.teacher[row * a.n_top + j];
+        if (!entry(id)) {
+          t = kMasked;
+          if (id != -1) atomicOr(a.status, AIS_STATUS_BAD_TOKEN);
+        }
+        accumulate<1>(&t, c, st);
+        listed.t[j] = t;
+      }
+    }
+    for (int s = tid; s < a.slots; s += THREADS) {
+      listed.token[s] = -1;
+      listed.mass[s] = 0;
+    }
+    sh.first[tid] = -1;
+    st = wave_merge(st);
+    if ((tid & 63) == 0) sh.teacher[tid >> 6] = st;
+  }
+  // After a barrier: whether there is anything to learn from.
+  __device__ __forceinline__ bool any() {
+    all = merge_all<THREADS / 64>(sh.teacher);
+    return all.s != 0.f;
+  }
+  // q of an entry: NaN, all of them, where the teacher has a NaN or +inf
+  __device__ __forceinline__ float q(int j) const { return exp2_fast(__builtin_fmaf(listed.t[j], c, -all.m)) / all.s; }
+  __device__ __forceinline__ bool fine() const { return all.s < 3.0e38f; }
+  // Entries into the table.  An entry that stands for its token is put on the list of the thread that `owner` names.  No barrier.
+  template <typename F>
+  __device__ __forceinline__ void insert(const T* zr, F owner) {
+    for (int j = threadIdx.x; j < a.n_top; j += THREADS) {
+      const int id = a.ids[row * a.n_top + j];
+      int slot = -1;
+      if (entry(id)) {
+        listed.z[j] = Vec<T>::load1(zr + id);
+        int s = (int)(((uint32_t)id * 2654435761u) >> 16) & (a.slots - 1);
+        while (true) {                                 // the table has twice as many slots as there are entries
+          const int held = atomicCAS(&listed.token[s], -1, id);
+          if (held == -1) slot = s;
+          if (held == -1 || held == id) break;
+          s = (s + 1) & (a.slots - 1);
+        }
+        atomicAdd(&listed.mass[s], (u64)ldexp((double)(fine() ? q(j) : 0.f), kQBits));
+        if (slot >= 0) listed.next[j] = atomicExch(&sh.first[owner(id)], j);
+      }
+      listed.slot[j] = slot;
+    }
+  }
+  // log q - log p of every entry, weighted by q, with q = 2^(t c - all.m) / all.s and p = 2^(z c - st.m) / st.s.  To the
+  // workgroup; no barrier.
+  __device__ __forceinline__ void diverge(MaxSum st) {
+    const int tid = threadIdx.x;
+    const double log_ratio = log((double)all.s) - log((double)st.s), ln2 = 0.6931471805599453 * a.exact;
+    double kl = 0.0;
+    for (int j = tid; j < a.n_top; j += THREADS) {
+      const float p = q(j);
+      if (p <= 0.f) continue;
+      const double t2 = (double)listed.t[j] * (double)c - (double)all.m, z2 = (double)listed.z[j] * (double)c - (double)st.m;
+      kl += (double)p * ((t2 - z2) * ln2 - log_ratio);
+    }
+    kl = wave_sum64(kl);
+    if ((tid & 63) == 0) sh.kl[tid >> 6] = kl;
+  }
+  // After a barrier, by thread 0.
+  __device__ __forceinline__ void report() const {
+    if (threadIdx.x != 0) return;
+    double kl = sh.kl[0];
 #pragma unroll
-  for (int w = 1; w < kRowWaves; ++w) v += sh.sum[w];
-  return v;
-}
+    for (int w = 1; w < THREADS / 64; ++w) kl += sh.kl[w];
+    a.kl[row] = (float)kl;
+  }
+  // Element of the gradient of an entry's token, less the factor g.
+  __device__ __forceinline__ float element(int j, MaxSum st) const {
+    const float sum = fine() ? (float)ldexp((double)listed.mass[listed.slot[j]], -kQBits) : __builtin_nanf("");
+    return exp2_fast(__builtin_fmaf(listed.z[j], c, -st.m)) / st.s - sum;
+  }
+  __device__ __forceinline__ float weight() const {
+    return (a.weight == nullptr ? a.inv_rows : a.weight[row]) * a.inv_temperature;
+  }
+};
+
+// ---- rows that are read twice: any width and alignment, and the loss alone ----------------------------------------------------
+constexpr int kTwiceThreads = 256;
 
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void distill_kernel(
-    const T* logits, long long row_stride, int vocab, const int* __restrict__ ids, const float* __restrict__ teacher, int n_top,
-    int slots, const unsigned char* __restrict__ valid, const float* __restrict__ weight, float inv_rows, float inv_temperature,
-    float* __restrict__ kl_out, T* dlogits, long long dlogits_stride, int* __restrict__ status) {
-  constexpr int N = Vec<T>::N;
+__global__ __launch_bounds__(kTwiceThreads) void distill_twice_kernel(const DistillArgs<T> a) {
+  constexpr int N = Vec<T>::N, kAhead = 4;
   extern __shared__ __align__(16) unsigned char lds[];
-  __shared__ RowShared sh;
-  const Listed listed(lds, n_top, slots);
+  __shared__ RowShared<kTwiceThreads> sh;
   const long long row = blockIdx.x;
-  const int tid = threadIdx.x;
-  const T* zr = logits + row * row_stride;
-  T* dr = dlogits == nullptr ? nullptr : dlogits + row * dlogits_stride;
-  const int* id_row = ids + row * n_top;
-  const float* t_row = teacher + row * n_top;
-  const float c = inv_temperature * kLog2e;
-
-  // ---- the teacher's distribution ----
-  float top = -__builtin_inff();
-  if (valid == nullptr || valid[row] != 0) {
-    for (int j = tid; j < n_top; j += kRowThreads) {
-      const int id = id_row[j];
-      if (id >= 0 && id < vocab) top = fmaxf(top, t_row[j]);
-      else if (id != -1) atomicOr(status, AIS_STATUS_BAD_TOKEN);
-    }
-    top = row_max(top, sh);
-  }
-  if (top == -__builtin_inff()) {                      // nothing to learn from: no loss, no gradient
-    if (tid == 0) kl_out[row] = 0.f;
+  const int tid = threadIdx.x, vocab = a.vocab;
+  const T* zr = a.logits + row * a.row_stride;
+  T* dr = a.dlogits == nullptr ? nullptr : a.dlogits + row * a.dlogits_stride;
+  Teacher<T, kTwiceThreads> teacher(lds, sh, a, row);
+  teacher.read();
+  __syncthreads();
+  if (!teacher.any()) {                                // nothing to learn from: no loss, no gradient
+    if (tid == 0) a.kl[row] = 0.f;
     if (dr != nullptr)
-      for (int v = tid; v < vocab; v += kRowThreads) Vec<T>::store1(dr + v, 0.f);
+      for (int v = tid; v < vocab; v += kTwiceThreads) Vec<T>::store1(dr + v, 0.f);
     return;
   }
-  for (int s = tid; s < slots; s += kRowThreads) {
-    listed.token[s] = -1;
-    listed.mass[s] = 0;
-  }
-  double own = 0.0;
-  for (int j = tid; j < n_top; j += kRowThreads) {
-    const int id = id_row[j];
-    if (id >= 0 && id < vocab) own += (double)exp2_fast((t_row[j] - top) * c);
-  }
-  const double q_sum = row_sum(own, sh);
-  const float q_scale = (float)(1.0 / q_sum);
-  const bool q_fine = q_sum < 1e30;                    // not where the teacher has a NaN or an infinity
-
-  // ---- the policy's soft-max ----
+  teacher.insert(zr, [](int) { return 0; });
   // where the gradient lies has no say in the order of the sums
-  const int nvec = (reinterpret_cast<uintptr_t>(zr) & 15) == 0 ? vocab / N : 0;
-  const bool dr_aligned = (reinterpret_cast<uintptr_t>(dr) & 15) == 0;
-  const u32x4* zv = reinterpret_cast<const u32x4*>(zr);
+  const int head = (reinterpret_cast<uintptr_t>(zr) & 15) == 0 ? 0 : head_elements(zr, vocab);
+  const int nvec = (vocab - head) / N, rest = vocab - nvec * N;
+  const u32x4* zv = reinterpret_cast<const u32x4*>(zr + head);
+  const float c = teacher.c;
   MaxSum st{kNegHuge, 0.f};
-  for (int i = tid; i < nvec; i += kRowThreads) {
+  int i = tid;
+  for (; i + (kAhead - 1) * kTwiceThreads < nvec; i += kAhead * kTwiceThreads) {
+    u32x4 q[kAhead];
+    float x[kAhead * N];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) q[u] = load_stream(zv + i + u * kTwiceThreads);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) Vec<T>::unpack(q[u], x + u * N);
+    accumulate<kAhead * N>(x, c, st);
+  }
+  for (; i < nvec; i += kTwiceThreads) {
     float x[N];
-    Vec<T>::unpack(zv[i], x);
+    Vec<T>::unpack(load_stream(zv + i), x);
     accumulate<N>(x, c, st);
   }
-  for (int v = nvec * N + tid; v < vocab; v += kRowThreads) {
-    const float x = Vec<T>::load1(zr + v);
+  for (int r = tid; r < rest; r += kTwiceThreads) {
+    const float x = Vec<T>::load1(zr + (r < head ? r : nvec * N + r));
     accumulate<1>(&x, c, st);
   }
   st = wave_merge(st);
-  if ((tid & 63) == 0) sh.soft[tid >> 6] = st;
+  if ((tid & 63) == 0) sh.policy[tid >> 6] = st;
   __syncthreads();
-  st = sh.soft[0];
-#pragma unroll
-  for (int w = 1; w < kRowWaves; ++w) st = merge(st, sh.soft[w]);
-
-  // ---- the divergence: log q - log p of every entry, with p = 2^(z c - st.m) / st.s ----
-  const double log_ratio = log(q_sum) - log((double)st.s);
-  double kl = 0.0;
-  for (int j = tid; j < n_top; j += kRowThreads) {
-    const int id = id_row[j];
-    int slot = -1;
-    if (id >= 0 && id < vocab) {
-      const float z = Vec<T>::load1(zr + id), t = (t_row[j] - top) * c, q = exp2_fast(t) * q_scale;
-      listed.z[j] = z;
-      if (!(q <= 0.f)) kl += (double)q * (((double)t - (double)__builtin_fmaf(z, c, -st.m)) * 0.6931471805599453 - log_ratio);
-      int s = (int)(((uint32_t)id * 2654435761u) >> 16) & (slots - 1);
-      while (true) {
-        const int held = atomicCAS(&listed.token[s], -1, id);
-        if (held == -1) slot = s;
-        if (held == -1 || held == id) break;
-        s = (s + 1) & (slots - 1);
-      }
-      atomicAdd(&listed.mass[s], (u64)ldexp((double)(q_fine ? q : 0.f), kQBits));
-    }
-    listed.slot[j] = slot;
-  }
-  kl = row_sum(kl, sh);
-  if (tid == 0) kl_out[row] = (float)kl;
+  st = merge_all<kTwiceThreads / 64>(sh.policy);
+  teacher.diverge(st);
+  __syncthreads();
+  teacher.report();
   if (dr == nullptr) return;
-
-  // ---- the gradient ----
-  const float g = (weight == nullptr ? inv_rows : weight[row]) * inv_temperature;
-  const float g_p = g / st.s;
-  for (int i = tid; i < nvec; i += kRowThreads) {
+  const float g = teacher.weight(), g_p = g / st.s;
+  const bool aligned = (reinterpret_cast<uintptr_t>(dr + head) & 15) == 0;
+  for (i = tid; i < nvec; i += kTwiceThreads) {
     float x[N];
     Vec<T>::unpack(zv[i], x);
 #pragma unroll
     for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, -st.m)) * g_p;
-    if (dr_aligned) {
-      reinterpret_cast<u32x4*>(dr)[i] = Vec<T>::pack(x);
+    T* d = dr + head + (long long)i * N;
+    if (aligned) {
+      *reinterpret_cast<u32x4*>(d) = Vec<T>::pack(x);
     } else {
 #pragma unroll
-      for (int j = 0; j < N; ++j) Vec<T>::store1(dr + i * N + j, x[j]);
+      for (int j = 0; j < N; ++j) Vec<T>::store1(d + j, x[j]);
     }
   }
-  for (int v = nvec * N + tid; v < vocab; v += kRowThreads)
+  for (int r = tid; r < rest; r += kTwiceThreads) {
+    const int v = r < head ? r : nvec * N + r;
     Vec<T>::store1(dr + v, exp2_fast(__builtin_fmaf(Vec<T>::load1(zr + v), c, -st.m)) * g_p);
+  }
   // the listed tokens' elements, once every wavefront's stores have completed
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  for (int j = tid; j < n_top; j += kRowThreads) {
-    const int s = listed.slot[j];
-    if (s < 0) continue;
-    const float q = q_fine ? (float)ldexp((double)listed.mass[s], -kQBits) : __builtin_nanf("");
-    const float p = exp2_fast(__builtin_fmaf(listed.z[j], c, -st.m)) / st.s;
-    Vec<T>::store1(dr + listed.token[s], g * (p - q));
+  for (int j = tid; j < a.n_top; j += kTwiceThreads)
+    if (teacher.listed.slot[j] >= 0)
+      Vec<T>::store1(dr + teacher.listed.token[teacher.listed.slot[j]], g * teacher.element(j, st));
+}
+
+// ---- rows that are held ---------------------------------------------------------------------------------------------------
+typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef const __attribute__((address_space(1))) void* glb_ptr;
+
+// A vector of excluded elements (-inf in the row's type), for lanes past the end of the row.
+template <typename T> __device__ __forceinline__ u32x4 masked_fill();
+template <> __device__ __forceinline__ u32x4 masked_fill<bf16_t>() {
+  return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
+}
+template <> __device__ __forceinline__ u32x4 masked_fill<float>() {
+  return u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
+}
+
+// ALIGNED: both rows are 16-byte aligned; otherwise both lie the same way relative to 128-byte lines, and the elements before the
+// row's first line boundary are handled one by one together with those after the last vector.  Vector k of a lane (vector tid +
+// THREADS k of the row) lies in register q[k] for k < NV and in slot k - NV of the dynamic LDS beyond.  The row has at least KFULL
+// THREADS vectors.
+template <typename T, bool ALIGNED, int THREADS, int NV, int NL, int KFULL>
+__global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs<T> a) {
+  constexpr int N = Vec<T>::N;
+  static_assert(ALIGNED || THREADS >= 128, "a thread for every element outside the vectors");
+  extern __shared__ __align__(16) unsigned char lds[];
+  __shared__ RowShared<THREADS> sh;
+  u32x4* slots = reinterpret_cast<u32x4*>(lds);
+  const long long row = blockIdx.x;
+  const int tid = threadIdx.x, vocab = a.vocab;
+  const T* zr = a.logits + row * a.row_stride;
+  T* dr = a.dlogits + row * a.dlogits_stride;
+  const int head = ALIGNED ? 0 : head_elements(zr, vocab);
+  const int nvec = (vocab - head) / N, rest = vocab - nvec * N;
+  const int v_rest = ALIGNED || tid >= head ? nvec * N + tid : tid;
+  const u32x4* zv = reinterpret_cast<const u32x4*>(zr + head);
+  u32x4* dv = reinterpret_cast<u32x4*>(dr + head);
+  Teacher<T, THREADS> teacher(lds + NL * THREADS * 16, sh, a, row);
+
+  // the whole row is asked for; the teacher's entries, which are waited for first, before it
+  u32x4 q[NV];
+  const bool live = a.valid == nullptr || a.valid[row] != 0;
+  teacher.read();
+  if (live) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int i = tid + k * THREADS;
+      if (k < KFULL) q[k] = load_stream(zv + i);
+      else q[k] = i < nvec ? load_stream(zv + i) : masked_fill<T>();
+    }
+    if (NL > 0) {
+      int tid0 = tid;                                  // opaque copies keep the per-vector offsets short-lived
+      asm volatile("" : "+v"(tid0));
+#pragma unroll
+      for (int k = 0; k < NL; ++k) {
+        // lanes past the end of the row fetch its last vector, which is masked later
+        const int i = min(tid0 + (NV + k) * THREADS, nvec - 1);
+        __builtin_amdgcn_global_load_lds((glb_ptr)(zv + i), (lds_ptr)(slots + k * THREADS + (tid0 & ~63)), 16, 0,
+                                         2 /* non-temporal */);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   }
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");        // without a wait for the row
+  if (!teacher.any()) {                                // nothing to learn from: no loss, no gradient
+    if (tid == 0) a.kl[row] = 0.f;
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int k = 0; k < NV + NL; ++k)
+      if (tid + k * THREADS < nvec) store_stream(dv + tid + k * THREADS, zero);
+    if (tid < rest) Vec<T>::store1(dr + v_rest, 0.f);
+    if (NL > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // copies into LDS that is about to be given back
+    return;
+  }
+  float xt = tid < rest ? Vec<T>::load1(zr + v_rest) : kMasked;
+  // an element belongs to the thread that holds its vector, or that has it as its one element outside them
+  teacher.insert(zr, [&](int id) {
+    const int at = id - head;
+    if (at >= 0 && at < nvec * N) return at / N % THREADS;
+    return at < 0 ? id : id - nvec * N;
+  });
+
+  const float c = teacher.c;
+  MaxSum st{kNegHuge, 0.f};
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    float x[N];
+    Vec<T>::unpack(q[k], x);
+    accumulate<N>(x, c, st);
+    __builtin_amdgcn_sched_barrier(0);                 // keeps the unpacked values of one vector short-lived
+  }
+  if (NL > 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the copies into the slots have landed
+    int tid1 = tid;
+    asm volatile("" : "+v"(tid1));
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      const int i = tid1 + (NV + k) * THREADS;
+      float x[N];
+      Vec<T>::unpack(slots[k * THREADS + tid1], x);
+      if (NV + k >= KFULL) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = i < nvec ? x[j] : kMasked;
+      }
+      accumulate<N>(x, c, st);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  accumulate<1>(&xt, c, st);
+  st = wave_merge(st);
+  if ((tid & 63) == 0) sh.policy[tid >> 6] = st;
+  __syncthreads();
+  st = merge_all<THREADS / 64>(sh.policy);
+  const float g = teacher.weight(), g_p = g / st.s, shift = -st.m;
+  // opaque until the sum is known: neither are unpacked values kept alive nor is the unpacking below moved up
+#pragma unroll
+  for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(q[k]) : "v"(shift));
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    float x[N];
+    Vec<T>::unpack(q[k], x);
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, shift)) * g_p;
+    q[k] = Vec<T>::pack(x);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  xt = exp2_fast(__builtin_fmaf(xt, c, shift)) * g_p;
+  if (NL > 0) {
+    int tid2 = tid;
+    asm volatile("" : "+v"(tid2));
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      float x[N];
+      Vec<T>::unpack(slots[k * THREADS + tid2], x);
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, shift)) * g_p;
+      slots[k * THREADS + tid2] = Vec<T>::pack(x);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // the listed tokens' elements among this thread's
+  for (int j = sh.first[tid]; j >= 0; j = teacher.listed.next[j]) {
+    const float d = g * teacher.element(j, st);
+    const int at = teacher.listed.token[teacher.listed.slot[j]] - head;
+    if (at < 0 || at >= nvec * N) {
+      xt = d;
+      continue;
+    }
+    const int slot = at / N / THREADS, sub = at & (N - 1);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (k == slot) q[k] = Vec<T>::put(q[k], sub, d);
+    if (NL > 0 && slot >= NV) {
+      u32x4* p = slots + (slot - NV) * THREADS + tid;
+      *p = Vec<T>::put(*p, sub, d);
+    }
+  }
+  // no store before every vector is there
+#pragma unroll
+  for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(q[k]));
+  int tid3 = tid;
+  asm volatile("" : "+v"(tid3));
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = tid3 + k * THREADS;
+    if (k < KFULL || i < nvec) store_stream(dv + i, q[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < NL; ++k) {
+    const int i = tid3 + (NV + k) * THREADS;
+    if (i < nvec) store_stream(dv + i, slots[k * THREADS + tid3]);
+  }
+  if (tid < rest) Vec<T>::store1(dr + v_rest, xt);
+  teacher.diverge(st);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");        // without a wait for the stores
+  teacher.report();
 }
 
 constexpr int kLossThreads = 1024;
@@ -208,6 +455,76 @@ __global__ __launch_bounds__(kLossThreads) void distill_loss_kernel(const float*
   *loss = (float)own;
 }
 
+constexpr int kMostVectors = 20;       // of a lane, in registers alone
+constexpr int kMostSlots = 13;         // ... and in LDS beside them
+constexpr int kLdsSlots = 9;           // 144 KiB of the 160
+constexpr int kWide = 1024;
+
+template <typename T, bool ALIGNED, int THREADS, int NV, int NL, int KFULL>
+int launch_held_as(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size_t listed_bytes) {
+  auto kernel = distill_held_kernel<T, ALIGNED, THREADS, NV, NL, KFULL>;
+  const size_t bytes = (size_t)NL * THREADS * 16 + listed_bytes;
+  if (NL > 0) {
+    static std::once_flag once[kMaxDevices];           // the attribute belongs to the function on one device
+    static bool ok[kMaxDevices];
+    if (!allow_dynamic_lds(ctx, reinterpret_cast<const void*>(kernel), 160 * 1024 - (int)sizeof(RowShared<THREADS>), once, ok))
+      return hip_fail(ctx, hipErrorInvalidValue);
+  }
+  kernel<<<dim3((unsigned)n_rows), dim3(THREADS), bytes, ctx->stream>>>(a);
+  return hip_fail(ctx, hipGetLastError());
+}
+
+template <typename T, bool ALIGNED>
+int launch_held(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size_t listed_bytes) {
+  const int nvec = a.vocab / Vec<T>::N, need = (nvec + kWide - 1) / kWide;
+  // NV is a compile-time constant (the row lives in named registers).  PREV: the widest row of the class before; a row that
+  // reaches this one has more than PREV * 1024 vectors, of which an unaligned row may have lost up to 8 to its head.
+#define AIS_HELD(THREADS, PREV, NVAL, NLVAL) \
+  return launch_held_as<T, ALIGNED, THREADS, NVAL, NLVAL, (ALIGNED || PREV == 0 ? PREV : PREV - 1)>(ctx, a, n_rows, listed_bytes)
+  if constexpr (ALIGNED) {
+    if (nvec <= 256) AIS_HELD(64, 0, 4, 0);
+  }
+  if (nvec <= 512) AIS_HELD(128, 0, 4, 0);
+  if (nvec <= 1024) AIS_HELD(256, 0, 4, 0);
+  if (nvec <= 2048) AIS_HELD(256, 0, 8, 0);
+  if (need <= 4) AIS_HELD(kWide, 0, 4, 0);
+  if (need <= 8) AIS_HELD(kWide, 4, 8, 0);
+  if (need <= 12) AIS_HELD(kWide, 8, 12, 0);
+  if (need <= 16) AIS_HELD(kWide, 12, 16, 0);
+  if (need <= 18) AIS_HELD(kWide, 16, 18, 0);
+  if (need <= 19) AIS_HELD(kWide, 18, 19, 0);
+  if (need <= 20) AIS_HELD(kWide, 19, 20, 0);
+  if (need <= 23) AIS_HELD(kWide, 20, 18, 5);
+  if (need <= 27) AIS_HELD(kWide, 23, 18, kLdsSlots);
+  if (need <= 29) AIS_HELD(kWide, 27, 20, kLdsSlots);
+  if (need <= 31) AIS_HELD(kWide, 29, 22, kLdsSlots);
+  AIS_HELD(kWide, 31, 24, kLdsSlots);
+#undef AIS_HELD
+}
+
+// Whether a row can be held: its width, and both arrays lie the same way relative to 128-byte lines.
+template <typename T>
+bool can_be_held(const DistillArgs<T>& a, size_t listed_bytes, bool* aligned) {
+  if (a.dlogits == nullptr || a.dlogits_stride != a.row_stride) return false;
+  const uintptr_t z = reinterpret_cast<uintptr_t>(a.logits), d = reinterpret_cast<uintptr_t>(a.dlogits);
+  *aligned = z % 16 == 0 && d % 16 == 0 && a.row_stride * (long long)sizeof(T) % 16 == 0;
+  if (!*aligned && (z - d) % 128 != 0) return false;
+  const int need = (a.vocab / Vec<T>::N + kWide - 1) / kWide;
+  if (need <= kMostVectors) return true;
+  return need <= kMostVectors + kMostSlots &&
+         (size_t)kLdsSlots * kWide * 16 + listed_bytes + sizeof(RowShared<kWide>) <= 160 * 1024;
+}
+
+template <typename T>
+int launch_rows(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows) {
+  const size_t listed_bytes = Listed::bytes(a.n_top, a.slots);
+  bool aligned = false;
+  if (can_be_held(a, listed_bytes, &aligned))
+    return aligned ? launch_held<T, true>(ctx, a, n_rows, listed_bytes) : launch_held<T, false>(ctx, a, n_rows, listed_bytes);
+  distill_twice_kernel<T><<<dim3((unsigned)n_rows), dim3(kTwiceThreads), listed_bytes, ctx->stream>>>(a);
+  return hip_fail(ctx, hipGetLastError());
+}
+
 }  // namespace
 
 int launch_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, int vocab, long long row_stride,
@@ -220,13 +537,12 @@ int launch_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long 
     while (slots < 2 * n_top) slots *= 2;
     auto run = [&](auto type) {
       typedef decltype(type) T;
-      distill_kernel<T><<<dim3((unsigned)n_rows), dim3(kRowThreads), Listed::bytes(n_top, slots), ctx->stream>>>(
-          static_cast<const T*>(logits), row_stride, vocab, ids, teacher, n_top, slots, valid, weight, inv_rows,
-          inv_temperature, kl_out, static_cast<T*>(dlogits), dlogits_stride, ctx->status_dev);
+      const DistillArgs<T> args{static_cast<const T*>(logits), row_stride, vocab, ids, teacher, n_top, slots, valid, weight,
+                                inv_rows, inv_temperature, exact_exponents(inv_temperature), kl_out,
+                                static_cast<T*>(dlogits), dlogits_stride, ctx->status_dev};
+      return launch_rows(ctx, args, n_rows);
     };
-    if (dtype == AIS_BF16) run(bf16_t{});
-    else run(float{});
-    const int rc = hip_fail(ctx, hipGetLastError());
+    const int rc = dtype == AIS_BF16 ? run(bf16_t{}) : run(float{});
     if (rc != AIS_OK) return rc;
   }
   distill_loss_kernel<<<dim3(1), dim3(kLossThreads), 0, ctx->stream>>>(kl_out, weight, valid, n_rows, inv_rows, loss_out);
