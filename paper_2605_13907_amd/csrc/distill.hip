@@ -10,8 +10,8 @@
 // not depend on the order.
 //
 // Rows that fit are held by one compute unit, in registers and, beyond 20 vectors a lane, in LDS: one read and one write of the
-// row.  The loads of a row are all on their way before the teacher's part begins, which they hide; the listed tokens' elements are
-// put into the registers of the threads that hold them, so that the row leaves in one burst of stores.
+// row.  The loads of a row are all on their way before the teacher's part begins, which they hide; a listed token's element is
+// written again by the thread that wrote it, so that nobody waits for the row's stores.
 #include "ais_internal.h"
 #include "device_utils.h"
 
@@ -55,11 +55,15 @@ __device__ __forceinline__ double wave_sum64(double v) {
   for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
   return v;
 }
+// The wavefronts' parts as one, in every lane: a few exchanges inside rows of 16 lanes.  (One after the other by every thread they
+// took 2 us of the 30 that a compute unit spends on a row of 151,936 logits.)
 template <int WAVES>
 __device__ __forceinline__ MaxSum merge_all(const MaxSum* part) {
-  MaxSum st = part[0];
-#pragma unroll
-  for (int w = 1; w < WAVES; ++w) st = merge(st, part[w]);
+  MaxSum st = part[threadIdx.x & (WAVES - 1)];
+  if constexpr (WAVES > 1) st = merge_dpp<kDppQuadXor1>(st);
+  if constexpr (WAVES > 2) st = merge_dpp<kDppQuadXor2>(st);
+  if constexpr (WAVES > 4) st = merge_dpp<kDppRowHalfMirror>(st);
+  if constexpr (WAVES > 8) st = merge_dpp<kDppRowMirror>(st);
   return st;
 }
 
@@ -95,22 +99,49 @@ struct Teacher {
       : listed(lds, a.n_top, a.slots), sh(sh), a(a), row(row), c(a.inv_temperature * kLog2e) {}
   __device__ __forceinline__ bool entry(int id) const { return id >= 0 && id < a.vocab; }
 
+  // f(entry) of this thread's entries.  A thousand threads have one each, and no loop: what is asked for from memory inside one
+  // would be waited for together with everything on its way, the whole row.
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    if constexpr (THREADS >= 1024) {
+      if ((int)threadIdx.x < a.n_top) f((int)threadIdx.x);
+    } else {
+      for (int j = threadIdx.x; j < a.n_top; j += THREADS) f(j);
+    }
+  }
+  // The thread's first entry, further ones when they are needed.
+  int id0 = -1;
+  float t0 = kMasked;
+  T z0{};
+  bool bad = false;                    // an id that is neither of the vocabulary nor -1
+  // Asks for the first entry.  Neither this nor the loads of the policy's logits branch: where paths with and without a load
+  // meet, the compiler waits for everything on its way, the whole row.
+  __device__ __forceinline__ void fetch() {
+    const long long at = row * a.n_top + min((int)threadIdx.x, a.n_top - 1);
+    id0 = a.ids[at];
+    t0 = a.teacher[at];
+  }
+  __device__ __forceinline__ bool first(int j) const { return THREADS >= 1024 || j < THREADS; }
+  __device__ __forceinline__ int id(int j) const {
+    if (first(j)) return id0;
+    return a.ids[row * a.n_top + j];
+  }
+
   // Entries to LDS, their sum to the workgroup; empties the table.  No barrier.
   __device__ __forceinline__ void read() {
     const int tid = threadIdx.x;
     MaxSum st{kNegHuge, 0.f};
-    if (a.valid == nullptr || a.valid[row] != 0) {
-      for (int j = tid; j < a.n_top; j += THREADS) {
-        const int id = a.ids[row * a.n_top + j];
-        float t = a.teacher[row * a.n_top + j];
-        if (!entry(id)) {
-          t = kMasked;
-          if (id != -1) atomicOr(a.status, AIS_STATUS_BAD_TOKEN);
-        }
-        accumulate<1>(&t, c, st);
-        listed.t[j] = t;
+    each([&](int j) {
+      float t = t0;
+      if (!first(j)) t = a.teacher[row * a.n_top + j];
+      const int token = id(j);
+      if (!entry(token)) {
+        t = kMasked;
+        bad = bad || token != -1;
       }
-    }
+      accumulate<1>(&t, c, st);
+      listed.t[j] = t;
+    });
     for (int s = tid; s < a.slots; s += THREADS) {
       listed.token[s] = -1;
       listed.mass[s] = 0;
@@ -127,44 +158,53 @@ struct Teacher {
   // q of an entry: NaN, all of them, where the teacher has a NaN or +inf
   __device__ __forceinline__ float q(int j) const { return exp2_fast(__builtin_fmaf(listed.t[j], c, -all.m)) / all.s; }
   __device__ __forceinline__ bool fine() const { return all.s < 3.0e38f; }
-  // Entries into the table.  An entry that stands for its token is put on the list of the thread that `owner` names.  No barrier.
+  // Entries into the table, their logits asked for.  An entry that stands for its token is put on the list of the thread that
+  // `owner` names.  No barrier.
   template <typename F>
   __device__ __forceinline__ void insert(const T* zr, F owner) {
-    for (int j = threadIdx.x; j < a.n_top; j += THREADS) {
-      const int id = a.ids[row * a.n_top + j];
+    z0 = zr[entry(id0) ? id0 : 0];
+    each([&](int j) {
+      const int token = id(j);
       int slot = -1;
-      if (entry(id)) {
-        listed.z[j] = Vec<T>::load1(zr + id);
-        int s = (int)(((uint32_t)id * 2654435761u) >> 16) & (a.slots - 1);
+      if (entry(token)) {
+        if (!first(j)) listed.z[j] = Vec<T>::load1(zr + token);
+        int s = (int)(((uint32_t)token * 2654435761u) >> 16) & (a.slots - 1);
         while (true) {                                 // the table has twice as many slots as there are entries
-          const int held = atomicCAS(&listed.token[s], -1, id);
+          const int held = atomicCAS(&listed.token[s], -1, token);
           if (held == -1) slot = s;
-          if (held == -1 || held == id) break;
+          if (held == -1 || held == token) break;
           s = (s + 1) & (a.slots - 1);
         }
         atomicAdd(&listed.mass[s], (u64)ldexp((double)(fine() ? q(j) : 0.f), kQBits));
-        if (slot >= 0) listed.next[j] = atomicExch(&sh.first[owner(id)], j);
+        if (slot >= 0) listed.next[j] = atomicExch(&sh.first[owner(token)], j);
       }
       listed.slot[j] = slot;
-    }
+    });
+  }
+  // The first entry's logit, once it is there.  No barrier.
+  __device__ __forceinline__ void keep() {
+    if ((int)threadIdx.x < a.n_top) listed.z[threadIdx.x] = Vec<T>::load1(&z0);
   }
   // log q - log p of every entry, weighted by q, with q = 2^(t c - all.m) / all.s and p = 2^(z c - st.m) / st.s.  To the
-  // workgroup; no barrier.
+  // workgroup; no barrier.  Wavefronts without entries have nothing to do with it.
   __device__ __forceinline__ void diverge(MaxSum st) {
     const int tid = threadIdx.x;
-    const double log_ratio = log((double)all.s) - log((double)st.s), ln2 = 0.6931471805599453 * a.exact;
     double kl = 0.0;
-    for (int j = tid; j < a.n_top; j += THREADS) {
-      const float p = q(j);
-      if (p <= 0.f) continue;
-      const double t2 = (double)listed.t[j] * (double)c - (double)all.m, z2 = (double)listed.z[j] * (double)c - (double)st.m;
-      kl += (double)p * ((t2 - z2) * ln2 - log_ratio);
+    if ((tid & ~63) < a.n_top) {
+      const double log_ratio = log((double)all.s) - log((double)st.s), ln2 = 0.6931471805599453 * a.exact;
+      each([&](int j) {
+        const float p = q(j);
+        if (p <= 0.f) return;
+        const double t2 = (double)listed.t[j] * (double)c - (double)all.m, z2 = (double)listed.z[j] * (double)c - (double)st.m;
+        kl += (double)p * ((t2 - z2) * ln2 - log_ratio);
+      });
+      kl = wave_sum64(kl);
     }
-    kl = wave_sum64(kl);
     if ((tid & 63) == 0) sh.kl[tid >> 6] = kl;
   }
-  // After a barrier, by thread 0.
+  // After a barrier.
   __device__ __forceinline__ void report() const {
+    if (bad) atomicOr(a.status, AIS_STATUS_BAD_TOKEN);
     if (threadIdx.x != 0) return;
     double kl = sh.kl[0];
 #pragma unroll
@@ -194,12 +234,21 @@ __global__ __launch_bounds__(kTwiceThreads) void distill_twice_kernel(const Dist
   const T* zr = a.logits + row * a.row_stride;
   T* dr = a.dlogits == nullptr ? nullptr : a.dlogits + row * a.dlogits_stride;
   Teacher<T, kTwiceThreads> teacher(lds, sh, a, row);
-  teacher.read();
-  __syncthreads();
-  if (!teacher.any()) {                                // nothing to learn from: no loss, no gradient
+  auto nothing = [&] {                                 // nothing to learn from: no loss, no gradient
     if (tid == 0) a.kl[row] = 0.f;
     if (dr != nullptr)
       for (int v = tid; v < vocab; v += kTwiceThreads) Vec<T>::store1(dr + v, 0.f);
+  };
+  if (a.valid != nullptr && a.valid[row] == 0) {
+    nothing();
+    return;
+  }
+  teacher.fetch();
+  teacher.read();
+  __syncthreads();
+  if (!teacher.any()) {
+    if (teacher.bad) atomicOr(a.status, AIS_STATUS_BAD_TOKEN);
+    nothing();
     return;
   }
   teacher.insert(zr, [](int) { return 0; });
@@ -230,6 +279,7 @@ __global__ __launch_bounds__(kTwiceThreads) void distill_twice_kernel(const Dist
   }
   st = wave_merge(st);
   if ((tid & 63) == 0) sh.policy[tid >> 6] = st;
+  teacher.keep();
   __syncthreads();
   st = merge_all<kTwiceThreads / 64>(sh.policy);
   teacher.diverge(st);
@@ -298,42 +348,50 @@ __global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs
   u32x4* dv = reinterpret_cast<u32x4*>(dr + head);
   Teacher<T, THREADS> teacher(lds + NL * THREADS * 16, sh, a, row);
 
-  // the whole row is asked for; the teacher's entries, which are waited for first, before it
-  u32x4 q[NV];
-  const bool live = a.valid == nullptr || a.valid[row] != 0;
-  teacher.read();
-  if (live) {
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int i = tid + k * THREADS;
-      if (k < KFULL) q[k] = load_stream(zv + i);
-      else q[k] = i < nvec ? load_stream(zv + i) : masked_fill<T>();
-    }
-    if (NL > 0) {
-      int tid0 = tid;                                  // opaque copies keep the per-vector offsets short-lived
-      asm volatile("" : "+v"(tid0));
-#pragma unroll
-      for (int k = 0; k < NL; ++k) {
-        // lanes past the end of the row fetch its last vector, which is masked later
-        const int i = min(tid0 + (NV + k) * THREADS, nvec - 1);
-        __builtin_amdgcn_global_load_lds((glb_ptr)(zv + i), (lds_ptr)(slots + k * THREADS + (tid0 & ~63)), 16, 0,
-                                         2 /* non-temporal */);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-  }
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");        // without a wait for the row
-  if (!teacher.any()) {                                // nothing to learn from: no loss, no gradient
+  auto nothing = [&] {                                 // nothing to learn from: no loss, no gradient
     if (tid == 0) a.kl[row] = 0.f;
     const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
     for (int k = 0; k < NV + NL; ++k)
       if (tid + k * THREADS < nvec) store_stream(dv + tid + k * THREADS, zero);
     if (tid < rest) Vec<T>::store1(dr + v_rest, 0.f);
+  };
+  if (a.valid != nullptr && a.valid[row] == 0) {
+    nothing();
+    return;
+  }
+  // the teacher's entries, which are waited for first, and the whole row are asked for
+  teacher.fetch();
+  const float g = teacher.weight();
+  u32x4 q[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int i = tid + k * THREADS;
+    if (k < KFULL) q[k] = load_stream(zv + i);
+    else q[k] = i < nvec ? load_stream(zv + i) : masked_fill<T>();
+    __builtin_amdgcn_sched_barrier(0);                 // in the order in which they are summed
+  }
+  if (NL > 0) {
+    int tid0 = tid;                                    // opaque copies keep the per-vector offsets short-lived
+    asm volatile("" : "+v"(tid0));
+#pragma unroll
+    for (int k = 0; k < NL; ++k) {
+      // lanes past the end of the row fetch its last vector, which is masked later
+      const int i = min(tid0 + (NV + k) * THREADS, nvec - 1);
+      __builtin_amdgcn_global_load_lds((glb_ptr)(zv + i), (lds_ptr)(slots + k * THREADS + (tid0 & ~63)), 16, 0,
+                                       2 /* non-temporal */);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  const T xt_raw = zr[min(v_rest, vocab - 1)];
+  teacher.read();
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");        // without a wait for the row
+  if (!teacher.any()) {
+    if (teacher.bad) atomicOr(a.status, AIS_STATUS_BAD_TOKEN);
+    nothing();
     if (NL > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // copies into LDS that is about to be given back
     return;
   }
-  float xt = tid < rest ? Vec<T>::load1(zr + v_rest) : kMasked;
   // an element belongs to the thread that holds its vector, or that has it as its one element outside them
   teacher.insert(zr, [&](int id) {
     const int at = id - head;
@@ -367,71 +425,33 @@ __global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  const float xt = tid < rest ? Vec<T>::load1(&xt_raw) : kMasked;
   accumulate<1>(&xt, c, st);
   st = wave_merge(st);
   if ((tid & 63) == 0) sh.policy[tid >> 6] = st;
+  teacher.keep();
   __syncthreads();
   st = merge_all<THREADS / 64>(sh.policy);
-  const float g = teacher.weight(), g_p = g / st.s, shift = -st.m;
+  const float g_p = g / st.s, shift = -st.m;
   // opaque until the sum is known: neither are unpacked values kept alive nor is the unpacking below moved up
 #pragma unroll
   for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(q[k]) : "v"(shift));
+  int tid2 = tid;                                      // opaque: the vectors' offsets are not kept from the loads on
+  asm volatile("" : "+v"(tid2));
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
+  for (int k = 0; k < NV + NL; ++k) {
+    const int i = tid2 + k * THREADS;
     float x[N];
-    Vec<T>::unpack(q[k], x);
+    Vec<T>::unpack(k < NV ? q[k < NV ? k : 0] : slots[(k - NV) * THREADS + tid2], x);
 #pragma unroll
     for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, shift)) * g_p;
-    q[k] = Vec<T>::pack(x);
+    if (k < KFULL || i < nvec) store_stream(dv + i, Vec<T>::pack(x));
     __builtin_amdgcn_sched_barrier(0);
   }
-  xt = exp2_fast(__builtin_fmaf(xt, c, shift)) * g_p;
-  if (NL > 0) {
-    int tid2 = tid;
-    asm volatile("" : "+v"(tid2));
-#pragma unroll
-    for (int k = 0; k < NL; ++k) {
-      float x[N];
-      Vec<T>::unpack(slots[k * THREADS + tid2], x);
-#pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, shift)) * g_p;
-      slots[k * THREADS + tid2] = Vec<T>::pack(x);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  }
-  // the listed tokens' elements among this thread's
-  for (int j = sh.first[tid]; j >= 0; j = teacher.listed.next[j]) {
-    const float d = g * teacher.element(j, st);
-    const int at = teacher.listed.token[teacher.listed.slot[j]] - head;
-    if (at < 0 || at >= nvec * N) {
-      xt = d;
-      continue;
-    }
-    const int slot = at / N / THREADS, sub = at & (N - 1);
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-      if (k == slot) q[k] = Vec<T>::put(q[k], sub, d);
-    if (NL > 0 && slot >= NV) {
-      u32x4* p = slots + (slot - NV) * THREADS + tid;
-      *p = Vec<T>::put(*p, sub, d);
-    }
-  }
-  // no store before every vector is there
-#pragma unroll
-  for (int k = 0; k < NV; ++k) asm volatile("" : "+v"(q[k]));
-  int tid3 = tid;
-  asm volatile("" : "+v"(tid3));
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int i = tid3 + k * THREADS;
-    if (k < KFULL || i < nvec) store_stream(dv + i, q[k]);
-  }
-#pragma unroll
-  for (int k = 0; k < NL; ++k) {
-    const int i = tid3 + (NV + k) * THREADS;
-    if (i < nvec) store_stream(dv + i, slots[k * THREADS + tid3]);
-  }
-  if (tid < rest) Vec<T>::store1(dr + v_rest, xt);
+  if (tid < rest) Vec<T>::store1(dr + v_rest, exp2_fast(__builtin_fmaf(xt, c, shift)) * g_p);
+  // the listed tokens' elements among those that this thread has written: a thread's own stores to a place keep their order
+  for (int j = sh.first[tid]; j >= 0; j = teacher.listed.next[j])
+    Vec<T>::store1(dr + teacher.listed.token[teacher.listed.slot[j]], g * teacher.element(j, st));
   teacher.diverge(st);
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");        // without a wait for the stores
   teacher.report();
@@ -477,7 +497,9 @@ int launch_held_as(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size
 template <typename T, bool ALIGNED>
 int launch_held(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size_t listed_bytes) {
   const int nvec = a.vocab / Vec<T>::N, need = (nvec + kWide - 1) / kWide;
-  // NV is a compile-time constant (the row lives in named registers).  PREV: the widest row of the class before; a row that
+  // NV is a compile-time constant (the row lives in named registers).  Up to 8,192 vectors two rows or more share a compute unit, so
+  // that one is read or written while another is summed: with 1,024 threads and with 512, us, 3,001 rows x 50,257 bf16 166 and
+  // 121, 8,000 x 32,000 301 and 184, 3,000 x 64,000 184 and 142; with 256 and 512, 20,000 x 8,000 fp32 249 and 235.  PREV: the widest row of the class before; a row that
   // reaches this one has more than PREV * 1024 vectors, of which an unaligned row may have lost up to 8 to its head.
 #define AIS_HELD(THREADS, PREV, NVAL, NLVAL) \
   return launch_held_as<T, ALIGNED, THREADS, NVAL, NLVAL, (ALIGNED || PREV == 0 ? PREV : PREV - 1)>(ctx, a, n_rows, listed_bytes)
@@ -486,9 +508,11 @@ int launch_held(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size_t 
   }
   if (nvec <= 512) AIS_HELD(128, 0, 4, 0);
   if (nvec <= 1024) AIS_HELD(256, 0, 4, 0);
-  if (nvec <= 2048) AIS_HELD(256, 0, 8, 0);
-  if (need <= 4) AIS_HELD(kWide, 0, 4, 0);
-  if (need <= 8) AIS_HELD(kWide, 4, 8, 0);
+  if (nvec <= 2048) AIS_HELD(512, 0, 4, 0);
+  if (nvec <= 4096) AIS_HELD(512, 0, 8, 0);
+  if (nvec <= 6144) AIS_HELD(512, 0, 12, 0);
+  if (nvec <= 7168) AIS_HELD(512, 0, 14, 0);
+  if (nvec <= 8192) AIS_HELD(512, 0, 16, 0);
   if (need <= 12) AIS_HELD(kWide, 8, 12, 0);
   if (need <= 16) AIS_HELD(kWide, 12, 16, 0);
   if (need <= 18) AIS_HELD(kWide, 16, 18, 0);
