@@ -118,7 +118,8 @@ _FAST = None
 # the entry points that the native form of the calls below uses, in the order of its table
 _FAST_ENTRIES = ("ais_set_stream", "ais_token_logprob", "ais_diagnostics", "ais_grpo_loss_grad", "ais_grpo_row_scale",
                  "ais_token_logprob_softmax_grad", "ais_fp8_quantize_rows", "ais_fp8_dequantize_rows",
-                 "ais_fp8_rollout_logprob", "ais_lm_head_logprob", "ais_lm_head_grad")
+                 "ais_fp8_rollout_logprob", "ais_lm_head_logprob", "ais_lm_head_grad", "ais_mxfp4_quantize_rows",
+                 "ais_mxfp4_logits", "ais_sample_tokens", "ais_distill_topk")
 
 
 def fast_stamp() -> str:
@@ -507,24 +508,33 @@ class AisContext:
     def mxfp4_quantize_rows(self, x, want_values: bool = False):
         """x [R, D] bf16 or fp32 -> (codes [R, 16 nb], scales [R, nb]) uint8, nb = ceil(D / 32); with want_values also what
         the codes stand for, [R, D] of x's dtype.  See ais_mxfp4_quantize_rows in include/ais.h."""
+        out = self._native("mxfp4_quantize_rows", x, 1 if want_values else 0)
+        if out is not None:
+            return out
         dev = self.device
         n_rows, width, row_stride = _logits_geometry(x, dev, "x")
         dtype = _dtype_code(x, "x")
         blocks = -(-width // MXFP4_BLOCK)
         codes = torch.empty((n_rows, 16 * blocks), dtype=torch.uint8, device=dev)
         # rows of scales padded to whole groups of 16 blocks: every row begins at a whole word
-        scales = torch.empty((n_rows, -(-blocks // 16) * 16), dtype=torch.uint8, device=dev)
+        pitch = -(-blocks // 16) * 16
+        scales = torch.empty_strided((n_rows, blocks), (pitch, 1), dtype=torch.uint8, device=dev)
         values = torch.empty((n_rows, width), dtype=x.dtype, device=dev) if want_values else None
         self._sync_stream()
         rc = self._lib.ais_mxfp4_quantize_rows(self._h, x.data_ptr(), dtype, n_rows, width, row_stride, _ptr(codes),
-                                               16 * blocks, _ptr(scales), scales.shape[1], _ptr(values), width)
+                                               16 * blocks, scales.data_ptr(), pitch, _ptr(values), width)
         if rc != 0:
             raise AisError(rc, "ais_mxfp4_quantize_rows")
-        return (codes, scales[:, :blocks], values) if want_values else (codes, scales[:, :blocks])
+        return (codes, scales, values) if want_values else (codes, scales)
 
     def mxfp4_logits(self, hidden_codes, hidden_scales, weight_codes, weight_scales, dtype=torch.bfloat16):
         """-> logits [R, V] of `dtype` (bfloat16 or float32): hidden states times output embedding, both as
         mxfp4_quantize_rows returns them.  See ais_mxfp4_logits in include/ais.h."""
+        if dtype is torch.bfloat16 or dtype is torch.float32:
+            out = self._native("mxfp4_logits", hidden_codes, hidden_scales, weight_codes, weight_scales,
+                               1 if dtype is torch.bfloat16 else 0)
+            if out is not None:
+                return out
         dev = self.device
         n_rows, blocks, *hidden = _mxfp4_rows(hidden_codes, hidden_scales, dev, "hidden")
         vocab, weight_blocks, *weight = _mxfp4_rows(weight_codes, weight_scales, dev, "weight")
@@ -544,6 +554,9 @@ class AisContext:
         """-> (tokens [R] int32, logp [R] fp32 of the policy that drew them, logp_full [R] fp32 over the whole vocabulary).
         noise [R, V] fp32: independent Exp(1) numbers (torch's exponential_).  The limits are tensors of one value a row
         (fp32, top_k int32), numbers for all rows, or None.  See ais_sample_tokens in include/ais.h."""
+        out = self._native("sample_tokens", logits, noise, valid, temperature, top_k, top_p, min_p)
+        if out is not None:
+            return out
         dev = self.device
         n_rows, vocab, row_stride = _logits_geometry(logits, dev)
         dtype = _dtype_code(logits)
@@ -578,6 +591,10 @@ class AisContext:
         distribution over the listed tokens (teacher_ids [R, K] int32, -1 for no entry; teacher_logits [R, K] fp32), and the
         gradient of sum_n weight[n] kl[n] (weight None: the mean).  Pass dlogits=logits to overwrite the logits in place.
         See ais_distill_topk in include/ais.h."""
+        out = self._native("distill_topk", logits, teacher_ids, teacher_logits, weight, valid, float(inv_temperature),
+                           1 if want_grad else 0, dlogits)
+        if out is not None:
+            return out
         dev = self.device
         n_rows, vocab, row_stride = _logits_geometry(logits, dev)
         dtype = _dtype_code(logits)
@@ -597,8 +614,11 @@ class AisContext:
         elif want_grad:
             # lies like the logits relative to 128-byte lines: rows that begin anywhere can then be held, too
             shift = logits.data_ptr() % 128 // logits.element_size()
-            dlogits = torch.empty(shift + (n_rows - 1) * row_stride + vocab if n_rows else 0, dtype=logits.dtype, device=dev)
-            dlogits = dlogits.as_strided(logits.shape, logits.stride(), shift if n_rows else 0)
+            if shift == 0 or n_rows == 0:
+                dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=dev)
+            else:
+                dlogits = torch.empty(shift + (n_rows - 1) * row_stride + vocab, dtype=logits.dtype, device=dev)
+                dlogits = dlogits.as_strided(logits.shape, logits.stride(), shift)
         kl = torch.empty(n_rows, dtype=torch.float32, device=dev)
         loss = torch.empty(1, dtype=torch.float32, device=dev)
         self._sync_stream()

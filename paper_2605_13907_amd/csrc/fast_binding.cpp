@@ -30,6 +30,10 @@ struct Library {
   decltype(&ais_fp8_rollout_logprob) fp8_rollout_logprob;
   decltype(&ais_lm_head_logprob) lm_head_logprob;
   decltype(&ais_lm_head_grad) lm_head_grad;
+  decltype(&ais_mxfp4_quantize_rows) mxfp4_quantize_rows;
+  decltype(&ais_mxfp4_logits) mxfp4_logits;
+  decltype(&ais_sample_tokens) sample_tokens;
+  decltype(&ais_distill_topk) distill_topk;
 } lib;
 
 // Reads positional arguments; `ok` turns false at the first one that is not what the call takes.
@@ -403,6 +407,125 @@ AIS_CALL(lm_head_grad) {
   return rc != 0 ? PyLong_FromLong(rc) : result(dh, dw);
 }
 
+// x, 1 for the values beside codes and scales or 0
+AIS_CALL(mxfp4_quantize_rows) {
+  const Matrix x(c);
+  const bool want_values = c.integer() != 0;
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const long long blocks = (x.width + 31) / 32, pitch = (blocks + 15) / 16 * 16;
+  const at::TensorOptions bytes = at::TensorOptions().dtype(at::kByte).device(x.t->device());
+  const at::Tensor codes = at::empty({x.rows, 16 * blocks}, bytes), scales = at::empty_strided({x.rows, blocks}, {pitch, 1}, bytes),
+                   values = want_values ? empty(c.device, {x.rows, x.width}, x.t->scalar_type()) : at::Tensor();
+  unsigned char *cp = codes.data_ptr<unsigned char>(), *sp = scales.data_ptr<unsigned char>();
+  void* vp = want_values ? values.data_ptr() : nullptr;
+  const int rc = c.run([&] {
+    return lib.mxfp4_quantize_rows(c.ctx, x.data(), x.dtype, x.rows, x.width, x.stride, cp, 16 * blocks, sp, pitch, vp, x.width);
+  });
+  if (rc != 0) return PyLong_FromLong(rc);
+  return want_values ? result(codes, scales, values) : result(codes, scales);
+}
+
+// Codes and scales of an MXFP4 matrix.
+struct Mxfp4 {
+  const at::Tensor *codes, *scales;
+  long long rows = 0, blocks = 0, codes_stride = 0, scales_stride = 0;
+  explicit Mxfp4(Call& c) : codes(c.tensor()), scales(c.ok ? c.tensor() : nullptr) {
+    if (!c.ok) return;
+    for (const at::Tensor* t : {codes, scales})
+      if (t->dim() != 2 || t->scalar_type() != at::kByte || (t->stride(1) != 1 && t->size(1) > 1)) {
+        c.ok = false;
+        return;
+      }
+    rows = scales->size(0);
+    blocks = scales->size(1);
+    if (codes->size(0) != rows || codes->size(1) != 16 * blocks) c.ok = false;
+    codes_stride = rows > 1 ? codes->stride(0) : 16 * blocks;
+    scales_stride = rows > 1 ? scales->stride(0) : (blocks + 3) / 4 * 4;
+  }
+  static const unsigned char* data(const at::Tensor* t) { return static_cast<const unsigned char*>(t->data_ptr()); }
+};
+
+// hidden codes and scales, weight codes and scales, 1 for a bf16 result or 0 for fp32
+AIS_CALL(mxfp4_logits) {
+  const Mxfp4 h(c);
+  if (!c.ok) AIS_REFUSE;
+  const Mxfp4 w(c);
+  if (!c.ok || w.blocks != h.blocks) AIS_REFUSE;
+  const bool bf16 = c.integer() != 0;
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const at::Tensor out = empty(c.device, {h.rows, w.rows}, bf16 ? at::kBFloat16 : at::kFloat);
+  void* op = out.data_ptr();
+  const int rc = c.run([&] {
+    return lib.mxfp4_logits(c.ctx, Mxfp4::data(h.codes), h.codes_stride, Mxfp4::data(h.scales), h.scales_stride, h.rows,
+                            Mxfp4::data(w.codes), w.codes_stride, Mxfp4::data(w.scales), w.scales_stride, w.rows, 32 * h.blocks,
+                            op, bf16 ? AIS_BF16 : AIS_F32, w.rows);
+  });
+  return rc != 0 ? PyLong_FromLong(rc) : THPVariable_Wrap(out);
+}
+
+AIS_CALL(sample_tokens) {
+  const Matrix z(c);
+  if (!c.ok) AIS_REFUSE;
+  const Matrix e(c);
+  if (!c.ok || e.dtype != AIS_F32 || e.rows != z.rows || e.width != z.width) AIS_REFUSE;
+  const unsigned char* valid = c.array<unsigned char>(at::kByte, z.rows, true);
+  const float* temperature = c.array<float>(at::kFloat, z.rows, true);
+  const int* top_k = c.array<int>(at::kInt, z.rows, true);
+  const float* top_p = c.array<float>(at::kFloat, z.rows, true);
+  const float* min_p = c.array<float>(at::kFloat, z.rows, true);
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const at::Tensor tokens = empty(c.device, {z.rows}, at::kInt), logp = empty(c.device, {z.rows}), full = empty(c.device, {z.rows});
+  int* tp = tokens.data_ptr<int>();
+  float *lp = logp.data_ptr<float>(), *fp = full.data_ptr<float>();
+  const int rc = c.run([&] {
+    return lib.sample_tokens(c.ctx, z.data(), z.dtype, z.rows, z.width, z.stride, static_cast<const float*>(e.data()), e.stride,
+                             valid, temperature, top_k, top_p, min_p, tp, lp, fp);
+  });
+  return rc != 0 ? PyLong_FromLong(rc) : result(tokens, logp, full);
+}
+
+// logits, teacher's ids and logits, weight, valid, inv_temperature, 1 for a gradient or 0, where to put it
+AIS_CALL(distill_topk) {
+  const Matrix z(c);
+  if (!c.ok) AIS_REFUSE;
+  const at::Tensor* ids = c.tensor();
+  if (!c.ok || ids->dim() != 2 || ids->size(0) != z.rows || ids->size(1) > 0x7fffffff) AIS_REFUSE;
+  const long long top = ids->size(1);
+  --c.at;
+  const int* ip = c.array<int>(at::kInt, z.rows * top);
+  const at::Tensor* teacher = c.tensor();
+  if (!c.ok || teacher->sizes() != ids->sizes()) AIS_REFUSE;
+  --c.at;
+  const float* tp = c.array<float>(at::kFloat, z.rows * top);
+  const float* weight = c.array<float>(at::kFloat, z.rows, true);
+  const unsigned char* valid = c.array<unsigned char>(at::kByte, z.rows, true);
+  const float inv_t = (float)c.real();
+  const bool want_grad = c.integer() != 0;
+  if (!c.ok) AIS_REFUSE;
+  at::Tensor dz;
+  if (want_grad && c.at < c.n && c.a[c.at] == Py_None) {
+    // lies like the logits relative to 128-byte lines
+    ++c.at;
+    const long long shift = reinterpret_cast<uintptr_t>(z.data()) % 128 / z.t->element_size();
+    dz = shift == 0 || z.rows == 0 ? at::empty_strided(z.t->sizes(), z.t->strides(), z.t->options())
+                                   : at::empty({shift + (z.rows - 1) * z.stride + z.width}, z.t->options())
+                                         .as_strided(z.t->sizes(), z.t->strides(), shift);
+  } else if (c.at < c.n && c.a[c.at] == Py_None) {
+    ++c.at;
+  } else {
+    dz = z.like(c);
+  }
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const at::Tensor kl = empty(c.device, {z.rows}), loss = empty(c.device, {1});
+  float *kp = kl.data_ptr<float>(), *lp = loss.data_ptr<float>();
+  void* dp = dz.defined() ? dz.data_ptr() : nullptr;
+  const int rc = c.run([&] {
+    return lib.distill_topk(c.ctx, z.data(), z.dtype, z.rows, z.width, z.stride, ip, tp, (int)top, valid, weight, inv_t, kp, lp, dp,
+                            z.stride);
+  });
+  return rc != 0 ? PyLong_FromLong(rc) : result(loss, kl, dz);
+}
+
 // init(addresses): the entry points, in the order of Library.
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t n) {
   constexpr Py_ssize_t kEntries = sizeof(Library) / sizeof(void*);
@@ -435,6 +558,10 @@ PyMethodDef methods[] = {AIS_METHOD(init),
                          AIS_METHOD(fp8_rollout_logprob),
                          AIS_METHOD(lm_head_logprob),
                          AIS_METHOD(lm_head_grad),
+                         AIS_METHOD(mxfp4_quantize_rows),
+                         AIS_METHOD(mxfp4_logits),
+                         AIS_METHOD(sample_tokens),
+                         AIS_METHOD(distill_topk),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ais_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
