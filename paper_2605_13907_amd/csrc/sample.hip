@@ -6,14 +6,15 @@
 // asks for is the place of a cut in that ranking: after k tokens, or where the mass before a token reaches its share.
 //
 // A workgroup owns a row.  A row without limits takes one pass over logits and random numbers.  Otherwise one pass finds the
-// largest logit, the sum of the exponentials, and each thread's own largest logit, of which a wavefront then makes a bound
+// largest logit, the sum of the exponentials, and the largest logit of each of four parts of every thread's, which make a bound
 // that leaves little more than the kept tokens:
-//   top-k   the k-th largest of the threads' own: at least k logits are no smaller;
-//   top-p   where the masses of the threads' own alone reach the share;
+//   top-k   the k-th largest of the parts' own: at least k logits are no smaller;
+//   top-p   where the masses of the parts' own alone reach the share;
 //   min-p   is a bound itself.
 // A second pass collects what is no smaller in LDS.  Up to 64 tokens are sorted, summed and drawn from by one wavefront in its
-// registers, up to 2,048 by the workgroup.  Where there is no such bound (flat rows, or more tokens than threads), tokens and
-// their masses are counted in 2,048 ranges of the exponent, and the range in which the cut lies is sorted.
+// registers.  Up to 4,096, tokens and masses are counted in 2,048 ranges of the exponent, and the range in which the cut lies is
+// sorted.  Where there is no such bound (flat rows, more tokens than parts) the same is done to the row itself; of a bf16 row the
+// tokens of every value are counted instead, whose masses follow from their number, so that a token costs one addition in LDS.
 // Masses are summed as fixed-point numbers, so no result depends on the order in which threads arrive.
 #include "ais_internal.h"
 #include "device_utils.h"
@@ -30,8 +31,11 @@ typedef unsigned long long u64;
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
-constexpr int kCap = 2048;             // candidates that LDS holds; two for each thread
+constexpr int kCap = 4096;             // candidates that LDS holds
+constexpr int kMembers = 2048;         // tokens of a range that are sorted; two for each thread
+constexpr int kParts = 4;              // of a thread's logits
 constexpr u64 kNoLimit = ~0ull;
+constexpr float kLowest = -3.4028235e38f, kHighest = 3.4028235e38f;
 
 // Numbers whose unsigned order is that of the floats (-0 is made +0 first).
 __device__ __forceinline__ uint32_t ordered(float x) {
@@ -50,18 +54,24 @@ __device__ __forceinline__ Best better(Best a, Best b) {
   return b.score > a.score || (b.score == a.score && b.token < a.token) ? b : a;
 }
 
+// Values of bf16 that are told apart: magnitudes of 64 octaves from 2^-32 on, of either sign; smaller ones count as zero.
+constexpr int kValues = 16384, kValueLow = 95 << 7;
+
 struct SampleShared {
-  u64 mass[kBins];
-  u64 keys[kCap];
-  uint32_t count[kBins];
-  float own_top[kThreads];
+  union {
+    struct {
+      u64 mass[kBins];                 // of the ranges, later the sorted tokens of one
+      uint32_t count[kBins];
+      u64 keys[kCap];
+    };
+    uint32_t value_count[kValues];
+  };
   u64 wave_mass[kWaves];
   uint32_t wave_count[kWaves];
   float wave_max[kWaves];
   MaxSum wave_sum[kWaves];
   Best wave_best[kWaves];
-  float least;
-  int bounded;
+  float vote_count[2][kWaves], vote_mass[2][kWaves];
   uint32_t n;
   int bin;                             // the range that holds the cut, -1: none does
   uint32_t bin_count;                  // its tokens
@@ -114,25 +124,20 @@ struct Row {
       g(Vec<T>::load1(z + v), v);
     }
   }
-  // f(logit, index) of every element that is no smaller than `least`.
+  // f(logit, index) of every element in [least, most].
   template <typename F>
-  __device__ __forceinline__ void visit_from(float least, F f) const {
+  __device__ __forceinline__ void visit_between(float least, float most, F f) const {
     constexpr int N = Vec<T>::N;
     auto one = [&](u32x4 q, int v) {
       float x[N];
       Vec<T>::unpack(q, x);
-      float m = x[0];
+      uint32_t found = 0;
 #pragma unroll
-      for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
-      if (m >= least) {
-        uint32_t found = 0;
-#pragma unroll
-        for (int j = 0; j < N; ++j) found |= (uint32_t)(x[j] >= least) << j;
-        while (found != 0) {                           // one copy of f, whatever the vector holds
-          const int j = __builtin_ctz(found);
-          found &= found - 1;
-          f(element<T>(q, j), v + j);
-        }
+      for (int j = 0; j < N; ++j) found |= (uint32_t)(x[j] >= least && x[j] <= most) << j;
+      while (found != 0) {                             // one copy of f, whatever the vector holds
+        const int j = __builtin_ctz(found);
+        found &= found - 1;
+        f(element<T>(q, j), v + j);
       }
     };
     visit<4>(
@@ -142,11 +147,26 @@ struct Row {
         },
         one,
         [&](float x, int v) {
-          if (x >= least) f(x, v);
+          if (x >= least && x <= most) f(x, v);
         });
+  }
+  template <typename F>
+  __device__ __forceinline__ void visit_from(float least, F f) const {
+    visit_between(least, kHighest, f);
   }
 };
 
+// N random numbers from p on, which lies at any multiple of four bytes.
+template <int N>
+__device__ __forceinline__ void load_noise(const float* p, float* w) {
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+  for (int j = 0; j < N; j += 4) {
+    const f32x4_any q = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(p + j));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[j + k] = q[k];
+  }
+}
 __device__ __forceinline__ float clamped_noise(float e) { return fmaxf(fminf(e, 3.0e38f), 1.17549435e-38f); }
 
 __device__ __forceinline__ Best wave_best(Best b) {
@@ -199,20 +219,42 @@ __device__ __forceinline__ Before scan(uint32_t count, u64 mass, SampleShared& s
   return b;
 }
 
-// Sorts sh.keys[0 .. n) in ascending order; what lies beyond, up to the next power of two, is overwritten.
-__device__ __forceinline__ void sort_keys(uint32_t n, SampleShared& sh) {
-  uint32_t size = 2;
+// A wavefront's keys in ascending order, by exchanges between its lanes.
+__device__ __forceinline__ u64 wave_sorted(u64 key) {
+  const uint32_t i = threadIdx.x & 63;
+#pragma unroll
+  for (uint32_t run = 2; run <= 64; run <<= 1)
+#pragma unroll
+    for (uint32_t d = run >> 1; d > 0; d >>= 1) {
+      const u64 other = __shfl_xor(key, (int)d);
+      const bool keep_less = ((i & d) == 0) == ((i & run) == 0);
+      key = (other < key) == keep_less ? other : key;
+    }
+  return key;
+}
+
+// Sorts keys[0 .. n), n <= kMembers, in ascending order; what lies beyond, up to the next power of two, is overwritten.
+__device__ __forceinline__ void sort_keys(uint32_t n, u64* keys) {
+  if (n <= 64) {
+    if (threadIdx.x < 64) {
+      const u64 key = wave_sorted(threadIdx.x < n ? keys[threadIdx.x] : kNoLimit);
+      if (threadIdx.x < n) keys[threadIdx.x] = key;
+    }
+    __syncthreads();
+    return;
+  }
+  uint32_t size = 128;
   while (size < n) size <<= 1;
-  for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) sh.keys[i] = ~0ull;
+  for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) keys[i] = kNoLimit;
   __syncthreads();
   for (uint32_t run = 2; run <= size; run <<= 1) {
     for (uint32_t d = run >> 1; d > 0; d >>= 1) {
       for (uint32_t p = threadIdx.x; p < size / 2; p += kThreads) {
         const uint32_t i = 2 * p - (p & (d - 1)), j = i + d;
-        const u64 a = sh.keys[i], b = sh.keys[j];
+        const u64 a = keys[i], b = keys[j];
         if ((a > b) == ((i & run) == 0)) {
-          sh.keys[i] = b;
-          sh.keys[j] = a;
+          keys[i] = b;
+          keys[j] = a;
         }
       }
       __syncthreads();
@@ -227,108 +269,248 @@ struct Cut {
   u64 mass;
 };
 
-// The cut among the sorted keys of LDS, before which `above` tokens rank: the first that is the limit_count-th or has
-// limit_mass before it.  All threads get it.
+// Tokens among which the cut lies: their keys are in [lo, hi), `above` tokens rank before them.
+struct Span {
+  u64 lo, hi;
+  uint32_t n, above_count;
+  u64 above_mass;
+};
+
+// The cut among n sorted keys: the first that is the limit_count-th or has limit_mass before it.  All threads get it.
 template <typename T>
-__device__ Cut cut_sorted(const Row<T>& row, uint32_t n, uint32_t above_count, u64 above_mass, uint32_t limit_count,
-                          u64 limit_mass, u64 end_key, SampleShared& sh) {
+__device__ Cut cut_sorted(const Row<T>& row, const Span& s, uint32_t limit_count, u64 limit_mass, const u64* keys,
+                          SampleShared& sh) {
+  const uint32_t n = s.n;
+  if (n <= 64) {                                       // one wavefront looks at them and tells the others
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const uint32_t i = threadIdx.x;
+      const u64 m = i < n ? row.mass(row.value(keys[i])) : 0;
+      u64 upto = m;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const u64 p = __shfl_up(upto, d);
+        if ((int)i >= d) upto += p;
+      }
+      const bool kept = i < n && s.above_count + i < limit_count && s.above_mass + upto - m < limit_mass;
+      const uint32_t all = (uint32_t)__builtin_popcountll(__ballot(kept));
+      const u64 mass = __shfl(upto, (int)max(all, 1u) - 1);
+      if (i == 0) {
+        sh.wave_count[0] = all;
+        sh.wave_mass[0] = all > 0 ? mass : 0;
+      }
+    }
+    __syncthreads();
+    const uint32_t all = sh.wave_count[0];
+    return Cut{all < n ? keys[all] : keys[n - 1] + 1, s.above_count + all, s.above_mass + sh.wave_mass[0]};
+  }
   const uint32_t i = 2 * threadIdx.x;
-  const u64 k0 = i < n ? sh.keys[i] : 0, k1 = i + 1 < n ? sh.keys[i + 1] : 0;
+  const u64 k0 = i < n ? keys[i] : 0, k1 = i + 1 < n ? keys[i + 1] : 0;
   const u64 m0 = i < n ? row.mass(row.value(k0)) : 0, m1 = i + 1 < n ? row.mass(row.value(k1)) : 0;
   const Before b = scan((i < n) + (i + 1 < n), m0 + m1, sh);
-  const u64 before0 = above_mass + b.mass, before1 = before0 + m0;
-  const bool kept0 = i < n && above_count + i < limit_count && before0 < limit_mass;
-  const bool kept1 = i + 1 < n && above_count + i + 1 < limit_count && before1 < limit_mass;
+  const u64 before0 = s.above_mass + b.mass, before1 = before0 + m0;
+  const bool kept0 = i < n && s.above_count + i < limit_count && before0 < limit_mass;
+  const bool kept1 = i + 1 < n && s.above_count + i + 1 < limit_count && before1 < limit_mass;
   const Before kept = scan((uint32_t)kept0 + (uint32_t)kept1, (kept0 ? m0 : 0) + (kept1 ? m1 : 0), sh);
-  Cut cut{end_key, above_count + kept.all_count, above_mass + kept.all_mass};
-  if (kept.all_count < n) cut.key = sh.keys[kept.all_count];
-  return cut;
+  // behind the last of them where all are kept, not at the span's end, which may reach over others
+  const u64 end = kept.all_count < n ? keys[kept.all_count] : keys[n - 1] + 1;
+  return Cut{end, s.above_count + kept.all_count, s.above_mass + kept.all_mass};
 }
 
-// The cut of the whole row: the tokens no smaller than `least`, and of those that `depth` (in log2 of the mass) below the largest
-// or deeper only the last range knows.
-template <typename T>
-__device__ Cut cut_row(const Row<T>& row, float least, float depth, uint32_t limit_count, u64 limit_mass, bool by_mass,
+// Where the cut lies among ranges of which each thread has kOwn: in the first one after which a limit is reached.  held(k, f) calls
+// f(tokens, mass) with what the thread's k-th holds.  Sets sh.bin and what belongs to it; the sums over all ranges are returned.
+template <int kOwn, typename Held>
+__device__ Before find_range(Held held, const Span& s, uint32_t limit_count, u64 limit_mass, SampleShared& sh) {
+  uint32_t c = 0;
+  u64 m = 0;
+#pragma unroll 2
+  for (int k = 0; k < kOwn; ++k)
+    held(k, [&](uint32_t count, u64 mass) {
+      c += count;
+      m += mass;
+    });
+  const Before before = scan(c, m, sh);
+  uint32_t above_count = s.above_count + before.count;
+  u64 above_mass = s.above_mass + before.mass;
+  // one thread at most has it among its own
+  if (above_count < limit_count && above_mass < limit_mass && (above_count + c >= limit_count || above_mass + m >= limit_mass)) {
+    for (int k = 0; k < kOwn; ++k)
+      held(k, [&](uint32_t count, u64 mass) {
+        const bool inside = above_count < limit_count && above_mass < limit_mass;
+        const bool after = above_count + count >= limit_count || above_mass + mass >= limit_mass;
+        if (count > 0 && inside && after) {
+          sh.bin = kOwn * (int)threadIdx.x + k;
+          sh.bin_count = count;
+          sh.above_count = above_count;
+          sh.above_mass = above_mass;
+        }
+        above_count += count;
+        above_mass += mass;
+      });
+  }
+  __syncthreads();
+  return before;
+}
+
+// Counts what `each` gives to add(range, logit) in kBins ranges and finds the one with the cut; false if there is none, with the
+// cut behind everything.
+template <typename T, typename Each>
+__device__ bool narrow(const Row<T>& row, Each each, bool by_mass, uint32_t limit_count, u64 limit_mass, Span* s, Cut* cut,
                        SampleShared& sh) {
+  __syncthreads();
+  for (int b = threadIdx.x; b < kBins; b += kThreads) {
+    sh.count[b] = 0;
+    sh.mass[b] = 0;
+  }
+  if (threadIdx.x == 0) sh.bin = -1;
+  __syncthreads();
+  each([&](uint32_t bin, float x) {
+    atomicAdd(&sh.count[bin], 1u);
+    if (by_mass) atomicAdd(&sh.mass[bin], row.mass(x));
+  });
+  __syncthreads();
+  constexpr int kOwn = kBins / kThreads;
+  const Before all = find_range<kOwn>(
+      [&](int k, auto f) { f(sh.count[kOwn * threadIdx.x + k], sh.mass[kOwn * threadIdx.x + k]); }, *s, limit_count, limit_mass, sh);
+  if (sh.bin < 0) {
+    *cut = Cut{s->hi, s->above_count + all.all_count, s->above_mass + all.all_mass};
+    return false;
+  }
+  s->n = sh.bin_count;
+  s->above_count = sh.above_count;
+  s->above_mass = sh.above_mass;
+  return true;
+}
+
+// The cut inside a span whose tokens are those of `each`: further ranges while there are more than can be sorted.
+template <typename T, typename Each>
+__device__ Cut finish_cut(const Row<T>& row, Each each, Span s, bool by_mass, uint32_t limit_count, u64 limit_mass,
+                          SampleShared& sh) {
+  while (s.n > (uint32_t)kMembers) {
+    int shift = 0;
+    while (((s.hi - s.lo - 1) >> shift) >= (u64)kBins) ++shift;
+    Cut cut;
+    const bool some = narrow(
+        row,
+        [&](auto add) {
+          each([&](float x, u64 key) {
+            if (key >= s.lo && key < s.hi) add((uint32_t)((key - s.lo) >> shift), x);
+          });
+        },
+        by_mass, limit_count, limit_mass, &s, &cut, sh);
+    if (!some) return cut;
+    const u64 start = s.lo + ((u64)sh.bin << shift), width = 1ull << shift;
+    s.hi = s.hi - start < width ? s.hi : start + width;
+    s.lo = start;
+  }
+  __syncthreads();                                     // the ranges have been read: their place is for the tokens now
+  if (threadIdx.x == 0) sh.n = 0;
+  __syncthreads();
+  each([&](float x, u64 key) {
+    if (key >= s.lo && key < s.hi) sh.mass[atomicAdd(&sh.n, 1u)] = key;
+  });
+  __syncthreads();
+  sort_keys(s.n, sh.mass);
+  return cut_sorted(row, s, limit_count, limit_mass, sh.mass, sh);
+}
+
+// The cut among the tokens that each(f, least, most) gives to f(logit, key), those between two logits where these are named, by ranges of the exponent down to `depth` (in log2 of the mass) below the largest logit's;
+// what lies deeper is in the last one.
+template <typename T, typename Each>
+__device__ Cut cut_by_exponent(const Row<T>& row, Each each, float depth, bool by_mass, uint32_t limit_count, u64 limit_mass,
+                               SampleShared& sh) {
   const float per_range = (float)kBins / depth;
   auto range_of = [&](float x) { return (int)fminf(-row.exponent(x) * per_range, (float)(kBins - 1)); };
-  int within = -1;                                     // the range that the ones below are parts of
-  uint32_t above_count = 0;
-  u64 above_mass = 0, lo = 0, hi = kNoLimit;
-  while (true) {
-    int shift = 0;
-    if (within >= 0)
-      while (((hi - lo - 1) >> shift) >= (u64)kBins) ++shift;
-    __syncthreads();
-    for (int b = threadIdx.x; b < kBins; b += kThreads) {
-      sh.count[b] = 0;
-      sh.mass[b] = 0;
+  Span s{0, kNoLimit, 0, 0, 0};
+  Cut cut;
+  if (!narrow(
+          row, [&](auto add) { each([&](float x, u64) { add((uint32_t)range_of(x), x); }, kLowest, kHighest); }, by_mass, limit_count,
+          limit_mass, &s, &cut, sh))
+    return cut;
+  // the keys of the range's logits, with room for the rounding of their exponents
+  const int bin = sh.bin;
+  const float upper = row.top - (float)bin / per_range / row.c, lower = row.top - (float)(bin + 1) / per_range / row.c;
+  const float room = 1e-5f * (fabsf(row.top) + fabsf(lower));
+  const float most = fminf(upper + room, row.top), least = bin == kBins - 1 ? kLowest : fmaxf(lower - room, kLowest);
+  s.lo = row.key(most, 0);
+  s.hi = row.key(least, row.vocab - 1) + 1;
+  auto inside = [&](auto f) {
+    each(
+        [&](float x, u64 key) {
+          if (range_of(x) == bin) f(x, key);
+        },
+        least, most);
+  };
+  return finish_cut(row, inside, s, by_mass, limit_count, limit_mass, sh);
+}
+
+// Place of a bf16 value, given as fp32, among those that are told apart, the largest first.
+__device__ __forceinline__ int value_place(float x) {
+  const int bits = __float_as_int(x + 0.f);            // a negative zero is a zero
+  const int m = min(max((int)((uint32_t)bits >> 16 & 0x7fffu) - kValueLow, 0), kValues / 2 - 1);
+  return kValues / 2 - 1 - (m ^ (bits >> 31));         // half + m where negative
+}
+
+// The cut among the tokens of a bf16 row that are no smaller than `least`: the tokens of every value are counted.
+__device__ Cut cut_by_value(const Row<bf16_t>& row, float least, uint32_t limit_count, u64 limit_mass, SampleShared& sh) {
+  constexpr int kOwn = kValues / kThreads;
+  __syncthreads();
+  for (int b = threadIdx.x; b < kValues; b += kThreads) sh.value_count[b] = 0;
+  if (threadIdx.x == 0) sh.bin = -1;
+  __syncthreads();
+  auto add = [&](float x) {
+    if (x >= least) atomicAdd(&sh.value_count[value_place(x)], 1u);
+  };
+  auto one = [&](u32x4 q, int) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      add(__uint_as_float(q[w] << 16));
+      add(__uint_as_float(q[w] & 0xffff0000u));
     }
-    if (threadIdx.x == 0) {
-      sh.bin = -1;
-      sh.n = 0;
-    }
-    __syncthreads();
-    auto add = [&](uint32_t bin, float x) {
-      atomicAdd(&sh.count[bin], 1u);
-      if (by_mass) atomicAdd(&sh.mass[bin], row.mass(x));
-    };
-    if (within < 0) {
-      row.visit_from(least, [&](float x, int) { add((uint32_t)range_of(x), x); });
-    } else {
-      row.visit_from(least, [&](float x, int v) {
-        if (range_of(x) != within) return;
-        const u64 k = row.key(x, v);
-        if (k >= lo && k < hi) add((uint32_t)((k - lo) >> shift), x);
-      });
-    }
-    __syncthreads();
-    const int b0 = 2 * threadIdx.x;
-    const uint32_t c0 = sh.count[b0], c1 = sh.count[b0 + 1];
-    const u64 m0 = sh.mass[b0], m1 = sh.mass[b0 + 1];
-    const Before before = scan(c0 + c1, m0 + m1, sh);
-    // the cut lies in the first range after which a limit is reached
-    auto look = [&](int b, uint32_t cb, u64 mb, uint32_t c, u64 m) {
-      const bool inside = above_count + cb < limit_count && above_mass + mb < limit_mass;
-      const bool after = above_count + cb + c >= limit_count || above_mass + mb + m >= limit_mass;
-      if (c > 0 && inside && after) {
-        sh.bin = b;
-        sh.bin_count = c;
-        sh.above_count = above_count + cb;
-        sh.above_mass = above_mass + mb;
-      }
-    };
-    look(b0, before.count, before.mass, c0, m0);
-    look(b0 + 1, before.count + c0, before.mass + m0, c1, m1);
-    __syncthreads();
-    const int bin = sh.bin;
-    if (bin < 0) return Cut{hi, above_count + before.all_count, above_mass + before.all_mass};
-    if (within < 0) {
-      // the keys of the range's logits, with room for the rounding of their exponents
-      within = bin;
-      const float upper = row.top - (float)bin / per_range / row.c, lower = row.top - (float)(bin + 1) / per_range / row.c;
-      const float room = 1e-5f * (fabsf(row.top) + fabsf(lower));
-      lo = row.key(fminf(upper + room, row.top), 0);
-      hi = row.key(bin == kBins - 1 ? -3.4028235e38f : fmaxf(lower - room, -3.4028235e38f), row.vocab - 1) + 1;
-    } else {
-      const u64 width = 1ull << shift;
-      const u64 start = lo + ((u64)bin << shift);
-      hi = hi - start < width ? hi : start + width;
-      lo = start;
-    }
-    above_count = sh.above_count;
-    above_mass = sh.above_mass;
-    const uint32_t n = sh.bin_count;
-    if (n > (uint32_t)kCap) continue;
-    row.visit_from(least, [&](float x, int v) {
-      if (range_of(x) != within) return;
-      const u64 k = row.key(x, v);
-      if (k >= lo && k < hi) sh.keys[atomicAdd(&sh.n, 1u)] = k;
-    });
-    __syncthreads();
-    sort_keys(n, sh);
-    return cut_sorted(row, n, above_count, above_mass, limit_count, limit_mass, hi, sh);
+  };
+  row.template visit<4>(
+      [&](const u32x4* q, int v) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) one(q[u], v);
+      },
+      one, [&](float x, int) { add(x); });
+  __syncthreads();
+  auto value_of = [&](int place) {
+    const int m = place >= kValues / 2 ? place - kValues / 2 : kValues / 2 - 1 - place;
+    const float x = m == 0 ? 0.f : __uint_as_float((uint32_t)(m + kValueLow) << 16);
+    return place >= kValues / 2 ? -x : x;
+  };
+  Span s{0, kNoLimit, 0, 0, 0};
+  const Before all = find_range<kOwn>(
+      [&](int k, auto f) {
+        const int place = kOwn * (int)threadIdx.x + k;
+        const uint32_t c = sh.value_count[place];
+        if (c > 0) f(c, c * row.mass(value_of(place)));
+      },
+      s, limit_count, limit_mass, sh);
+  if (sh.bin < 0) return Cut{kNoLimit, all.all_count, all.all_mass};
+  const int bin = sh.bin;
+  s.n = sh.bin_count;
+  s.above_count = sh.above_count;
+  s.above_mass = sh.above_mass;
+  // one value, or, at the ends of what is told apart, several
+  const int from_zero = bin >= kValues / 2 ? bin - kValues / 2 : kValues / 2 - 1 - bin;
+  const float x = value_of(bin), small = __uint_as_float((uint32_t)kValueLow << 16);
+  float upper = x, lower = x;
+  if (from_zero == 0) {
+    upper = bin < kValues / 2 ? small : 0.f;
+    lower = bin < kValues / 2 ? 0.f : -small;
   }
+  if (bin == 0) upper = row.top;
+  if (bin == kValues - 1) lower = kLowest;
+  s.lo = row.key(upper, 0);
+  s.hi = row.key(lower, row.vocab - 1) + 1;
+  auto inside = [&](auto f) {
+    row.visit_between(lower, upper, [&](float x, int v) {
+      if (value_place(x) == bin) f(x, row.key(x, v));
+    });
+  };
+  return finish_cut(row, inside, s, true, limit_count, limit_mass, sh);
 }
 
 // What a row's limits ask for.
@@ -340,55 +522,98 @@ struct Limits {
   __device__ __forceinline__ u64 part_of(double m) const { return (u64)fmax((double)top_p * m, 1.0); }
 };
 
-// A bound on the kept logits from the threads' own largest, by one wavefront; false if they allow none.
+// Sum of the wavefronts' votes, in every lane: exchanges inside rows of 16 lanes, one for each wavefront.
+__device__ __forceinline__ float votes_of(const float* votes) {
+  static_assert(kWaves == 16, "");
+  float v = votes[threadIdx.x & 15];
+  v += dpp_move<kDppQuadXor1>(v);
+  v += dpp_move<kDppQuadXor2>(v);
+  v += dpp_move<kDppRowHalfMirror>(v);
+  return v + dpp_move<kDppRowMirror>(v);
+}
+
+// A bound on the kept logits from the largest of the parts of every thread's logits; false if they allow none.
 template <typename T>
-__device__ bool bound(const Row<T>& row, const Limits& lim, float total, const float* own_top, float* least) {
-  constexpr int kOwn = kThreads / 64;
-  const int lane = threadIdx.x & 63;
-  float v[kOwn];
+__device__ bool bound(const Row<T>& row, const Limits& lim, float total, const float* own_top, float* least, SampleShared& sh) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int turn = 0;
+  // one barrier for each question: the answers of the one before are read while those of the next are written
+  auto count = [&](float from) {
+    uint32_t c = 0;
 #pragma unroll
-  for (int j = 0; j < kOwn; ++j) v[j] = own_top[j * 64 + lane];
+    for (int j = 0; j < kParts; ++j) c += (uint32_t)__builtin_popcountll(__ballot(own_top[j] >= from));
+    float* votes = sh.vote_count[turn ^= 1];           // at most 4,096: exact
+    if (lane == 0) votes[wave] = (float)c;
+    __syncthreads();
+    return (uint32_t)votes_of(votes);
+  };
+  float lo = row.top - 32.f / row.c, hi = row.top;
   if (lim.by_count) {
-    auto count = [&](float from) {
-      uint32_t c = 0;
-#pragma unroll
-      for (int j = 0; j < kOwn; ++j) c += (uint32_t)__builtin_popcountll(__ballot(v[j] >= from));
-      return c;
-    };
-    const float lowest = -3.4028235e38f;
-    if (count(lowest) < lim.count) return false;
-    uint32_t lo = ordered(lowest), hi = ordered(row.top);
+    if (lim.count > (uint32_t)(kParts * kThreads) || count(kLowest) < lim.count) return false;
     const uint32_t enough = lim.count + (lim.count >> 3) + 2;
-    while (hi - lo > 1) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      const uint32_t c = count(from_ordered(mid));
+    if (count(lo) >= lim.count) {
+      for (int k = 0; k < 14; ++k) {
+        const float mid = 0.5f * (lo + hi);
+        const uint32_t c = count(mid);
+        if (c < lim.count) {
+          hi = mid;
+        } else {
+          lo = mid;
+          if (c <= enough) break;
+        }
+      }
+      *least = lo;
+      return true;
+    }
+    // far below the largest, masked tokens perhaps: by the numbers' own order
+    uint32_t a = ordered(kLowest), b = ordered(lo);
+    while (b - a > 1) {
+      const uint32_t mid = a + (b - a) / 2, c = count(from_ordered(mid));
       if (c < lim.count) {
-        hi = mid;
+        b = mid;
       } else {
-        lo = mid;
+        a = mid;
         if (c <= enough) break;
       }
     }
-    *least = from_ordered(lo);
+    *least = from_ordered(a);
     return true;
   }
-  float p[kOwn];
+  float p[kParts];
 #pragma unroll
-  for (int j = 0; j < kOwn; ++j) p[j] = exp2_fast(row.exponent(v[j]));
+  for (int j = 0; j < kParts; ++j) p[j] = exp2_fast(row.exponent(own_top[j]));
+  uint32_t parts = 0;                                  // as large as the last question's
   auto mass = [&](float from) {
     float m = 0.f;
+    uint32_t c = 0;
 #pragma unroll
-    for (int j = 0; j < kOwn; ++j) m += v[j] >= from ? p[j] : 0.f;
-    return wave_sum(m);
+    for (int j = 0; j < kParts; ++j) {
+      m += own_top[j] >= from ? p[j] : 0.f;
+      c += (uint32_t)__builtin_popcountll(__ballot(own_top[j] >= from));
+    }
+    m = wave_sum(m);
+    turn ^= 1;
+    if (lane == 0) {
+      sh.vote_mass[turn][wave] = m;
+      sh.vote_count[turn][wave] = (float)c;
+    }
+    __syncthreads();
+    parts = (uint32_t)votes_of(sh.vote_count[turn]);
+    return votes_of(sh.vote_mass[turn]);
   };
   // rounding of the sums must not cost a token that the fixed-point sums keep
   const float wanted = lim.top_p * total * 1.00001f;
-  float hi = row.top, lo = row.top - 32.f / row.c;
   if (!(mass(lo) >= wanted)) return false;
-  for (int k = 0; k < 13; ++k) {
+  // until few enough for one wavefront are left, most likely
+  for (int k = 0; k < 12 && parts > 32; ++k) {
     const float mid = 0.5f * (lo + hi);
-    if (mass(mid) >= wanted) lo = mid;
-    else hi = mid;
+    const uint32_t before = parts;
+    if (mass(mid) >= wanted) {
+      lo = mid;
+    } else {
+      hi = mid;
+      parts = before;
+    }
   }
   *least = lo;
   return true;
@@ -403,15 +628,7 @@ struct Drawn {
 template <typename T, typename S>
 __device__ Drawn draw_from_few(const Row<T>& row, const Limits& lim, uint32_t n, const u64* keys, S scored) {
   const uint32_t i = threadIdx.x & 63;
-  u64 key = i < n ? keys[i] : kNoLimit;
-#pragma unroll
-  for (uint32_t run = 2; run <= 64; run <<= 1)
-#pragma unroll
-    for (uint32_t d = run >> 1; d > 0; d >>= 1) {
-      const u64 other = __shfl_xor(key, (int)d);
-      const bool keep_less = ((i & d) == 0) == ((i & run) == 0);
-      key = (other < key) == keep_less ? other : key;
-    }
+  const u64 key = wave_sorted(i < n ? keys[i] : kNoLimit);
   const float x = i < n ? row.value(key) : row.top;
   const u64 m = i < n ? row.mass(x) : 0;
   auto sum_to = [&](u64 own) {
@@ -491,12 +708,15 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   MaxSum st{kNegHuge, 0.f};
   float top = -__builtin_inff();
   Best best{-__builtin_inff(), vocab};
-  auto fold = [&](const float* x, auto count) {
-    constexpr int n = decltype(count)::value;
-    accumulate<n>(x, row.c, st);
+  auto largest = [](const float* x) {
+    float m = x[0];
 #pragma unroll
-    for (int j = 0; j < n; ++j) top = fmaxf(top, x[j]);
+    for (int j = 1; j < N; ++j) m = fmaxf(m, x[j]);
+    return m;
   };
+  float own_top[kParts];                               // of a thread's first, second, ... vectors of four, and the rest
+#pragma unroll
+  for (int j = 0; j < kParts; ++j) own_top[j] = top;
   if (open) {
     // indices rise, so that an equal score does not take a lower one's place; the threads' best are scored again below, relative
     // to the largest logit
@@ -507,9 +727,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     auto one = [&](u32x4 q, int v) {
       float x[N], w[N];
       Vec<T>::unpack(q, x);
-#pragma unroll
-      for (int j = 0; j < N; ++j) w[j] = __builtin_nontemporal_load(e + v + j);
-      fold(x, std::integral_constant<int, N>{});
+      load_noise<N>(e + v, w);
+      accumulate<N>(x, row.c, st);
+      top = fmaxf(top, largest(x));
 #pragma unroll
       for (int j = 0; j < N; ++j) race(x[j], w[j], v + j);
     };
@@ -517,12 +737,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
         [&](const u32x4* q, int v) {
           float x[2 * N], w[2 * N];
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int j = 0; j < N; ++j) w[u * N + j] = __builtin_nontemporal_load(e + v + u * kThreads * N + j);
+          for (int u = 0; u < 2; ++u) load_noise<N>(e + v + u * kThreads * N, w + u * N);
 #pragma unroll
           for (int u = 0; u < 2; ++u) Vec<T>::unpack(q[u], x + u * N);
-          fold(x, std::integral_constant<int, 2 * N>{});
+          accumulate<2 * N>(x, row.c, st);
+          top = fmaxf(top, fmaxf(largest(x), largest(x + N)));
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -530,25 +749,37 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
         },
         one,
         [&](float x, int v) {
-          fold(&x, std::integral_constant<int, 1>{});
+          accumulate<1>(&x, row.c, st);
+          top = fmaxf(top, x);
           const float score = __builtin_fmaf(x, row.c, -log2_fast(clamped_noise(e[v])));
           best = better(best, Best{score, v});
         });
   } else {
-    row.template visit<4>(
+    int single = 0;
+    row.template visit<kParts>(
         [&](const u32x4* q, int) {
-          float x[4 * N];
+          float x[kParts * N];
 #pragma unroll
-          for (int u = 0; u < 4; ++u) Vec<T>::unpack(q[u], x + u * N);
-          fold(x, std::integral_constant<int, 4 * N>{});
+          for (int u = 0; u < kParts; ++u) Vec<T>::unpack(q[u], x + u * N);
+          accumulate<kParts * N>(x, row.c, st);
+#pragma unroll
+          for (int u = 0; u < kParts; ++u) own_top[u] = fmaxf(own_top[u], largest(x + u * N));
         },
         [&](u32x4 q, int) {
           float x[N];
           Vec<T>::unpack(q, x);
-          fold(x, std::integral_constant<int, N>{});
+          accumulate<N>(x, row.c, st);
+          const float m = largest(x);
+#pragma unroll
+          for (int u = 0; u < kParts; ++u) own_top[u] = u == single ? fmaxf(own_top[u], m) : own_top[u];
+          ++single;                                    // at most three of them
         },
-        [&](float x, int) { fold(&x, std::integral_constant<int, 1>{}); });
-    sh.own_top[tid] = top;
+        [&](float x, int) {
+          accumulate<1>(&x, row.c, st);
+          own_top[kParts - 1] = fmaxf(own_top[kParts - 1], x);
+        });
+#pragma unroll
+    for (int j = 0; j < kParts; ++j) top = fmaxf(top, own_top[j]);
   }
   st = wave_merge(st);
   top = wave_max(top);
@@ -597,32 +828,52 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   if (lim.by_mass && !lim.by_count) lim.mass = lim.part_of(ldexp((double)total, row.mass_bits));
   // (x - top) c >= the least exponent, with room for its rounding: the condition itself is looked at again
   auto from_exponent = [&](float low) { return top + low / row.c - 1e-5f * (fabsf(top) + fabsf(low / row.c)); };
-  const float lowest = -3.4028235e38f;
-  float least = lim.by_share && !lim.by_count ? fmaxf(from_exponent(lim.share), lowest) : lowest;
+  float least = lim.by_share && !lim.by_count ? fmaxf(from_exponent(lim.share), kLowest) : kLowest;
   u64 kept_mass = 0, end_key = kNoLimit;
-  auto look = [&](float x, u64 key) {
-    if (key >= end_key || row.exponent(x) < lim.share) return;
-    kept_mass += row.mass(x);
-    best = better(best, scored(x, row.token(key)));
-  };
   if (lim.by_count || lim.by_mass) {
     // ---- candidates ----
-    if (tid < 64) {
-      float bounded = lowest;
-      const bool some = bound(row, lim, total, sh.own_top, &bounded);
-      if (tid == 0) {
-        sh.bounded = some;
-        sh.least = bounded;
-      }
-    }
-    __syncthreads();
+    float bounded = kLowest;
+    const bool some = bound(row, lim, total, own_top, &bounded, sh);
+    if (some) least = fmaxf(least, bounded);
     uint32_t n = 0xffffffffu;
-    if (sh.bounded) {
-      const float from = fmaxf(least, sh.least);
-      row.visit_from(from, [&](float x, int v) {
-        const uint32_t at = atomicAdd(&sh.n, 1u);
+    if (some) {
+      // a part whose largest logit is smaller has none
+      const u32x4* zv = reinterpret_cast<const u32x4*>(row.z + row.head);
+      auto keep = [&](uint32_t at, float x, int v) {
         if (at < (uint32_t)kCap) sh.keys[at] = row.key(x, v);
-      });
+      };
+#pragma unroll
+      for (int u = 0; u < kParts; ++u) {
+        if (own_top[u] < least) continue;
+        constexpr int kAhead = 5;
+        for (int i = tid + u * kThreads; i < row.nvec; i += kAhead * kParts * kThreads) {
+          u32x4 q[kAhead];
+#pragma unroll
+          for (int a = 0; a < kAhead; ++a) q[a] = zv[min(i + a * kParts * kThreads, row.nvec - 1)];
+          u64 found = 0;
+#pragma unroll
+          for (int a = 0; a < kAhead; ++a) {
+            float x[N];
+            Vec<T>::unpack(q[a], x);
+            uint32_t here = 0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) here |= (uint32_t)(x[j] >= least) << j;
+            if (i + a * kParts * kThreads < row.nvec) found |= (u64)here << (a * N);
+          }
+          if (found == 0) continue;
+          uint32_t at = atomicAdd(&sh.n, (uint32_t)__popcll(found));
+          for (; found != 0; found &= found - 1) {     // read again: they are few
+            const int j = __builtin_ctzll(found);
+            const int v = row.head + (i + j / N * (kParts * kThreads)) * N + j % N;
+            keep(at++, Vec<T>::load1(row.z + v), v);
+          }
+        }
+        if (u == kParts - 1 && tid < row.rest) {
+          const int v = tid < row.head ? tid : row.nvec * N + tid;
+          const float x = Vec<T>::load1(row.z + v);
+          if (x >= least) keep(atomicAdd(&sh.n, 1u), x, v);
+        }
+      }
       __syncthreads();
       n = sh.n;
     }
@@ -632,37 +883,90 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
       finish(d.best.token, d.kept_mass);
       return;
     }
-    Cut cut;
-    if (n <= (uint32_t)kCap) {
-      sort_keys(n, sh);
-      cut = cut_sorted(row, n, 0, 0, lim.count, lim.mass, kNoLimit, sh);
-      if (lim.by_count && lim.by_mass) cut = cut_sorted(row, n, 0, 0, lim.count, lim.part_of((double)cut.mass), kNoLimit, sh);
-      end_key = cut.key;
-      for (uint32_t i = tid; i < n; i += kThreads) look(row.value(sh.keys[i]), sh.keys[i]);
-      best = block_best(best, sh);
-      kept_mass = scan(0, kept_mass, sh).all_mass;
-      finish(best.token, kept_mass);
-      return;
-    }
-    // tokens of at most (1 - top_p) / vocab of the mass each hold no more than 1 - top_p together
-    float depth = 64.f;
-    if (!lim.by_count) {
-      const float low = fmaxf(lim.share, log2_fast((1.f - lim.top_p) * total / (float)vocab) - 0.01f);
+    const bool listed = n <= (uint32_t)kCap;
+    // log2 of the least mass that a token can be kept with, by the candidates' bound; without one, tokens of at most
+    // (1 - top_p) / vocab of the mass each hold no more than 1 - top_p together
+    float low = row.exponent(least);
+    if (!some && !lim.by_count) {
+      low = fmaxf(lim.share, log2_fast((1.f - lim.top_p) * total / (float)vocab) - 0.01f);
       least = fmaxf(least, from_exponent(low));
-      depth = fmaxf(-low, 1.f);
     }
+    const float depth = fminf(fmaxf(-low, 1.f), 64.f);
     // with both limits the first cut, by count, tells the mass that top-p is a share of
+    Cut cut;
     u64 limit_mass = lim.mass;
     for (int pass = lim.by_count && lim.by_mass ? 0 : 1; pass < 2; ++pass) {
-      cut = cut_row(row, least, depth, lim.count, limit_mass, lim.by_mass, sh);
+      if (listed) {
+        auto each = [&](auto f, float, float) {
+          for (uint32_t i = tid; i < n; i += kThreads) f(row.value(sh.keys[i]), sh.keys[i]);
+        };
+        cut = cut_by_exponent(row, each, depth, lim.by_mass, lim.count, limit_mass, sh);
+      } else {
+        bool done = false;
+        if constexpr (sizeof(T) == 2) {
+          if (fabsf(top) < 2147483648.f) {
+            cut = cut_by_value(row, least, lim.count, limit_mass, sh);
+            done = true;
+          }
+        }
+        if (!done) {
+          auto each = [&](auto f, float from, float to) {
+            row.visit_between(fmaxf(from, least), to, [&](float x, int v) { f(x, row.key(x, v)); });
+          };
+          cut = cut_by_exponent(row, each, depth, lim.by_mass, lim.count, limit_mass, sh);
+        }
+      }
       limit_mass = lim.part_of((double)cut.mass);
     }
     end_key = cut.key;
+    if (lim.by_mass && !lim.by_share) kept_mass = cut.mass;
+    if (listed) {
+      for (uint32_t i = tid; i < n; i += kThreads) {
+        const float x = row.value(sh.keys[i]);
+        if (sh.keys[i] >= end_key || row.exponent(x) < lim.share) continue;
+        if (!lim.by_mass || lim.by_share) kept_mass += row.mass(x);
+        best = better(best, scored(x, row.token(sh.keys[i])));
+      }
+      best = block_best(best, sh);
+      if (!lim.by_mass || lim.by_share) kept_mass = scan(0, kept_mass, sh).all_mass;
+      finish(best.token, kept_mass);
+      return;
+    }
   }
-  // ---- the draw from the row itself ----
-  row.visit_from(least, [&](float x, int v) { look(x, row.key(x, v)); });
+  // ---- the draw from the row itself: the random numbers of a vector that has a kept token are asked for together ----
+  const bool sum_mass = !lim.by_mass || lim.by_share;
+  const float last = end_key == kNoLimit ? least : fmaxf(least, row.value(end_key));
+  auto race = [&](float x, float noise_of, int v) {
+    if (x < last || (x == last && row.key(x, v) >= end_key)) return;
+    const float t = row.exponent(x);
+    if (t < lim.share) return;
+    if (sum_mass) kept_mass += row.mass(x);
+    best = better(best, Best{t - log2_fast(clamped_noise(noise_of)), v});
+  };
+  auto one = [&](u32x4 q, int v) {
+    float x[N], w[N];
+    Vec<T>::unpack(q, x);
+    if (largest(x) < last) return;
+    load_noise<N>(e + v, w);
+#pragma unroll
+    for (int j = 0; j < N; ++j) race(x[j], w[j], v + j);
+  };
+  row.template visit<2>(
+      [&](const u32x4* q, int v) {
+        float x[2 * N], w[2 * N];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) Vec<T>::unpack(q[u], x + u * N);
+        if (fmaxf(largest(x), largest(x + N)) < last) return;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) load_noise<N>(e + v + u * kThreads * N, w + u * N);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < N; ++j) race(x[u * N + j], w[u * N + j], v + u * kThreads * N + j);
+      },
+      one, [&](float x, int v) { race(x, e[v], v); });
   best = block_best(best, sh);
-  kept_mass = scan(0, kept_mass, sh).all_mass;
+  if (sum_mass) kept_mass = scan(0, kept_mass, sh).all_mass;
   finish(best.token, kept_mass);
 }
 
