@@ -398,8 +398,8 @@ int ais_mxfp4_logits(ais_ctx* ctx, const unsigned char* hidden_codes, long long 
  * the first one always is.  The drawn token is the arg-max over the kept of  t - log(noise[n, v]),  the lowest index on
  * ties: with independent Exp(1) noise that is a draw from p restricted to the kept tokens.
  *   logits      [n_rows, row_stride] of `dtype`, read only on rows with valid != 0
- *   noise       [n_rows, noise_stride] fp32, of kept tokens alone.  Numbers outside [2^-126, 3e38] count as the nearest of
- *               these, NaN as the largest.
+ *   noise       [n_rows, noise_stride] fp32.  Numbers outside [2^-126, 3e38] count as the nearest of these, NaN as the
+ *               largest (one with its sign bit set as the smallest).
  *   valid       [n_rows] or NULL; rows with valid == 0 get token -1 and log-probs 0
  *   temperature [n_rows] fp32 or NULL (all 1): 0 takes the first ranked token (greedy), with log-probs 0
  *   top_k       [n_rows] int32 or NULL; top_k <= 0 is no limit

@@ -201,6 +201,14 @@ def test_small_temperatures(ctx):
     check(ctx, z, e, temperature=50.0, top_p=0.5)
 
 
+@pytest.mark.parametrize("vocab", [700, 40_000])
+def test_scores_that_a_large_offset_would_round_to_one(ctx, vocab):
+    """x / T is up to 1e6, where floats lie 1/16 apart: many tokens of a row, of one thread too, come that near its best."""
+    z, e = logits(12, vocab, torch.float32, 59)
+    check(ctx, 1000.0 + z * 1e-3, e, temperature=1e-3)
+    check(ctx, z * 1e-3 - 1000.0, e, temperature=1e-3)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("offset", [0, 1, 3, 7, 33])
 def test_rows_that_begin_anywhere(ctx, dtype, offset):
