@@ -25,6 +25,18 @@ typedef const __attribute__((address_space(1))) void* glb_ptr;
 constexpr int kFp4 = 4;                // the instruction's code of the E2M1 format
 constexpr int kGroup = 16;             // blocks whose scales are one 16-byte vector
 
+// Vectors that lie at any multiple of an element: rows of logits begin anywhere.  (Element by element 333 f32 rows x 50,257 x 1,100
+// took 94 us, so 49.)
+template <typename O>
+struct Unaligned {
+  typedef uint32_t four __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <>
+struct Unaligned<bf16_t> {
+  typedef uint32_t four __attribute__((ext_vector_type(4), aligned(2)));
+  typedef uint32_t two __attribute__((ext_vector_type(2), aligned(2)));
+};
+
 // c += w h over four blocks, the scales in the words' low bytes.
 __device__ __forceinline__ void multiply(f32x4& c, i32x4 w, uint32_t w_scale, i32x4 h, uint32_t h_scale) {
   const i32x8 x = {w[0], w[1], w[2], w[3], 0, 0, 0, 0}, y = {h[0], h[1], h[2], h[3], 0, 0, 0, 0};
@@ -64,8 +76,7 @@ struct StreamLds {
 
 template <typename O, int NT, int GPW>
 __global__ __launch_bounds__(kStreamThreads) __attribute__((amdgpu_waves_per_eu(1, 1))) void mxfp4_stream_kernel(
-    Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab, int blocks, O* __restrict__ out, long long out_stride,
-    int out_fours) {
+    Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab, int blocks, O* __restrict__ out, long long out_stride) {
   typedef StreamLds<NT, GPW> L;
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
@@ -176,15 +187,13 @@ __global__ __launch_bounds__(kStreamThreads) __attribute__((amdgpu_waves_per_eu(
         const int t = (int)(blockIdx.y * NT + j) * 16 + a, v = tile * 16 + 4 * quarter;
         if (t >= n_rows) continue;
         O* o = out + (long long)t * out_stride + v;
-        if (out_fours && v + 4 <= vocab) {
-          if constexpr (sizeof(O) == 4) {
-            *reinterpret_cast<f32x4*>(o) = z;
-          } else {
-            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-            const float x[8] = {z[0], z[1], z[2], z[3]};
-            const u32x4 q = Vec<O>::pack(x);
-            *reinterpret_cast<u32x2*>(o) = u32x2{q[0], q[1]};
-          }
+        if (v + 4 <= vocab) {
+          const float x[8] = {z[0], z[1], z[2], z[3]};
+          const u32x4 q = Vec<O>::pack(x);
+          if constexpr (sizeof(O) == 4)
+            *reinterpret_cast<typename Unaligned<O>::four*>(o) = q;
+          else
+            *reinterpret_cast<typename Unaligned<O>::two*>(o) = {q[0], q[1]};
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -255,7 +264,7 @@ struct TileLds {
 template <typename O, int NJ, bool RAGGED>
 __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void mxfp4_tile_kernel(
     Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab, int blocks, TilePlan plan, O* __restrict__ out,
-    long long out_stride, int out_vectors) {
+    long long out_stride) {
   typedef TileLds<NJ> L;
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
@@ -450,10 +459,10 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
         float z[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] = acc[i + (e >> 2)][j][e & 3];
-        if (out_vectors && v + 8 <= vocab) {
+        if (v + 8 <= vocab) {
           constexpr int N = Vec<O>::N;
 #pragma unroll
-          for (int e = 0; e < 8; e += N) *reinterpret_cast<u32x4*>(row + v + e) = Vec<O>::pack(z + e);
+          for (int e = 0; e < 8; e += N) *reinterpret_cast<typename Unaligned<O>::four*>(row + v + e) = Vec<O>::pack(z + e);
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -483,9 +492,8 @@ int launch_tiles(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4R
   plan.n_items = (int)items;
   plan.per_xcd = (plan.n_items + 7) / 8;
   const int locals = plan.per_xcd < (ctx->n_cus + 7) / 8 ? plan.per_xcd : (ctx->n_cus + 7) / 8;
-  const int vectors = reinterpret_cast<uintptr_t>(out) % 16 == 0 && out_stride * (long long)sizeof(O) % 16 == 0;
   kernel<<<dim3((unsigned)(8 * locals)), dim3(kTileThreads), L::kBytes, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, plan,
-                                                                                      out, out_stride, vectors);
+                                                                                      out, out_stride);
   return hip_fail(ctx, hipGetLastError());
 }
 
@@ -499,8 +507,7 @@ int launch_stream(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4
   if (!allow_dynamic_lds(ctx, reinterpret_cast<const void*>(kernel), kBytes, once, ok)) return hip_fail(ctx, hipErrorInvalidValue);
   const int tiles = (vocab + 15) / 16;
   const dim3 grid((unsigned)std::min(tiles, ctx->n_cus), (unsigned)((n_rows + 16 * NT - 1) / (16 * NT)));
-  const int fours = reinterpret_cast<uintptr_t>(out) % (4 * sizeof(O)) == 0 && out_stride % 4 == 0;
-  kernel<<<grid, dim3(kStreamThreads), kBytes, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, out, out_stride, fours);
+  kernel<<<grid, dim3(kStreamThreads), kBytes, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, out, out_stride);
   return hip_fail(ctx, hipGetLastError());
 }
 
@@ -533,9 +540,17 @@ int launch_typed(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4R
     return ragged ? launch_tiles<O, NJ, true>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride)
                   : launch_tiles<O, NJ, false>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
   };
-  if (n_rows <= 64) return tiles(One{});
-  if (n_rows <= 128) return tiles(Two{});
-  return tiles(Four{});
+  // Tiles of 64, 128 or 256 tokens take about 4 : 5 : 8 of time each (x 4,096: 20, 25 and 42 us), and every compute unit one at a
+  // time: what comes out least, the larger ones where that is equal.  us with tiles of 64, 128 and 256: 70 rows x 50,257 x 1,024
+  // 22.0, 17.4 and 21.7; 130 x 151,936 x 4,096 162, 135 and 128; 333 x 151,936 x 2,048 154, 107 and 117; 520 x 50,257 x 4,096 163, 116
+  // and 131; 1,000 x 2,000 x 2,048 17.6, 19.7 and 26.6; 2,048 x 32,000 x 4,096 362, 222 and 169.
+  auto time = [&](int nj, long long each) {
+    const long long items = (long long)((vocab + kTileV - 1) / kTileV) * ((n_rows + 64 * nj - 1) / (64 * nj));
+    return ((items + ctx->n_cus - 1) / ctx->n_cus) * each;
+  };
+  const long long one = time(1, 4), two = time(2, 5), four = time(4, 8);
+  if (four <= two && four <= one) return tiles(Four{});
+  return two <= one ? tiles(Two{}) : tiles(One{});
 }
 
 }  // namespace

@@ -130,6 +130,45 @@ def test_product_sizes(ctx, dtype, rows, vocab, width):
     check_product(ctx, hidden, weight, dtype)
 
 
+@pytest.mark.parametrize("rows,vocab,width", [
+    (5, 700, 2048), (20, 900, 2000), (20, 333, 2080), (13, 5003, 3100), (40, 500, 4096), (64, 1000, 3000), (16, 300, 5120),
+    (30, 300, 6200), (32, 270, 8192), (9, 17, 8180), (33, 4100, 2100)])
+def test_product_of_few_long_rows(ctx, rows, vocab, width):
+    """Contractions of 64 to 256 blocks, whole and with a rest, that wavefronts share."""
+    hidden = ctx.mxfp4_quantize_rows(operand(rows, width, rows))
+    weight = ctx.mxfp4_quantize_rows(operand(vocab, width, vocab + 1))
+    check_product(ctx, hidden, weight, torch.bfloat16)
+
+
+@pytest.mark.parametrize("rows,vocab,width", [
+    (65, 33_500, 40), (128, 40_001, 512), (200, 33_100, 70), (256, 33_281, 1024), (700, 30_000, 96), (1, 70_001, 33)])
+def test_product_of_more_tiles_than_compute_units(ctx, rows, vocab, width):
+    hidden = ctx.mxfp4_quantize_rows(operand(rows, width, rows))
+    weight = ctx.mxfp4_quantize_rows(operand(vocab, width, vocab + 1))
+    check_product(ctx, hidden, weight, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab,width", [(5, 333, 2048), (70, 333, 100), (90, 34_000, 40)])
+@pytest.mark.parametrize("offset,beside", [(1, 0), (3, 2), (0, 5)])
+def test_product_into_rows_that_begin_anywhere(ctx, dtype, rows, vocab, width, offset, beside):
+    hidden = ctx.mxfp4_quantize_rows(operand(rows, width, rows))
+    weight = ctx.mxfp4_quantize_rows(operand(vocab, width, vocab + 1))
+    want = ctx.mxfp4_logits(*hidden, *weight, dtype=dtype)
+    stride = vocab + beside
+    room = torch.full((rows * stride + 16,), 7.0, device="cuda", dtype=dtype)
+    out = room[offset:offset + rows * stride].view(rows, stride)
+    ctx._sync_stream()
+    rc = B._lib().ais_mxfp4_logits(ctx._h, hidden[0].data_ptr(), hidden[0].stride(0), hidden[1].data_ptr(), hidden[1].stride(0),
+                                   rows, weight[0].data_ptr(), weight[0].stride(0), weight[1].data_ptr(), weight[1].stride(0),
+                                   vocab, width, out.data_ptr(), B._dtype_code(out), stride)
+    assert rc == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, :vocab], want)
+    out[:, :vocab] = 7.0
+    assert bool((room == 7.0).all())           # nothing beside the logits was written
+
+
 @pytest.mark.parametrize("rows", [1, 20, 130])
 def test_product_of_views(ctx, rows):
     """Rows of a larger matrix, every other row, and a column range of whole blocks."""
