@@ -15,10 +15,11 @@
 // registers.  Up to 4,096, tokens and masses are counted in 2,048 ranges of the exponent, and the range in which the cut lies is
 // sorted.  Where there is no such bound (flat rows, more tokens than parts) the same is done to the row itself; of a bf16 row the
 // tokens of every value are counted instead, whose masses follow from their number, so that a token costs one addition in LDS.
+// The tokens that share the cut's value are found by the draw, which passes over such a row sixteen tokens at a time.
 // Masses are summed as fixed-point numbers, so no result depends on the order in which threads arrive.
 //
 // Measured, us a call, logits in the cache of a step that made them: bf16 rows of 151,936 without limits 19 (1 row), 22 (64) and
-// 51 (256: 233 MB, 4.6 TB/s); of 64 such rows with limits 44 (top-k), 22 (min-p), 97 (top-p over flat rows, all of whose tokens
+// 51 (256: 233 MB, 4.6 TB/s); of 64 such rows with limits 45 (top-k), 21 (min-p), 79 (top-p over flat rows, all of whose tokens
 // pass the bound).  Few rows are bound by one compute unit's reading of its row and the barriers between the passes, many without
 // limits by memory.
 #include "ais_internal.h"
@@ -50,6 +51,9 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 __device__ __forceinline__ float from_ordered(uint32_t o) {
   return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu));
 }
+
+// A number that all lanes have, as one of the wavefront.
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
 struct Best {
   float score;
@@ -284,11 +288,14 @@ __device__ __forceinline__ void sort_keys(uint32_t n, u64* keys) {
   }
 }
 
-// Where the kept tokens end: those whose key is less than `key` are kept.
+// Where the kept tokens end: those whose key is less than `key` are kept, and of those of the logit `edge`, if take > 0, the first
+// `take`, whose keys are not less.
 struct Cut {
   u64 key;
   uint32_t count;
   u64 mass;
+  uint32_t take = 0;
+  float edge = 0.f;
 };
 
 // Tokens among which the cut lies: their keys are in [lo, hi), `above` tokens rank before them.
@@ -477,7 +484,8 @@ __device__ __forceinline__ int value_place(float x) {
 __device__ Cut cut_by_value(const Row<bf16_t>& row, float least, uint32_t limit_count, u64 limit_mass, SampleShared& sh) {
   constexpr int kOwn = kValues / kThreads;
   __syncthreads();
-  for (int b = threadIdx.x; b < kValues; b += kThreads) sh.value_count[b] = 0;
+  u32x4* counts = reinterpret_cast<u32x4*>(sh.value_count);
+  for (int b = threadIdx.x; b < kValues / 4; b += kThreads) counts[b] = u32x4{0, 0, 0, 0};
   if (threadIdx.x == 0) sh.bin = -1;
   __syncthreads();
   auto add = [&](float x) {
@@ -503,11 +511,15 @@ __device__ Cut cut_by_value(const Row<bf16_t>& row, float least, uint32_t limit_
     return place >= kValues / 2 ? -x : x;
   };
   Span s{0, kNoLimit, 0, 0, 0};
+  u32x4 own[kOwn / 4];
+#pragma unroll
+  for (int k = 0; k < kOwn / 4; ++k) own[k] = counts[kOwn / 4 * (int)threadIdx.x + k];
   const Before all = find_range<kOwn>(
       [&](int k, auto f) {
-        const int place = kOwn * (int)threadIdx.x + k;
-        const uint32_t c = sh.value_count[place];
-        if (c > 0) f(c, c * row.mass(value_of(place)));
+        uint32_t c = 0;
+#pragma unroll
+        for (int j = 0; j < kOwn; ++j) c = j == k ? own[j / 4][j % 4] : c;
+        if (c > 0) f(c, c * row.mass(value_of(kOwn * (int)threadIdx.x + k)));
       },
       s, limit_count, limit_mass, sh);
   if (sh.bin < 0) return Cut{kNoLimit, all.all_count, all.all_mass};
@@ -525,6 +537,14 @@ __device__ Cut cut_by_value(const Row<bf16_t>& row, float least, uint32_t limit_
   }
   if (bin == 0) upper = row.top;
   if (bin == kValues - 1) lower = kLowest;
+  if (upper == lower && s.n <= (uint32_t)kMembers) {   // as many of them as the limits allow: the draw finds the first ones
+    const u64 each = row.mass(x);
+    u64 take = min(s.n, limit_count - s.above_count);
+    if (each > 0 && limit_mass != kNoLimit) take = min(take, (limit_mass - s.above_mass + each - 1) / each);
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    return Cut{row.key(x, 0), s.above_count + (uint32_t)take, s.above_mass + take * each, (uint32_t)take, x};
+  }
   s.lo = row.key(upper, 0);
   s.hi = row.key(lower, row.vocab - 1) + 1;
   auto inside = [&](auto f) {
@@ -711,7 +731,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   lim.by_mass = lim.top_p < 1.f;
   lim.by_share = min_p > 0.f;
   lim.count = lim.by_count ? (uint32_t)k : 0xffffffffu;
-  lim.share = lim.by_share ? log2_fast(min_p) : -__builtin_inff();
+  lim.share = uniform(lim.by_share ? log2_fast(min_p) : -__builtin_inff());
   lim.mass = kNoLimit;
 
   Row<T> row;
@@ -722,7 +742,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   row.rest = vocab - row.nvec * N;
   row.index_bits = vocab > 1 ? 32 - __builtin_clz((unsigned)(vocab - 1)) : 1;
   row.mass_bits = min(40, 62 - row.index_bits);
-  row.c = greedy ? kLog2e : kLog2e / temperature;
+  row.c = uniform(greedy ? kLog2e : kLog2e / temperature);
   const float* e = noise + r * noise_stride;
   const bool open = k != 1 && !lim.by_count && !lim.by_mass && !lim.by_share;
 
@@ -852,6 +872,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     if (w > 0) st = merge(st, sh.wave_sum[w]);
     top = fmaxf(top, sh.wave_max[w]);
   }
+  top = uniform(top);
   row.top = top;
   // a NaN or +inf makes the sum NaN; nothing but -inf leaves no largest
   if (!(st.s > 0.f) || !(st.m < 3.4e38f) || !(top > -3.4e38f)) {
@@ -859,7 +880,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     return;
   }
   // the sum relative to the largest logit's exponential: st.m is the rounded product top * c
-  const float total = st.s * exp2_fast(-__builtin_fmaf(top, row.c, -st.m));
+  const float total = uniform(st.s * exp2_fast(-__builtin_fmaf(top, row.c, -st.m)));
   auto scored = [&](float x, int v) { return Best{row.exponent(x) - log2_fast(clamped_noise(e[v])), v}; };
   auto finish = [&](int token, u64 kept_mass) {
     if (tid != 0) return;
@@ -870,6 +891,16 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     const double at = (double)row.exponent(Vec<T>::load1(row.z + token)) * 0.6931471805599453;
     const double full = at - log((double)total);
     answer(token, (float)(kept_mass > 0 ? at - log(ldexp((double)kept_mass, -row.mass_bits)) : full), (float)full);
+  };
+  // Scores the best vectors, or all vectors, of the threads that ask for it once more, the wavefront for each of them together.
+  auto look_again = [&](bool ask, bool all, auto score) {
+    for (u64 who = __ballot(ask); who != 0; who &= who - 1) {
+      const int lane = __builtin_ctzll(who);
+      const bool every = __shfl((int)all, lane) != 0;
+      const int from = every ? (tid & ~63) + lane : __shfl(best_at, lane);
+      const int n = (every ? (row.nvec - from + kThreads - 1) / kThreads : __shfl(best_many, lane)) * N;
+      for (int j = tid & 63; j < n; j += 64) best = better(best, score(row.head + (from + j / N * kThreads) * N + j % N));
+    }
   };
   if (k == 1) {
     best = Best{-__builtin_inff(), vocab};
@@ -884,15 +915,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     near -= 1e-6f * (fabsf(near) + fabsf(top * row.c) + 300.f);                // some times what the scores are rounded by
     best = best.score >= near && best.token < vocab ? scored(Vec<T>::load1(row.z + best.token), best.token)
                                                     : Best{-__builtin_inff(), vocab};
-    if (best_score >= near) {
-      const bool all = second_score >= near;           // of the thread's vectors; rare, except at very large logits / temperature
-      const int last = all ? row.nvec : min(row.nvec, best_at + best_many * kThreads);
-      for (int i = all ? tid : best_at; i < last; i += kThreads)
-        for (int j = 0; j < N; ++j) {
-          const int v = row.head + i * N + j;
-          best = better(best, scored(Vec<T>::load1(row.z + v), v));
-        }
-    }
+    // all of a thread's vectors: rare, except at very large logits over the temperature
+    look_again(best_score >= near, second_score >= near, [&](int v) { return scored(Vec<T>::load1(row.z + v), v); });
     finish(block_best(best, sh).token, 0);
     return;
   }
@@ -900,61 +924,64 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   // (x - top) c >= the least exponent, with room for its rounding: the condition itself is looked at again
   auto from_exponent = [&](float low) { return top + low / row.c - 1e-5f * (fabsf(top) + fabsf(low / row.c)); };
   float least = lim.by_share && !lim.by_count ? fmaxf(from_exponent(lim.share), kLowest) : kLowest;
-  u64 kept_mass = 0, end_key = kNoLimit;
-  if (lim.by_count || lim.by_mass) {
-    // ---- candidates ----
-    float bounded = kLowest;
-    const bool some = bound(row, lim, total, own_top, &bounded, sh);
-    if (some) least = fmaxf(least, bounded);
-    uint32_t n = 0xffffffffu;
-    if (some) {
-      // a part whose largest logit is smaller has none
-      const u32x4* zv = reinterpret_cast<const u32x4*>(row.z + row.head);
-      auto keep = [&](uint32_t at, float x, int v) {
-        if (at < (uint32_t)kCap) sh.keys[at] = row.key(x, v);
-      };
+  u64 kept_mass = 0;
+  Cut cut{kNoLimit, 0, 0};
+  const bool sum_mass = !lim.by_mass || lim.by_share;  // of the kept tokens; otherwise the cut tells it
+  // ---- candidates ----
+  float bounded = kLowest;
+  const bool cuts = lim.by_count || lim.by_mass;        // min-p is a bound by itself
+  const bool some = !cuts || bound(row, lim, total, own_top, &bounded, sh);
+  if (some) least = fmaxf(least, bounded);
+  uint32_t n = 0xffffffffu;
+  if (some) {
+    // a part whose largest logit is smaller has none
+    const u32x4* zv = reinterpret_cast<const u32x4*>(row.z + row.head);
+    auto keep = [&](uint32_t at, float x, int v) {
+      if (at < (uint32_t)kCap) sh.keys[at] = row.key(x, v);
+    };
 #pragma unroll
-      for (int u = 0; u < kParts; ++u) {
-        if (own_top[u] < least) continue;
-        constexpr int kAhead = 5;
-        for (int i = tid + u * kThreads; i < row.nvec; i += kAhead * kParts * kThreads) {
-          u32x4 q[kAhead];
+    for (int u = 0; u < kParts; ++u) {
+      if (own_top[u] < least) continue;
+      constexpr int kAhead = 5;
+      for (int i = tid + u * kThreads; i < row.nvec; i += kAhead * kParts * kThreads) {
+        u32x4 q[kAhead];
 #pragma unroll
-          for (int a = 0; a < kAhead; ++a) q[a] = zv[min(i + a * kParts * kThreads, row.nvec - 1)];
-          u64 found = 0;
+        for (int a = 0; a < kAhead; ++a) q[a] = zv[min(i + a * kParts * kThreads, row.nvec - 1)];
+        u64 found = 0;
 #pragma unroll
-          for (int a = 0; a < kAhead; ++a) {
-            float x[N];
-            Vec<T>::unpack(q[a], x);
-            uint32_t here = 0;
+        for (int a = 0; a < kAhead; ++a) {
+          float x[N];
+          Vec<T>::unpack(q[a], x);
+          uint32_t here = 0;
 #pragma unroll
-            for (int j = 0; j < N; ++j) here |= (uint32_t)(x[j] >= least) << j;
-            if (i + a * kParts * kThreads < row.nvec) found |= (u64)here << (a * N);
-          }
-          if (found == 0) continue;
-          uint32_t at = atomicAdd(&sh.n, (uint32_t)__popcll(found));
-          for (; found != 0; found &= found - 1) {     // read again: they are few
-            const int j = __builtin_ctzll(found);
-            const int v = row.head + (i + j / N * (kParts * kThreads)) * N + j % N;
-            keep(at++, Vec<T>::load1(row.z + v), v);
-          }
+          for (int j = 0; j < N; ++j) here |= (uint32_t)(x[j] >= least) << j;
+          if (i + a * kParts * kThreads < row.nvec) found |= (u64)here << (a * N);
         }
-        if (u == kParts - 1 && tid < row.rest) {
-          const int v = tid < row.head ? tid : row.nvec * N + tid;
-          const float x = Vec<T>::load1(row.z + v);
-          if (x >= least) keep(atomicAdd(&sh.n, 1u), x, v);
+        if (found == 0) continue;
+        uint32_t at = atomicAdd(&sh.n, (uint32_t)__popcll(found));
+        for (; found != 0 && at < (uint32_t)kCap; found &= found - 1) {        // read again: they are few, or counted only
+          const int j = __builtin_ctzll(found);
+          const int v = row.head + (i + j / N * (kParts * kThreads)) * N + j % N;
+          keep(at++, Vec<T>::load1(row.z + v), v);
         }
       }
-      __syncthreads();
-      n = sh.n;
+      if (u == kParts - 1 && tid < row.rest) {
+        const int v = tid < row.head ? tid : row.nvec * N + tid;
+        const float x = Vec<T>::load1(row.z + v);
+        if (x >= least) keep(atomicAdd(&sh.n, 1u), x, v);
+      }
     }
-    if (n <= 64) {
-      if (tid >= 64) return;
-      const Drawn d = draw_from_few(row, lim, n, sh.keys, scored);
-      finish(d.best.token, d.kept_mass);
-      return;
-    }
-    const bool listed = n <= (uint32_t)kCap;
+    __syncthreads();
+    n = sh.n;
+  }
+  if (n <= 64) {
+    if (tid >= 64) return;
+    const Drawn d = draw_from_few(row, lim, n, sh.keys, scored);
+    finish(d.best.token, d.kept_mass);
+    return;
+  }
+  const bool listed = n <= (uint32_t)kCap;
+  if (cuts) {
     // log2 of the least mass that a token can be kept with, by the candidates' bound; without one, tokens of at most
     // (1 - top_p) / vocab of the mass each hold no more than 1 - top_p together
     float low = row.exponent(least);
@@ -964,7 +991,6 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     }
     const float depth = fminf(fmaxf(-low, 1.f), 64.f);
     // with both limits the first cut, by count, tells the mass that top-p is a share of
-    Cut cut;
     u64 limit_mass = lim.mass;
     for (int pass = lim.by_count && lim.by_mass ? 0 : 1; pass < 2; ++pass) {
       if (listed) {
@@ -975,7 +1001,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
       } else {
         bool done = false;
         if constexpr (sizeof(T) == 2) {
-          if (fabsf(top) < 2147483648.f) {
+          // what counts as zero has the same mass but for 2^-32 c < 2^-20 of the exponent
+          if (fabsf(top) < 2147483648.f && row.c < 4096.f) {
             cut = cut_by_value(row, least, lim.count, limit_mass, sh);
             done = true;
           }
@@ -989,53 +1016,111 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
       }
       limit_mass = lim.part_of((double)cut.mass);
     }
-    end_key = cut.key;
-    if (lim.by_mass && !lim.by_share) kept_mass = cut.mass;
-    if (listed) {
-      for (uint32_t i = tid; i < n; i += kThreads) {
-        const float x = row.value(sh.keys[i]);
-        if (sh.keys[i] >= end_key || row.exponent(x) < lim.share) continue;
-        if (!lim.by_mass || lim.by_share) kept_mass += row.mass(x);
-        best = better(best, scored(x, row.token(sh.keys[i])));
+    if (!sum_mass) kept_mass = cut.mass;
+  }
+  if (listed) {
+    for (uint32_t i = tid; i < n; i += kThreads) {
+      const float x = row.value(sh.keys[i]);
+      if (sh.keys[i] >= cut.key || row.exponent(x) < lim.share) continue;
+      if (sum_mass) kept_mass += row.mass(x);
+      best = better(best, scored(x, row.token(sh.keys[i])));
+    }
+    best = block_best(best, sh);
+    if (sum_mass) kept_mass = scan(0, kept_mass, sh).all_mass;
+    finish(best.token, kept_mass);
+    return;
+  }
+  // ---- the draw from the row itself: sixteen logits at a time, of which only the best score is looked at, as above; their random
+  // numbers are asked for where one of them may be kept.
+  const float last = uniform(cut.key == kNoLimit ? least : fmaxf(least, row.value(cut.key)));
+  const int end = __builtin_amdgcn_readfirstlane(
+      cut.key != kNoLimit && row.value(cut.key) == last ? row.token(cut.key) : vocab);        // of the tokens of that logit
+  const uint32_t take = __builtin_amdgcn_readfirstlane(cut.take);
+  const float edge = uniform(cut.edge);
+  constexpr int kOpen = 16 / N;
+  const int head = __builtin_amdgcn_readfirstlane(row.head), nvec = __builtin_amdgcn_readfirstlane(row.nvec);
+  const u32x4* zv = reinterpret_cast<const u32x4*>(logits + r * row_stride + head);
+  const float* ev = noise + r * noise_stride + head;
+  const float share = uniform(lim.share), scale = uniform(row.c), origin = uniform(row.top);
+  auto full_score = [&](float x, float noise_of) { return (x - origin) * scale - log2_fast(clamped_noise(noise_of)); };
+  auto score_of = [&](float x, float noise_of, int v) {
+    float score = full_score(x, noise_of);
+    asm volatile("" : "+v"(score));                    // a choice of two numbers, no branch for each token
+    const bool kept = ((x > last) | ((x == last) & (v < end))) & ((x - origin) * scale >= share);
+    return kept ? score : -__builtin_inff();
+  };
+  auto at_edge = [&](float x, int v) {                 // no more than there is room for
+    sh.mass[atomicAdd(&sh.n, 1u)] = (u64)v << 32 | __float_as_uint(full_score(x, ev[v - head]));
+  };
+  auto race = [&](auto many, int i) {
+    constexpr int kMany = decltype(many)::value;
+    u32x4 q[kMany];
+    float x[kMany * N], w[kMany * N];
+#pragma unroll
+    for (int u = 0; u < kMany; ++u) q[u] = zv[i + u * kThreads];
+#pragma unroll
+    for (int u = 0; u < kMany; ++u) load_noise<N>(ev + (i + u * kThreads) * N, w + u * N);
+#pragma unroll
+    for (int u = 0; u < kMany; ++u) Vec<T>::unpack(q[u], x + u * N);
+#pragma unroll
+    for (int j = 0; j < kMany * N; ++j) w[j] = score_of(x[j], w[j], head + (i + j / N * kThreads) * N + j % N);
+    float m = w[0];
+#pragma unroll
+    for (int j = 1; j < kMany * N; ++j) m = fmaxf(m, w[j]);
+    auto each = [&](uint32_t found, auto f) {          // f(logit, index): few of them, mostly
+      for (; found != 0; found &= found - 1) {
+        const int j = __builtin_ctz(found);
+        u32x4 own = q[0];
+#pragma unroll
+        for (int u = 1; u < kMany; ++u) own = j / N == u ? q[u] : own;
+        f(element<T>(own, j % N), head + (i + j / N * kThreads) * N + j % N);
       }
-      best = block_best(best, sh);
-      if (!lim.by_mass || lim.by_share) kept_mass = scan(0, kept_mass, sh).all_mass;
-      finish(best.token, kept_mass);
-      return;
+    };
+    if (sum_mass && m > -__builtin_inff()) {
+      uint32_t found = 0;
+#pragma unroll
+      for (int j = 0; j < kMany * N; ++j) found |= (uint32_t)(w[j] > -__builtin_inff()) << j;
+      each(found, [&](float z, int) { kept_mass += row.mass(z); });
+    }
+    if (take > 0) {
+      uint32_t found = 0;
+#pragma unroll
+      for (int j = 0; j < kMany * N; ++j) found |= (uint32_t)(x[j] == edge) << j;
+      each(found, at_edge);
+    }
+    if (m > best_score) {
+      best_score = m;
+      best_at = i;
+      best_many = kMany;
+    }
+  };
+  int i = tid;
+  for (; i + (kOpen - 1) * kThreads < nvec; i += kOpen * kThreads) race(std::integral_constant<int, kOpen>{}, i);
+  for (; i < nvec; i += kThreads) race(std::integral_constant<int, 1>{}, i);
+  best = Best{-__builtin_inff(), vocab};
+  if (tid < row.rest) {
+    const int v = tid < head ? tid : nvec * N + tid;
+    const float x = Vec<T>::load1(row.z + v);
+    best.score = score_of(x, e[v], v);
+    if (best.score > -__builtin_inff()) {
+      best.token = v;
+      if (sum_mass) kept_mass += row.mass(x);
+    }
+    if (take > 0 && x == edge) at_edge(x, v);
+  }
+  const float won = wave_max(fmaxf(best_score, best.score));
+  if ((tid & 63) == 0) sh.vote_mass[0][tid >> 6] = won;
+  __syncthreads();
+  float first = sh.vote_mass[0][0];
+  for (int w = 1; w < kWaves; ++w) first = fmaxf(first, sh.vote_mass[0][w]);
+  look_again(best_score >= first, false, [&](int v) { return Best{score_of(Vec<T>::load1(row.z + v), e[v], v), v}; });
+  if (take > 0 && row.exponent(edge) >= share) {
+    sort_keys(sh.n, sh.mass);
+    for (uint32_t j = tid; j < take; j += kThreads) {
+      if (sum_mass) kept_mass += row.mass(edge);
+      best = better(best, Best{__uint_as_float((uint32_t)sh.mass[j]), (int)(sh.mass[j] >> 32)});
     }
   }
-  // ---- the draw from the row itself: the random numbers of a vector that has a kept token are asked for together ----
-  const bool sum_mass = !lim.by_mass || lim.by_share;
-  const float last = end_key == kNoLimit ? least : fmaxf(least, row.value(end_key));
-  auto race = [&](float x, float noise_of, int v) {
-    if (x < last || (x == last && row.key(x, v) >= end_key)) return;
-    const float t = row.exponent(x);
-    if (t < lim.share) return;
-    if (sum_mass) kept_mass += row.mass(x);
-    best = better(best, Best{t - log2_fast(clamped_noise(noise_of)), v});
-  };
-  auto one = [&](u32x4 q, int v) {
-    float x[N], w[N];
-    Vec<T>::unpack(q, x);
-    if (largest(x) < last) return;
-    load_noise<N>(e + v, w);
-#pragma unroll
-    for (int j = 0; j < N; ++j) race(x[j], w[j], v + j);
-  };
-  row.template visit<2>(
-      [&](const u32x4* q, int v) {
-        float x[2 * N], w[2 * N];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) Vec<T>::unpack(q[u], x + u * N);
-        if (fmaxf(largest(x), largest(x + N)) < last) return;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) load_noise<N>(e + v + u * kThreads * N, w + u * N);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int j = 0; j < N; ++j) race(x[u * N + j], w[u * N + j], v + u * kThreads * N + j);
-      },
-      one, [&](float x, int v) { race(x, e[v], v); });
   best = block_best(best, sh);
   if (sum_mass) kept_mass = scan(0, kept_mass, sh).all_mass;
   finish(best.token, kept_mass);

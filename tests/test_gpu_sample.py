@@ -113,6 +113,19 @@ def test_many_tokens_kept(ctx, kind, limits):
     check(ctx, z.to(torch.bfloat16 if kind != "flat" else torch.float32), e, **limits)
 
 
+@pytest.mark.parametrize("limits", [dict(top_p=0.97), dict(top_k=6000), dict(top_k=9000, top_p=0.9), dict(min_p=0.5),
+                                    dict(top_p=0.97, min_p=0.6), dict(top_k=7000, min_p=0.6), dict(top_p=0.3)])
+@pytest.mark.parametrize("centre", [0.0, 1e-12, -5.0, 100.0, -3e4, 4e9, -4e9])
+def test_flat_rows_of_few_values(ctx, centre, limits):
+    """bf16 rows whose every token is about as likely, at both ends of the values that are told apart and beyond them."""
+    z, e = logits(3, 30_001, torch.float32, 31, scale=1.0)
+    spread = max(0.02 * abs(centre), 1e-14)
+    z = (centre + spread * z).to(torch.bfloat16)
+    z[1, 5::7] = -math.inf
+    z[2, :20_000] = z[2, 0]
+    check(ctx, z, e, temperature=2.5 * spread, **limits)
+
+
 def test_the_cut_between_equal_logits(ctx):
     """2,500 equal logits, the random numbers favour the last of those kept."""
     for k in (1, 2, 63, 64, 65, 1000, 1024, 1025, 2048, 2049, 2499, 2500):
