@@ -479,6 +479,7 @@ constexpr int kMostVectors = 20;       // of a lane, in registers alone
 constexpr int kMostSlots = 13;         // ... and in LDS beside them
 constexpr int kLdsSlots = 9;           // 144 KiB of the 160
 constexpr int kWide = 1024;
+constexpr long long kMostRows = 1LL << 21;              // of a launch
 
 template <typename T, bool ALIGNED, int THREADS, int NV, int NL, int KFULL>
 int launch_held_as(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size_t listed_bytes) {
@@ -561,10 +562,28 @@ int launch_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long 
     while (slots < 2 * n_top) slots *= 2;
     auto run = [&](auto type) {
       typedef decltype(type) T;
-      const DistillArgs<T> args{static_cast<const T*>(logits), row_stride, vocab, ids, teacher, n_top, slots, valid, weight,
-                                inv_rows, inv_temperature, exact_exponents(inv_temperature), kl_out,
-                                static_cast<T*>(dlogits), dlogits_stride, ctx->status_dev};
-      return launch_rows(ctx, args, n_rows);
+      // no more than 2^31 threads to a launch
+      for (long long r = 0; r < n_rows; r += kMostRows) {
+        const DistillArgs<T> args{static_cast<const T*>(logits) + r * row_stride,
+                                  row_stride,
+                                  vocab,
+                                  ids + r * n_top,
+                                  teacher + r * n_top,
+                                  n_top,
+                                  slots,
+                                  valid != nullptr ? valid + r : nullptr,
+                                  weight != nullptr ? weight + r : nullptr,
+                                  inv_rows,
+                                  inv_temperature,
+                                  exact_exponents(inv_temperature),
+                                  kl_out + r,
+                                  dlogits != nullptr ? static_cast<T*>(dlogits) + r * dlogits_stride : nullptr,
+                                  dlogits_stride,
+                                  ctx->status_dev};
+        const int rc = launch_rows(ctx, args, n_rows - r < kMostRows ? n_rows - r : kMostRows);
+        if (rc != AIS_OK) return rc;
+      }
+      return (int)AIS_OK;
     };
     const int rc = dtype == AIS_BF16 ? run(bf16_t{}) : run(float{});
     if (rc != AIS_OK) return rc;

@@ -1133,15 +1133,18 @@ int launch_sample_tokens(ais_ctx* ctx, const void* logits, ais_dtype dtype, long
                          int* token_out, float* logp_out, float* logp_full_out) {
   if (n_rows == 0) return AIS_OK;
   ScopedTimer timer(ctx, AIS_K_SAMPLE);
-  const dim3 grid((unsigned)n_rows), block(kThreads);
-  if (dtype == AIS_BF16)
-    sample_kernel<bf16_t><<<grid, block, 0, ctx->stream>>>(static_cast<const bf16_t*>(logits), row_stride, vocab, noise,
-                                                           noise_stride, valid, limits, token_out, logp_out, logp_full_out,
-                                                           ctx->status_dev);
-  else
-    sample_kernel<float><<<grid, block, 0, ctx->stream>>>(static_cast<const float*>(logits), row_stride, vocab, noise,
-                                                          noise_stride, valid, limits, token_out, logp_out, logp_full_out,
-                                                          ctx->status_dev);
+  auto run = [&](auto type) {
+    typedef decltype(type) T;
+    constexpr long long kMostRows = (1LL << 31) / kThreads;                    // of a launch
+    auto from = [](auto* p, long long r) { return p != nullptr ? p + r : nullptr; };
+    for (long long r = 0; r < n_rows; r += kMostRows)
+      sample_kernel<T><<<dim3((unsigned)(n_rows - r < kMostRows ? n_rows - r : kMostRows)), dim3(kThreads), 0, ctx->stream>>>(
+          static_cast<const T*>(logits) + r * row_stride, row_stride, vocab, noise + r * noise_stride, noise_stride, from(valid, r),
+          SampleLimits{from(limits.temperature, r), from(limits.top_k, r), from(limits.top_p, r), from(limits.min_p, r)},
+          token_out + r, logp_out + r, from(logp_full_out, r), ctx->status_dev);
+  };
+  if (dtype == AIS_BF16) run(bf16_t{});
+  else run(float{});
   return hip_fail(ctx, hipGetLastError());
 }
 
