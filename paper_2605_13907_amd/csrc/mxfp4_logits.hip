@@ -261,11 +261,15 @@ struct TileLds {
   static constexpr int kBytes = kScales + 2 * kScaleBytes;
 };
 
-template <typename O, int NJ, bool RAGGED>
+// What the last group of a row's blocks holds: all 16, nine or more, or no more than eight, which are a step by themselves.
+enum Tail { kWhole, kLong, kShort };
+
+template <typename O, int NJ, Tail TAIL>
 __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void mxfp4_tile_kernel(
     Mxfp4Rows hidden, int n_rows, Mxfp4Rows weight, int vocab, int blocks, TilePlan plan, O* __restrict__ out,
     long long out_stride) {
   typedef TileLds<NJ> L;
+  constexpr bool RAGGED = TAIL != kWhole;
   extern __shared__ __align__(16) unsigned char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4;
   const int wv = wave & 1, wt = wave >> 1;
@@ -313,18 +317,18 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
   // the cursor of the copies
   int c_item = item0, c_group = 0;
   point(item0);
-  auto copy_codes = [&](int half) {                             // of step 2 c_group + half, into buffer `half`
+  auto copy_codes = [&](int half, int to) {                     // of step 2 c_group + half, into buffer `to`
     const int block = c_group * kGroup + half * kStepBlocks;
     const uint32_t wb = 16u * (uint32_t)(RAGGED ? min(block + w_chunk, blocks - 1) : block + w_chunk);
     const uint32_t hb = 16u * (uint32_t)(RAGGED ? min(block + h_chunk, blocks - 1) : block + h_chunk);
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       __builtin_amdgcn_global_load_lds((glb_ptr)(w_base + (w_off[q] + wb)),
-                                       (lds_ptr)(lds + L::kW + half * kTileV * kRowBytes + (8 * wave + 64 * q) * kRowBytes), 16, 0, 0);
+                                       (lds_ptr)(lds + L::kW + to * kTileV * kRowBytes + (8 * wave + 64 * q) * kRowBytes), 16, 0, 0);
 #pragma unroll
     for (int q = 0; q < NJ; ++q)
       __builtin_amdgcn_global_load_lds((glb_ptr)(h_base + (h_off[q] + hb)),
-                                       (lds_ptr)(lds + L::kH + half * L::kTileT * kRowBytes + (8 * wave + 64 * q) * kRowBytes), 16, 0,
+                                       (lds_ptr)(lds + L::kH + to * L::kTileT * kRowBytes + (8 * wave + 64 * q) * kRowBytes), 16, 0,
                                        0);
   };
   auto copy_scales = [&](int buffer) {
@@ -352,8 +356,8 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
 
   f32x4 acc[kNI][NJ];
   copy_scales(0);
-  copy_codes(0);
-  int scale_buffer = 0;
+  copy_codes(0, 0);
+  int scale_buffer = 0, buffer = 0;
   for (int item = item0; item < item_end; item += locals) {
 #pragma unroll
     for (int i = 0; i < kNI; ++i)
@@ -363,17 +367,19 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
         asm volatile("" : "+a"(acc[i][j]));
       }
     wait();
-    // A group of blocks: two steps.  No branch inside: the compiler would move products across it, and accumulators with them.
+    // A group of blocks: two steps, or one.  No branch inside: the compiler would move products across it, and accumulators with them.
     auto two_steps = [&](int g, auto last) __attribute__((always_inline)) {
+      constexpr bool kLast = decltype(last)::value;
+      constexpr int kHalves = kLast && TAIL == kShort ? 1 : 2;
       uint32_t ws[kNI], hs[NJ];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+      for (int half = 0; half < kHalves; ++half) {
         // this step's copies, the only ones in flight, have landed everywhere, and nobody reads the step before any more
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (half == 0) {
-          copy_codes(1);
+        if (half + 1 < kHalves) {
+          copy_codes(1, buffer ^ 1);
         } else {
-          if constexpr (decltype(last)::value) {                // on to the next tile; after the last one once more to its beginning
+          if constexpr (kLast) {                // on to the next tile; after the last one once more to its beginning
             c_group = 0;
             c_item = c_item + locals < item_end ? c_item + locals : c_item;
             point(c_item);
@@ -381,7 +387,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
             ++c_group;
           }
           copy_scales(scale_buffer ^ 1);
-          copy_codes(0);
+          copy_codes(0, buffer ^ 1);
         }
         if (half == 0) {
           const unsigned char* sl = lds + L::kScales + scale_buffer * L::kScaleBytes;
@@ -407,8 +413,9 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
           for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(hs[j]));
           wait();
         }
-        const unsigned char* wl = lds + L::kW + half * kTileV * kRowBytes;
-        const unsigned char* hl = lds + L::kH + half * L::kTileT * kRowBytes;
+        const unsigned char* wl = lds + L::kW + buffer * kTileV * kRowBytes;
+        const unsigned char* hl = lds + L::kH + buffer * L::kTileT * kRowBytes;
+        buffer ^= 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           // the embedding's fragments are read two MFMA tiles ahead
@@ -474,11 +481,11 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // copies for nobody land before the LDS is given back
 }
 
-template <typename O, int NJ, bool RAGGED>
+template <typename O, int NJ, Tail TAIL>
 int launch_tiles(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4Rows& weight, int vocab, int blocks, O* out,
                  long long out_stride) {
   typedef TileLds<NJ> L;
-  auto kernel = mxfp4_tile_kernel<O, NJ, RAGGED>;
+  auto kernel = mxfp4_tile_kernel<O, NJ, TAIL>;
   static std::once_flag once[kMaxDevices];
   static bool ok[kMaxDevices];
   if (!allow_dynamic_lds(ctx, reinterpret_cast<const void*>(kernel), L::kBytes, once, ok))
@@ -534,11 +541,14 @@ int launch_typed(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4R
     return n_rows <= 16 ? rows(One{}) : rows(Two{});
   }
   if (n_rows <= 64 && groups > 4 && groups <= 8) return stream(Four{}, Two{});
-  const bool ragged = blocks % kGroup != 0;
+  const int tail = blocks % kGroup;
   auto tiles = [&](auto nj) {
     constexpr int NJ = decltype(nj)::value;
-    return ragged ? launch_tiles<O, NJ, true>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride)
-                  : launch_tiles<O, NJ, false>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+    auto run = [&](auto kind) {
+      return launch_tiles<O, NJ, decltype(kind)::value>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
+    };
+    if (tail == 0) return run(std::integral_constant<Tail, kWhole>{});
+    return tail > kStepBlocks ? run(std::integral_constant<Tail, kLong>{}) : run(std::integral_constant<Tail, kShort>{});
   };
   // Tiles of 64, 128 or 256 tokens take about 4 : 5 : 8 of time each (x 4,096: 20, 25 and 42 us), and every compute unit one at a
   // time: what comes out least, the larger ones where that is equal.  us with tiles of 64, 128 and 256: 70 rows x 50,257 x 1,024

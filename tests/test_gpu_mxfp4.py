@@ -141,7 +141,8 @@ def test_product_of_few_long_rows(ctx, rows, vocab, width):
 
 
 @pytest.mark.parametrize("rows,vocab,width", [
-    (65, 33_500, 40), (128, 40_001, 512), (200, 33_100, 70), (256, 33_281, 1024), (700, 30_000, 96), (1, 70_001, 33)])
+    (65, 33_500, 40), (128, 40_001, 512), (200, 33_100, 70), (256, 33_281, 1024), (700, 30_000, 96), (1, 70_001, 33),
+    (129, 66_000, 600), (300, 33_000, 1100), (40, 70_000, 800)])
 def test_product_of_more_tiles_than_compute_units(ctx, rows, vocab, width):
     hidden = ctx.mxfp4_quantize_rows(operand(rows, width, rows))
     weight = ctx.mxfp4_quantize_rows(operand(vocab, width, vocab + 1))
