@@ -133,6 +133,27 @@ struct Row {
       g(Vec<T>::load1(z + v), v);
     }
   }
+  // f(logit) of every element from `least` on, where that is most of them.
+  template <typename F>
+  __device__ __forceinline__ void visit_most(float least, F f) const {
+    constexpr int N = Vec<T>::N;
+    auto one = [&](u32x4 q, int) {
+      float x[N];
+      Vec<T>::unpack(q, x);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (x[j] >= least) f(x[j]);
+    };
+    visit<16 / N>(
+        [&](const u32x4* q, int) {
+#pragma unroll
+          for (int u = 0; u < 16 / N; ++u) one(q[u], 0);
+        },
+        one,
+        [&](float x, int) {
+          if (x >= least) f(x);
+        });
+  }
   // f(logit, index) of every element in [least, most].
   template <typename F>
   __device__ __forceinline__ void visit_between(float least, float most, F f) const {
@@ -443,17 +464,17 @@ __device__ Cut finish_cut(const Row<T>& row, Each each, Span s, bool by_mass, ui
   return cut_sorted(row, s, limit_count, limit_mass, sh.mass, sh);
 }
 
-// The cut among the tokens that each(f, least, most) gives to f(logit, key), those between two logits where these are named, by ranges of the exponent down to `depth` (in log2 of the mass) below the largest logit's;
-// what lies deeper is in the last one.
-template <typename T, typename Each>
-__device__ Cut cut_by_exponent(const Row<T>& row, Each each, float depth, bool by_mass, uint32_t limit_count, u64 limit_mass,
+// The cut among the tokens whose logits all(f) gives to f, and each(f, least, most), those between two logits, with their keys: by
+// ranges of the exponent down to `depth` (in log2 of the mass) below the largest logit's; what lies deeper is in the last one.
+template <typename T, typename All, typename Each>
+__device__ Cut cut_by_exponent(const Row<T>& row, All all, Each each, float depth, bool by_mass, uint32_t limit_count, u64 limit_mass,
                                SampleShared& sh) {
   const float per_range = (float)kBins / depth;
   auto range_of = [&](float x) { return (int)fminf(-row.exponent(x) * per_range, (float)(kBins - 1)); };
   Span s{0, kNoLimit, 0, 0, 0};
   Cut cut;
   if (!narrow(
-          row, [&](auto add) { each([&](float x, u64) { add((uint32_t)range_of(x), x); }, kLowest, kHighest); }, by_mass, limit_count,
+          row, [&](auto add) { all([&](float x) { add((uint32_t)range_of(x), x); }); }, by_mass, limit_count,
           limit_mass, &s, &cut, sh))
     return cut;
   // the keys of the range's logits, with room for the rounding of their exponents
@@ -997,7 +1018,10 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
         auto each = [&](auto f, float, float) {
           for (uint32_t i = tid; i < n; i += kThreads) f(row.value(sh.keys[i]), sh.keys[i]);
         };
-        cut = cut_by_exponent(row, each, depth, lim.by_mass, lim.count, limit_mass, sh);
+        auto all = [&](auto f) {
+          for (uint32_t i = tid; i < n; i += kThreads) f(row.value(sh.keys[i]));
+        };
+        cut = cut_by_exponent(row, all, each, depth, lim.by_mass, lim.count, limit_mass, sh);
       } else {
         bool done = false;
         if constexpr (sizeof(T) == 2) {
@@ -1011,7 +1035,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
           auto each = [&](auto f, float from, float to) {
             row.visit_between(fmaxf(from, least), to, [&](float x, int v) { f(x, row.key(x, v)); });
           };
-          cut = cut_by_exponent(row, each, depth, lim.by_mass, lim.count, limit_mass, sh);
+          auto all = [&](auto f) { row.visit_most(least, f); };
+          cut = cut_by_exponent(row, all, each, depth, lim.by_mass, lim.count, limit_mass, sh);
         }
       }
       limit_mass = lim.part_of((double)cut.mass);
