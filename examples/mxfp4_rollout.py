@@ -1,9 +1,9 @@
 """A 4-bit rollout policy, its AIS-corrected update, and its distillation, on one GPU.
 
-    python examples/mxfp4_rollout.py [--vocab 32000] [--width 1024] [--prompts 4] [--length 32] [--rounds 3]
+    python examples/mxfp4_rollout.py [--vocab 32000] [--width 1024] [--prompts 4] [--length 32] [--iterations 3]
 
 A toy policy: the hidden state of a position is a function of the state before and of the token drawn there, and the read-out
-is an output embedding W [V, D].  The trainer's W is bf16; the rollout engine has an MXFP4 copy.  A round is
+is an output embedding W [V, D].  The trainer's W is bf16; the rollout engine has an MXFP4 copy.  An iteration is
 
 1. rollout: quantise the hidden states, 4-bit logits, draw a token of every live response and keep the log-probability it was
    drawn with (Alg. 1, "sample a group of responses");
@@ -93,8 +93,8 @@ def main(argv=None):
     parser.add_argument("--width", type=int, default=1_024, help="a multiple of 32")
     parser.add_argument("--prompts", type=int, default=4)
     parser.add_argument("--length", type=int, default=32)
-    parser.add_argument("--rounds", type=int, default=3)
-    parser.add_argument("--steps", type=int, default=8, help="of the distillation in each round")
+    parser.add_argument("--iterations", type=int, default=3)
+    parser.add_argument("--steps", type=int, default=8, help="of the distillation in each iteration")
     parser.add_argument("--top", type=int, default=64, help="tokens of the trainer that the rollout's copy is pulled towards")
     args = parser.parse_args(argv)
 
@@ -110,7 +110,7 @@ def main(argv=None):
     ctx = B.AisContext()
     rollouts = Rollouts(ctx, embedding, args.length, gen)
     out = []
-    for r in range(args.rounds):
+    for r in range(args.iterations):
         hidden, tokens, logp_roll, valid = rollouts.run(ctx.mxfp4_quantize_rows(student), start)
         # a reward that any policy can learn: for even tokens
         even = ((tokens % 2 == 0).float() * valid).view(n, -1).sum(dim=1) / valid.view(n, -1).sum(dim=1)
@@ -119,7 +119,7 @@ def main(argv=None):
         kl = distill(ctx, student, weight, hidden, valid, min(args.top, args.vocab), rate=0.5 * rows / args.width,
                      steps=args.steps)
         out.append(dict(diag, kl=kl, hidden=hidden, tokens=tokens, logp_roll=logp_roll, valid=valid))
-        print(f"round {r}: {rows} tokens, alpha {diag['alpha']:.4f}, loss {diag['loss']:+.4e}, "
+        print(f"iteration {r}: {rows} tokens, alpha {diag['alpha']:.4f}, loss {diag['loss']:+.4e}, "
               f"divergence {kl[0]:.4f} -> {kl[-1]:.4f}", flush=True)
     status = ctx.status()
     ctx.close()

@@ -11,10 +11,10 @@ from paper_2605_13907_amd import binding as B
 pytestmark = pytest.mark.gpu
 
 
-def test_rounds():
-    rounds = mxfp4_rollout.main(["--vocab", "5003", "--width", "224", "--prompts", "3", "--length", "9", "--rounds", "2"])
-    assert len(rounds) == 2
-    for r in rounds:
+def test_iterations():
+    out = mxfp4_rollout.main(["--vocab", "5003", "--width", "224", "--prompts", "3", "--length", "9", "--iterations", "2"])
+    assert len(out) == 2
+    for r in out:
         assert 0.0 <= r["alpha"] <= 1.0 and np.isfinite(r["loss"])
         assert r["n_valid"] == int(r["valid"].sum())
         assert len(r["kl"]) == 9 and r["kl"][-1] < 0.9 * r["kl"][0]
