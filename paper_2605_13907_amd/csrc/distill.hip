@@ -330,9 +330,9 @@ template <> __device__ __forceinline__ u32x4 masked_fill<float>() {
 
 // ALIGNED: both rows are 16-byte aligned; otherwise both lie the same way relative to 128-byte lines, and the elements before the
 // row's first line boundary are handled one by one together with those after the last vector.  Vector k of a lane (vector tid +
-// THREADS k of the row) lies in register q[k] for k < NV and in slot k - NV of the dynamic LDS beyond.  The row has at least KFULL
-// THREADS vectors.
-template <typename T, bool ALIGNED, int THREADS, int NV, int NL, int KFULL>
+// THREADS k of the row) lies in register q[k] for k < NV and in slot k - NV of the dynamic LDS for the NL after them; up to NR more,
+// of the widest rows, are read again.  (Held in registers too they made those spill.)  The row has at least KFULL THREADS vectors.
+template <typename T, bool ALIGNED, int THREADS, int NV, int NL, int NR, int KFULL>
 __global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs<T> a) {
   constexpr int N = Vec<T>::N;
   static_assert(ALIGNED || THREADS >= 128, "a thread for every element outside the vectors");
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs
     if (tid == 0) a.kl[row] = 0.f;
     const u32x4 zero = {0u, 0u, 0u, 0u};
 #pragma unroll
-    for (int k = 0; k < NV + NL; ++k)
+    for (int k = 0; k < NV + NL + NR; ++k)
       if (tid + k * THREADS < nvec) store_stream(dv + tid + k * THREADS, zero);
     if (tid < rest) Vec<T>::store1(dr + v_rest, 0.f);
   };
@@ -427,6 +427,12 @@ __global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+#pragma unroll 1
+  for (int i = tid + (NV + NL) * THREADS; NR > 0 && i < nvec; i += THREADS) {
+    float x[N];
+    Vec<T>::unpack(zv[i], x);
+    accumulate<N>(x, c, st);
+  }
   const float xt = tid < rest ? Vec<T>::load1(&xt_raw) : kMasked;
   accumulate<1>(&xt, c, st);
   st = wave_merge(st);
@@ -449,6 +455,14 @@ __global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs
     for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, shift)) * g_p;
     if (k < KFULL || i < nvec) store_stream(dv + i, Vec<T>::pack(x));
     __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll 1
+  for (int i = tid2 + (NV + NL) * THREADS; NR > 0 && i < nvec; i += THREADS) {
+    float x[N];
+    Vec<T>::unpack(zv[i], x);
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, shift)) * g_p;
+    store_stream(dv + i, Vec<T>::pack(x));
   }
   if (tid < rest) Vec<T>::store1(dr + v_rest, exp2_fast(__builtin_fmaf(xt, c, shift)) * g_p);
   // the listed tokens' elements among those that this thread has written: a thread's own stores to a place keep their order
@@ -483,9 +497,9 @@ constexpr int kLdsSlots = 9;           // 144 KiB of the 160
 constexpr int kWide = 1024;
 constexpr long long kMostRows = 1LL << 21;              // of a launch
 
-template <typename T, bool ALIGNED, int THREADS, int NV, int NL, int KFULL>
+template <typename T, bool ALIGNED, int THREADS, int NV, int NL, int NR, int KFULL>
 int launch_held_as(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size_t listed_bytes) {
-  auto kernel = distill_held_kernel<T, ALIGNED, THREADS, NV, NL, KFULL>;
+  auto kernel = distill_held_kernel<T, ALIGNED, THREADS, NV, NL, NR, KFULL>;
   const size_t bytes = (size_t)NL * THREADS * 16 + listed_bytes;
   if (NL > 0) {
     static std::once_flag once[kMaxDevices];           // the attribute belongs to the function on one device
@@ -504,28 +518,28 @@ int launch_held(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size_t 
   // that one is read or written while another is summed: with 1,024 threads and with 512, us, 3,001 rows x 50,257 bf16 166 and
   // 121, 8,000 x 32,000 301 and 184, 3,000 x 64,000 184 and 142; with 256 and 512, 20,000 x 8,000 fp32 249 and 235.  PREV: the widest row of the class before; a row that
   // reaches this one has more than PREV * 1024 vectors, of which an unaligned row may have lost up to 8 to its head.
-#define AIS_HELD(THREADS, PREV, NVAL, NLVAL) \
-  return launch_held_as<T, ALIGNED, THREADS, NVAL, NLVAL, (ALIGNED || PREV == 0 ? PREV : PREV - 1)>(ctx, a, n_rows, listed_bytes)
+#define AIS_HELD(THREADS, PREV, NVAL, NLVAL, NRVAL) \
+  return launch_held_as<T, ALIGNED, THREADS, NVAL, NLVAL, NRVAL, (ALIGNED || PREV == 0 ? PREV : PREV - 1)>(ctx, a, n_rows, listed_bytes)
   if constexpr (ALIGNED) {
-    if (nvec <= 256) AIS_HELD(64, 0, 4, 0);
+    if (nvec <= 256) AIS_HELD(64, 0, 4, 0, 0);
   }
-  if (nvec <= 512) AIS_HELD(128, 0, 4, 0);
-  if (nvec <= 1024) AIS_HELD(256, 0, 4, 0);
-  if (nvec <= 2048) AIS_HELD(512, 0, 4, 0);
-  if (nvec <= 4096) AIS_HELD(512, 0, 8, 0);
-  if (nvec <= 6144) AIS_HELD(512, 0, 12, 0);
-  if (nvec <= 7168) AIS_HELD(512, 0, 14, 0);
-  if (nvec <= 8192) AIS_HELD(512, 0, 16, 0);
-  if (need <= 12) AIS_HELD(kWide, 8, 12, 0);
-  if (need <= 16) AIS_HELD(kWide, 12, 16, 0);
-  if (need <= 18) AIS_HELD(kWide, 16, 18, 0);
-  if (need <= 19) AIS_HELD(kWide, 18, 19, 0);
-  if (need <= 20) AIS_HELD(kWide, 19, 20, 0);
-  if (need <= 23) AIS_HELD(kWide, 20, 18, 5);
-  if (need <= 27) AIS_HELD(kWide, 23, 18, kLdsSlots);
-  if (need <= 29) AIS_HELD(kWide, 27, 20, kLdsSlots);
-  if (need <= 31) AIS_HELD(kWide, 29, 22, kLdsSlots);
-  AIS_HELD(kWide, 31, 24, kLdsSlots);
+  if (nvec <= 512) AIS_HELD(128, 0, 4, 0, 0);
+  if (nvec <= 1024) AIS_HELD(256, 0, 4, 0, 0);
+  if (nvec <= 2048) AIS_HELD(512, 0, 4, 0, 0);
+  if (nvec <= 4096) AIS_HELD(512, 0, 8, 0, 0);
+  if (nvec <= 6144) AIS_HELD(512, 0, 12, 0, 0);
+  if (nvec <= 7168) AIS_HELD(512, 0, 14, 0, 0);
+  if (nvec <= 8192) AIS_HELD(512, 0, 16, 0, 0);
+  if (need <= 12) AIS_HELD(kWide, 8, 12, 0, 0);
+  if (need <= 16) AIS_HELD(kWide, 12, 16, 0, 0);
+  if (need <= 18) AIS_HELD(kWide, 16, 18, 0, 0);
+  if (need <= 19) AIS_HELD(kWide, 18, 19, 0, 0);
+  if (need <= 20) AIS_HELD(kWide, 19, 20, 0, 0);
+  if (need <= 23) AIS_HELD(kWide, 20, 18, 5, 0);
+  if (need <= 27) AIS_HELD(kWide, 23, 18, kLdsSlots, 0);
+  if (need <= 29) AIS_HELD(kWide, 27, 20, kLdsSlots, 0);
+  if (need <= 31) AIS_HELD(kWide, 29, 22, kLdsSlots, 0);
+  AIS_HELD(kWide, 31, 21, kLdsSlots, 3);
 #undef AIS_HELD
 }
 
