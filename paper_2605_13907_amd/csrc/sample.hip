@@ -18,10 +18,11 @@
 // The tokens that share the cut's value are found by the draw, which passes over such a row sixteen tokens at a time.
 // Masses are summed as fixed-point numbers, so no result depends on the order in which threads arrive.
 //
-// Measured, us a call, logits in the cache of a step that made them: bf16 rows of 151,936 without limits 19 (1 row), 22 (64) and
-// 51 (256: 233 MB, 4.6 TB/s); of 64 such rows with limits 45 (top-k), 21 (min-p), 79 (top-p over flat rows, all of whose tokens
-// pass the bound).  Few rows are bound by one compute unit's reading of its row and the barriers between the passes, many without
-// limits by memory.
+// Measured, us a call, logits in the cache of a step that made them: bf16 rows of 151,936 without limits 19 (1 row), 21 (64) and
+// 46 (256: 233 MB, 5.1 TB/s); of 64 such rows with limits 36 (top-k), 19 (min-p), 68 (top-p over flat rows, all of whose tokens
+// pass the bound).  Few rows are bound by one compute unit's exponentials and reading of its row and the barriers between the passes,
+// many without limits by memory.  A kernel of 1,024 threads has 128 registers to each: what the compiler would compute early and keep
+// (indices, addresses, widened numbers) went to scratch memory, and with it 64 rows under top-k took 46 us and 256 without limits 52.
 #include "ais_internal.h"
 #include "device_utils.h"
 
@@ -52,6 +53,23 @@ __device__ __forceinline__ float from_ordered(uint32_t o) {
   return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu));
 }
 
+// The thread's index, anew: what is derived from it is not computed once and kept, in scratch memory for want of registers, over a loop
+// or a whole kernel.
+__device__ __forceinline__ int fresh_thread() {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+// A number that all lanes have as a wider one, here and not earlier.
+__device__ __forceinline__ double widened(float x) {
+  asm volatile("" : "+s"(x));
+  return (double)x;
+}
+// What another lane of the wavefront has, the lane's index modulo 64.
+__device__ __forceinline__ uint32_t from_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_ds_bpermute(lane << 2, (int)x); }
+__device__ __forceinline__ u64 from_lane(u64 x, int lane) {
+  return (u64)from_lane((uint32_t)(x >> 32), lane) << 32 | from_lane((uint32_t)x, lane);
+}
 // A number that all lanes have, as one of the wavefront.
 __device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
@@ -119,7 +137,8 @@ struct Row {
   __device__ __forceinline__ void visit(F f, F1 f1, G g) const {
     constexpr int N = Vec<T>::N;
     const u32x4* zv = reinterpret_cast<const u32x4*>(z + head);
-    int i = threadIdx.x;
+    int i = fresh_thread();
+    const int r = i;
     for (; i + (kUnroll - 1) * kThreads < nvec; i += kUnroll * kThreads) {
       u32x4 q[kUnroll];
 #pragma unroll
@@ -127,7 +146,6 @@ struct Row {
       f(q, head + i * N);
     }
     for (; i < nvec; i += kThreads) f1(zv[i], head + i * N);
-    const int r = threadIdx.x;
     if (r < rest) {
       const int v = r < head ? r : nvec * N + r;
       g(Vec<T>::load1(z + v), v);
@@ -217,8 +235,10 @@ __device__ __forceinline__ void add_to(const float* x, float most, float scale, 
 }
 
 __device__ __forceinline__ Best wave_best(Best b) {
+  const int tid = fresh_thread();
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) b = better(b, Best{__shfl_xor(b.score, d), __shfl_xor(b.token, d)});
+  for (int d = 1; d < 64; d <<= 1)
+    b = better(b, Best{__uint_as_float(from_lane(__float_as_uint(b.score), tid ^ d)), (int)from_lane((uint32_t)b.token, tid ^ d)});
   return b;
 }
 __device__ __forceinline__ Best block_best(Best b, SampleShared& sh) {
@@ -236,13 +256,14 @@ struct Before {
   u64 mass, all_mass;
 };
 __device__ __forceinline__ Before scan(uint32_t count, u64 mass, SampleShared& sh) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int tid = fresh_thread();
+  const int lane = tid & 63, wave = tid >> 6;
   uint32_t c = count;
   u64 m = mass;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t pc = __shfl_up(c, d);
-    const u64 pm = __shfl_up(m, d);
+    const uint32_t pc = from_lane(c, lane - d);
+    const u64 pm = from_lane(m, lane - d);
     if (lane >= d) {
       c += pc;
       m += pm;
@@ -268,12 +289,12 @@ __device__ __forceinline__ Before scan(uint32_t count, u64 mass, SampleShared& s
 
 // A wavefront's keys in ascending order, by exchanges between its lanes.
 __device__ __forceinline__ u64 wave_sorted(u64 key) {
-  const uint32_t i = threadIdx.x & 63;
+  const uint32_t i = fresh_thread() & 63;
 #pragma unroll
   for (uint32_t run = 2; run <= 64; run <<= 1)
 #pragma unroll
     for (uint32_t d = run >> 1; d > 0; d >>= 1) {
-      const u64 other = __shfl_xor(key, (int)d);
+      const u64 other = from_lane(key, (int)(i ^ d));
       const bool keep_less = ((i & d) == 0) == ((i & run) == 0);
       key = (other < key) == keep_less ? other : key;
     }
@@ -282,21 +303,22 @@ __device__ __forceinline__ u64 wave_sorted(u64 key) {
 
 // Sorts keys[0 .. n), n <= kMembers, in ascending order; what lies beyond, up to the next power of two, is overwritten.
 __device__ __forceinline__ void sort_keys(uint32_t n, u64* keys) {
+  const int tid = fresh_thread();
   if (n <= 64) {
-    if (threadIdx.x < 64) {
-      const u64 key = wave_sorted(threadIdx.x < n ? keys[threadIdx.x] : kNoLimit);
-      if (threadIdx.x < n) keys[threadIdx.x] = key;
+    if (tid < 64) {
+      const u64 key = wave_sorted(tid < n ? keys[tid] : kNoLimit);
+      if (tid < n) keys[tid] = key;
     }
     __syncthreads();
     return;
   }
   uint32_t size = 128;
   while (size < n) size <<= 1;
-  for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) keys[i] = kNoLimit;
+  for (uint32_t i = n + tid; i < size; i += kThreads) keys[i] = kNoLimit;
   __syncthreads();
   for (uint32_t run = 2; run <= size; run <<= 1) {
     for (uint32_t d = run >> 1; d > 0; d >>= 1) {
-      for (uint32_t p = threadIdx.x; p < size / 2; p += kThreads) {
+      for (uint32_t p = tid; p < size / 2; p += kThreads) {
         const uint32_t i = 2 * p - (p & (d - 1)), j = i + d;
         const u64 a = keys[i], b = keys[j];
         if ((a > b) == ((i & run) == 0)) {
@@ -328,23 +350,24 @@ struct Span {
 
 // The cut among n sorted keys: the first that is the limit_count-th or has limit_mass before it.  All threads get it.
 template <typename T>
-__device__ Cut cut_sorted(const Row<T>& row, const Span& s, uint32_t limit_count, u64 limit_mass, const u64* keys,
+__device__ __forceinline__ Cut cut_sorted(const Row<T>& row, const Span& s, uint32_t limit_count, u64 limit_mass, const u64* keys,
                           SampleShared& sh) {
+  const int tid = fresh_thread();
   const uint32_t n = s.n;
   if (n <= 64) {                                       // one wavefront looks at them and tells the others
     __syncthreads();
-    if (threadIdx.x < 64) {
-      const uint32_t i = threadIdx.x;
+    if (tid < 64) {
+      const uint32_t i = tid;
       const u64 m = i < n ? row.mass(row.value(keys[i])) : 0;
       u64 upto = m;
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
-        const u64 p = __shfl_up(upto, d);
+        const u64 p = from_lane(upto, (int)i - d);
         if ((int)i >= d) upto += p;
       }
       const bool kept = i < n && s.above_count + i < limit_count && s.above_mass + upto - m < limit_mass;
       const uint32_t all = (uint32_t)__builtin_popcountll(__ballot(kept));
-      const u64 mass = __shfl(upto, (int)max(all, 1u) - 1);
+      const u64 mass = from_lane(upto, (int)max(all, 1u) - 1);
       if (i == 0) {
         sh.wave_count[0] = all;
         sh.wave_mass[0] = all > 0 ? mass : 0;
@@ -354,7 +377,7 @@ __device__ Cut cut_sorted(const Row<T>& row, const Span& s, uint32_t limit_count
     const uint32_t all = sh.wave_count[0];
     return Cut{all < n ? keys[all] : keys[n - 1] + 1, s.above_count + all, s.above_mass + sh.wave_mass[0]};
   }
-  const uint32_t i = 2 * threadIdx.x;
+  const uint32_t i = 2 * tid;
   const u64 k0 = i < n ? keys[i] : 0, k1 = i + 1 < n ? keys[i + 1] : 0;
   const u64 m0 = i < n ? row.mass(row.value(k0)) : 0, m1 = i + 1 < n ? row.mass(row.value(k1)) : 0;
   const Before b = scan((i < n) + (i + 1 < n), m0 + m1, sh);
@@ -370,7 +393,8 @@ __device__ Cut cut_sorted(const Row<T>& row, const Span& s, uint32_t limit_count
 // Where the cut lies among ranges of which each thread has kOwn: in the first one after which a limit is reached.  held(k, f) calls
 // f(tokens, mass) with what the thread's k-th holds.  Sets sh.bin and what belongs to it; the sums over all ranges are returned.
 template <int kOwn, typename Held>
-__device__ Before find_range(Held held, const Span& s, uint32_t limit_count, u64 limit_mass, SampleShared& sh) {
+__device__ __forceinline__ Before find_range(Held held, const Span& s, uint32_t limit_count, u64 limit_mass, SampleShared& sh) {
+  const int tid = fresh_thread();
   uint32_t c = 0;
   u64 m = 0;
 #pragma unroll 2
@@ -389,7 +413,7 @@ __device__ Before find_range(Held held, const Span& s, uint32_t limit_count, u64
         const bool inside = above_count < limit_count && above_mass < limit_mass;
         const bool after = above_count + count >= limit_count || above_mass + mass >= limit_mass;
         if (count > 0 && inside && after) {
-          sh.bin = kOwn * (int)threadIdx.x + k;
+          sh.bin = kOwn * tid + k;
           sh.bin_count = count;
           sh.above_count = above_count;
           sh.above_mass = above_mass;
@@ -405,14 +429,15 @@ __device__ Before find_range(Held held, const Span& s, uint32_t limit_count, u64
 // Counts what `each` gives to add(range, logit) in kBins ranges and finds the one with the cut; false if there is none, with the
 // cut behind everything.
 template <typename T, typename Each>
-__device__ bool narrow(const Row<T>& row, Each each, bool by_mass, uint32_t limit_count, u64 limit_mass, Span* s, Cut* cut,
+__device__ __forceinline__ bool narrow(const Row<T>& row, Each each, bool by_mass, uint32_t limit_count, u64 limit_mass, Span* s, Cut* cut,
                        SampleShared& sh) {
+  const int tid = fresh_thread();
   __syncthreads();
-  for (int b = threadIdx.x; b < kBins; b += kThreads) {
+  for (int b = tid; b < kBins; b += kThreads) {
     sh.count[b] = 0;
     sh.mass[b] = 0;
   }
-  if (threadIdx.x == 0) sh.bin = -1;
+  if (tid == 0) sh.bin = -1;
   __syncthreads();
   each([&](uint32_t bin, float x) {
     atomicAdd(&sh.count[bin], 1u);
@@ -421,7 +446,7 @@ __device__ bool narrow(const Row<T>& row, Each each, bool by_mass, uint32_t limi
   __syncthreads();
   constexpr int kOwn = kBins / kThreads;
   const Before all = find_range<kOwn>(
-      [&](int k, auto f) { f(sh.count[kOwn * threadIdx.x + k], sh.mass[kOwn * threadIdx.x + k]); }, *s, limit_count, limit_mass, sh);
+      [&](int k, auto f) { f(sh.count[kOwn * tid + k], sh.mass[kOwn * tid + k]); }, *s, limit_count, limit_mass, sh);
   if (sh.bin < 0) {
     *cut = Cut{s->hi, s->above_count + all.all_count, s->above_mass + all.all_mass};
     return false;
@@ -434,8 +459,9 @@ __device__ bool narrow(const Row<T>& row, Each each, bool by_mass, uint32_t limi
 
 // The cut inside a span whose tokens are those of `each`: further ranges while there are more than can be sorted.
 template <typename T, typename Each>
-__device__ Cut finish_cut(const Row<T>& row, Each each, Span s, bool by_mass, uint32_t limit_count, u64 limit_mass,
+__device__ __forceinline__ Cut finish_cut(const Row<T>& row, Each each, Span s, bool by_mass, uint32_t limit_count, u64 limit_mass,
                           SampleShared& sh) {
+  const int tid = fresh_thread();
   while (s.n > (uint32_t)kMembers) {
     int shift = 0;
     while (((s.hi - s.lo - 1) >> shift) >= (u64)kBins) ++shift;
@@ -454,7 +480,7 @@ __device__ Cut finish_cut(const Row<T>& row, Each each, Span s, bool by_mass, ui
     s.lo = start;
   }
   __syncthreads();                                     // the ranges have been read: their place is for the tokens now
-  if (threadIdx.x == 0) sh.n = 0;
+  if (tid == 0) sh.n = 0;
   __syncthreads();
   each([&](float x, u64 key) {
     if (key >= s.lo && key < s.hi) sh.mass[atomicAdd(&sh.n, 1u)] = key;
@@ -467,7 +493,7 @@ __device__ Cut finish_cut(const Row<T>& row, Each each, Span s, bool by_mass, ui
 // The cut among the tokens whose logits all(f) gives to f, and each(f, least, most), those between two logits, with their keys: by
 // ranges of the exponent down to `depth` (in log2 of the mass) below the largest logit's; what lies deeper is in the last one.
 template <typename T, typename All, typename Each>
-__device__ Cut cut_by_exponent(const Row<T>& row, All all, Each each, float depth, bool by_mass, uint32_t limit_count, u64 limit_mass,
+__device__ __forceinline__ Cut cut_by_exponent(const Row<T>& row, All all, Each each, float depth, bool by_mass, uint32_t limit_count, u64 limit_mass,
                                SampleShared& sh) {
   const float per_range = (float)kBins / depth;
   auto range_of = [&](float x) { return (int)fminf(-row.exponent(x) * per_range, (float)(kBins - 1)); };
@@ -502,12 +528,13 @@ __device__ __forceinline__ int value_place(float x) {
 }
 
 // The cut among the tokens of a bf16 row that are no smaller than `least`: the tokens of every value are counted.
-__device__ Cut cut_by_value(const Row<bf16_t>& row, float least, uint32_t limit_count, u64 limit_mass, SampleShared& sh) {
+__device__ __forceinline__ Cut cut_by_value(const Row<bf16_t>& row, float least, uint32_t limit_count, u64 limit_mass, SampleShared& sh) {
   constexpr int kOwn = kValues / kThreads;
+  const int tid = fresh_thread();
   __syncthreads();
   u32x4* counts = reinterpret_cast<u32x4*>(sh.value_count);
-  for (int b = threadIdx.x; b < kValues / 4; b += kThreads) counts[b] = u32x4{0, 0, 0, 0};
-  if (threadIdx.x == 0) sh.bin = -1;
+  for (int b = tid; b < kValues / 4; b += kThreads) counts[b] = u32x4{0, 0, 0, 0};
+  if (tid == 0) sh.bin = -1;
   __syncthreads();
   auto add = [&](float x) {
     if (x >= least) atomicAdd(&sh.value_count[value_place(x)], 1u);
@@ -534,13 +561,13 @@ __device__ Cut cut_by_value(const Row<bf16_t>& row, float least, uint32_t limit_
   Span s{0, kNoLimit, 0, 0, 0};
   u32x4 own[kOwn / 4];
 #pragma unroll
-  for (int k = 0; k < kOwn / 4; ++k) own[k] = counts[kOwn / 4 * (int)threadIdx.x + k];
+  for (int k = 0; k < kOwn / 4; ++k) own[k] = counts[kOwn / 4 * tid + k];
   const Before all = find_range<kOwn>(
       [&](int k, auto f) {
         uint32_t c = 0;
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) c = j == k ? own[j / 4][j % 4] : c;
-        if (c > 0) f(c, c * row.mass(value_of(kOwn * (int)threadIdx.x + k)));
+        if (c > 0) f(c, c * row.mass(value_of(kOwn * tid + k)));
       },
       s, limit_count, limit_mass, sh);
   if (sh.bin < 0) return Cut{kNoLimit, all.all_count, all.all_mass};
@@ -562,7 +589,7 @@ __device__ Cut cut_by_value(const Row<bf16_t>& row, float least, uint32_t limit_
     const u64 each = row.mass(x);
     u64 take = min(s.n, limit_count - s.above_count);
     if (each > 0 && limit_mass != kNoLimit) take = min(take, (limit_mass - s.above_mass + each - 1) / each);
-    if (threadIdx.x == 0) sh.n = 0;
+    if (tid == 0) sh.n = 0;
     __syncthreads();
     return Cut{row.key(x, 0), s.above_count + (uint32_t)take, s.above_mass + take * each, (uint32_t)take, x};
   }
@@ -582,13 +609,14 @@ struct Limits {
   uint32_t count;
   float top_p, share;                  // share: log2 of min-p
   u64 mass;                            // that top-p without top-k ends at
-  __device__ __forceinline__ u64 part_of(double m) const { return (u64)fmax((double)top_p * m, 1.0); }
+  __device__ __forceinline__ u64 part_of(double m) const { return (u64)fmax(widened(top_p) * m, 1.0); }
 };
 
 // Sum of the wavefronts' votes, in every lane: exchanges inside rows of 16 lanes, one for each wavefront.
 __device__ __forceinline__ float votes_of(const float* votes) {
+  const int tid = fresh_thread();
   static_assert(kWaves == 16, "");
-  float v = votes[threadIdx.x & 15];
+  float v = votes[tid & 15];
   v += dpp_move<kDppQuadXor1>(v);
   v += dpp_move<kDppQuadXor2>(v);
   v += dpp_move<kDppRowHalfMirror>(v);
@@ -597,8 +625,9 @@ __device__ __forceinline__ float votes_of(const float* votes) {
 
 // A bound on the kept logits from the largest of the parts of every thread's logits; false if they allow none.
 template <typename T>
-__device__ bool bound(const Row<T>& row, const Limits& lim, float total, const float* own_top, float* least, SampleShared& sh) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ bool bound(const Row<T>& row, const Limits& lim, float total, const float* own_top, float* least, SampleShared& sh) {
+  const int tid = fresh_thread();
+  const int lane = tid & 63, wave = tid >> 6;
   int turn = 0;
   // one barrier for each question: the answers of the one before are read while those of the next are written
   auto count = [&](float from) {
@@ -689,8 +718,9 @@ struct Drawn {
 
 // Up to 64 candidates, by one wavefront: sorted by exchanges between its lanes, lane i then has the i-th.
 template <typename T, typename S>
-__device__ Drawn draw_from_few(const Row<T>& row, const Limits& lim, uint32_t n, const u64* keys, S scored) {
-  const uint32_t i = threadIdx.x & 63;
+__device__ __forceinline__ Drawn draw_from_few(const Row<T>& row, const Limits& lim, uint32_t n, const u64* keys, S scored) {
+  const int tid = fresh_thread();
+  const uint32_t i = tid & 63;
   const u64 key = wave_sorted(i < n ? keys[i] : kNoLimit);
   const float x = i < n ? row.value(key) : row.top;
   const u64 m = i < n ? row.mass(x) : 0;
@@ -698,16 +728,16 @@ __device__ Drawn draw_from_few(const Row<T>& row, const Limits& lim, uint32_t n,
     u64 s = own;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const u64 p = __shfl_up(s, d);
+      const u64 p = from_lane(s, (int)i - d);
       if ((int)i >= d) s += p;
     }
     return s;
   };
   const u64 upto = sum_to(m);
   u64 limit = lim.mass;
-  if (lim.by_count && lim.by_mass) limit = lim.part_of((double)__shfl(upto, (int)min(n, lim.count) - 1));
+  if (lim.by_count && lim.by_mass) limit = lim.part_of((double)from_lane(upto, (int)min(n, lim.count) - 1));
   const bool kept = i < n && i < lim.count && upto - m < limit && row.exponent(x) >= lim.share;
-  Drawn d{{-__builtin_inff(), row.vocab}, __shfl(sum_to(kept ? m : 0), 63)};
+  Drawn d{{-__builtin_inff(), row.vocab}, from_lane(sum_to(kept ? m : 0), 63)};
   if (kept) d.best = scored(x, row.token(key));
   d.best = wave_best(d.best);
   return d;
@@ -737,7 +767,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   const float min_p = limits.min_p != nullptr ? limits.min_p[r] : 0.f;
   int k = limits.top_k != nullptr ? limits.top_k[r] : 0;
   Limits lim;
-  lim.top_p = limits.top_p != nullptr ? limits.top_p[r] : 1.f;
+  lim.top_p = uniform(limits.top_p != nullptr ? limits.top_p[r] : 1.f);
   auto refuse = [&] {
     if (tid == 0) atomicOr(status, AIS_STATUS_BAD_ROW);
     answer(-1, 0.f, 0.f);
@@ -910,7 +940,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
       return;
     }
     const double at = (double)row.exponent(Vec<T>::load1(row.z + token)) * 0.6931471805599453;
-    const double full = at - log((double)total);
+    const double full = at - log(widened(total));
     answer(token, (float)(kept_mass > 0 ? at - log(ldexp((double)kept_mass, -row.mass_bits)) : full), (float)full);
   };
   // Scores the best vectors, or all vectors, of the threads that ask for it once more, the wavefront for each of them together.
@@ -927,7 +957,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     best = Best{-__builtin_inff(), vocab};
     row.visit_from(top, [&](float, int v) { best = better(best, Best{0.f, v}); });
     best = block_best(best, sh);
-    answer(best.token, 0.f, greedy ? 0.f : (float)-log((double)total));
+    answer(best.token, 0.f, greedy ? 0.f : (float)-log(widened(total)));
     return;
   }
   if (open) {
@@ -941,7 +971,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     finish(block_best(best, sh).token, 0);
     return;
   }
-  if (lim.by_mass && !lim.by_count) lim.mass = lim.part_of(ldexp((double)total, row.mass_bits));
+  best = Best{-__builtin_inff(), vocab};
+  if (lim.by_mass && !lim.by_count) lim.mass = lim.part_of(ldexp(widened(total), row.mass_bits));
   // (x - top) c >= the least exponent, with room for its rounding: the condition itself is looked at again
   auto from_exponent = [&](float low) { return top + low / row.c - 1e-5f * (fabsf(top) + fabsf(low / row.c)); };
   float least = lim.by_share && !lim.by_count ? fmaxf(from_exponent(lim.share), kLowest) : kLowest;
@@ -1014,6 +1045,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     // with both limits the first cut, by count, tells the mass that top-p is a share of
     u64 limit_mass = lim.mass;
     for (int pass = lim.by_count && lim.by_mass ? 0 : 1; pass < 2; ++pass) {
+      // nothing that follows from these is computed before the loop and kept
+      asm volatile("" : "+s"(row.top), "+s"(row.c), "+s"(row.mass_bits), "+s"(row.index_bits));
       if (listed) {
         auto each = [&](auto f, float, float) {
           for (uint32_t i = tid; i < n; i += kThreads) f(row.value(sh.keys[i]), sh.keys[i]);
@@ -1067,6 +1100,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   const u32x4* zv = reinterpret_cast<const u32x4*>(logits + r * row_stride + head);
   const float* ev = noise + r * noise_stride + head;
   const float share = uniform(lim.share), scale = uniform(row.c), origin = uniform(row.top);
+  best_score = -__builtin_inff();
+  best_at = -1;
+  best_many = 0;
   auto full_score = [&](float x, float noise_of) { return (x - origin) * scale - log2_fast(clamped_noise(noise_of)); };
   auto score_of = [&](float x, float noise_of, int v) {
     float score = full_score(x, noise_of);
@@ -1094,11 +1130,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     for (int j = 1; j < kMany * N; ++j) m = fmaxf(m, w[j]);
     auto each = [&](uint32_t found, auto f) {          // f(logit, index): few of them, mostly
       for (; found != 0; found &= found - 1) {
-        const int j = __builtin_ctz(found);
-        u32x4 own = q[0];
-#pragma unroll
-        for (int u = 1; u < kMany; ++u) own = j / N == u ? q[u] : own;
-        f(element<T>(own, j % N), head + (i + j / N * kThreads) * N + j % N);
+        const int j = __builtin_ctz(found), v = head + (i + j / N * kThreads) * N + j % N;
+        f(Vec<T>::load1(row.z + v), v);
       }
     };
     if (sum_mass && m > -__builtin_inff()) {
@@ -1119,7 +1152,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
       best_many = kMany;
     }
   };
-  int i = tid;
+  int i = fresh_thread();
   for (; i + (kOpen - 1) * kThreads < nvec; i += kOpen * kThreads) race(std::integral_constant<int, kOpen>{}, i);
   for (; i < nvec; i += kThreads) race(std::integral_constant<int, 1>{}, i);
   best = Best{-__builtin_inff(), vocab};
