@@ -36,6 +36,14 @@ __device__ __forceinline__ double log1p_scaled(float s, double e) {
 __device__ __forceinline__ u32x4 load_stream(const u32x4* p) { return __builtin_nontemporal_load(p); }
 __device__ __forceinline__ void store_stream(u32x4* p, u32x4 v) { __builtin_nontemporal_store(v, p); }
 
+// The thread's index, anew: what is derived from it is not computed once and kept, in scratch memory for want of registers, over a loop
+// or a whole kernel.
+__device__ __forceinline__ int fresh_thread() {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  return tid;
+}
+
 template <typename T> struct Vec;
 template <> struct Vec<bf16_t> {
   static constexpr int N = 8;

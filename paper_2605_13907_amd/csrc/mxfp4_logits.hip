@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kStreamThreads) __attribute__((amdgpu_waves_per_eu(
 // memory into one of two LDS buffers; the copies of the next step are on their way while a step is multiplied.  Scales come
 // for two steps at a time.  A workgroup walks through its tiles without a pause: the first step of the next tile is copied during
 // the last of this one.
-// 2,048 rows x 151,936 x 4,096 765 us, 3.3 PFLOP/s.  There copies and LDS reads without the products take 520 us, products and LDS
+// 2,048 rows x 151,936 x 4,096 740 us, 3.4 PFLOP/s.  There copies and LDS reads without the products take 520 us, products and LDS
 // reads without the copies 502 (the instructions by themselves 253), and the stores, which all workgroups make at about the same
 // time, 115.
 //
@@ -294,14 +294,13 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
   // Scales: 16 rows of four words to an instruction, the rows of both operands numbered in one go.  Offsets are from the tile's
   // first row, 32 bits.  Blocks beyond a row's end are its last one again: a code is always a finite number, and two scales of
   // 2^-127 leave nothing of it.
-  const int crow = 8 * wave + (lane >> 3);
-  const int w_chunk = (lane & 7) ^ swizzle_w(crow), h_chunk = (lane & 7) ^ swizzle_h(crow);
   constexpr int kScaleCopies = L::kScaleCopies;
   const unsigned char *w_base, *h_base, *ws_base, *hs_base;
   uint32_t w_off[4], h_off[NJ], s_off[kScaleCopies];
   auto point = [&](int item) {
     int v0, t0;
     place(item, v0, t0);
+    const int lane = fresh_thread() & 63, crow = 8 * wave + (lane >> 3);
     w_base = weight.codes + (long long)v0 * weight.codes_stride;
     h_base = hidden.codes + (long long)t0 * hidden.codes_stride;
     ws_base = weight.scales + (long long)v0 * weight.scales_stride;
@@ -323,6 +322,8 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
   point(item0);
   auto copy_codes = [&](int half, int to) {                     // of step 2 c_group + half, into buffer `to`
     const int block = c_group * kGroup + half * kStepBlocks;
+    const int lane = fresh_thread() & 63, crow = 8 * wave + (lane >> 3);
+    const int w_chunk = (lane & 7) ^ swizzle_w(crow), h_chunk = (lane & 7) ^ swizzle_h(crow);
     const uint32_t wb = 16u * (uint32_t)(RAGGED ? min(block + w_chunk, blocks - 1) : block + w_chunk);
     const uint32_t hb = 16u * (uint32_t)(RAGGED ? min(block + h_chunk, blocks - 1) : block + h_chunk);
 #pragma unroll
@@ -336,7 +337,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
                                        0);
   };
   auto copy_scales = [&](int buffer) {
-    const int word = c_group * kGroup + 4 * (lane & 3);
+    const int word = c_group * kGroup + 4 * (fresh_thread() & 3);
     const uint32_t sb = (uint32_t)(RAGGED ? min(word, (blocks - 1) & ~3) : word);
 #pragma unroll
     for (int q = 0; q < kScaleCopies; ++q) {
@@ -350,13 +351,11 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
   const int a = lane & 15;
   const int arow = wv * 128 + 8 * (a >> 2) + (a & 3);          // tile i: + tile_entry(i, 0)
   const int brow = wt * 16 * NJ + a;
-  const uint32_t pick = (quarter & 1) ? 0x07060302u : 0x05040100u;
   // swizzles do not depend on the MFMA tile: a fragment lies at a constant distance from the first one
   const int w_at[2] = {arow * kRowBytes + ((2 * quarter ^ swizzle_w(arow)) << 4),
                        arow * kRowBytes + (((2 * quarter + 1) ^ swizzle_w(arow)) << 4)};
   const int h_at[2] = {brow * kRowBytes + ((2 * quarter ^ swizzle_h(brow)) << 4),
                        brow * kRowBytes + (((2 * quarter + 1) ^ swizzle_h(brow)) << 4)};
-  const int ws_at = arow * kGroup + 4 * (quarter >> 1), hs_at = (kTileV + brow) * kGroup + 4 * (quarter >> 1);
 
   f32x4 acc[kNI][NJ];
   copy_scales(0);
@@ -395,6 +394,10 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
         }
         if (half == 0) {
           const unsigned char* sl = lds + L::kScales + scale_buffer * L::kScaleBytes;
+          const int lane = fresh_thread() & 63, quarter = lane >> 4, a = lane & 15;
+          const int ws_at = (wv * 128 + 8 * (a >> 2) + (a & 3)) * kGroup + 4 * (quarter >> 1);
+          const int hs_at = (kTileV + wt * 16 * NJ + a) * kGroup + 4 * (quarter >> 1);
+          const uint32_t pick = (quarter & 1) ? 0x07060302u : 0x05040100u;
           // scales beyond the row's end count as zero
           uint32_t keep = ~0u;
           if (RAGGED) {
@@ -459,6 +462,7 @@ __global__ __launch_bounds__(kTileThreads) __attribute__((amdgpu_waves_per_eu(2,
       for (int j = 0; j < NJ; ++j) asm volatile("" : "+a"(acc[i][j]));
     int v0, t0;
     place(item, v0, t0);
+    const int lane = fresh_thread() & 63, quarter = lane >> 4, brow = wt * 16 * NJ + (lane & 15);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const int t = t0 + brow + 16 * j;

@@ -53,13 +53,6 @@ __device__ __forceinline__ float from_ordered(uint32_t o) {
   return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu));
 }
 
-// The thread's index, anew: what is derived from it is not computed once and kept, in scratch memory for want of registers, over a loop
-// or a whole kernel.
-__device__ __forceinline__ int fresh_thread() {
-  int tid = threadIdx.x;
-  asm volatile("" : "+v"(tid));
-  return tid;
-}
 // A number that all lanes have as a wider one, here and not earlier.
 __device__ __forceinline__ double widened(float x) {
   asm volatile("" : "+s"(x));
