@@ -409,8 +409,9 @@ int ais_mxfp4_logits(ais_ctx* ctx, const unsigned char* hidden_codes, long long 
  *   logp_out    [n_rows] fp32   log-prob of the drawn token among the kept ones: that of the policy that drew it
  *   logp_full_out [n_rows] fp32 or NULL   its log softmax(t) over the whole vocabulary
  * A logit of -inf is a token that cannot be drawn and does not count.  A row without a distribution (a NaN or +inf among its
- * logits, nothing but -inf, a largest z / temperature beyond 2e38, a temperature that is negative or not finite, a NaN limit) gets token -1 and log-probs 0, and
- * AIS_STATUS_BAD_ROW is set in the status word.
+ * logits, nothing but -inf, a temperature that is negative or not finite, a NaN limit) gets token -1 and log-probs 0, and
+ * AIS_STATUS_BAD_ROW is set in the status word.  Of a row of nothing but one finite value, the type's lowest perhaps, every token is
+ * as likely.
  * Errors: as ais_token_logprob for the logits, NULL noise / token_out / logp_out (with n_rows > 0), noise_stride < vocab. */
 int ais_sample_tokens(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
                       long long row_stride, const float* noise, long long noise_stride, const unsigned char* valid,

@@ -786,7 +786,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   row.rest = vocab - row.nvec * N;
   row.index_bits = vocab > 1 ? 32 - __builtin_clz((unsigned)(vocab - 1)) : 1;
   row.mass_bits = min(40, 62 - row.index_bits);
-  row.c = uniform(greedy ? kLog2e : kLog2e / temperature);
+  row.c = uniform(greedy ? kLog2e : fminf(kLog2e / temperature, 3e38f));
   const float* e = noise + r * noise_stride;
   const bool open = k != 1 && !lim.by_count && !lim.by_mass && !lim.by_share;
 
@@ -918,13 +918,29 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   }
   top = uniform(top);
   row.top = top;
-  // a NaN or +inf makes the sum NaN; nothing but -inf leaves no largest
-  if (!(st.s > 0.f) || !(st.m < 3.4e38f) || !(top > -3.4e38f)) {
+  // the sum relative to the largest logit's exponential: st.m is the rounded product top * c
+  float total = st.s * exp2_fast(-__builtin_fmaf(top, row.c, -st.m));
+  // Far from zero products are rounded to whole numbers or do not fit.  If the largest logit's is, or if a thread that has nothing but the
+  // type's lowest value made the sum something else than a number, it is taken again.
+  const bool far = !(fabsf(top * row.c) < 1e9f);
+  if (far || !(total > 0.5f) || !(total < kHighest)) {
+    float own = 0.f;
+    if (fabsf(top) <= kHighest) {
+      for (int v = tid; v < vocab; v += kThreads) own += exp2_fast(row.exponent(Vec<T>::load1(row.z + v)));
+    }
+    own = wave_sum(own);
+    __syncthreads();
+    if ((tid & 63) == 0) sh.vote_mass[1][tid >> 6] = own;
+    __syncthreads();
+    total = 0.f;
+    for (int w = 0; w < kWaves; ++w) total += sh.vote_mass[1][w];
+  }
+  total = uniform(total);
+  // none of +inf, NaN and nothing but -inf has a sum of 1 or more
+  if (!(total > 0.5f) || !(total < kHighest)) {
     refuse();
     return;
   }
-  // the sum relative to the largest logit's exponential: st.m is the rounded product top * c
-  const float total = uniform(st.s * exp2_fast(-__builtin_fmaf(top, row.c, -st.m)));
   auto scored = [&](float x, int v) { return Best{row.exponent(x) - log2_fast(clamped_noise(e[v])), v}; };
   auto finish = [&](int token, u64 kept_mass) {
     if (tid != 0) return;
@@ -957,10 +973,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     float near = sh.vote_mass[0][0];
     for (int w = 1; w < kWaves; ++w) near = fmaxf(near, sh.vote_mass[0][w]);
     near -= 1e-6f * (fabsf(near) + fabsf(top * row.c) + 300.f);                // some times what the scores are rounded by
-    best = best.score >= near && best.token < vocab ? scored(Vec<T>::load1(row.z + best.token), best.token)
-                                                    : Best{-__builtin_inff(), vocab};
+    if (far) best.token = tid < row.rest ? (tid < row.head ? tid : row.nvec * N + tid) : vocab;
+    best = (far || best.score >= near) && best.token < vocab ? scored(Vec<T>::load1(row.z + best.token), best.token)
+                                                             : Best{-__builtin_inff(), vocab};
     // all of a thread's vectors: rare, except at very large logits over the temperature
-    look_again(best_score >= near, second_score >= near, [&](int v) { return scored(Vec<T>::load1(row.z + v), v); });
+    look_again(far || best_score >= near, far || second_score >= near, [&](int v) { return scored(Vec<T>::load1(row.z + v), v); });
     finish(block_best(best, sh).token, 0);
     return;
   }

@@ -178,6 +178,49 @@ def test_masks(ctx, dtype, limits):
     assert (got[[0, 4, 5, 6, 10]] == -1).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("limits", [dict(), dict(top_k=5), dict(top_p=0.9), dict(min_p=0.1), dict(temperature=0.0), dict(top_k=900),
+                                    dict(temperature=5.0, top_p=0.5), dict(top_p=0.7, min_p=0.2)])
+@pytest.mark.parametrize("vocab", [9, 777, 40_001])
+def test_logits_as_large_as_the_type_holds(ctx, dtype, vocab, limits):
+    z, e = logits(7, vocab, dtype, 61)
+    lowest, most = torch.finfo(dtype).min, torch.finfo(dtype).max
+    z[0] = lowest                              # nothing but masked tokens, all alike
+    z[1] = lowest
+    z[1, ::3] = -math.inf
+    z[2] = most
+    z[3, :] = lowest
+    z[3, 5] = most
+    z[4] = z[4] * 1e30                         # one token takes everything, its products with 1 / T fit
+    z[5] = 1e10
+    z[6] = lowest
+    z[6, vocab - 1] = math.nan
+    got = check(ctx, z, e, **limits)
+    assert got[3] == 5 and got[1] % 3 != 0 and got[6] == -1
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("limits", [dict(), dict(top_k=5), dict(top_p=0.9), dict(min_p=0.1), dict(top_k=900)])
+@pytest.mark.parametrize("temperature", [0.3, 1.6, 1.7, 5.0, 1000.0])
+def test_lowest_masks_at_any_temperature(ctx, dtype, limits, temperature):
+    z, e = logits(6, 30_000, dtype, 73)
+    lowest = torch.finfo(dtype).min
+    for r, left in enumerate((1, 2, 40, 1000, 20_000)):
+        z[r, left:] = lowest
+    z[5, 100:] = lowest
+    z[5, 20_000:] = -math.inf
+    check(ctx, z, e, temperature=temperature, **limits)
+
+
+def test_temperatures_as_small_as_there_are(ctx):
+    z, e = logits(4, 3000, torch.float32, 67)
+    temperature = torch.tensor([1e-9, 1e-30, 1e-38, 1e-44], device="cuda")
+    for limits in (dict(), dict(top_k=5), dict(top_p=0.9)):
+        token, logp, full = ctx.sample_tokens(z, e, temperature=temperature, **limits)
+        assert torch.equal(token.long(), z.argmax(dim=1)) and not logp.any() and not full.any()
+    assert ctx.status() == 0
+
+
 def test_limits_without_a_meaning(ctx):
     z, e = logits(8, 100, torch.float32, 19)
     nan, inf = math.nan, math.inf
