@@ -223,6 +223,34 @@ struct Teacher {
   }
 };
 
+// Products with c far from zero are rounded to whole numbers or do not fit.  Where the largest logit's is, or where a thread that has
+// nothing but the type's lowest value has made the sum something else than a number: the largest logit and the sum relative to it, from
+// memory.  False without a finite largest one.
+template <typename T, int THREADS>
+__device__ __forceinline__ bool recentre(const T* zr, int vocab, float c, RowShared<THREADS>& sh, float* top, float* sum) {
+  const int tid = fresh_thread();
+  float m = -__builtin_inff(), s = 0.f;
+#pragma unroll 1
+  for (int v = tid; v < vocab; v += THREADS) m = fmaxf(m, Vec<T>::load1(zr + v));
+  m = wave_max(m);
+  __syncthreads();
+  if ((tid & 63) == 0) sh.policy[tid >> 6].m = m;
+  __syncthreads();
+  for (int w = 0; w < THREADS / 64; ++w) m = fmaxf(m, sh.policy[w].m);
+  if (!(fabsf(m) <= 3.4028235e38f)) return false;
+#pragma unroll 1
+  for (int v = tid; v < vocab; v += THREADS) s += exp2_fast((Vec<T>::load1(zr + v) - m) * c);
+  s = wave_sum(s);
+  if ((tid & 63) == 0) sh.policy[tid >> 6].s = s;
+  __syncthreads();
+  s = 0.f;
+  for (int w = 0; w < THREADS / 64; ++w) s += sh.policy[w].s;
+  *top = m;
+  *sum = s;
+  return true;
+}
+constexpr float kFar = 1e9f;           // of a product with c
+
 // ---- rows that are read twice: any width and alignment, and the loss alone ----------------------------------------------------
 constexpr int kTwiceThreads = 256;
 
@@ -284,6 +312,16 @@ __global__ __launch_bounds__(kTwiceThreads) void distill_twice_kernel(const Dist
   teacher.keep();
   __syncthreads();
   st = merge_all<kTwiceThreads / 64>(sh.policy);
+  float origin = 0.f;                                  // that is taken from the logits
+  if (!(fabsf(st.m) < kFar) || !(st.s < 3e38f)) {
+    float top, sum;
+    if (recentre(zr, vocab, c, sh, &top, &sum)) {
+      origin = top;
+      st = MaxSum{0.f, sum};
+      for (int j = tid; j < a.n_top; j += kTwiceThreads) teacher.listed.z[j] -= top;
+      __syncthreads();
+    }
+  }
   teacher.diverge(st);
   __syncthreads();
   teacher.report();
@@ -294,7 +332,7 @@ __global__ __launch_bounds__(kTwiceThreads) void distill_twice_kernel(const Dist
     float x[N];
     Vec<T>::unpack(zv[i], x);
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j], c, -st.m)) * g_p;
+    for (int j = 0; j < N; ++j) x[j] = exp2_fast(__builtin_fmaf(x[j] - origin, c, -st.m)) * g_p;
     T* d = dr + head + (long long)i * N;
     if (aligned) {
       *reinterpret_cast<u32x4*>(d) = Vec<T>::pack(x);
@@ -305,7 +343,7 @@ __global__ __launch_bounds__(kTwiceThreads) void distill_twice_kernel(const Dist
   }
   for (int r = tid; r < rest; r += kTwiceThreads) {
     const int v = r < head ? r : nvec * N + r;
-    Vec<T>::store1(dr + v, exp2_fast(__builtin_fmaf(Vec<T>::load1(zr + v), c, -st.m)) * g_p);
+    Vec<T>::store1(dr + v, exp2_fast(__builtin_fmaf(Vec<T>::load1(zr + v) - origin, c, -st.m)) * g_p);
   }
   // the listed tokens' elements, once every wavefront's stores have completed
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -440,6 +478,26 @@ __global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs
   teacher.keep();
   __syncthreads();
   st = merge_all<THREADS / 64>(sh.policy);
+  if (!(fabsf(st.m) < kFar) || !(st.s < 3e38f)) {
+    float top, sum;
+    if (recentre(zr, vocab, c, sh, &top, &sum)) {
+      st = MaxSum{0.f, sum};
+      for (int j = tid; j < a.n_top; j += THREADS) teacher.listed.z[j] -= top;
+#pragma unroll 1
+      for (int v = tid; v < vocab; v += THREADS)
+        Vec<T>::store1(dr + v, exp2_fast((Vec<T>::load1(zr + v) - top) * c) * (g / sum));
+      // the listed tokens' elements after them, whoever wrote those
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      for (int j = tid; j < a.n_top; j += THREADS)
+        if (teacher.listed.slot[j] >= 0)
+          Vec<T>::store1(dr + teacher.listed.token[teacher.listed.slot[j]], g * teacher.element(j, st));
+      teacher.diverge(st);
+      __syncthreads();
+      teacher.report();
+      return;
+    }
+  }
   const float g_p = g / st.s, shift = -st.m;
   // opaque until the sum is known: neither are unpacked values kept alive nor is the unpacking below moved up
 #pragma unroll
@@ -538,7 +596,7 @@ int launch_held(ais_ctx* ctx, const DistillArgs<T>& a, long long n_rows, size_t 
   if (need <= 23) AIS_HELD(kWide, 20, 18, 5, 0);
   if (need <= 27) AIS_HELD(kWide, 23, 18, kLdsSlots, 0);
   if (need <= 29) AIS_HELD(kWide, 27, 20, kLdsSlots, 0);
-  if (need <= 31) AIS_HELD(kWide, 29, 22, kLdsSlots, 0);
+  if (need <= 31) AIS_HELD(kWide, 29, 21, kLdsSlots, 1);
   AIS_HELD(kWide, 31, 21, kLdsSlots, 3);
 #undef AIS_HELD
 }

@@ -186,6 +186,44 @@ def test_gradient_against_differences(ctx):
         assert (up - down) / 2e-2 == pytest.approx((grad * d).sum().item(), abs=64 * 1e-4 + 64 * 60 * 2e-6 / 1e-2 * 0.1)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [9, 1000, 50_257, 152_000, 270_000])
+def test_logits_as_large_as_the_type_holds(ctx, dtype, vocab):
+    """Rows whose products with 1 / T do not fit: of equal values, every token is as likely."""
+    z, ids, teacher, weight = case(5, vocab, 7, dtype, 71)
+    lowest, most = torch.finfo(dtype).min, torch.finfo(dtype).max
+    z[0] = lowest
+    z[1] = lowest
+    z[1, ::2] = -math.inf
+    z[1, ids[1].long()] = lowest
+    z[2] = most
+    z[3] = 1e10
+    for want_grad in (True, False):
+        check(ctx, z, ids, teacher, weight, want_grad=want_grad)
+    shifted = torch.zeros(5, vocab + 3, dtype=dtype, device="cuda")[:, 1:vocab + 1]
+    shifted.copy_(z)
+    check(ctx, shifted, ids, teacher, weight)
+    loss, kl, grad = ctx.distill_topk(z, ids, teacher, weight)
+    again = ctx.distill_topk(z, ids, teacher, weight, dlogits=z)
+    assert torch.equal(grad, again[2]) and torch.equal(kl, again[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("inv_t", [0.001, 0.2, 0.6, 1.0, 3.0])
+@pytest.mark.parametrize("vocab", [300, 20_000, 152_000])
+def test_lowest_masks_at_any_temperature(ctx, dtype, inv_t, vocab):
+    z, ids, teacher, weight = case(4, vocab, 6, dtype, 79)
+    lowest = torch.finfo(dtype).min
+    keep = z.gather(1, ids.long())
+    z[0] = lowest
+    z[1, 10:] = lowest
+    z[2, vocab // 2:] = lowest
+    z[3, 100:] = -math.inf
+    z.scatter_(1, ids.long(), keep)
+    check(ctx, z, ids, teacher, weight, inv_t=inv_t)
+    check(ctx, z, ids, teacher, weight, inv_t=inv_t, want_grad=False)
+
+
 def test_no_rows_streams_and_graphs(ctx):
     z, ids, teacher, weight = case(3, 50, 4, torch.float32, 1)
     loss, kl, grad = ctx.distill_topk(z[:0], ids[:0], teacher[:0])
