@@ -431,7 +431,8 @@ int ais_sample_tokens(ais_ctx* ctx, const void* logits, ais_dtype dtype, long lo
  *               tokens), any other id outside [0, vocab) is left out and sets AIS_STATUS_BAD_TOKEN; an id listed twice counts
  *               with both its entries
  *   weight      [n_rows] fp32, or NULL: 1 / n_rows each
- *   kl_out      [n_rows] fp32;  0 where valid == 0 or no entry has a finite logit
+ *   kl_out      [n_rows] fp32;  0 where valid == 0 or no entry has a finite logit; NaN, like the row's gradient, where the row has a
+ *               NaN, +inf or nothing but -inf among its logits
  *   loss_out    one fp32 (the sum is taken in fp64, in a fixed order)
  *   dlogits     [n_rows, dlogits_stride] of `dtype`, or NULL (loss alone); the first `vocab` elements of each row are written, 0
  *               where kl_out is 0 for one of these reasons.  May be `logits` itself with dlogits_stride == row_stride.

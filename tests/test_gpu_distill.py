@@ -134,6 +134,20 @@ def test_numbers_that_are_none(ctx):
     assert torch.isnan(grad[1][ids[1].long()]).all() and torch.isnan(grad[2][ids[2].long()]).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [600, 152_000])
+def test_rows_without_a_distribution(ctx, dtype, vocab):
+    z, ids, teacher, weight = case(4, vocab, 5, dtype, 10)
+    z[0] = -math.inf
+    z[1, 17] = math.inf
+    z[2, vocab - 1] = math.nan
+    _, kl, grad = ctx.distill_topk(z, ids, teacher, weight)
+    assert torch.isnan(kl[:3]).all() and torch.isnan(grad[:3]).all()
+    assert torch.isfinite(kl[3]) and torch.isfinite(grad[3]).all()
+    alone = ctx.distill_topk(z, ids, teacher, weight, want_grad=False)[1]
+    assert torch.isnan(alone[:3]).all() and torch.isfinite(alone[3])
+
+
 def test_policy_that_is_its_teacher(ctx):
     """The whole vocabulary listed with the policy's own logits: divergence and gradient vanish."""
     z, _, _, weight = case(8, 500, 1, torch.float32, 11)
