@@ -380,9 +380,9 @@ int ais_mxfp4_quantize_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long l
  *   out         [n_rows, out_stride] of `out_dtype`, the first `vocab` elements of each row are written (bf16: rounded to
  *               nearest even)
  * A block of scale 255 makes every logit that it enters NaN.  One row at a time is the same call as many.
- * Errors: NULL arrays (with n_rows > 0), n_rows < 0, vocab < 1, width < 1 or >= 2^31 - 64, strides of codes or scales of 16 MiB and
- * more (AIS_ERR_SIZE), a stride that does not hold the row's blocks (or out_stride < vocab), misaligned codes, scales or out or a stride that is not a multiple (16 bytes for
- * codes, 4 for scales), unknown dtype. */
+ * Errors: NULL arrays (with n_rows > 0), n_rows < 0, vocab < 1, either above 2^31 - 1025, width < 1 or >= 2^31 - 64, strides of
+ * codes or scales of 16 MiB and more (AIS_ERR_SIZE), a stride that does not hold the row's blocks (or out_stride < vocab),
+ * misaligned codes, scales or out or a stride that is not a multiple (16 bytes for codes, 4 for scales), unknown dtype. */
 int ais_mxfp4_logits(ais_ctx* ctx, const unsigned char* hidden_codes, long long hidden_codes_stride,
                      const unsigned char* hidden_scales, long long hidden_scales_stride, long long n_rows,
                      const unsigned char* weight_codes, long long weight_codes_stride,

@@ -688,7 +688,8 @@ int ais_mxfp4_logits(ais_ctx* ctx, const unsigned char* hidden_codes, long long 
   if (rc != AIS_OK) return rc;
   rc = check_mxfp4_rows(hidden_codes, hidden_codes_stride, hidden_scales, hidden_scales_stride, n_rows, width);
   if (rc != AIS_OK) return rc;
-  // offsets inside a tile of 256 rows are 32 bits wide
+  // indices behind the last row of a tile, and offsets inside a tile of 256 rows, are 32 bits wide
+  if (std::max(n_rows, vocab) > 0x7fffffffLL - 1024) return AIS_ERR_SIZE;
   if (std::max(std::max(hidden_codes_stride, hidden_scales_stride), std::max(weight_codes_stride, weight_scales_stride)) >= 1LL << 24)
     return AIS_ERR_SIZE;
   // an empty batch needs no embedding either

@@ -231,7 +231,7 @@ __device__ __forceinline__ bool recentre(const T* zr, int vocab, float c, RowSha
   const int tid = fresh_thread();
   float m = -__builtin_inff(), s = 0.f;
 #pragma unroll 1
-  for (int v = tid; v < vocab; v += THREADS) m = fmaxf(m, Vec<T>::load1(zr + v));
+  for (uint32_t v = tid; v < (uint32_t)vocab; v += THREADS) m = fmaxf(m, Vec<T>::load1(zr + v));
   m = wave_max(m);
   __syncthreads();
   if ((tid & 63) == 0) sh.policy[tid >> 6].m = m;
@@ -239,7 +239,7 @@ __device__ __forceinline__ bool recentre(const T* zr, int vocab, float c, RowSha
   for (int w = 0; w < THREADS / 64; ++w) m = fmaxf(m, sh.policy[w].m);
   if (!(fabsf(m) <= 3.4028235e38f)) return false;
 #pragma unroll 1
-  for (int v = tid; v < vocab; v += THREADS) s += exp2_fast((Vec<T>::load1(zr + v) - m) * c);
+  for (uint32_t v = tid; v < (uint32_t)vocab; v += THREADS) s += exp2_fast((Vec<T>::load1(zr + v) - m) * c);
   s = wave_sum(s);
   if ((tid & 63) == 0) sh.policy[tid >> 6].s = s;
   __syncthreads();
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(kTwiceThreads) void distill_twice_kernel(const Dist
   auto nothing = [&] {                                 // nothing to learn from: no loss, no gradient
     if (tid == 0) a.kl[row] = 0.f;
     if (dr != nullptr)
-      for (int v = tid; v < vocab; v += kTwiceThreads) Vec<T>::store1(dr + v, 0.f);
+      for (uint32_t v = tid; v < (uint32_t)vocab; v += kTwiceThreads) Vec<T>::store1(dr + v, 0.f);
   };
   if (a.valid != nullptr && a.valid[row] == 0) {
     nothing();
@@ -484,7 +484,7 @@ __global__ __launch_bounds__(THREADS) void distill_held_kernel(const DistillArgs
       st = MaxSum{0.f, sum};
       for (int j = tid; j < a.n_top; j += THREADS) teacher.listed.z[j] -= top;
 #pragma unroll 1
-      for (int v = tid; v < vocab; v += THREADS)
+      for (uint32_t v = tid; v < (uint32_t)vocab; v += THREADS)
         Vec<T>::store1(dr + v, exp2_fast((Vec<T>::load1(zr + v) - top) * c) * (g / sum));
       // the listed tokens' elements after them, whoever wrote those
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");

@@ -926,7 +926,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   if (far || !(total > 0.5f) || !(total < kHighest)) {
     float own = 0.f;
     if (fabsf(top) <= kHighest) {
-      for (int v = tid; v < vocab; v += kThreads) own += exp2_fast(row.exponent(Vec<T>::load1(row.z + v)));
+      for (uint32_t v = tid; v < (uint32_t)vocab; v += kThreads) own += exp2_fast(row.exponent(Vec<T>::load1(row.z + v)));
     }
     own = wave_sum(own);
     __syncthreads();

@@ -83,3 +83,13 @@ def test_distill_topk():
     assert call(inv_t=0.0) == -5 and call(inv_t=float("inf")) == -5 and call(inv_t=float("nan")) == -5
     assert call(dtype=-1) == -7
     assert call(n_rows=0, z=None, ids=None, teacher=None, kl=None, dz=None) == -1
+
+
+def test_logits_whose_indices_reach_beyond_32_bits():
+    """A tile's indices go on behind the last row: the sizes that leave no room for that are refused."""
+    order = "ctx h hs hsc hscs n_rows w ws wsc wscs vocab width out dtype out_stride".split()
+    call = caller("ais_mxfp4_logits", order, dict(ctx=None, h=P, hs=64, hsc=P, hscs=4, n_rows=5, w=Q, ws=64, wsc=Q, wscs=4, vocab=50,
+                                                  width=128, out=P, dtype=B.AIS_F32, out_stride=2 ** 31))
+    most = 2 ** 31 - 1025
+    assert call(vocab=most) == -1 and call(vocab=most + 1) == -2
+    assert call(n_rows=most) == -1 and call(n_rows=most + 1) == -2
