@@ -934,6 +934,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     __syncthreads();
     total = 0.f;
     for (int w = 0; w < kWaves; ++w) total += sh.vote_mass[1][w];
+    __syncthreads();                                   // the bound's questions write there again
   }
   total = uniform(total);
   // none of +inf, NaN and nothing but -inf has a sum of 1 or more
@@ -1101,8 +1102,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   // ---- the draw from the row itself: sixteen logits at a time, of which only the best score is looked at, as above; their random
   // numbers are asked for where one of them may be kept.
   const float last = uniform(cut.key == kNoLimit ? least : fmaxf(least, row.value(cut.key)));
+  // of the tokens of that logit; all of them where the cut is the next smaller one's, of which zero's next is a zero too
   const int end = __builtin_amdgcn_readfirstlane(
-      cut.key != kNoLimit && row.value(cut.key) == last ? row.token(cut.key) : vocab);        // of the tokens of that logit
+      cut.key >> row.index_bits == row.key(last, 0) >> row.index_bits ? row.token(cut.key) : vocab);
   const uint32_t take = __builtin_amdgcn_readfirstlane(cut.take);
   const float edge = uniform(cut.edge);
   constexpr int kOpen = 16 / N;

@@ -113,6 +113,18 @@ def test_many_tokens_kept(ctx, kind, limits):
     check(ctx, z.to(torch.bfloat16 if kind != "flat" else torch.float32), e, **limits)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [1, 4, 9, 70, 5000, 30_000])
+@pytest.mark.parametrize("value", [0.0, 1e-45, -1e-45, 1.0, -1.0])
+def test_rows_of_one_value(ctx, dtype, vocab, value):
+    """The cut lies behind the last token of a value; a zero of either sign is a zero."""
+    z, e = logits(4, vocab, dtype, 83)
+    z = torch.full_like(z, value) * torch.where(z > 0, 1.0, -1.0 if value == 0.0 else 1.0).to(dtype)
+    for limits in (dict(top_p=0.99), dict(top_p=0.9999, min_p=1.0), dict(top_p=0.3), dict(top_k=vocab - 1, top_p=0.9999),
+                   dict(top_k=max(vocab // 2, 1)), dict(min_p=1.0)):
+        check(ctx, z, e, **limits)
+
+
 @pytest.mark.parametrize("limits", [dict(top_p=0.97), dict(top_k=6000), dict(top_k=9000, top_p=0.9), dict(min_p=0.5),
                                     dict(top_p=0.97, min_p=0.6), dict(top_k=7000, min_p=0.6), dict(top_p=0.3)])
 @pytest.mark.parametrize("centre", [0.0, 1e-12, -5.0, 100.0, -3e4, 4e9, -4e9])
