@@ -476,7 +476,9 @@ __device__ __forceinline__ Cut finish_cut(const Row<T>& row, Each each, Span s, 
   if (tid == 0) sh.n = 0;
   __syncthreads();
   each([&](float x, u64 key) {
-    if (key >= s.lo && key < s.hi) sh.mass[atomicAdd(&sh.n, 1u)] = key;
+    if (key < s.lo || key >= s.hi) return;
+    const uint32_t at = atomicAdd(&sh.n, 1u);          // as many as were counted
+    if (at < (uint32_t)kMembers) sh.mass[at] = key;
   });
   __syncthreads();
   sort_keys(s.n, sh.mass);
@@ -586,6 +588,7 @@ __device__ __forceinline__ Cut cut_by_value(const Row<bf16_t>& row, float least,
     __syncthreads();
     return Cut{row.key(x, 0), s.above_count + (uint32_t)take, s.above_mass + take * each, (uint32_t)take, x};
   }
+  lower = uniform(fmaxf(lower, least));                       // several values may lie on both sides of the bound: those counted
   s.lo = row.key(upper, 0);
   s.hi = row.key(lower, row.vocab - 1) + 1;
   auto inside = [&](auto f) {
