@@ -25,12 +25,13 @@ using namespace dev;
 typedef unsigned long long u64;
 
 constexpr int kQBits = 62;             // q as a fixed-point number
+constexpr float kLowest = -3.4028235e38f;
 
 // What a row's listed tokens need of LDS: `slots` (a power of two >= 2 n_top) of the table and n_top entries.
 struct Listed {
   u64* mass;                           // [slots] sum of q of the token in the slot
   int* token;                          // [slots] or -1
-  float* t;                            // [n_top] the teacher's logit in base 2; -inf where there is no entry
+  float* t;                            // [n_top] the teacher's logit; -inf where there is no entry
   float* z;                            // [n_top] the policy's
   int* next;                           // [n_top] next entry of the same thread's row elements, or -1
   int* slot;                           // [n_top] of an entry that stands for its token, else -1
@@ -45,9 +46,16 @@ struct Listed {
   }
 };
 
+// A largest logit, as it is, and the sum of 2^((t - largest) c).  Lists are padded with numbers far below zero, whose products with c are
+// rounded by more than an exponent holds: differences are taken before they are multiplied.
+struct TopSum {
+  float top, s;
+};
+
 template <int THREADS>
 struct RowShared {
-  MaxSum teacher[THREADS / 64], policy[THREADS / 64];
+  TopSum teacher[THREADS / 64];
+  MaxSum policy[THREADS / 64];
   double kl[THREADS / 64];
   int first[THREADS];                  // first entry of each thread's row elements, or -1
 };
@@ -67,6 +75,21 @@ __device__ __forceinline__ MaxSum merge_all(const MaxSum* part) {
   if constexpr (WAVES > 4) st = merge_dpp<kDppRowHalfMirror>(st);
   if constexpr (WAVES > 8) st = merge_dpp<kDppRowMirror>(st);
   return st;
+}
+
+template <int WAVES, typename Op>
+__device__ __forceinline__ float fold_all(float v, Op op) {
+  if constexpr (WAVES > 1) v = op(v, dpp_move<kDppQuadXor1>(v));
+  if constexpr (WAVES > 2) v = op(v, dpp_move<kDppQuadXor2>(v));
+  if constexpr (WAVES > 4) v = op(v, dpp_move<kDppRowHalfMirror>(v));
+  if constexpr (WAVES > 8) v = op(v, dpp_move<kDppRowMirror>(v));
+  return v;
+}
+template <int WAVES>
+__device__ __forceinline__ TopSum join_all(const TopSum* part, float c) {
+  const TopSum own = part[threadIdx.x & (WAVES - 1)];
+  const float top = fold_all<WAVES>(own.top, [](float a, float b) { return fmaxf(a, b); });
+  return {top, fold_all<WAVES>(own.s * exp2_fast((own.top - top) * c), [](float a, float b) { return a + b; })};
 }
 
 // The arguments of a row's kernels.
@@ -96,7 +119,7 @@ struct Teacher {
   const DistillArgs<T>& a;
   const long long row;
   const float c;
-  MaxSum all;
+  TopSum all;
   __device__ __forceinline__ Teacher(unsigned char* lds, RowShared<THREADS>& sh, const DistillArgs<T>& a, long long row)
       : listed(lds, a.n_top, a.slots), sh(sh), a(a), row(row), c(a.inv_temperature * kLog2e) {}
   __device__ __forceinline__ bool entry(int id) const { return id >= 0 && id < a.vocab; }
@@ -132,7 +155,7 @@ struct Teacher {
   // Entries to LDS, their sum to the workgroup; empties the table.  No barrier.
   __device__ __forceinline__ void read() {
     const int tid = threadIdx.x;
-    MaxSum st{kNegHuge, 0.f};
+    TopSum st{kLowest, 0.f};                           // finite also where there is no entry
     each([&](int j) {
       float t = t0;
       if (!first(j)) t = a.teacher[row * a.n_top + j];
@@ -141,24 +164,26 @@ struct Teacher {
         t = kMasked;
         bad = bad || token != -1;
       }
-      accumulate<1>(&t, c, st);
+      st.top = fmaxf(st.top, t);
       listed.t[j] = t;
     });
+    st.top = wave_max(st.top);
+    each([&](int j) { st.s += exp2_fast((listed.t[j] - st.top) * c); });
+    st.s = wave_sum(st.s);
     for (int s = tid; s < a.slots; s += THREADS) {
       listed.token[s] = -1;
       listed.mass[s] = 0;
     }
     sh.first[tid] = -1;
-    st = wave_merge(st);
     if ((tid & 63) == 0) sh.teacher[tid >> 6] = st;
   }
   // After a barrier: whether there is anything to learn from.
   __device__ __forceinline__ bool any() {
-    all = merge_all<THREADS / 64>(sh.teacher);
+    all = join_all<THREADS / 64>(sh.teacher, c);
     return all.s != 0.f;
   }
   // q of an entry: NaN, all of them, where the teacher has a NaN or +inf
-  __device__ __forceinline__ float q(int j) const { return exp2_fast(__builtin_fmaf(listed.t[j], c, -all.m)) / all.s; }
+  __device__ __forceinline__ float q(int j) const { return exp2_fast((listed.t[j] - all.top) * c) / all.s; }
   __device__ __forceinline__ bool fine() const { return all.s < 3.0e38f; }
   // Entries into the table, their logits asked for.  An entry that stands for its token is put on the list of the thread that
   // `owner` names.  No barrier.
@@ -187,7 +212,7 @@ struct Teacher {
   __device__ __forceinline__ void keep() {
     if ((int)threadIdx.x < a.n_top) listed.z[threadIdx.x] = Vec<T>::load1(&z0);
   }
-  // log q - log p of every entry, weighted by q, with q = 2^(t c - all.m) / all.s and p = 2^(z c - st.m) / st.s.  To the
+  // log q - log p of every entry, weighted by q, with q = 2^((t - all.top) c) / all.s and p = 2^(z c - st.m) / st.s.  To the
   // workgroup; no barrier.  Wavefronts without entries have nothing to do with it.
   __device__ __forceinline__ void diverge(MaxSum st) {
     const int tid = threadIdx.x;
@@ -197,7 +222,7 @@ struct Teacher {
       each([&](int j) {
         const float p = q(j);
         if (p <= 0.f) return;
-        const double t2 = (double)listed.t[j] * (double)c - (double)all.m, z2 = (double)listed.z[j] * (double)c - (double)st.m;
+        const double t2 = ((double)listed.t[j] - (double)all.top) * (double)c, z2 = (double)listed.z[j] * (double)c - (double)st.m;
         kl += (double)p * ((t2 - z2) * ln2 - log_ratio);
       });
       kl = wave_sum64(kl);
