@@ -769,7 +769,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     answer(-1, 0.f, 0.f);
   };
   const bool greedy = temperature == 0.f;
-  if (!(temperature >= 0.f) || temperature > 3.0e38f || lim.top_p != lim.top_p || min_p != min_p) {
+  if (!(temperature >= 0.f) || temperature > kHighest || lim.top_p != lim.top_p || min_p != min_p) {
     refuse();
     return;
   }
