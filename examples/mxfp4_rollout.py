@@ -74,7 +74,7 @@ def distill(ctx, student, weight, hidden, valid, n_top, rate, steps):
     """`steps` steps of the fp32 weights behind the 4-bit read-out, in place -> the divergence before each, and after the last."""
     best = torch.topk(hidden.float() @ weight.float().T, n_top, dim=1)
     ids, teacher = best.indices.int(), best.values.contiguous()
-    hidden4 = ctx.mxfp4_quantize_rows(hidden)
+    *hidden4, values = ctx.mxfp4_quantize_rows(hidden, want_values=True)     # the logits' gradient is taken at the values
     losses = []
     for step in range(steps + 1):
         logits = ctx.mxfp4_logits(*hidden4, *ctx.mxfp4_quantize_rows(student))
@@ -83,7 +83,7 @@ def distill(ctx, student, weight, hidden, valid, n_top, rate, steps):
                                             dlogits=None if last else logits)
         losses.append(loss)
         if not last:
-            student -= rate * (dlogits.float().T @ hidden.float())
+            student -= rate * (dlogits.float().T @ values.float())
     return torch.cat(losses).tolist()
 
 
