@@ -328,7 +328,6 @@ __device__ __forceinline__ void sort_keys(uint32_t n, u64* keys) {
 // `take`, whose keys are not less.
 struct Cut {
   u64 key;
-  uint32_t count;
   u64 mass;
   uint32_t take = 0;
   float edge = 0.f;
@@ -368,7 +367,7 @@ __device__ __forceinline__ Cut cut_sorted(const Row<T>& row, const Span& s, uint
     }
     __syncthreads();
     const uint32_t all = sh.wave_count[0];
-    return Cut{all < n ? keys[all] : keys[n - 1] + 1, s.above_count + all, s.above_mass + sh.wave_mass[0]};
+    return Cut{all < n ? keys[all] : keys[n - 1] + 1, s.above_mass + sh.wave_mass[0]};
   }
   const uint32_t i = 2 * tid;
   const u64 k0 = i < n ? keys[i] : 0, k1 = i + 1 < n ? keys[i + 1] : 0;
@@ -380,7 +379,7 @@ __device__ __forceinline__ Cut cut_sorted(const Row<T>& row, const Span& s, uint
   const Before kept = scan((uint32_t)kept0 + (uint32_t)kept1, (kept0 ? m0 : 0) + (kept1 ? m1 : 0), sh);
   // behind the last of them where all are kept, not at the span's end, which may reach over others
   const u64 end = kept.all_count < n ? keys[kept.all_count] : keys[n - 1] + 1;
-  return Cut{end, s.above_count + kept.all_count, s.above_mass + kept.all_mass};
+  return Cut{end, s.above_mass + kept.all_mass};
 }
 
 // Where the cut lies among ranges of which each thread has kOwn: in the first one after which a limit is reached.  held(k, f) calls
@@ -441,7 +440,7 @@ __device__ __forceinline__ bool narrow(const Row<T>& row, Each each, bool by_mas
   const Before all = find_range<kOwn>(
       [&](int k, auto f) { f(sh.count[kOwn * tid + k], sh.mass[kOwn * tid + k]); }, *s, limit_count, limit_mass, sh);
   if (sh.bin < 0) {
-    *cut = Cut{s->hi, s->above_count + all.all_count, s->above_mass + all.all_mass};
+    *cut = Cut{s->hi, s->above_mass + all.all_mass};
     return false;
   }
   s->n = sh.bin_count;
@@ -565,7 +564,7 @@ __device__ __forceinline__ Cut cut_by_value(const Row<bf16_t>& row, float least,
         if (c > 0) f(c, c * row.mass(value_of(kOwn * tid + k)));
       },
       s, limit_count, limit_mass, sh);
-  if (sh.bin < 0) return Cut{kNoLimit, all.all_count, all.all_mass};
+  if (sh.bin < 0) return Cut{kNoLimit, all.all_mass};
   const int bin = sh.bin;
   s.n = sh.bin_count;
   s.above_count = sh.above_count;
@@ -586,7 +585,7 @@ __device__ __forceinline__ Cut cut_by_value(const Row<bf16_t>& row, float least,
     if (each > 0 && limit_mass != kNoLimit) take = min(take, (limit_mass - s.above_mass + each - 1) / each);
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    return Cut{row.key(x, 0), s.above_count + (uint32_t)take, s.above_mass + take * each, (uint32_t)take, x};
+    return Cut{row.key(x, 0), s.above_mass + take * each, (uint32_t)take, x};
   }
   lower = uniform(fmaxf(lower, least));                       // several values may lie on both sides of the bound: those counted
   s.lo = row.key(upper, 0);
@@ -991,7 +990,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
   auto from_exponent = [&](float low) { return top + low / row.c - 1e-5f * (fabsf(top) + fabsf(low / row.c)); };
   float least = lim.by_share && !lim.by_count ? fmaxf(from_exponent(lim.share), kLowest) : kLowest;
   u64 kept_mass = 0;
-  Cut cut{kNoLimit, 0, 0};
+  Cut cut{kNoLimit, 0};
   const bool sum_mass = !lim.by_mass || lim.by_share;  // of the kept tokens; otherwise the cut tells it
   // ---- candidates ----
   float bounded = kLowest;
