@@ -100,6 +100,24 @@ template <> struct Vec<float> {
   static __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 };
 
+// Vectors of four words, or two, that lie at any multiple of an element.
+template <typename T> struct Unaligned {
+  typedef uint32_t four __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <> struct Unaligned<bf16_t> {
+  typedef uint32_t four __attribute__((ext_vector_type(4), aligned(2)));
+  typedef uint32_t two __attribute__((ext_vector_type(2), aligned(2)));
+};
+
+// A vector of excluded elements (-inf in the row's type), for lanes past the end of the row.
+template <typename T> __device__ __forceinline__ u32x4 masked_fill();
+template <> __device__ __forceinline__ u32x4 masked_fill<bf16_t>() {
+  return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
+}
+template <> __device__ __forceinline__ u32x4 masked_fill<float>() {
+  return u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
+}
+
 // Rows that are not 16-byte aligned (an odd vocabulary makes every row start somewhere else) are split into the
 // elements before their first 128-byte boundary, whole 16-byte vectors from there on, and the elements after the last
 // vector: the vectors of a wavefront then cover whole lines like those of an aligned row.  Number of elements before

@@ -406,15 +406,6 @@ __global__ __launch_bounds__(kTwiceThreads) void distill_twice_kernel(const Dist
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef const __attribute__((address_space(1))) void* glb_ptr;
 
-// A vector of excluded elements (-inf in the row's type), for lanes past the end of the row.
-template <typename T> __device__ __forceinline__ u32x4 masked_fill();
-template <> __device__ __forceinline__ u32x4 masked_fill<bf16_t>() {
-  return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
-}
-template <> __device__ __forceinline__ u32x4 masked_fill<float>() {
-  return u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
-}
-
 // ALIGNED: both rows are 16-byte aligned; otherwise both lie the same way relative to 128-byte lines, and the elements before the
 // row's first line boundary are handled one by one together with those after the last vector.  Vector k of a lane (vector tid +
 // THREADS k of the row) lies in register q[k] for k < NV and in slot k - NV of the dynamic LDS for the NL after them; up to NR more,

@@ -25,15 +25,6 @@ using namespace dev;
 
 constexpr int kRowThreads = 1024;
 
-// A vector of excluded elements (-inf in the row's type), for lanes past the end of the row.
-template <typename T> __device__ __forceinline__ u32x4 masked_fill();
-template <> __device__ __forceinline__ u32x4 masked_fill<bf16_t>() {
-  return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
-}
-template <> __device__ __forceinline__ u32x4 masked_fill<float>() {
-  return u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u};
-}
-
 // q with its element `sub` excluded (replaced by -inf in the row's type).
 template <typename T> __device__ __forceinline__ u32x4 patch_masked(u32x4 q, int sub);
 template <> __device__ __forceinline__ u32x4 patch_masked<bf16_t>(u32x4 q, int sub) {

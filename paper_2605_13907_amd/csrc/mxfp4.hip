@@ -19,19 +19,9 @@ constexpr int kQuantThreads = 256;
 // with values 450 us, 6.3 TB/s; 64 rows 3.4 us, which is the launch.  A lane has one unit: with four, one after the other, these
 // were 503 and 4.4.  Rows begin at any element: vectors that lie anywhere cost 151,936 x 1,025 125 us, single elements 392.
 
-// A vector that lies at any multiple of an element.
-template <typename T>
-struct Unaligned {
-  typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4)));
-};
-template <>
-struct Unaligned<bf16_t> {
-  typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2)));
-};
-
 template <typename T>
 __device__ __forceinline__ void load_unit(const T* p, int left, float* x) {
-  typedef typename Unaligned<T>::type Any;
+  typedef typename Unaligned<T>::four Any;
   if (left >= kUnit) {
     constexpr int N = Vec<T>::N;
 #pragma unroll
@@ -44,7 +34,7 @@ __device__ __forceinline__ void load_unit(const T* p, int left, float* x) {
 
 template <typename T>
 __device__ __forceinline__ void store_unit(T* p, int left, const float* x) {
-  typedef typename Unaligned<T>::type Any;
+  typedef typename Unaligned<T>::four Any;
   if (left >= kUnit) {
     constexpr int N = Vec<T>::N;
 #pragma unroll
