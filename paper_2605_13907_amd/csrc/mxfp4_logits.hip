@@ -48,7 +48,7 @@ __device__ __forceinline__ int swizzle_w(int row) { return (row >> 1 & 1) | (row
 constexpr int kStreamThreads = 256;
 constexpr int kStreamWaves = kStreamThreads / 64;
 
-// NT: tiles of 16 tokens; GPW: groups of 16 blocks of each wavefront.
+// NT: tiles of 16 tokens, which hold all rows; GPW: groups of 16 blocks of each wavefront.
 template <int NT, int GPW>
 struct StreamLds {
   static constexpr int kCodes = GPW * 16 * 2 * kRowBytes;                       // of 16 rows: [group][half][row][128]
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kStreamThreads) __attribute__((amdgpu_waves_per_eu(
   for (int g = 0; g < GPW; ++g)
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const long long row = min((int)(blockIdx.y * NT + j) * 16 + (lane & 15), n_rows - 1);
+      const long long row = min(j * 16 + (lane & 15), n_rows - 1);
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const int b = block0 + g * kGroup + 4 * s + quarter;
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kStreamThreads) __attribute__((amdgpu_waves_per_eu(
         f32x4 z = mine[j * 64 + lane];
 #pragma unroll
         for (int p = 1; p < kStreamWaves; ++p) z += mine[(p * NT + j) * 64 + lane];
-        const int t = (int)(blockIdx.y * NT + j) * 16 + a, v = tile * 16 + 4 * quarter;
+        const int t = j * 16 + a, v = tile * 16 + 4 * quarter;
         if (t >= n_rows) continue;
         O* o = out + (long long)t * out_stride + v;
         if (v + 4 <= vocab) {
@@ -510,8 +510,7 @@ int launch_stream(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4
   static bool ok[kMaxDevices];
   if (!allow_dynamic_lds(ctx, reinterpret_cast<const void*>(kernel), kBytes, once, ok)) return hip_fail(ctx, hipErrorInvalidValue);
   const int tiles = (vocab + 15) / 16;
-  const dim3 grid((unsigned)std::min(tiles, ctx->n_cus), (unsigned)((n_rows + 16 * NT - 1) / (16 * NT)));
-  kernel<<<grid, dim3(kStreamThreads), kBytes, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, out, out_stride);
+  kernel<<<dim3((unsigned)std::min(tiles, ctx->n_cus)), dim3(kStreamThreads), kBytes, ctx->stream>>>(hidden, n_rows, weight, vocab, blocks, out, out_stride);
   return hip_fail(ctx, hipGetLastError());
 }
 
