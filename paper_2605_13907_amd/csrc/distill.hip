@@ -12,8 +12,9 @@
 // Rows that fit are held by one compute unit, in registers and, beyond 20 vectors a lane, in LDS: one read and one write of the
 // row.  The loads of a row are all on their way before the teacher's part begins, which they hide; a listed token's element is
 // written again by the thread that wrote it, so that nobody waits for the row's stores.
-// 8,192 bf16 rows x 151,936 with 64 listed tokens 1,010 us: 4.98 GB at 4.93 TB/s (a copy 5.15); 3,001 x 50,257 with 200 listed, 0.6 of the
-// rows valid, 108 us; 512 fp32 rows x 1,024 6.4 us and the loss 1.6.  The other kernel reads a row twice, or once for the loss alone.
+// 8,192 bf16 rows x 151,936 with 64 listed tokens 1,014 us: 4.98 GB at 4.91 TB/s (a copy 5.15); 3,001 x 50,257 with 200 listed, 0.6 of the
+// rows valid, 109 us; 512 fp32 rows x 1,024 6.5 us and the loss 1.8.  The other kernel reads a row twice, or once for the loss alone:
+// 2,048 fp32 rows x 151,936 754 us, 3.73 GB at 4.95 TB/s; the loss of 8,192 bf16 rows 363.
 #include "ais_internal.h"
 #include "device_utils.h"
 

@@ -43,7 +43,7 @@ __device__ __forceinline__ int swizzle_w(int row) { return (row >> 1 & 1) | (row
 // on every compute unit walks through its share of the vocabulary, 16 entries at a time, with all of LDS as a ring of what is on
 // its way.  Its four wavefronts have a quarter of the contraction each, whose hidden states stay in registers.  A wavefront
 // copies and awaits its own share of the embedding, whole lines of 128 bytes, and nobody else's; the four sums of a tile meet
-// in LDS, and the wavefronts take turns in writing them out.  Bound by reading: 16 rows x 151,936 x 4,096 57 us, 331 MB at 5.8
+// in LDS, and the wavefronts take turns in writing them out.  Bound by reading: 16 rows x 151,936 x 4,096 58 us, 331 MB at 5.7
 // TB/s (a sum over 4 GiB reads 6.1).
 constexpr int kStreamThreads = 256;
 constexpr int kStreamWaves = kStreamThreads / 64;
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(kStreamThreads) __attribute__((amdgpu_waves_per_eu(
 // memory into one of two LDS buffers; the copies of the next step are on their way while a step is multiplied.  Scales come
 // for two steps at a time.  A workgroup walks through its tiles without a pause: the first step of the next tile is copied during
 // the last of this one.
-// 2,048 rows x 151,936 x 4,096 740 us, 3.4 PFLOP/s.  There copies and LDS reads without the products take 520 us, products and LDS
+// 2,048 rows x 151,936 x 4,096 745 us, 3.4 PFLOP/s.  There copies and LDS reads without the products take 520 us, products and LDS
 // reads without the copies 502 (the instructions by themselves 253), and the stores, which all workgroups make at about the same
 // time, 115.
 //
@@ -519,10 +519,10 @@ int launch_typed(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4R
                  long long out_stride) {
   const int groups = (blocks + kGroup - 1) / kGroup;
   // Few rows of long contractions: the stream.  A tile of it costs the same however short its quarters are, and 64 rows want
-  // twice the registers of 32.  us, stream and tiles, with the quantisation of the hidden states: 16 rows x 151,936 x 512 25.2 and
-  // 17.0, x 1,024 27.2 and 23.7, x 4,096 65.0 and 87.4, 16 x 50,257 x 1,100 20.6 and 20.1; 4 x 32,000 x 2,048 14.8 and 16.7, x 4,096 (one
-  // row) 19.2 and 23.6; 32 x 151,936 x 1,024 34.0 and 25.6, x 2,048 41.9 and 49.9, x 4,096 70.8 and 91.5, x 8,192 125 and 179; 64 x
-  // 50,304 x 2,048 28.0 and 20.0, x 151,936 x 2,048 51.3 and 52.7, x 4,096 80.0 and 97.7, x 64,000 x 4,096 42.9 and 41.2.
+  // twice the registers of 32.  us, stream and tiles, with the quantisation of the hidden states, the embedding not in any cache:
+  // 16 rows x 151,936 x 512 24 and 16, x 1,024 26 and 26, x 4,096 61 and 79, 16 x 50,257 x 1,100 15 and 16; 4 x 32,000 x 2,048 14 and 16,
+  // x 4,096 (one row) 19 and 26; 32 x 151,936 x 1,024 32 and 27, x 2,048 39 and 45, x 4,096 67 and 85, x 8,192 120 and 176; 64 x
+  // 50,304 x 2,048 25 and 20, x 151,936 x 2,048 49 and 48, x 4,096 77 and 91, x 64,000 x 4,096 40 and 36.
   auto stream = [&](auto nt, auto gpw) {
     return launch_stream<O, decltype(nt)::value, decltype(gpw)::value>(ctx, hidden, n_rows, weight, vocab, blocks, out, out_stride);
   };
@@ -548,8 +548,8 @@ int launch_typed(ais_ctx* ctx, const Mxfp4Rows& hidden, int n_rows, const Mxfp4R
   };
   // Tiles of 64, 128 or 256 tokens take about 4 : 5 : 8 of time each (x 4,096: 20, 25 and 42 us), and every compute unit one at a
   // time: what comes out least, the larger ones where that is equal.  us with tiles of 64, 128 and 256: 70 rows x 50,257 x 1,024
-  // 22.0, 17.4 and 21.7; 130 x 151,936 x 4,096 162, 135 and 128; 333 x 151,936 x 2,048 154, 107 and 117; 520 x 50,257 x 4,096 163, 116
-  // and 131; 1,000 x 2,000 x 2,048 17.6, 19.7 and 26.6; 2,048 x 32,000 x 4,096 362, 222 and 169.
+  // 21, 16 and 18; 130 x 151,936 x 4,096 153, 130 and 118; 333 x 151,936 x 2,048 147, 106 and 107; 520 x 50,257 x 4,096 156, 112 and
+  // 124; 1,000 x 2,000 x 2,048 15, 18 and 23; 2,048 x 32,000 x 4,096 331, 214 and 162.
   auto time = [&](int nj, long long each) {
     const long long items = (long long)((vocab + kTileV - 1) / kTileV) * ((n_rows + 64 * nj - 1) / (64 * nj));
     return ((items + ctx->n_cus - 1) / ctx->n_cus) * each;

@@ -1,8 +1,8 @@
 // The next token of every row under temperature, top-k, top-p and min-p, from given Exp(1) random numbers.
 //
 // With t = z / temperature and independent E ~ Exp(1), the arg-max of t - log E over a set of tokens is a draw from softmax(t)
-// restricted to that set: no normalisation, no running sum over the vocabulary whose rounding decides the token, and random
-// numbers are read for the kept tokens alone.  The kept tokens are a prefix of the ranking by (logit, index), so what a limit
+// restricted to that set: no normalisation, no running sum over the vocabulary whose rounding decides the token.  Random numbers
+// are read for the kept tokens alone, except where the draw passes over the row itself, which reads them all.  The kept tokens are a prefix of the ranking by (logit, index), so what a limit
 // asks for is the place of a cut in that ranking: after k tokens, or where the mass before a token reaches its share.
 //
 // A workgroup owns a row.  A row without limits takes one pass over logits and random numbers.  Otherwise one pass finds the
@@ -18,9 +18,10 @@
 // The tokens that share the cut's value are found by the draw, which passes over such a row sixteen tokens at a time.
 // Masses are summed as fixed-point numbers, so no result depends on the order in which threads arrive.
 //
-// Measured, us a call, logits in the cache of a step that made them: bf16 rows of 151,936 without limits 19 (1 row), 21 (64) and
-// 46 (256: 233 MB, 5.1 TB/s); of 64 such rows with limits 36 (top-k), 19 (min-p), 68 (top-p over flat rows, all of whose tokens
-// pass the bound).  Few rows are bound by one compute unit's exponentials and reading of its row and the barriers between the passes,
+// Measured, us a call, logits in the cache of a step that made them: bf16 rows of 151,936 without limits 18 (1 row), 21 (64) and
+// 45 (256: 233 MB, 5.2 TB/s); of 64 such rows with limits 35 (top-k), 17 (min-p), 67 (top-p over flat rows, all of whose tokens
+// pass the bound).  64 rows with limits of their own take as long as the slowest of them: of 60 batches 32 took 22 to 27, where no row
+// has many candidates, 21 took 30 to 55, and 7 with a row that keeps 8,000 tokens or more 61 to 89.  Few rows are bound by one compute unit's exponentials and reading of its row and the barriers between the passes,
 // many without limits by memory.  A kernel of 1,024 threads has 128 registers to each: what the compiler would compute early and keep
 // (indices, addresses, widened numbers) went to scratch memory, and with it 64 rows under top-k took 46 us and 256 without limits 52.
 #include "ais_internal.h"
@@ -1101,8 +1102,8 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
     finish(best.token, kept_mass);
     return;
   }
-  // ---- the draw from the row itself: sixteen logits at a time, of which only the best score is looked at, as above; their random
-  // numbers are asked for where one of them may be kept.
+  // ---- the draw from the row itself: sixteen logits at a time, of which only the best score is looked at, as above; all of the
+  // row's random numbers are read, at the same time as its logits.
   const float last = uniform(cut.key == kNoLimit ? least : fmaxf(least, row.value(cut.key)));
   // of the tokens of that logit; all of them where the cut is the next smaller one's, of which zero's next is a zero too
   const int end = __builtin_amdgcn_readfirstlane(
