@@ -1072,8 +1072,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T* __restrict__ 
       } else {
         bool done = false;
         if constexpr (sizeof(T) == 2) {
-          // what counts as zero has the same mass but for 2^-32 c < 2^-20 of the exponent
-          if (fabsf(top) < 2147483648.f && row.c < 4096.f) {
+          // what counts as zero has the same mass but for 2^-32 c < 2^-20 of the exponent; the last value and what lies beyond, almost
+          // 2^31 below the largest logit and more, none
+          if (fabsf(top) < 2147483648.f && row.c < 4096.f && row.c > 3.1e-8f) {
             cut = cut_by_value(row, least, lim.count, limit_mass, sh);
             done = true;
           }
