@@ -25,7 +25,8 @@ using namespace dev;
 
 typedef unsigned long long u64;
 
-constexpr int kQBits = 62;             // q as a fixed-point number
+// q as a fixed-point number: a token's is off by 2^-62 at most, which shows in the gradient only where p and q are below some 1e-14.
+constexpr int kQBits = 62;
 constexpr float kLowest = -3.4028235e38f;
 
 // What a row's listed tokens need of LDS: `slots` (a power of two >= 2 n_top) of the table and n_top entries.
