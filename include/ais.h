@@ -443,13 +443,157 @@ int ais_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long lon
                      const unsigned char* valid, const float* weight, float inv_temperature, float* kl_out,
                      float* loss_out, void* dlogits, long long dlogits_stride);
 
+/* ---- a loss over pairs of whole responses -------------------------------------------------------------- */
+
+/* Hyper-parameters of the preference loss; ais_preference_params_default() fills in the values behind the names. */
+typedef struct ais_preference_params {
+  float beta;            /* 0.1  weight of the log-ratios, > 0                                           */
+  int   kind;            /* 0: logistic;  1: hinge;  2: squared                                          */
+  float label_smoothing; /* 0.0  share of pairs taken to be labelled the wrong way round, in [0, 0.5];
+                            other than 0 with kind 0 alone                                               */
+  float margin;          /* 0.0  what the preferred response has to be ahead by                          */
+  int   mean_logp;       /* 0: sums over a response's tokens;  1: means                                  */
+  float inv_temperature; /* 1.0  of the log-probabilities, > 0                                           */
+} ais_preference_params;
+/* Writes the values above into *p (host memory); NULL is allowed.  Eq. 19 and App. "AIS hyperparameters" have none of them. */
+void ais_preference_params_default(ais_preference_params* p);
+
+/* Preference loss of paired responses and its gradient: the trainer's counterpart of Eq. 19 where a prompt's two responses
+ * are ranked instead of rewarded, with the same reference policy as that equation's KL term.  Responses 2p (preferred) and
+ * 2p + 1 are a pair.  Over the valid tokens of response i,
+ *   d_i = sum_t (logp_train[t] - logp_ref[t])          (their mean with mean_logp; 0 without a valid token)
+ *   h_p = beta (d_2p - d_2p+1) - margin
+ *   l_p = -(1 - label_smoothing) log sigmoid(h_p) - label_smoothing log sigmoid(-h_p)      kind 0
+ *         max(0, 1 - h_p)                                                                  kind 1
+ *         ((h_p - 1/2) / beta)^2                                                           kind 2
+ *   loss = sum_p weight[p] l_p,     c_t = -d loss / d logp_train[t]
+ * The sums are taken in fp64, in a fixed order.  At h_p = 1 the hinge has no slope.
+ *   logp_train  [n_rows] fp32, output of ais_token_logprob or ais_lm_head_logprob
+ *   logp_ref    [n_rows] fp32, or NULL: no reference (0 everywhere)
+ *   valid, cu_rows   as above, n_resp even; neither log-prob is read where valid == 0
+ *   weight      [n_resp / 2] fp32, or NULL: 2 / n_resp each
+ *   reward_out  [n_resp] fp32   beta d_i
+ *   loss_out    one fp32
+ * ais_preference_row_scale writes
+ *   g_out       [n_rows] fp32: c_t times inv_temperature, 0 where valid == 0: the `coeff` of ais_lm_head_grad, and the
+ *               scale of what ais_token_logprob_softmax_grad writes
+ * ais_preference_loss_grad writes, from logits, token_ids and lse (output of ais_token_logprob) as ais_grpo_loss_grad takes them,
+ *   dlogits     [n_rows, row_stride] of `dtype`: c_t inv_temperature (softmax(inv_temperature z_t) - 1[v = y_t]); 0 in rows
+ *               with c_t = 0, which are not read.  May be `logits` itself.
+ * A response whose sum is not finite makes its pair's loss, rewards and coefficients what the formulas give; other pairs are
+ * not touched by it.  Rows outside every response (a faulty cu_rows) get 0 and set AIS_STATUS_BAD_CU.
+ * Errors: as ais_grpo_row_scale and ais_grpo_loss_grad, with n_resp odd AIS_ERR_GROUP; NULL reward_out or loss_out; beta <= 0,
+ * kind outside {0, 1, 2}, label_smoothing outside [0, 0.5] or with another kind, mean_logp outside {0, 1}, inv_temperature <= 0,
+ * any not finite (AIS_ERR_PARAM). */
+int ais_preference_row_scale(ais_ctx* ctx, const float* logp_train, const float* logp_ref, const unsigned char* valid,
+                             long long n_rows, const long long* cu_rows, int n_resp, const float* weight,
+                             const ais_preference_params* params, float* reward_out, float* loss_out, float* g_out);
+int ais_preference_loss_grad(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
+                             long long row_stride, const int* token_ids, const unsigned char* valid,
+                             const long long* cu_rows, int n_resp, const float* logp_train, const float* lse,
+                             const float* logp_ref, const float* weight, const ais_preference_params* params,
+                             float* reward_out, float* loss_out, void* dlogits);
+
+/* ---- the rows before the read-out ------------------------------------------------------------------------ */
+
+/* Normalised rows: the last hidden states as the policy's read-out takes them (Alg. 1, "Compute full-precision log-probs").
+ * With `centered`, layer norm:
+ *   mean = sum_d x[d] / width,  rstd = (sum_d (x[d] - mean)^2 / width + eps)^(-1/2),  y[d] = (x[d] - mean) rstd weight[d] + bias[d]
+ * without, root-mean-square norm: the same with 0 for the mean.  Statistics in fp32, deviations from the mean squared; they and
+ * the sums of ais_norm_rows_grad overflow where fp32 does (deviations from about 1e19 / sqrt(width)).
+ *   x           [n_rows, row_stride] of `dtype`, read only on rows with valid != 0 (valid NULL: all)
+ *   weight, bias   [width] of `param_dtype`, each NULL where there is none (1 and 0)
+ *   y           [n_rows, y_stride] of `dtype`, the first `width` of each row written, 0 where valid == 0; rounded once.  May be x
+ *               itself with y_stride == row_stride.
+ *   mean_out    [n_rows] fp32 with `centered`, not written without;  rstd_out  [n_rows] fp32;  0 where valid == 0
+ * Errors: NULL x / y / rstd_out, NULL mean_out with `centered` (with n_rows > 0), n_rows < 0, width < 1 or >= 2^31 - 8, strides <
+ * width, unknown dtypes, x, y, weight or bias misaligned, eps <= 0 or not finite, centered outside {0, 1} (AIS_ERR_PARAM). */
+int ais_norm_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, long long width, long long row_stride,
+                  const unsigned char* valid, const void* weight, const void* bias, ais_dtype param_dtype, float eps,
+                  int centered, void* y, long long y_stride, float* mean_out, float* rstd_out);
+
+/* Its gradient (Alg. 1, "Policy Update").  With n = (x - mean) rstd and u = dy weight, over the rows with valid != 0,
+ *   dx[r, :]   = rstd (u - [mean given] sum_d u / width - n sum_d u n / width)
+ *   dweight[d] = sum_r dy[r, d] n[r, d],     dbias[d] = sum_r dy[r, d]
+ *   dy          [n_rows, dy_stride] of `dy_dtype` (the dhidden of ais_lm_head_grad is fp32 whatever x is)
+ *   x, weight   as above;  mean, rstd  outputs of ais_norm_rows; mean NULL: root-mean-square norm
+ *   dx          [n_rows, dx_stride] of `dtype`, 0 where valid == 0.  May be dy itself (same type and stride), or x.
+ *   dweight_out, dbias_out   [width] fp32, each NULL where it is not wanted; summed in a fixed order, without atomics
+ * Uses up to 8 * width bytes of the context workspace for each of up to 2 (dweight alone: 1) workgroups a compute unit, and 8 *
+ * n_rows beside for rows of more than 16,384 elements.
+ * Errors: NULL dy / x / rstd / dx (with n_rows > 0), otherwise as ais_norm_rows. */
+int ais_norm_rows_grad(ais_ctx* ctx, const void* dy, ais_dtype dy_dtype, long long dy_stride, const void* x, ais_dtype dtype,
+                       long long n_rows, long long width, long long row_stride, const unsigned char* valid,
+                       const void* weight, ais_dtype param_dtype, const float* mean, const float* rstd, void* dx,
+                       long long dx_stride, float* dweight_out, float* dbias_out);
+
+/* ---- the step of the weights --------------------------------------------------------------------------------- */
+
+/* One tensor of ais_adamw_step.  Every array has `n` elements and lies anywhere but the moments, which are 16-byte aligned. */
+typedef struct ais_adamw_tensor {
+  void* param;             /* of param_dtype, stepped in place                                                  */
+  const void* grad;        /* of grad_dtype                                                                     */
+  void* copy;              /* bf16, or NULL: receives the stepped parameters, rounded to nearest even           */
+  void* m;                 /* first moment: fp32, or bytes                                                      */
+  void* v;                 /* second moment: fp32, or bytes                                                     */
+  unsigned char* m_scale;  /* [ceil(n / 32)] bytes, with 8-bit moments                                          */
+  unsigned char* v_scale;
+  long long n;             /* below 2^32; 0 is allowed                                                          */
+  int param_dtype, grad_dtype;
+} ais_adamw_tensor;
+
+typedef struct ais_adamw_params {
+  double lr;               /* 1e-3, >= 0                                                                        */
+  double beta1, beta2;     /* 0.9, 0.999, in [0, 1)                                                             */
+  double eps;              /* 1e-8, at least 1e-30                                                              */
+  double weight_decay;     /* 0.01, >= 0                                                                        */
+  int   state_bits;        /* 32 or 8                                                                           */
+  unsigned int seed;       /* of the random numbers that 8-bit moments are rounded with                         */
+  long long step;          /* number of this step, from 1 on                                                    */
+} ais_adamw_params;
+/* Writes the values above into *p (host memory); NULL is allowed.  (The paper's optimiser of Alg. 1, "Policy Update", is AdamW
+ * with beta2 0.99 and weight_decay 0.1.) */
+void ais_adamw_params_default(ais_adamw_params* p);
+
+/* An AdamW step over many tensors at once: the "Policy Update" of Alg. 1 with the gradients of ais_lm_head_grad,
+ * ais_norm_rows_grad and the caller's own.  With g = grad_scale grad,
+ *   m <- beta1 m + (1 - beta1) g,    v <- beta2 v + (1 - beta2) g^2                (in fp64, rounded to fp32)
+ *   param <- param - lr (weight_decay param + (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps))     (in fp32)
+ * A bf16 param is rounded to nearest even, which loses steps below half its spacing: fp32 params with a bf16 copy keep them.
+ * With state_bits 8 each 32 consecutive elements of a moment share a scale 2^(byte - 127).  m is held in E4M3 (sign, 4 bits of
+ * exponent with bias 7, 3 of fraction), with byte = max(E - 7, 7), E being the biased fp32 exponent of the block's largest
+ * magnitude; v, which has no sign, in 5 bits of exponent with bias 15 and 3 of fraction, every code a number, with byte =
+ * max(E - 15, 15).  A value between two codes goes to the upper one with the probability of its place between them,
+ * so that decaying averages, whose steps are smaller than a code's, keep their mean; the random numbers are 16 bits each of a
+ * hash of (seed, step, the tensor's number in the list, the element's index), m's the lower ones:
+ *   mix(x) = y ^ (y >> 16), y = (x ^ (x >> 15)) 0x6A09E667 mod 2^32;      key = mix(mix(seed ^ step P) ^ tensor P), P = 0x9E3779B1
+ *   bits = mix(index P ^ key)
+ * v > 0 never becomes 0.  A block with a NaN or infinity has byte 255 and stands for NaN.
+ *   tensors     HOST array of n_tensors, read before the call returns; arrays of different tensors must not overlap, but for grads
+ *   grad_scale  one fp32 in device memory, or NULL (1): a factor from a clipped norm or a loss scale
+ *   step_dev, lr_dev   one int64 and one fp32 in device memory that replace params->step and params->lr, or NULL: what a HIP graph
+ *               that is replayed needs (the step is read, not counted)
+ * One launch for each 48 tensors of the same types; no workspace.
+ * Errors: NULL tensors (with n_tensors > 0) / params, n_tensors < 0, n < 0 or >= 2^32 - 4096, NULL or misaligned arrays of a tensor
+ * with n > 0, unknown dtypes, parameters outside their ranges, step < 1 without step_dev (AIS_ERR_PARAM). */
+int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, int n_tensors, const ais_adamw_params* params,
+                   const float* grad_scale, const long long* step_dev, const float* lr_dev);
+
+/* What the codes of 8-bit moments stand for (the other half of the round trip, as in Sec. 2.1), exactly in either type (but where bf16 or fp32 has no number as small).
+ *   codes       [n] bytes, 16-byte aligned;  scales  [ceil(n / 32)] bytes;  moment  1 (signed) or 2
+ *   values_out  [n] of `dtype`
+ * Errors: NULL arrays (with n > 0), n < 0 or above 2^40, moment outside {1, 2} (AIS_ERR_PARAM), misaligned arrays, unknown dtype. */
+int ais_adamw_values(ais_ctx* ctx, const unsigned char* codes, const unsigned char* scales, long long n, int moment,
+                     void* values_out, ais_dtype dtype);
+
 /* ---- measurement helpers -------------------------------------------------------------------- */
 
 /* Kernels whose device time can be read back. */
 typedef enum ais_kernel {
   AIS_K_LOGPROB = 0, AIS_K_DLOGITS = 1, AIS_K_COPY = 2, AIS_K_FP8_QUANT = 3, AIS_K_FP8_DEQUANT = 4,
   AIS_K_FP8_LOGPROB = 5, AIS_K_FUSED = 6, AIS_K_LM_HEAD = 7, AIS_K_LM_HEAD_GRAD = 8,
-  AIS_K_MXFP4_QUANT = 9, AIS_K_MXFP4_LOGITS = 10, AIS_K_SAMPLE = 11, AIS_K_DISTILL = 12, AIS_K_COUNT_ = 13
+  AIS_K_MXFP4_QUANT = 9, AIS_K_MXFP4_LOGITS = 10, AIS_K_SAMPLE = 11, AIS_K_DISTILL = 12,
+  AIS_K_PREFERENCE = 13, AIS_K_NORM = 14, AIS_K_NORM_GRAD = 15, AIS_K_ADAMW = 16, AIS_K_COUNT_ = 17
 } ais_kernel;
 
 /* With `enable` != 0 every launch of the kernels above is bracketed by HIP events on the

@@ -28,9 +28,12 @@ AIS_K_FUSED = 6
 AIS_K_LM_HEAD = 7
 AIS_K_LM_HEAD_GRAD = 8
 AIS_K_MXFP4_QUANT, AIS_K_MXFP4_LOGITS, AIS_K_SAMPLE, AIS_K_DISTILL = range(9, 13)
+AIS_K_PREFERENCE, AIS_K_NORM, AIS_K_NORM_GRAD, AIS_K_ADAMW = range(13, 17)
 AIS_STATUS_LIVE_OVERFLOW = 4
 STATUS_BAD_TOKEN, STATUS_BAD_CU, STATUS_BAD_ROW = 1, 2, 8
 MXFP4_BLOCK = 32            # elements that share a scale
+MOMENT_BLOCK = 32           # the same, of AdamW's 8-bit moments
+PREFERENCE_LOGISTIC, PREFERENCE_HINGE, PREFERENCE_SQUARED = range(3)
 
 ERRORS = {
     0: "AIS_OK", -1: "AIS_ERR_NULL", -2: "AIS_ERR_SIZE", -3: "AIS_ERR_STRIDE", -4: "AIS_ERR_ALIGN",
@@ -55,6 +58,22 @@ class AisDiag(C.Structure):
 
     def as_dict(self):
         return {name: getattr(self, name) for name, _ in self._fields_ if name != "reserved"}
+
+
+class AisPreferenceParams(C.Structure):
+    _fields_ = [("beta", C.c_float), ("kind", C.c_int), ("label_smoothing", C.c_float), ("margin", C.c_float),
+                ("mean_logp", C.c_int), ("inv_temperature", C.c_float)]
+
+
+class AisAdamWParams(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("state_bits", C.c_int), ("seed", C.c_uint), ("step", C.c_longlong)]
+
+
+class AisAdamWTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_longlong), ("param_dtype", C.c_int),
+                ("grad_dtype", C.c_int)]
 
 
 class AisError(RuntimeError):
@@ -93,6 +112,15 @@ SYMBOLS = {
     "ais_mxfp4_logits": (_I, [_P, _P, _LL, _P, _LL, _LL, _P, _LL, _P, _LL, _LL, _LL, _P, _I, _LL]),
     "ais_sample_tokens": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _LL, _P, _P, _P, _P, _P, _P, _P, _P]),
     "ais_distill_topk": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _I, _P, _P, _F, _P, _P, _P, _LL]),
+    "ais_preference_params_default": (None, [C.POINTER(AisPreferenceParams)]),
+    "ais_preference_row_scale": (_I, [_P, _P, _P, _P, _LL, _P, _I, _P, C.POINTER(AisPreferenceParams), _P, _P, _P]),
+    "ais_preference_loss_grad": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _P, _I, _P, _P, _P, _P,
+                                      C.POINTER(AisPreferenceParams), _P, _P, _P]),
+    "ais_norm_rows": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _P, _I, _F, _I, _P, _LL, _P, _P]),
+    "ais_norm_rows_grad": (_I, [_P, _P, _I, _LL, _P, _I, _LL, _LL, _LL, _P, _P, _I, _P, _P, _P, _LL, _P, _P]),
+    "ais_adamw_params_default": (None, [C.POINTER(AisAdamWParams)]),
+    "ais_adamw_step": (_I, [_P, C.POINTER(AisAdamWTensor), _I, C.POINTER(AisAdamWParams), _P, _P, _P]),
+    "ais_adamw_values": (_I, [_P, _P, _P, _LL, _I, _P, _I]),
     "ais_profile": (_I, [_P, _I]),
     "ais_profile_read": (_I, [_P, _I, C.POINTER(_F), C.POINTER(_I)]),
     "ais_copy": (_I, [_P, _P, _P, _LL]),
@@ -119,7 +147,8 @@ _FAST = None
 _FAST_ENTRIES = ("ais_set_stream", "ais_token_logprob", "ais_diagnostics", "ais_grpo_loss_grad", "ais_grpo_row_scale",
                  "ais_token_logprob_softmax_grad", "ais_fp8_quantize_rows", "ais_fp8_dequantize_rows",
                  "ais_fp8_rollout_logprob", "ais_lm_head_logprob", "ais_lm_head_grad", "ais_mxfp4_quantize_rows",
-                 "ais_mxfp4_logits", "ais_sample_tokens", "ais_distill_topk")
+                 "ais_mxfp4_logits", "ais_sample_tokens", "ais_distill_topk", "ais_preference_row_scale",
+                 "ais_preference_loss_grad", "ais_norm_rows", "ais_norm_rows_grad", "ais_adamw_step", "ais_adamw_values")
 
 
 def fast_stamp() -> str:
@@ -154,14 +183,21 @@ def _load_fast():
     return _FAST or None
 
 
-def default_params(**overrides) -> AisParams:
-    p = AisParams()
-    _lib().ais_params_default(C.byref(p))
+def _defaults(p, fill, overrides):
+    fill(C.byref(p))
     for k, v in overrides.items():
         if not hasattr(p, k):
             raise AttributeError(k)
         setattr(p, k, v)
     return p
+
+
+def default_params(**overrides) -> AisParams:
+    return _defaults(AisParams(), _lib().ais_params_default, overrides)
+
+
+def default_preference_params(**overrides) -> AisPreferenceParams:
+    return _defaults(AisPreferenceParams(), _lib().ais_preference_params_default, overrides)
 
 
 def _dtype_code(t: torch.Tensor, name: str = "logits") -> int:
@@ -224,6 +260,88 @@ def _mxfp4_rows(codes: torch.Tensor, scales: torch.Tensor, device: torch.device,
         raise ValueError(f"{name}_codes: expected {(rows, 16 * blocks)} bytes for the scales' blocks, got {tuple(codes.shape)}")
     return (rows, blocks, _dev_ptr(codes, device, f"{name}_codes"), codes.stride(0) if rows > 1 else 16 * blocks,
             _dev_ptr(scales, device, f"{name}_scales"), scales.stride(0) if rows > 1 else -(-blocks // 4) * 4)
+
+
+class AdamWState:
+    """The weights that adamw_step steps and their moments, which a program keeps from step to step.
+
+    params       list of contiguous bf16 or fp32 tensors on one GPU, stepped in place
+    bits         of the moments: 32 (fp32) or 8 (codes under a scale for each 32 elements)
+    copies       None, or a list with a bf16 tensor of the size of each parameter (or None) that receives its rounded values
+    m, v         flat buffers of all tensors' moments (fp32, or uint8 codes with m_scale, v_scale), zeros where they are not given:
+                 tensor i begins at offsets[i], a multiple of 32; of() gives the part of one tensor.  A state that goes on from
+                 stored moments is made with them, or has them copied into its buffers; the buffers stay the same ones.
+    step         number of steps made; an int, or an int64 tensor of one element on the GPU, which a HIP graph counts on when it
+                 is replayed
+    seed         of the random numbers that 8-bit moments are rounded with
+    """
+
+    def __init__(self, params, bits: int = 32, copies=None, seed: int = 0, step=0, m=None, v=None, m_scale=None, v_scale=None):
+        self.params = tuple(params)
+        self.copies = (None,) * len(self.params) if copies is None else tuple(copies)
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        if len(self.copies) != len(self.params):
+            raise ValueError("copies: expected one for each parameter")
+        if not self.params:
+            raise ValueError("params is empty")
+        self.bits, self.seed, self.step = bits, int(seed) & 0xFFFFFFFF, step
+        self.device = self.params[0].device
+        if self.device.type != "cuda":
+            raise ValueError(f"params[0] is on {self.device}, expected a GPU")
+        if isinstance(step, torch.Tensor):
+            _ptr(step, torch.int64, 1, "step", self.device)
+        self.offsets = [0]
+        written = []
+        for i, (p, c) in enumerate(zip(self.params, self.copies)):
+            for name, t in ((f"params[{i}]", p), (f"copies[{i}]", c)):
+                if t is None and name[0] == "c":
+                    continue
+                if not isinstance(t, torch.Tensor):
+                    raise TypeError(f"{name} must be a torch.Tensor")
+                _dtype_code(t, name)
+                at = _ptr(t, torch.bfloat16 if name[0] == "c" else None, p.numel(), name, self.device)
+                if t.numel() > 0:
+                    written.append((at, at + t.numel() * t.element_size(), name))
+            self.offsets.append(self.offsets[-1] + -(-p.numel() // MOMENT_BLOCK) * MOMENT_BLOCK)
+        kind, total = torch.uint8 if bits == 8 else torch.float32, self.offsets[-1]
+        zeros = lambda n, t: torch.zeros(n, dtype=t, device=self.device)
+        self.m = zeros(total, kind) if m is None else m
+        self.v = zeros(total, kind) if v is None else v
+        if bits == 8:
+            self.m_scale = zeros(total // MOMENT_BLOCK, kind) if m_scale is None else m_scale
+            self.v_scale = zeros(total // MOMENT_BLOCK, kind) if v_scale is None else v_scale
+        elif m_scale is not None or v_scale is not None:
+            raise ValueError("moments of 32 bits have no scales")
+        else:
+            self.m_scale = self.v_scale = None
+        for name, t, n in (("m", self.m, total), ("v", self.v, total), ("m_scale", self.m_scale, total // MOMENT_BLOCK),
+                           ("v_scale", self.v_scale, total // MOMENT_BLOCK)):
+            at = _ptr(t, kind, n, name, self.device)
+            if at is None or n == 0:
+                continue
+            if name in ("m", "v") and at % 16 != 0:
+                raise ValueError(f"{name} must be 16-byte aligned")
+            written.append((at, at + t.numel() * t.element_size(), name))
+        written.sort()
+        for (_, end, name), (begin, _, other) in zip(written, written[1:]):
+            if begin < end:
+                raise ValueError(f"{name} and {other} share memory")
+        self._table = (AisAdamWTensor * len(self.params))()
+        e = 1 if bits == 8 else 4
+        for row, p, c, at in zip(self._table, self.params, self.copies, self.offsets):
+            row.param, row.copy = p.data_ptr(), None if c is None else c.data_ptr()
+            row.m, row.v = self.m.data_ptr() + at * e, self.v.data_ptr() + at * e
+            if bits == 8:
+                row.m_scale, row.v_scale = self.m_scale.data_ptr() + at // MOMENT_BLOCK, self.v_scale.data_ptr() + at // MOMENT_BLOCK
+            row.n, row.param_dtype = p.numel(), _dtype_code(p)
+        self._rule = AisAdamWParams()
+        _lib().ais_adamw_params_default(C.byref(self._rule))
+        self._rule.state_bits, self._rule.seed = bits, self.seed
+
+    def of(self, flat, i: int):
+        """The part of a flat buffer (moments or their values) that is tensor i's, in its shape."""
+        return flat[self.offsets[i]:self.offsets[i] + self.params[i].numel()].view(self.params[i].shape)
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)      # not part of torch's public interface
@@ -628,6 +746,200 @@ class AisContext:
         if rc != 0:
             raise AisError(rc, "ais_distill_topk")
         return loss, kl, dlogits
+
+    # ------------------------------------------------------------------ a loss over pairs of responses
+    def preference_row_scale(self, logp_train, logp_ref, valid, cu_rows, params: Optional[AisPreferenceParams] = None, weight=None):
+        """-> (loss [1] fp32, reward [B] fp32, g [R] fp32) of responses in pairs, the preferred one first: g is the coefficient that
+        lm_head_grad takes, and the scale of token_logprob_softmax_grad's direction.  logp_ref None: no reference; weight [B / 2]
+        fp32 or None (the mean over the pairs).  See ais_preference_row_scale in include/ais.h."""
+        p = params or default_preference_params()
+        if p.__class__ is AisPreferenceParams:
+            out = self._native("preference_row_scale", logp_train, logp_ref, valid, cu_rows, weight, C.addressof(p))
+            if out is not None:
+                return out
+        dev = self.device
+        n_rows, n_resp = logp_train.numel(), cu_rows.numel() - 1
+        ptrs = [_ptr(logp_train, torch.float32, n_rows, "logp_train", dev), _ptr(logp_ref, torch.float32, n_rows, "logp_ref", dev),
+                _ptr(valid, torch.uint8, n_rows, "valid", dev), n_rows, _ptr(cu_rows, torch.int64, n_resp + 1, "cu_rows", dev), n_resp,
+                _ptr(weight, torch.float32, n_resp // 2, "weight", dev)]
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        reward = torch.empty(max(n_resp, 0), dtype=torch.float32, device=dev)
+        g = torch.empty(n_rows, dtype=torch.float32, device=dev)
+        self._sync_stream()
+        rc = self._lib.ais_preference_row_scale(self._h, *ptrs, C.byref(p), _ptr(reward), _ptr(loss), _ptr(g))
+        if rc != 0:
+            raise AisError(rc, "ais_preference_row_scale")
+        return loss, reward, g
+
+    def preference_loss_grad(self, logits, token_ids, valid, cu_rows, logp_train, lse, logp_ref,
+                             params: Optional[AisPreferenceParams] = None, weight=None, dlogits=None):
+        """-> (loss [1] fp32, reward [B] fp32, dlogits like logits); logp_train and lse as token_logprob returns them.
+        Pass dlogits=logits to overwrite the logits in place.  See ais_preference_loss_grad in include/ais.h."""
+        p = params or default_preference_params()
+        if p.__class__ is AisPreferenceParams:
+            out = self._native("preference_loss_grad", logits, token_ids, lse, logp_train, logp_ref, valid, cu_rows, weight,
+                               C.addressof(p), dlogits)
+            if out is not None:
+                return out
+        dev = self.device
+        n_rows, vocab, row_stride = _logits_geometry(logits, dev)
+        dtype, n_resp = _dtype_code(logits), cu_rows.numel() - 1
+        if dlogits is None:
+            dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=dev)
+        elif dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.stride() != logits.stride():
+            raise ValueError("dlogits must have the dtype, shape and strides of logits")
+        _dev_ptr(dlogits, dev, "dlogits")
+        ptrs = [_ptr(token_ids, torch.int32, n_rows, "token_ids", dev), _ptr(valid, torch.uint8, n_rows, "valid", dev),
+                _ptr(cu_rows, torch.int64, n_resp + 1, "cu_rows", dev), n_resp,
+                _ptr(logp_train, torch.float32, n_rows, "logp_train", dev), _ptr(lse, torch.float32, n_rows, "lse", dev),
+                _ptr(logp_ref, torch.float32, n_rows, "logp_ref", dev), _ptr(weight, torch.float32, n_resp // 2, "weight", dev)]
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        reward = torch.empty(max(n_resp, 0), dtype=torch.float32, device=dev)
+        self._sync_stream()
+        rc = self._lib.ais_preference_loss_grad(self._h, logits.data_ptr(), dtype, n_rows, vocab, row_stride, *ptrs, C.byref(p),
+                                                _ptr(reward), _ptr(loss), dlogits.data_ptr())
+        if rc != 0:
+            raise AisError(rc, "ais_preference_loss_grad")
+        return loss, reward, dlogits
+
+    # ------------------------------------------------------------------ the rows before the read-out
+    def norm_rows(self, x, weight=None, bias=None, eps: float = 1e-5, centered: bool = True, valid=None):
+        """x [R, D] bf16 or fp32 -> (y [R, D] of x's dtype, mean [R] fp32, rstd [R] fp32): layer norm, or with centered=False
+        root-mean-square norm (mean None).  weight and bias [D], bf16 or fp32 alike, or None.  See ais_norm_rows in include/ais.h."""
+        out = self._native("norm_rows", x, weight, bias, float(eps), 1 if centered else 0, valid)
+        if out is not None:
+            return out
+        dev = self.device
+        n_rows, width, row_stride = _logits_geometry(x, dev, "x")
+        dtype = _dtype_code(x, "x")
+        param_dtype = self._affine(width, weight=weight, bias=bias)
+        valid_ptr = _ptr(valid, torch.uint8, n_rows, "valid", dev)
+        y = torch.empty((n_rows, width), dtype=x.dtype, device=dev)
+        mean = torch.empty(n_rows, dtype=torch.float32, device=dev) if centered else None
+        rstd = torch.empty(n_rows, dtype=torch.float32, device=dev)
+        self._sync_stream()
+        rc = self._lib.ais_norm_rows(self._h, x.data_ptr(), dtype, n_rows, width, row_stride, valid_ptr, _ptr(weight), _ptr(bias),
+                                     param_dtype, float(eps), 1 if centered else 0, _ptr(y), width, _ptr(mean), _ptr(rstd))
+        if rc != 0:
+            raise AisError(rc, "ais_norm_rows")
+        return y, mean, rstd
+
+    def norm_rows_grad(self, dy, x, weight, mean, rstd, valid=None, want_bias: bool = True):
+        """-> (dx [R, D] of x's dtype, dweight [D] fp32 or None without a weight, dbias [D] fp32 or None) from dy [R, D] bf16 or fp32
+        and what norm_rows was given and returned (mean None: root-mean-square norm).  See ais_norm_rows_grad in include/ais.h."""
+        out = self._native("norm_rows_grad", dy, x, weight, mean, rstd, valid, 1 if want_bias else 0)
+        if out is not None:
+            return out
+        dev = self.device
+        n_rows, width, row_stride = _logits_geometry(x, dev, "x")
+        dtype = _dtype_code(x, "x")
+        dy_rows, dy_width, dy_stride = _logits_geometry(dy, dev, "dy")
+        dy_dtype = _dtype_code(dy, "dy")
+        if (dy_rows, dy_width) != (n_rows, width):
+            raise ValueError(f"dy: expected {(n_rows, width)}, got {(dy_rows, dy_width)}")
+        param_dtype = self._affine(width, weight=weight)
+        ptrs = [_ptr(mean, torch.float32, n_rows, "mean", dev), _ptr(rstd, torch.float32, n_rows, "rstd", dev)]
+        valid_ptr = _ptr(valid, torch.uint8, n_rows, "valid", dev)
+        dx = torch.empty((n_rows, width), dtype=x.dtype, device=dev)
+        dweight = torch.empty(width, dtype=torch.float32, device=dev) if weight is not None else None
+        dbias = torch.empty(width, dtype=torch.float32, device=dev) if want_bias else None
+        self._sync_stream()
+        rc = self._lib.ais_norm_rows_grad(self._h, dy.data_ptr(), dy_dtype, dy_stride, x.data_ptr(), dtype, n_rows, width, row_stride,
+                                          valid_ptr, _ptr(weight), param_dtype, *ptrs, _ptr(dx), width, _ptr(dweight), _ptr(dbias))
+        if rc != 0:
+            raise AisError(rc, "ais_norm_rows_grad")
+        return dx, dweight, dbias
+
+    def _affine(self, width, **params):
+        """The type that weight and bias have in common."""
+        code = None
+        for name, t in params.items():
+            if t is None:
+                continue
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name} must be a torch.Tensor")
+            if code is not None and _dtype_code(t, name) != code:
+                raise TypeError("weight and bias must have one dtype")
+            code = _dtype_code(t, name)
+            _ptr(t, None, width, name, self.device)
+        return AIS_F32 if code is None else code
+
+    # ------------------------------------------------------------------ the step of the weights
+    def adamw_step(self, state: AdamWState, grads, lr=1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                   weight_decay: float = 0.01, grad_scale=None):
+        """One AdamW step of state.params, in place, with a gradient (bf16 or fp32, contiguous) for each, or None for those that
+        stay as they are.  lr: a number, or an fp32 tensor of one element on the GPU; grad_scale: such a tensor that the gradients
+        are multiplied by, or None.  See ais_adamw_step in include/ais.h."""
+        r, step = state._rule, state.step
+        on_gpu = isinstance(step, torch.Tensor)
+        lr_dev = lr if isinstance(lr, torch.Tensor) else None
+        r.lr, r.beta1, r.beta2, r.eps, r.weight_decay = 0.0 if lr_dev is not None else lr, beta1, beta2, eps, weight_decay
+        r.step = 0 if on_gpu else step + 1
+        dev = self.device
+        if not on_gpu:
+            out = self._native("adamw_step", C.addressof(state._table), C.addressof(r), state.params, state.copies, state.m, state.v,
+                               state.m_scale, state.v_scale, grads, grad_scale, lr_dev)
+            if out is not None:
+                state.step = step + 1
+                return
+        if state.device != dev:
+            raise ValueError(f"state is on {state.device}, expected {dev}")
+        if len(grads) != len(state.params):
+            raise ValueError(f"grads: expected {len(state.params)}, got {len(grads)}")
+        if on_gpu:
+            _ptr(step, torch.int64, 1, "step", dev)
+        table = (AisAdamWTensor * len(grads)).from_buffer_copy(state._table)
+        for name, t in (("m", state.m), ("v", state.v), ("m_scale", state.m_scale), ("v_scale", state.v_scale)):
+            if t is not None and t.data_ptr() != (getattr(table[0], name) or 0):
+                raise ValueError(f"{name} is not where it was when the state was made")
+        for i, (row, p, copy, g) in enumerate(zip(table, state.params, state.copies, grads)):
+            if p.data_ptr() != (row.param or 0) or p.numel() != row.n or _dtype_code(p, f"params[{i}]") != row.param_dtype:
+                raise ValueError(f"params[{i}] is not where it was when the state was made")
+            if copy is not None and copy.data_ptr() != (row.copy or 0):
+                raise ValueError(f"copies[{i}] is not where it was when the state was made")
+            if g is None:
+                row.n = 0
+                continue
+            if not isinstance(g, torch.Tensor):
+                raise TypeError(f"grads[{i}] must be a torch.Tensor")
+            row.grad_dtype = _dtype_code(g, f"grads[{i}]")
+            row.grad = _ptr(g, None, p.numel(), f"grads[{i}]", dev)
+        scale_ptr, lr_ptr = _ptr(grad_scale, torch.float32, 1, "grad_scale", dev), _ptr(lr_dev, torch.float32, 1, "lr", dev)
+        self._sync_stream()
+        step_ptr = None
+        if on_gpu:
+            step.add_(1)
+            step_ptr = step.data_ptr()
+        rc = self._lib.ais_adamw_step(self._h, table, len(grads), C.byref(r), scale_ptr, step_ptr, lr_ptr)
+        if rc != 0:
+            if on_gpu:
+                step.sub_(1)                                     # nothing was launched
+            raise AisError(rc, "ais_adamw_step")
+        if not on_gpu:
+            state.step = step + 1
+
+    def adamw_values(self, state: AdamWState, dtype=torch.float32):
+        """-> (m, v): what a state's 8-bit moments stand for, flat like state.m and of `dtype` (float32 or bfloat16); fp32 moments
+        of a state of 32 bits are its own buffers."""
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(f"moments must be bfloat16 or float32, not {dtype}")
+        if state.bits == 32:
+            return state.m.to(dtype), state.v.to(dtype)
+        if state.device != self.device:
+            raise ValueError(f"state is on {state.device}, expected {self.device}")
+        out = self._native("adamw_values", state.m, state.m_scale, state.v, state.v_scale, 1 if dtype is torch.bfloat16 else 0)
+        if out is not None:
+            return out
+        out = []
+        for moment, codes, scales in ((1, state.m, state.m_scale), (2, state.v, state.v_scale)):
+            values = torch.empty(codes.numel(), dtype=dtype, device=self.device)
+            self._sync_stream()
+            rc = self._lib.ais_adamw_values(self._h, codes.data_ptr(), scales.data_ptr(), codes.numel(), moment, _ptr(values),
+                                            _dtype_code(values))
+            if rc != 0:
+                raise AisError(rc, "ais_adamw_values")
+            out.append(values)
+        return tuple(out)
 
     # ------------------------------------------------------------------ log-probs without materialised logits
     def lm_head_logprob(self, hidden, weight, token_ids, valid=None, inv_temperature: float = 1.0):

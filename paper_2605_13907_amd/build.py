@@ -13,7 +13,8 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libais_gfx950.so")
 FAST = os.path.join(PKG, "_ais_fast.so")
 SOURCES = ("api.hip", "sweeps.hip", "reductions.hip", "fp8.hip", "fp8_rows.hip", "fp8_table.hip", "fused.hip", "lm_head.hip",
-           "lm_grad_gemm.hip", "mxfp4.hip", "mxfp4_logits.hip", "sample.hip", "distill.hip")
+           "lm_grad_gemm.hip", "mxfp4.hip", "mxfp4_logits.hip", "sample.hip", "distill.hip", "preference.hip", "norm.hip",
+           "adamw.hip")
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -241,6 +241,28 @@ int launch_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long 
                         const int* ids, const float* teacher, int n_top, const unsigned char* valid, const float* weight,
                         float inv_temperature, float* kl_out, float* loss_out, void* dlogits, long long dlogits_stride);
 
+// Where the arrays of the preference loss lie in the workspace, which begins with the tiles' sums (byte offsets).
+struct PreferenceRoom {
+  size_t counts, loss, coeff, g, total;
+};
+PreferenceRoom preference_room(long long n_rows, int n_resp);
+int launch_preference(ais_ctx* ctx, const float* logp, const float* ref, const unsigned char* valid, long long n_rows,
+                      const long long* cu_rows, int n_resp, const float* weight, const ais_preference_params& p,
+                      const PreferenceRoom& room, float scale, float* reward, float* loss_out, float* g);
+int norm_grad_parts(long long n_rows, long long width, int n_cus);
+size_t norm_grad_bytes(long long n_rows, long long width, int sums, int n_cus);
+int launch_norm_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, int width, long long row_stride,
+                     const unsigned char* valid, const void* weight, const void* bias, ais_dtype param_dtype, float eps,
+                     int centered, void* y, long long y_stride, float* mean, float* rstd);
+int launch_norm_rows_grad(ais_ctx* ctx, const void* dy, ais_dtype dy_dtype, long long dy_stride, const void* x, ais_dtype dtype,
+                          long long n_rows, int width, long long row_stride, const unsigned char* valid, const void* weight,
+                          ais_dtype param_dtype, const float* mean, const float* rstd, void* dx, long long dx_stride,
+                          float* dweight, float* dbias);
+int launch_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, int n_tensors, const ais_adamw_params& p,
+                      const float* grad_scale, const long long* step_dev, const float* lr_dev);
+int launch_adamw_values(ais_ctx* ctx, const unsigned char* codes, const unsigned char* scales, long long n, int moment,
+                        void* out, ais_dtype dtype);
+
 int launch_lm_head_grad_setup(ais_ctx* ctx, const unsigned char* live_mask, long long n_rows, int n_cap, int width,
                               int width_last, int* row_index, int* row_pos, void* dev_plan);
 int launch_lm_head_dlogits_chunk(ais_ctx* ctx, const void* hidden, long long ld_h, const void* weight,

@@ -169,6 +169,33 @@ int check_batch(long long n_rows, int n_resp, int group_size) {
   return AIS_OK;
 }
 
+int check_preference(const ais_preference_params* p) {
+  if (p == nullptr) return AIS_ERR_NULL;
+  auto fin = [](float v) { return std::isfinite(v); };
+  if (!fin(p->beta) || p->beta <= 0.f) return AIS_ERR_PARAM;
+  if (p->kind < 0 || p->kind > 2) return AIS_ERR_PARAM;
+  if (!(p->label_smoothing >= 0.f && p->label_smoothing <= (p->kind == 0 ? 0.5f : 0.f))) return AIS_ERR_PARAM;
+  if (!fin(p->margin)) return AIS_ERR_PARAM;
+  if (p->mean_logp != 0 && p->mean_logp != 1) return AIS_ERR_PARAM;
+  if (!fin(p->inv_temperature) || p->inv_temperature <= 0.f) return AIS_ERR_PARAM;
+  return AIS_OK;
+}
+
+bool aligned_to(const void* p, ais_dtype dtype) { return reinterpret_cast<uintptr_t>(p) % (dtype == AIS_BF16 ? 2 : 4) == 0; }
+
+int check_adamw_tensor(const ais_adamw_tensor& t, int bits) {
+  if (t.n < 0 || t.n >= (1LL << 32) - 4096) return AIS_ERR_SIZE;
+  if ((t.param_dtype != AIS_BF16 && t.param_dtype != AIS_F32) || (t.grad_dtype != AIS_BF16 && t.grad_dtype != AIS_F32))
+    return AIS_ERR_DTYPE;
+  if (t.n == 0) return AIS_OK;
+  if (t.param == nullptr || t.grad == nullptr || t.m == nullptr || t.v == nullptr) return AIS_ERR_NULL;
+  if (bits == 8 && (t.m_scale == nullptr || t.v_scale == nullptr)) return AIS_ERR_NULL;
+  if (!aligned_to(t.param, (ais_dtype)t.param_dtype) || !aligned_to(t.grad, (ais_dtype)t.grad_dtype) || !aligned_to(t.copy, AIS_BF16) ||
+      reinterpret_cast<uintptr_t>(t.m) % 16 != 0 || reinterpret_cast<uintptr_t>(t.v) % 16 != 0)
+    return AIS_ERR_ALIGN;
+  return AIS_OK;
+}
+
 // Address of the current device's copy of the static scratch array; looked up once per device.  The caller has
 // made `device` current.
 std::mutex g_scratch_mutex;
@@ -735,6 +762,150 @@ int ais_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long lon
   DeviceGuard guard(ctx->device);
   return launch_distill_topk(ctx, logits, dtype, n_rows, (int)vocab, row_stride, teacher_ids, teacher_logits, n_top, valid,
                              weight, inv_temperature, kl_out, loss_out, dlogits, dlogits_stride);
+}
+
+void ais_preference_params_default(ais_preference_params* p) {
+  if (p == nullptr) return;
+  p->beta = 0.1f;
+  p->kind = 0;
+  p->label_smoothing = 0.0f;
+  p->margin = 0.0f;
+  p->mean_logp = 0;
+  p->inv_temperature = 1.0f;
+}
+
+int ais_preference_row_scale(ais_ctx* ctx, const float* logp_train, const float* logp_ref, const unsigned char* valid,
+                             long long n_rows, const long long* cu_rows, int n_resp, const float* weight,
+                             const ais_preference_params* params, float* reward_out, float* loss_out, float* g_out) {
+  int rc = check_batch(n_rows, n_resp, 2);
+  if (rc != AIS_OK) return rc;
+  rc = check_preference(params);
+  if (rc != AIS_OK) return rc;
+  if (cu_rows == nullptr || reward_out == nullptr || loss_out == nullptr) return AIS_ERR_NULL;
+  if (n_rows > 0 && (logp_train == nullptr || g_out == nullptr)) return AIS_ERR_NULL;
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  const PreferenceRoom room = preference_room(n_rows, n_resp);
+  rc = ensure_workspace(ctx, room.total);
+  if (rc != AIS_OK) return rc;
+  ctx->plan.valid = false;             // the sums overwrite whatever tiling the workspace held
+  return launch_preference(ctx, logp_train, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room,
+                           params->inv_temperature, reward_out, loss_out, g_out);
+}
+
+int ais_preference_loss_grad(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
+                             long long row_stride, const int* token_ids, const unsigned char* valid,
+                             const long long* cu_rows, int n_resp, const float* logp_train, const float* lse,
+                             const float* logp_ref, const float* weight, const ais_preference_params* params,
+                             float* reward_out, float* loss_out, void* dlogits) {
+  int rc = check_logits(logits, dtype, n_rows, vocab, row_stride);
+  if (rc != AIS_OK) return rc;
+  rc = check_batch(n_rows, n_resp, 2);
+  if (rc != AIS_OK) return rc;
+  rc = check_preference(params);
+  if (rc != AIS_OK) return rc;
+  if (cu_rows == nullptr || reward_out == nullptr || loss_out == nullptr) return AIS_ERR_NULL;
+  if (n_rows > 0 && (token_ids == nullptr || logp_train == nullptr || lse == nullptr || dlogits == nullptr)) return AIS_ERR_NULL;
+  if (!aligned_to(dlogits, dtype)) return AIS_ERR_ALIGN;
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  const PreferenceRoom room = preference_room(n_rows, n_resp);
+  rc = ensure_workspace(ctx, room.total);
+  if (rc != AIS_OK) return rc;
+  ctx->plan.valid = false;             // the sums overwrite whatever tiling the workspace held
+  float* g = reinterpret_cast<float*>(static_cast<char*>(ctx->ws) + room.g);
+  rc = launch_preference(ctx, logp_train, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room, 1.0f, reward_out,
+                         loss_out, g);
+  if (rc != AIS_OK) return rc;
+  return launch_dlogits(ctx, logits, dtype, n_rows, (int)vocab, row_stride, token_ids, g, nullptr, lse, logp_train,
+                        params->inv_temperature, dlogits);
+}
+
+int ais_norm_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, long long width, long long row_stride,
+                  const unsigned char* valid, const void* weight, const void* bias, ais_dtype param_dtype, float eps,
+                  int centered, void* y, long long y_stride, float* mean_out, float* rstd_out) {
+  int rc = check_logits(x, dtype, n_rows, width, row_stride);
+  if (rc != AIS_OK) return rc;
+  if (param_dtype != AIS_BF16 && param_dtype != AIS_F32) return AIS_ERR_DTYPE;
+  if (y_stride < width) return AIS_ERR_STRIDE;
+  if (centered != 0 && centered != 1) return AIS_ERR_PARAM;
+  if (!std::isfinite(eps) || eps <= 0.f) return AIS_ERR_PARAM;
+  if (n_rows > 0 && (y == nullptr || rstd_out == nullptr || (centered && mean_out == nullptr))) return AIS_ERR_NULL;
+  if (!aligned_to(y, dtype) || !aligned_to(weight, param_dtype) || !aligned_to(bias, param_dtype)) return AIS_ERR_ALIGN;
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  return launch_norm_rows(ctx, x, dtype, n_rows, (int)width, row_stride, valid, weight, bias, param_dtype, eps, centered, y, y_stride,
+                          mean_out, rstd_out);
+}
+
+int ais_norm_rows_grad(ais_ctx* ctx, const void* dy, ais_dtype dy_dtype, long long dy_stride, const void* x, ais_dtype dtype,
+                       long long n_rows, long long width, long long row_stride, const unsigned char* valid,
+                       const void* weight, ais_dtype param_dtype, const float* mean, const float* rstd, void* dx,
+                       long long dx_stride, float* dweight_out, float* dbias_out) {
+  int rc = check_logits(x, dtype, n_rows, width, row_stride);
+  if (rc != AIS_OK) return rc;
+  rc = check_logits(dy, dy_dtype, n_rows, width, dy_stride);
+  if (rc != AIS_OK) return rc;
+  if (param_dtype != AIS_BF16 && param_dtype != AIS_F32) return AIS_ERR_DTYPE;
+  if (dx_stride < width) return AIS_ERR_STRIDE;
+  if (n_rows > 0 && (rstd == nullptr || dx == nullptr)) return AIS_ERR_NULL;
+  if (!aligned_to(dx, dtype) || !aligned_to(weight, param_dtype)) return AIS_ERR_ALIGN;
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  if (n_rows == 0) {                   // no rows: the sums are zero
+    for (float* out : {dweight_out, dbias_out})
+      if (out != nullptr)
+        zero_fill_kernel<<<(unsigned)std::min<size_t>(((size_t)width + 255) / 256, (size_t)ctx->n_cus * 8), 256, 0, ctx->stream>>>(
+            out, (size_t)width);
+    return hip_fail(ctx, hipGetLastError());
+  }
+  rc = ensure_workspace(ctx, norm_grad_bytes(n_rows, width, (dweight_out != nullptr) + (dbias_out != nullptr), ctx->n_cus));
+  if (rc != AIS_OK) return rc;
+  ctx->plan.valid = false;             // the partial sums overwrite whatever tiling the workspace held
+  return launch_norm_rows_grad(ctx, dy, dy_dtype, dy_stride, x, dtype, n_rows, (int)width, row_stride, valid, weight, param_dtype,
+                               mean, rstd, dx, dx_stride, dweight_out, dbias_out);
+}
+
+void ais_adamw_params_default(ais_adamw_params* p) {
+  if (p == nullptr) return;
+  p->lr = 1e-3;
+  p->beta1 = 0.9;
+  p->beta2 = 0.999;
+  p->eps = 1e-8;
+  p->weight_decay = 0.01;
+  p->state_bits = 32;
+  p->seed = 0;
+  p->step = 1;
+}
+
+int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, int n_tensors, const ais_adamw_params* p,
+                   const float* grad_scale, const long long* step_dev, const float* lr_dev) {
+  if (p == nullptr || (n_tensors > 0 && tensors == nullptr)) return AIS_ERR_NULL;
+  if (n_tensors < 0) return AIS_ERR_SIZE;
+  auto least = [](double v, double lo) { return std::isfinite(v) && v >= lo; };
+  if (!least(p->lr, 0.0) || !least(p->eps, 1e-30) || !least(p->weight_decay, 0.0)) return AIS_ERR_PARAM;
+  if (!least(p->beta1, 0.0) || p->beta1 >= 1.0 || !least(p->beta2, 0.0) || p->beta2 >= 1.0) return AIS_ERR_PARAM;
+  if (p->state_bits != 32 && p->state_bits != 8) return AIS_ERR_PARAM;
+  if (p->step < 1 && step_dev == nullptr) return AIS_ERR_PARAM;
+  for (int i = 0; i < n_tensors; ++i) {
+    const int rc = check_adamw_tensor(tensors[i], p->state_bits);
+    if (rc != AIS_OK) return rc;
+  }
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  return launch_adamw_step(ctx, tensors, n_tensors, *p, grad_scale, step_dev, lr_dev);
+}
+
+int ais_adamw_values(ais_ctx* ctx, const unsigned char* codes, const unsigned char* scales, long long n, int moment,
+                     void* values_out, ais_dtype dtype) {
+  if (dtype != AIS_BF16 && dtype != AIS_F32) return AIS_ERR_DTYPE;
+  if (n < 0 || n > 1LL << 40) return AIS_ERR_SIZE;
+  if (moment != 1 && moment != 2) return AIS_ERR_PARAM;
+  if (n > 0 && (codes == nullptr || scales == nullptr || values_out == nullptr)) return AIS_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(codes) % 16 != 0 || !aligned_to(values_out, dtype)) return AIS_ERR_ALIGN;
+  if (ctx == nullptr) return AIS_ERR_NULL;
+  DeviceGuard guard(ctx->device);
+  return launch_adamw_values(ctx, codes, scales, n, moment, values_out, dtype);
 }
 
 int ais_profile(ais_ctx* ctx, int enable) {

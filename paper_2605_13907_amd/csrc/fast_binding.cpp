@@ -12,6 +12,7 @@
 #include <ATen/ATen.h>
 
 #include <algorithm>
+#include <vector>
 
 #include "ais.h"
 
@@ -34,6 +35,12 @@ struct Library {
   decltype(&ais_mxfp4_logits) mxfp4_logits;
   decltype(&ais_sample_tokens) sample_tokens;
   decltype(&ais_distill_topk) distill_topk;
+  decltype(&ais_preference_row_scale) preference_row_scale;
+  decltype(&ais_preference_loss_grad) preference_loss_grad;
+  decltype(&ais_norm_rows) norm_rows;
+  decltype(&ais_norm_rows_grad) norm_rows_grad;
+  decltype(&ais_adamw_step) adamw_step;
+  decltype(&ais_adamw_values) adamw_values;
 } lib;
 
 // Reads positional arguments; `ok` turns false at the first one that is not what the call takes.
@@ -526,6 +533,203 @@ AIS_CALL(distill_topk) {
   return rc != 0 ? PyLong_FromLong(rc) : result(loss, kl, dz);
 }
 
+// The arguments that the preference loss's two calls share, in their order.
+struct PreferenceArgs {
+  const float *lt, *ref, *weight;
+  const unsigned char* valid;
+  const long long* cu;
+  const ais_preference_params* p;
+  long long resp = 0;
+  PreferenceArgs(Call& c, long long rows) {
+    lt = c.array<float>(at::kFloat, rows);
+    ref = c.array<float>(at::kFloat, rows, true);
+    valid = c.array<unsigned char>(at::kByte, rows, true);
+    const at::Tensor* offsets = c.tensor();
+    if (!c.ok) return;
+    resp = offsets->numel() - 1;
+    if (resp < 0 || resp > 0x7fffffff) c.ok = false;
+    --c.at;
+    cu = reinterpret_cast<const long long*>(c.array<int64_t>(at::kLong, resp + 1));
+    weight = c.array<float>(at::kFloat, resp / 2, true);
+    p = static_cast<const ais_preference_params*>(c.pointer());
+    if (p == nullptr) c.ok = false;
+  }
+};
+
+AIS_CALL(preference_row_scale) {
+  const at::Tensor* train = c.tensor();
+  if (!c.ok) AIS_REFUSE;
+  const long long rows = train->numel();
+  --c.at;
+  const PreferenceArgs l(c, rows);
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const at::Tensor loss = empty(c.device, {1}), reward = empty(c.device, {l.resp}), g = empty(c.device, {rows});
+  float *lp = loss.data_ptr<float>(), *rp = reward.data_ptr<float>(), *gp = g.data_ptr<float>();
+  const int rc = c.run([&] {
+    return lib.preference_row_scale(c.ctx, l.lt, l.ref, l.valid, rows, l.cu, (int)l.resp, l.weight, l.p, rp, lp, gp);
+  });
+  return rc != 0 ? PyLong_FromLong(rc) : result(loss, reward, g);
+}
+
+AIS_CALL(preference_loss_grad) {
+  const Matrix z(c);
+  if (!c.ok) AIS_REFUSE;
+  const int* ids = c.array<int>(at::kInt, z.rows);
+  const float* lse = c.array<float>(at::kFloat, z.rows);
+  if (!c.ok) AIS_REFUSE;
+  const PreferenceArgs l(c, z.rows);
+  if (!c.ok) AIS_REFUSE;
+  const at::Tensor dz = z.like(c);
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const at::Tensor loss = empty(c.device, {1}), reward = empty(c.device, {l.resp});
+  float *lp = loss.data_ptr<float>(), *rp = reward.data_ptr<float>();
+  void* dp = dz.data_ptr();
+  const int rc = c.run([&] {
+    return lib.preference_loss_grad(c.ctx, z.data(), z.dtype, z.rows, z.width, z.stride, ids, l.valid, l.cu, (int)l.resp, l.lt, lse,
+                                    l.ref, l.weight, l.p, rp, lp, dp);
+  });
+  return rc != 0 ? PyLong_FromLong(rc) : result(loss, reward, dz);
+}
+
+// A weight or bias of `width` elements, bf16 or fp32 (the same type as the one before it), or None.
+const void* affine(Call& c, long long width, int* dtype) {
+  if (c.at < c.n && c.a[c.at] == Py_None) {
+    ++c.at;
+    return nullptr;
+  }
+  const at::Tensor* t = c.tensor();
+  if (t == nullptr) return nullptr;
+  const int code = t->scalar_type() == at::kBFloat16 ? AIS_BF16 : t->scalar_type() == at::kFloat ? AIS_F32 : -1;
+  if (code < 0 || (*dtype >= 0 && *dtype != code) || !t->is_contiguous() || t->numel() != width) return c.ok = false, nullptr;
+  *dtype = code;
+  return t->data_ptr();
+}
+
+// x, weight, bias, eps, 1 for layer norm, valid
+AIS_CALL(norm_rows) {
+  const Matrix x(c);
+  if (!c.ok) AIS_REFUSE;
+  int type = -1;
+  const void *w = affine(c, x.width, &type), *b = affine(c, x.width, &type);
+  const float eps = (float)c.real();
+  const int centered = (int)c.integer();
+  const unsigned char* valid = c.array<unsigned char>(at::kByte, x.rows, true);
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const at::Tensor y = empty(c.device, {x.rows, x.width}, x.t->scalar_type()),
+                   mean = centered ? empty(c.device, {x.rows}) : at::Tensor(), rstd = empty(c.device, {x.rows});
+  void* yp = y.data_ptr();
+  float *mp = centered ? mean.data_ptr<float>() : nullptr, *rp = rstd.data_ptr<float>();
+  const int rc = c.run([&] {
+    return lib.norm_rows(c.ctx, x.data(), x.dtype, x.rows, x.width, x.stride, valid, w, b, type < 0 ? AIS_F32 : (ais_dtype)type, eps,
+                         centered, yp, x.width, mp, rp);
+  });
+  return rc != 0 ? PyLong_FromLong(rc) : result(y, mean, rstd);
+}
+
+// dy, x, weight, mean, rstd, valid, 1 for the bias's gradient
+AIS_CALL(norm_rows_grad) {
+  const Matrix dy(c);
+  if (!c.ok) AIS_REFUSE;
+  const Matrix x(c);
+  if (!c.ok || dy.rows != x.rows || dy.width != x.width) AIS_REFUSE;
+  int type = -1;
+  const void* w = affine(c, x.width, &type);
+  const float* mean = c.array<float>(at::kFloat, x.rows, true);
+  const float* rstd = c.array<float>(at::kFloat, x.rows);
+  const unsigned char* valid = c.array<unsigned char>(at::kByte, x.rows, true);
+  const bool want_bias = c.integer() != 0;
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  // by the type that was found: an empty weight has no address
+  const at::Tensor dx = empty(c.device, {x.rows, x.width}, x.t->scalar_type()),
+                   dw = type >= 0 ? empty(c.device, {x.width}) : at::Tensor(), db = want_bias ? empty(c.device, {x.width}) : at::Tensor();
+  void* xp = dx.data_ptr();
+  float *wp = type >= 0 ? dw.data_ptr<float>() : nullptr, *bp = want_bias ? db.data_ptr<float>() : nullptr;
+  const int rc = c.run([&] {
+    return lib.norm_rows_grad(c.ctx, dy.data(), dy.dtype, dy.stride, x.data(), x.dtype, x.rows, x.width, x.stride, valid, w,
+                              type < 0 ? AIS_F32 : (ais_dtype)type, mean, rstd, xp, x.width, wp, bp);
+  });
+  return rc != 0 ? PyLong_FromLong(rc) : result(dx, dw, db);
+}
+
+// The state's table and rule, parameters, copies and moments, which have to be where the table says; gradients, grad_scale, lr.
+AIS_CALL(adamw_step) {
+  const ais_adamw_tensor* table = static_cast<const ais_adamw_tensor*>(c.pointer());
+  const ais_adamw_params* rule = static_cast<const ais_adamw_params*>(c.pointer());
+  PyObject *params = c.next(), *copies = c.next();
+  if (!c.ok || table == nullptr || rule == nullptr || !PyTuple_CheckExact(params) || !PyTuple_CheckExact(copies) ||
+      PyTuple_GET_SIZE(params) != PyTuple_GET_SIZE(copies) || PyTuple_GET_SIZE(params) == 0)
+    AIS_REFUSE;
+  for (const void* at : {(const void*)table[0].m, (const void*)table[0].v, (const void*)table[0].m_scale, (const void*)table[0].v_scale}) {
+    if (c.at < c.n && c.a[c.at] == Py_None && at == nullptr) {
+      ++c.at;
+      continue;
+    }
+    const at::Tensor* t = c.tensor();
+    if (!c.ok || t->data_ptr() != at) AIS_REFUSE;
+  }
+  PyObject* grads = c.next();
+  if (!c.ok || !(PyList_CheckExact(grads) || PyTuple_CheckExact(grads)) || Py_SIZE(grads) != PyTuple_GET_SIZE(params)) AIS_REFUSE;
+  const float* scale = c.array<float>(at::kFloat, 1, true);
+  const float* lr = c.array<float>(at::kFloat, 1, true);
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const Py_ssize_t n = PyTuple_GET_SIZE(params);
+  std::vector<ais_adamw_tensor> t(table, table + n);
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    PyObject* some[3] = {PyTuple_GET_ITEM(params, i), PySequence_Fast_GET_ITEM(grads, i), PyTuple_GET_ITEM(copies, i)};
+    const bool skipped = some[1] == Py_None;
+    if (some[2] != Py_None) {
+      Args other{some + 2, 1};
+      other.device = c.device;
+      const at::Tensor* copy = other.tensor();
+      if (!other.ok || copy->data_ptr() != t[i].copy) AIS_REFUSE;
+    }
+    Args one{some, 2};
+    one.device = c.device;
+    const at::Tensor* p = one.tensor();
+    if (!one.ok || p->data_ptr() != t[i].param || p->numel() != t[i].n ||
+        p->scalar_type() != (t[i].param_dtype == AIS_BF16 ? at::kBFloat16 : at::kFloat))
+      AIS_REFUSE;
+    if (skipped) {
+      t[i].n = 0;
+      continue;
+    }
+    const at::Tensor* g = one.tensor();
+    if (!one.ok || (g->scalar_type() != at::kBFloat16 && g->scalar_type() != at::kFloat) || !g->is_contiguous() ||
+        g->numel() != t[i].n)
+      AIS_REFUSE;
+    t[i].grad = g->data_ptr();
+    t[i].grad_dtype = g->scalar_type() == at::kBFloat16 ? AIS_BF16 : AIS_F32;
+  }
+  const int rc = c.run([&] { return lib.adamw_step(c.ctx, t.data(), (int)n, rule, scale, nullptr, lr); });
+  if (rc != 0) return PyLong_FromLong(rc);
+  Py_RETURN_TRUE;
+}
+
+// codes and scales of both moments, 1 for bf16 values or 0 for fp32
+AIS_CALL(adamw_values) {
+  const unsigned char *codes[2], *scales[2];
+  long long n = 0;
+  for (int k = 0; k < 2; ++k) {
+    const at::Tensor* t = c.tensor();
+    if (!c.ok) AIS_REFUSE;
+    n = t->numel();
+    --c.at;
+    codes[k] = c.array<unsigned char>(at::kByte, n);
+    scales[k] = c.array<unsigned char>(at::kByte, n / 32);
+  }
+  const bool bf16 = c.integer() != 0;
+  if (!c.ok || c.at != c.n) AIS_REFUSE;
+  const at::Tensor m = empty(c.device, {n}, bf16 ? at::kBFloat16 : at::kFloat), v = at::empty_like(m);
+  void* out[2] = {m.data_ptr(), v.data_ptr()};
+  const int rc = c.run([&] {
+    int bad = 0;
+    for (int k = 0; k < 2 && bad == 0; ++k)
+      bad = lib.adamw_values(c.ctx, codes[k], scales[k], n, k + 1, out[k], bf16 ? AIS_BF16 : AIS_F32);
+    return bad;
+  });
+  return rc != 0 ? PyLong_FromLong(rc) : result(m, v);
+}
+
 // init(addresses): the entry points, in the order of Library.
 PyObject* init(PyObject*, PyObject* const* args, Py_ssize_t n) {
   constexpr Py_ssize_t kEntries = sizeof(Library) / sizeof(void*);
@@ -562,6 +766,12 @@ PyMethodDef methods[] = {AIS_METHOD(init),
                          AIS_METHOD(mxfp4_logits),
                          AIS_METHOD(sample_tokens),
                          AIS_METHOD(distill_topk),
+                         AIS_METHOD(preference_row_scale),
+                         AIS_METHOD(preference_loss_grad),
+                         AIS_METHOD(norm_rows),
+                         AIS_METHOD(norm_rows_grad),
+                         AIS_METHOD(adamw_step),
+                         AIS_METHOD(adamw_values),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ais_fast", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,181 @@
+"""The preference loss on the GPU against its 64-bit form: tiles that responses begin and end in, empty responses, masks, every form,
+rows that must not be read, faulty offsets, and the gradient through logits.
+
+Tolerances.  Sums and pairs are formed in fp64 from the same fp32 numbers; a reward and a loss are rounded once (2^-24) and a
+coefficient up to three times (itself, times the temperature, and that product's operand), each allowed twice over for the fp64
+sums' own order: 2^-23 and 2^-22.  Sums that cancel add their terms' absolute sum times 2^-50."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.training_oracle as O
+from paper_2605_13907_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TILE = 2048
+FORMS = [dict(), dict(label_smoothing=0.2, margin=0.1), dict(kind=1, margin=0.3, beta=0.5), dict(kind=2, beta=0.5),
+         dict(kind=2, mean_logp=1, beta=0.7, margin=0.1), dict(mean_logp=1, beta=2.0, inv_temperature=0.8)]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.AisContext()
+    yield c
+    c.close()
+
+
+def cuda(a, dtype=None):
+    return None if a is None else torch.tensor(a, dtype=dtype, device="cuda")
+
+
+def compare(ctx, logp, ref, valid, cu, weight, **form):
+    p = B.default_preference_params(**form)
+    loss, reward, g = ctx.preference_row_scale(cuda(logp), cuda(ref), cuda(valid), cuda(cu, torch.int64), p, weight=cuda(weight))
+    exact = dict(form)
+    for k in ("beta", "label_smoothing", "margin", "inv_temperature"):
+        exact[k] = float(getattr(p, k))                          # as the fp32 fields hold them
+    want, want_reward, want_g = O.preference(logp, ref, valid, cu, weight, **exact)
+    live = np.ones(len(logp), bool) if valid is None else valid != 0
+    size = np.abs(np.where(live, logp, 0.0)).sum() + (0 if ref is None else np.abs(np.where(live, ref, 0.0)).sum())
+    beta = exact.get("beta", 0.1)
+    noise = beta * size * 2.0 ** -50
+    reward, g = reward.cpu().numpy(), g.cpu().numpy()
+    assert np.abs(reward - want_reward).max(initial=0.0) <= np.abs(want_reward).max(initial=0.0) * 2.0 ** -23 + noise
+    assert np.allclose(reward, want_reward, rtol=2.0 ** -23, atol=noise)
+    assert np.allclose(g, want_g, rtol=2.0 ** -22, atol=beta * 40 * noise)
+    assert (g[~live] == 0).all()
+    assert loss.item() == pytest.approx(want, rel=2.0 ** -22, abs=40 * noise + 1e-300)
+    assert ctx.status() == 0
+
+
+def batch(lengths, seed=0, live=0.8, with_ref=True):
+    r = np.random.default_rng(seed)
+    cu = np.concatenate(([0], np.cumsum(lengths))).astype(np.int64)
+    n = int(cu[-1])
+    logp = (-r.exponential(size=n)).astype(np.float32)
+    ref = (logp + 0.2 * r.standard_normal(n)).astype(np.float32) if with_ref else None
+    valid = None if live >= 1 else (r.random(n) < live).astype(np.uint8)
+    return logp, ref, valid, cu, r.random(len(lengths) // 2).astype(np.float32)
+
+
+LENGTHS = {
+    "one row": [1, 0], "two rows": [1, 1], "nothing": [0, 0], "empty ones between": [0, 3, 0, 0, 5, 0, 0, 0, 7, 2],
+    "a tile": [TILE, 0], "a tile and one": [TILE, 1], "borders": [TILE - 1, 1, 1, TILE - 1, TILE, TILE],
+    "inside tiles": [700, 900, 1_100, 3_000, 5, 6_001], "long": [50_001, 3], "many short": [1, 2, 0, 3] * 1_500,
+    "mixed": [9_000, 1, 1, 1, 0, 4_096, 2, 2], "ragged": [int(v) for v in np.random.default_rng(5).integers(0, 400, 600)],
+}
+
+
+@pytest.mark.parametrize("name", LENGTHS)
+def test_lengths(ctx, name):
+    lengths = LENGTHS[name]
+    compare(ctx, *batch(lengths), **FORMS[0])
+    compare(ctx, *batch(lengths, seed=1, live=1.0, with_ref=False), **FORMS[4])
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_forms(ctx, form):
+    logp, ref, valid, cu, weight = batch([300, 200, 1, 900, 0, 12, 2_500, 2_100], seed=2)
+    compare(ctx, logp, ref, valid, cu, weight, **form)
+    compare(ctx, logp, ref, None, cu, None, **form)
+
+
+def test_a_response_without_a_valid_token(ctx):
+    logp, ref, _, cu, weight = batch([10, 20, 30, 40], live=1.0)
+    valid = np.ones(100, np.uint8)
+    valid[10:30] = 0
+    for form in FORMS:
+        compare(ctx, logp, ref, valid, cu, weight, **form)
+    compare(ctx, logp, ref, np.zeros(100, np.uint8), cu, weight)
+
+
+def test_masked_rows_are_not_looked_at(ctx):
+    logp, ref, valid, cu, weight = batch([40, 60, 30, 70], seed=3, live=0.5)
+    p = B.default_preference_params()
+    run = lambda a, b: ctx.preference_row_scale(cuda(a), cuda(b), cuda(valid), cuda(cu), p, weight=cuda(weight))
+    want = run(logp, ref)
+    a, b = logp.copy(), ref.copy()
+    a[valid == 0], b[valid == 0] = np.nan, np.inf
+    for x, y in zip(want, run(a, b)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("value", [np.nan, -np.inf])
+def test_what_is_not_finite_stays_in_its_pair(ctx, value):
+    logp, ref, _, cu, weight = batch([1_500, 900, 700, 300, 2_000, 100], live=1.0)
+    run = lambda a: ctx.preference_row_scale(cuda(a), cuda(ref), None, cuda(cu), B.default_preference_params(), weight=cuda(weight))
+    _, reward, g = run(logp)
+    bad = logp.copy()
+    bad[2_600] = value                                           # the third response
+    loss, bad_reward, bad_g = run(bad)
+    keep = [0, 1, 4, 5]
+    assert torch.equal(bad_reward[keep], reward[keep])
+    rows = np.r_[0:2_400, 3_400:5_500]
+    assert torch.equal(bad_g[rows], g[rows])
+    assert not torch.isfinite(bad_reward[2]) and not torch.isfinite(loss)
+    assert bool(torch.isnan(bad_g[2_400:3_400]).all()) == bool(np.isnan(value))
+
+
+@pytest.mark.parametrize("h", [-2_000.0, -40.0, -1e-3, 0.0, 1e-3, 40.0, 700.0])
+def test_far_margins(ctx, h):
+    logp = np.array([h, 0.0], np.float32)
+    for form in (dict(beta=1.0), dict(beta=1.0, label_smoothing=0.25), dict(beta=1.0, kind=1), dict(beta=1.0, kind=2)):
+        compare(ctx, logp, None, None, np.array([0, 1, 2]), None, **form)
+
+
+@pytest.mark.parametrize("cu", [[1, 4, 8, 9, 10], [0, 4, 3, 9, 10], [0, 4, 8, 9, 9], [0, 4, 8, 30, 10], [-5, 4, 8, 9, 10],
+                                [0, 2 ** 40, 8, 9, 10]])
+def test_faulty_offsets_are_reported(ctx, cu):
+    logp = cuda(np.full(10, -1.0, np.float32))
+    _, _, g = ctx.preference_row_scale(logp, None, None, cuda(cu, torch.int64))
+    assert g.shape == (10,)
+    assert ctx.status() == B.STATUS_BAD_CU and ctx.status() == 0
+
+
+def test_no_rows(ctx):
+    none = torch.empty(0, device="cuda")
+    loss, reward, g = ctx.preference_row_scale(none, None, None, cuda([0, 0, 0], torch.int64), B.default_preference_params(margin=1.0))
+    assert loss.item() == pytest.approx(np.log1p(np.exp(1.0)), rel=2.0 ** -22) and reward.tolist() == [0.0, 0.0] and g.numel() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab,pitch", [(1, 1), (70, 70), (1_000, 1_003), (4_096, 4_096), (33_001, 33_001)])
+def test_through_logits(ctx, dtype, vocab, pitch):
+    """dlogits are the coefficients times softmax less the token's one: a rounding to the type (half a step), and in fp32 the
+    exponential (2^-22 and the shift's 2^-24 times the logit's size, at most 2^-19)."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    logp0, _, valid, cu, weight = batch([5, 11, 0, 40, 17, 3], seed=4)
+    rows = len(logp0)
+    z = (3 * torch.randn(rows, pitch, generator=gen, device="cuda")).to(dtype)[:, :vocab]
+    ids = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    valid, cu, weight = cuda(valid), cuda(cu), cuda(weight)
+    p = B.default_preference_params(beta=0.3, inv_temperature=0.9)
+    logp, lse = ctx.token_logprob(z, ids, valid, 0.9)
+    ref = logp + 0.1 * torch.randn(rows, generator=gen, device="cuda")
+    loss, reward, dz = ctx.preference_loss_grad(z, ids, valid, cu, logp, lse, ref, p, weight=weight)
+    want_loss, want_reward, g = ctx.preference_row_scale(logp, ref, valid, cu, p, weight=weight)
+    assert torch.equal(loss, want_loss) and torch.equal(reward, want_reward)
+    temperature = float(np.float32(0.9))
+    soft = torch.softmax(z.double() * temperature, dim=1)
+    soft[torch.arange(rows), ids.long()] -= 1.0
+    want = g.double()[:, None] * soft
+    tol = want.abs() * (2.0 ** -9 * 1.01 if dtype == torch.bfloat16 else 0.0) * 2 + want.abs() * 2.0 ** -19 + g.double().abs()[:, None] * 2.0 ** -22
+    assert ((dz.double() - want).abs() <= tol).all()
+    kept = z.clone()
+    inplace = ctx.preference_loss_grad(z, ids, valid, cu, logp, lse, ref, p, weight=weight, dlogits=z)[2]
+    assert inplace.data_ptr() == z.data_ptr() and torch.equal(inplace, dz)
+    _, _, one = ctx.preference_loss_grad(kept, ids, valid, cu, logp, lse, ref, p, weight=weight)
+    assert torch.equal(one, dz)
+
+
+def test_more_rows_than_a_launch_of_tiles_fills(ctx):
+    compare(ctx, *batch([int(v) for v in np.random.default_rng(9).integers(0, 3_000, 400)], seed=9))
+
+
+def test_runs_alike(ctx):
+    logp, ref, valid, cu, weight = (cuda(a) for a in batch([5_000, 7_000, 3, 9_000], seed=6))
+    first = ctx.preference_row_scale(logp, ref, valid, cu, weight=weight)
+    for _ in range(5):
+        for a, b in zip(first, ctx.preference_row_scale(logp, ref, valid, cu, weight=weight)):
+            assert torch.equal(a, b)
