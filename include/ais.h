@@ -477,9 +477,12 @@ void ais_preference_params_default(ais_preference_params* p);
  * ais_preference_row_scale writes
  *   g_out       [n_rows] fp32: c_t times inv_temperature, 0 where valid == 0: the `coeff` of ais_lm_head_grad, and the
  *               scale of what ais_token_logprob_softmax_grad writes
- * ais_preference_loss_grad writes, from logits, token_ids and lse (output of ais_token_logprob) as ais_grpo_loss_grad takes them,
- *   dlogits     [n_rows, row_stride] of `dtype`: c_t inv_temperature (softmax(inv_temperature z_t) - 1[v = y_t]); 0 in rows
- *               with c_t = 0, which are not read.  May be `logits` itself.
+ * ais_preference_loss_grad forms the log-probs itself, from logits and token_ids as ais_token_logprob takes them.  A response's
+ * log-ratios nearly cancel, so a row's sum is kept in 64 bits there, and its log-prob until it has been added up; it writes
+ *   logp_out    [n_rows] fp32: the log-probs, 0 where valid == 0
+ *   dlogits     [n_rows, row_stride] of `dtype`, or NULL (loss alone): c_t inv_temperature (softmax(inv_temperature z_t) - 1[v =
+ *               y_t]); 0 in rows with c_t = 0, which are not read again.  May be `logits` itself.
+ * It keeps 16 bytes a row in the context's workspace beside the sums.
  * A response whose sum is not finite makes its pair's loss, rewards and coefficients what the formulas give; other pairs are
  * not touched by it.  Rows outside every response (a faulty cu_rows) get 0 and set AIS_STATUS_BAD_CU.
  * Errors: as ais_grpo_row_scale and ais_grpo_loss_grad, with n_resp odd AIS_ERR_GROUP; NULL reward_out or loss_out; beta <= 0,
@@ -490,9 +493,9 @@ int ais_preference_row_scale(ais_ctx* ctx, const float* logp_train, const float*
                              const ais_preference_params* params, float* reward_out, float* loss_out, float* g_out);
 int ais_preference_loss_grad(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
                              long long row_stride, const int* token_ids, const unsigned char* valid,
-                             const long long* cu_rows, int n_resp, const float* logp_train, const float* lse,
-                             const float* logp_ref, const float* weight, const ais_preference_params* params,
-                             float* reward_out, float* loss_out, void* dlogits);
+                             const long long* cu_rows, int n_resp, const float* logp_ref, const float* weight,
+                             const ais_preference_params* params, float* reward_out, float* loss_out, float* logp_out,
+                             void* dlogits);
 
 /* ---- the rows before the read-out ------------------------------------------------------------------------ */
 

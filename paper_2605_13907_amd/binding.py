@@ -114,8 +114,7 @@ SYMBOLS = {
     "ais_distill_topk": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _I, _P, _P, _F, _P, _P, _P, _LL]),
     "ais_preference_params_default": (None, [C.POINTER(AisPreferenceParams)]),
     "ais_preference_row_scale": (_I, [_P, _P, _P, _P, _LL, _P, _I, _P, C.POINTER(AisPreferenceParams), _P, _P, _P]),
-    "ais_preference_loss_grad": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _P, _I, _P, _P, _P, _P,
-                                      C.POINTER(AisPreferenceParams), _P, _P, _P]),
+    "ais_preference_loss_grad": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _P, _I, _P, _P, C.POINTER(AisPreferenceParams), _P, _P, _P, _P]),
     "ais_norm_rows": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _P, _I, _F, _I, _P, _LL, _P, _P]),
     "ais_norm_rows_grad": (_I, [_P, _P, _I, _LL, _P, _I, _LL, _LL, _LL, _P, _P, _I, _P, _P, _P, _LL, _P, _P]),
     "ais_adamw_params_default": (None, [C.POINTER(AisAdamWParams)]),
@@ -771,36 +770,38 @@ class AisContext:
             raise AisError(rc, "ais_preference_row_scale")
         return loss, reward, g
 
-    def preference_loss_grad(self, logits, token_ids, valid, cu_rows, logp_train, lse, logp_ref,
-                             params: Optional[AisPreferenceParams] = None, weight=None, dlogits=None):
-        """-> (loss [1] fp32, reward [B] fp32, dlogits like logits); logp_train and lse as token_logprob returns them.
-        Pass dlogits=logits to overwrite the logits in place.  See ais_preference_loss_grad in include/ais.h."""
+    def preference_loss_grad(self, logits, token_ids, valid, cu_rows, logp_ref, params: Optional[AisPreferenceParams] = None,
+                             weight=None, want_grad: bool = True, dlogits=None):
+        """-> (loss [1] fp32, reward [B] fp32, logp [R] fp32, dlogits like logits or None): the loss through logits, whose tokens'
+        log-probs are formed in the call.  Pass dlogits=logits to overwrite the logits in place.  See ais_preference_loss_grad in
+        include/ais.h."""
         p = params or default_preference_params()
         if p.__class__ is AisPreferenceParams:
-            out = self._native("preference_loss_grad", logits, token_ids, lse, logp_train, logp_ref, valid, cu_rows, weight,
-                               C.addressof(p), dlogits)
+            out = self._native("preference_loss_grad", logits, token_ids, logp_ref, valid, cu_rows, weight, C.addressof(p),
+                               1 if want_grad else 0, dlogits)
             if out is not None:
                 return out
         dev = self.device
         n_rows, vocab, row_stride = _logits_geometry(logits, dev)
         dtype, n_resp = _dtype_code(logits), cu_rows.numel() - 1
-        if dlogits is None:
+        if dlogits is not None:
+            if dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.stride() != logits.stride():
+                raise ValueError("dlogits must have the dtype, shape and strides of logits")
+            _dev_ptr(dlogits, dev, "dlogits")
+        elif want_grad:
             dlogits = torch.empty_strided(logits.shape, logits.stride(), dtype=logits.dtype, device=dev)
-        elif dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or dlogits.stride() != logits.stride():
-            raise ValueError("dlogits must have the dtype, shape and strides of logits")
-        _dev_ptr(dlogits, dev, "dlogits")
         ptrs = [_ptr(token_ids, torch.int32, n_rows, "token_ids", dev), _ptr(valid, torch.uint8, n_rows, "valid", dev),
-                _ptr(cu_rows, torch.int64, n_resp + 1, "cu_rows", dev), n_resp,
-                _ptr(logp_train, torch.float32, n_rows, "logp_train", dev), _ptr(lse, torch.float32, n_rows, "lse", dev),
-                _ptr(logp_ref, torch.float32, n_rows, "logp_ref", dev), _ptr(weight, torch.float32, n_resp // 2, "weight", dev)]
+                _ptr(cu_rows, torch.int64, n_resp + 1, "cu_rows", dev), n_resp, _ptr(logp_ref, torch.float32, n_rows, "logp_ref", dev),
+                _ptr(weight, torch.float32, n_resp // 2, "weight", dev)]
         loss = torch.empty(1, dtype=torch.float32, device=dev)
         reward = torch.empty(max(n_resp, 0), dtype=torch.float32, device=dev)
+        logp = torch.empty(n_rows, dtype=torch.float32, device=dev)
         self._sync_stream()
         rc = self._lib.ais_preference_loss_grad(self._h, logits.data_ptr(), dtype, n_rows, vocab, row_stride, *ptrs, C.byref(p),
-                                                _ptr(reward), _ptr(loss), dlogits.data_ptr())
+                                                _ptr(reward), _ptr(loss), _ptr(logp), None if dlogits is None else dlogits.data_ptr())
         if rc != 0:
             raise AisError(rc, "ais_preference_loss_grad")
-        return loss, reward, dlogits
+        return loss, reward, logp, dlogits
 
     # ------------------------------------------------------------------ the rows before the read-out
     def norm_rows(self, x, weight=None, bias=None, eps: float = 1e-5, centered: bool = True, valid=None):

@@ -176,9 +176,10 @@ struct ScopedTimer {
 };
 
 // Launchers (each checks nothing: arguments were validated by the entry point).
+// logp_fine: [n_rows] log-probs in 64 bits for sums over many rows, or null.
 int launch_token_logprob(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, int vocab,
                          long long row_stride, const int* token_ids, const unsigned char* valid,
-                         float inv_temperature, float* logp_out, float* lse_out);
+                         float inv_temperature, float* logp_out, float* lse_out, double* logp_fine = nullptr);
 int launch_dlogits(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, int vocab,
                    long long row_stride, const int* token_ids, const float* g, const unsigned char* valid,
                    const float* lse, const float* logp, float inv_temperature, void* dlogits);
@@ -243,11 +244,14 @@ int launch_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long 
 
 // Where the arrays of the preference loss lie in the workspace, which begins with the tiles' sums (byte offsets).
 struct PreferenceRoom {
-  size_t counts, loss, coeff, g, total;
+  size_t counts, loss, coeff;
+  size_t g, lse, fine;         // of the call through logits
+  size_t total;
 };
-PreferenceRoom preference_room(long long n_rows, int n_resp);
-int launch_preference(ais_ctx* ctx, const float* logp, const float* ref, const unsigned char* valid, long long n_rows,
-                      const long long* cu_rows, int n_resp, const float* weight, const ais_preference_params& p,
+PreferenceRoom preference_room(long long n_rows, int n_resp, bool through_logits);
+// The log-probs in fp32 or, where `fine` is given, in 64 bits.
+int launch_preference(ais_ctx* ctx, const float* logp, const double* fine, const float* ref, const unsigned char* valid,
+                      long long n_rows, const long long* cu_rows, int n_resp, const float* weight, const ais_preference_params& p,
                       const PreferenceRoom& room, float scale, float* reward, float* loss_out, float* g);
 int norm_grad_parts(long long n_rows, long long width, int n_cus);
 size_t norm_grad_bytes(long long n_rows, long long width, int sums, int n_cus);

@@ -785,19 +785,19 @@ int ais_preference_row_scale(ais_ctx* ctx, const float* logp_train, const float*
   if (n_rows > 0 && (logp_train == nullptr || g_out == nullptr)) return AIS_ERR_NULL;
   if (ctx == nullptr) return AIS_ERR_NULL;
   DeviceGuard guard(ctx->device);
-  const PreferenceRoom room = preference_room(n_rows, n_resp);
+  const PreferenceRoom room = preference_room(n_rows, n_resp, false);
   rc = ensure_workspace(ctx, room.total);
   if (rc != AIS_OK) return rc;
   ctx->plan.valid = false;             // the sums overwrite whatever tiling the workspace held
-  return launch_preference(ctx, logp_train, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room,
+  return launch_preference(ctx, logp_train, nullptr, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room,
                            params->inv_temperature, reward_out, loss_out, g_out);
 }
 
 int ais_preference_loss_grad(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
                              long long row_stride, const int* token_ids, const unsigned char* valid,
-                             const long long* cu_rows, int n_resp, const float* logp_train, const float* lse,
-                             const float* logp_ref, const float* weight, const ais_preference_params* params,
-                             float* reward_out, float* loss_out, void* dlogits) {
+                             const long long* cu_rows, int n_resp, const float* logp_ref, const float* weight,
+                             const ais_preference_params* params, float* reward_out, float* loss_out, float* logp_out,
+                             void* dlogits) {
   int rc = check_logits(logits, dtype, n_rows, vocab, row_stride);
   if (rc != AIS_OK) return rc;
   rc = check_batch(n_rows, n_resp, 2);
@@ -805,19 +805,24 @@ int ais_preference_loss_grad(ais_ctx* ctx, const void* logits, ais_dtype dtype, 
   rc = check_preference(params);
   if (rc != AIS_OK) return rc;
   if (cu_rows == nullptr || reward_out == nullptr || loss_out == nullptr) return AIS_ERR_NULL;
-  if (n_rows > 0 && (token_ids == nullptr || logp_train == nullptr || lse == nullptr || dlogits == nullptr)) return AIS_ERR_NULL;
+  if (n_rows > 0 && (token_ids == nullptr || logp_out == nullptr)) return AIS_ERR_NULL;
   if (!aligned_to(dlogits, dtype)) return AIS_ERR_ALIGN;
   if (ctx == nullptr) return AIS_ERR_NULL;
   DeviceGuard guard(ctx->device);
-  const PreferenceRoom room = preference_room(n_rows, n_resp);
+  const PreferenceRoom room = preference_room(n_rows, n_resp, true);
   rc = ensure_workspace(ctx, room.total);
   if (rc != AIS_OK) return rc;
   ctx->plan.valid = false;             // the sums overwrite whatever tiling the workspace held
-  float* g = reinterpret_cast<float*>(static_cast<char*>(ctx->ws) + room.g);
-  rc = launch_preference(ctx, logp_train, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room, 1.0f, reward_out,
-                         loss_out, g);
+  char* ws = static_cast<char*>(ctx->ws);
+  float *g = reinterpret_cast<float*>(ws + room.g), *lse = reinterpret_cast<float*>(ws + room.lse);
+  double* fine = reinterpret_cast<double*>(ws + room.fine);
+  rc = launch_token_logprob(ctx, logits, dtype, n_rows, (int)vocab, row_stride, token_ids, valid, params->inv_temperature, logp_out,
+                            lse, fine);
   if (rc != AIS_OK) return rc;
-  return launch_dlogits(ctx, logits, dtype, n_rows, (int)vocab, row_stride, token_ids, g, nullptr, lse, logp_train,
+  rc = launch_preference(ctx, logp_out, fine, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room, 1.0f, reward_out,
+                         loss_out, g);
+  if (rc != AIS_OK || dlogits == nullptr) return rc;
+  return launch_dlogits(ctx, logits, dtype, n_rows, (int)vocab, row_stride, token_ids, g, nullptr, lse, logp_out,
                         params->inv_temperature, dlogits);
 }
 

@@ -180,6 +180,38 @@ __device__ __forceinline__ void accumulate(const float* x, float scale, MaxSum& 
 }
 
 
+// The same state for log-probabilities that are added up over whole responses, where what every row has too little adds up, too: a
+// thread that has met the row's largest logits drops what is small beside them, 3e-7 of the row's sum on the average of 151,936
+// logits.  Here a batch of terms is summed by itself and then added with what the addition drops.
+struct FineSum {
+  float m;
+  double s;
+};
+template <int n>
+__device__ __forceinline__ void accumulate(const float* x, float scale, FineSum& st) {
+  float cm = x[0];
+#pragma unroll
+  for (int k = 1; k < n; ++k) cm = fmaxf(cm, x[k]);
+  const float mn = fmaxf(st.m, cm * scale);
+  float acc0 = 0.f, acc1 = 0.f;
+#pragma unroll
+  for (int k = 0; k < n; k += 2) {
+    acc0 += exp2_fast(__builtin_fmaf(x[k], scale, -mn));
+    if (k + 1 < n) acc1 += exp2_fast(__builtin_fmaf(x[k + 1], scale, -mn));
+  }
+  st.s = st.s * (double)exp2_fast(st.m - mn) + (double)(acc0 + acc1);
+  st.m = mn;
+}
+__device__ __forceinline__ FineSum merge(FineSum a, FineSum b) {
+  const float m = fmaxf(a.m, b.m);
+  return {m, a.s * (double)exp2_fast(a.m - m) + b.s * (double)exp2_fast(b.m - m)};
+}
+__device__ __forceinline__ FineSum wave_merge(FineSum a) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) a = merge(a, FineSum{__shfl_xor(a.m, off), __shfl_xor(a.s, off)});
+  return a;
+}
+
 // Wavefront-wide maximum, same exchange pattern as wave_merge.
 __device__ __forceinline__ float wave_max(float v) {
   v = fmaxf(v, dpp_move<kDppQuadXor1>(v));

@@ -535,13 +535,12 @@ AIS_CALL(distill_topk) {
 
 // The arguments that the preference loss's two calls share, in their order.
 struct PreferenceArgs {
-  const float *lt, *ref, *weight;
-  const unsigned char* valid;
-  const long long* cu;
-  const ais_preference_params* p;
+  const float *ref = nullptr, *weight = nullptr;
+  const unsigned char* valid = nullptr;
+  const long long* cu = nullptr;
+  const ais_preference_params* p = nullptr;
   long long resp = 0;
   PreferenceArgs(Call& c, long long rows) {
-    lt = c.array<float>(at::kFloat, rows);
     ref = c.array<float>(at::kFloat, rows, true);
     valid = c.array<unsigned char>(at::kByte, rows, true);
     const at::Tensor* offsets = c.tensor();
@@ -561,34 +560,38 @@ AIS_CALL(preference_row_scale) {
   if (!c.ok) AIS_REFUSE;
   const long long rows = train->numel();
   --c.at;
+  const float* lt = c.array<float>(at::kFloat, rows);
   const PreferenceArgs l(c, rows);
   if (!c.ok || c.at != c.n) AIS_REFUSE;
   const at::Tensor loss = empty(c.device, {1}), reward = empty(c.device, {l.resp}), g = empty(c.device, {rows});
   float *lp = loss.data_ptr<float>(), *rp = reward.data_ptr<float>(), *gp = g.data_ptr<float>();
   const int rc = c.run([&] {
-    return lib.preference_row_scale(c.ctx, l.lt, l.ref, l.valid, rows, l.cu, (int)l.resp, l.weight, l.p, rp, lp, gp);
+    return lib.preference_row_scale(c.ctx, lt, l.ref, l.valid, rows, l.cu, (int)l.resp, l.weight, l.p, rp, lp, gp);
   });
   return rc != 0 ? PyLong_FromLong(rc) : result(loss, reward, g);
 }
 
+// logits, token_ids, the shared ones, 1 for a gradient or 0, where to put it
 AIS_CALL(preference_loss_grad) {
   const Matrix z(c);
   if (!c.ok) AIS_REFUSE;
   const int* ids = c.array<int>(at::kInt, z.rows);
-  const float* lse = c.array<float>(at::kFloat, z.rows);
   if (!c.ok) AIS_REFUSE;
   const PreferenceArgs l(c, z.rows);
+  const bool want_grad = c.integer() != 0;
   if (!c.ok) AIS_REFUSE;
-  const at::Tensor dz = z.like(c);
+  at::Tensor dz;
+  if (!want_grad && c.at < c.n && c.a[c.at] == Py_None) ++c.at;
+  else dz = z.like(c);
   if (!c.ok || c.at != c.n) AIS_REFUSE;
-  const at::Tensor loss = empty(c.device, {1}), reward = empty(c.device, {l.resp});
-  float *lp = loss.data_ptr<float>(), *rp = reward.data_ptr<float>();
-  void* dp = dz.data_ptr();
+  const at::Tensor loss = empty(c.device, {1}), reward = empty(c.device, {l.resp}), logp = empty(c.device, {z.rows});
+  float *lp = loss.data_ptr<float>(), *rp = reward.data_ptr<float>(), *tp = logp.data_ptr<float>();
+  void* dp = dz.defined() ? dz.data_ptr() : nullptr;
   const int rc = c.run([&] {
-    return lib.preference_loss_grad(c.ctx, z.data(), z.dtype, z.rows, z.width, z.stride, ids, l.valid, l.cu, (int)l.resp, l.lt, lse,
-                                    l.ref, l.weight, l.p, rp, lp, dp);
+    return lib.preference_loss_grad(c.ctx, z.data(), z.dtype, z.rows, z.width, z.stride, ids, l.valid, l.cu, (int)l.resp, l.ref,
+                                    l.weight, l.p, rp, lp, tp, dp);
   });
-  return rc != 0 ? PyLong_FromLong(rc) : result(loss, reward, dz);
+  return rc != 0 ? PyLong_FromLong(rc) : result(loss, reward, logp, dz);
 }
 
 // A weight or bias of `width` elements, bf16 or fp32 (the same type as the one before it), or None.

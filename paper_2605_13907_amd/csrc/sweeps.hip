@@ -32,11 +32,14 @@ using namespace dev;
 // too, those past the end of the row masked, instead of one by one, each waiting for its own: 8,192 x 32,003 bf16 87.9 ->
 // 84.8 us with 256 threads, no difference at 151,936.  (Three of them as four, one masked: 512 x 6,000 4.55 instead of 4.29
 // us, 1,000 x 6,000 5.75 and 5.40.)
-template <typename T, bool ALIGNED, int THREADS, int UNROLL>
+//
+// State: MaxSum, or FineSum for log-probabilities that are summed afterwards; these are then left in 64 bits, too.
+template <typename T, bool ALIGNED, int THREADS, int UNROLL, typename State = MaxSum>
 __global__ __launch_bounds__(THREADS) void token_logprob_kernel(
     const T* __restrict__ logits, long long row_stride, int vocab, const int* __restrict__ token_ids,
     const unsigned char* __restrict__ valid, float inv_temperature, double exact, float* __restrict__ logp_out,
-    float* __restrict__ lse_out, int* __restrict__ status) {
+    float* __restrict__ lse_out, int* __restrict__ status, double* __restrict__ logp_fine = nullptr) {
+  constexpr bool kFine = std::is_same_v<State, FineSum>;
   static_assert(UNROLL == 4, "the last vectors of a row are loaded by one to four a thread");
   constexpr int N = Vec<T>::N;
   const long long row = blockIdx.x;
@@ -45,6 +48,7 @@ __global__ __launch_bounds__(THREADS) void token_logprob_kernel(
     if (tid == 0) {
       logp_out[row] = 0.f;
       lse_out[row] = 0.f;
+      if constexpr (kFine) logp_fine[row] = 0.0;
     }
     return;
   }
@@ -64,7 +68,7 @@ __global__ __launch_bounds__(THREADS) void token_logprob_kernel(
   const int yvec = (y_ok && yb >= 0 && yb < nvec * N && (yb / N) % THREADS == tid) ? yb / N : -(1 << 30);
   const int ysub = yb & (N - 1);
 
-  MaxSum st{kNegHuge, 0.f};
+  State st{kNegHuge, 0.f};
   {
     const u32x4* zv = reinterpret_cast<const u32x4*>(zr + head);
     // COUNT vectors of every thread from vector `base` on, all in flight at once; TAIL: some lie past the end of the row
@@ -113,25 +117,45 @@ __global__ __launch_bounds__(THREADS) void token_logprob_kernel(
   }
 
   st = wave_merge(st);
-  __shared__ MaxSum lds[THREADS / 64];
+  __shared__ State lds[THREADS / 64];
   if ((tid & 63) == 0) lds[tid >> 6] = st;
   __syncthreads();
-  if (tid >= 64) return;
-  MaxSum t = lds[tid & (THREADS / 64 - 1)];         // the wavefronts' states, in lanes of the first
-  if (THREADS > 64) t = merge_dpp<kDppQuadXor1>(t);
-  if (THREADS > 128) t = merge_dpp<kDppQuadXor2>(t);
-  if (THREADS > 256) t = merge_dpp<kDppRowHalfMirror>(t);
-  if (THREADS > 512) t = merge_dpp<kDppRowMirror>(t);
-  if (tid == 0) {
+  if constexpr (kFine) {
+    if (tid != 0) return;
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) st = merge(st, lds[w]);
+    double l1p = 0.0, lse;
     if (y_ok) {
-      // once per row, in fp64: r = S_o / e^{z_y/T};  logp = -log1p(r);  lse = z_y/T + log1p(r)
-      const double l1p = log1p_scaled(t.s, ((double)t.m - (double)zy * (double)scale) * exact);
-      logp_out[row] = (float)(-l1p);
-      lse_out[row] = (float)((double)zy * (double)inv_temperature + l1p);
+      // the terms' exponents are those of a `scale` that is off by `exact`: what that does to the sum is below 2e-8 of a log-prob
+      const double e = ((double)st.m - (double)zy * (double)scale) * exact;
+      l1p = st.s > 0.0 ? e > 64.0 ? e * 0.6931471805599453 + log(st.s) : log1p(st.s * exp2(e)) : st.s;
+      lse = (double)zy * (double)inv_temperature + l1p;
     } else {
-      lse_out[row] = (t.m + log2_fast(t.s)) * kLn2;
-      logp_out[row] = 0.f;
+      lse = (double)st.m * exact * 0.6931471805599453 + log(st.s);
       atomicOr(status, AIS_STATUS_BAD_TOKEN);
+    }
+    logp_out[row] = (float)-l1p;
+    lse_out[row] = (float)lse;
+    logp_fine[row] = -l1p;
+    return;
+  } else {
+    if (tid >= 64) return;
+    MaxSum t = lds[tid & (THREADS / 64 - 1)];         // the wavefronts' states, in lanes of the first
+    if (THREADS > 64) t = merge_dpp<kDppQuadXor1>(t);
+    if (THREADS > 128) t = merge_dpp<kDppQuadXor2>(t);
+    if (THREADS > 256) t = merge_dpp<kDppRowHalfMirror>(t);
+    if (THREADS > 512) t = merge_dpp<kDppRowMirror>(t);
+    if (tid == 0) {
+      if (y_ok) {
+        // once per row, in fp64: r = S_o / e^{z_y/T};  logp = -log1p(r);  lse = z_y/T + log1p(r)
+        const double l1p = log1p_scaled(t.s, ((double)t.m - (double)zy * (double)scale) * exact);
+        logp_out[row] = (float)(-l1p);
+        lse_out[row] = (float)((double)zy * (double)inv_temperature + l1p);
+      } else {
+        lse_out[row] = (t.m + log2_fast(t.s)) * kLn2;
+        logp_out[row] = 0.f;
+        atomicOr(status, AIS_STATUS_BAD_TOKEN);
+      }
     }
   }
 }
@@ -471,7 +495,7 @@ int logprob_threads(const ais_ctx* ctx, long long n_rows, long long nvec, bool b
 
 int launch_token_logprob(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, int vocab,
                          long long row_stride, const int* token_ids, const unsigned char* valid,
-                         float inv_temperature, float* logp_out, float* lse_out) {
+                         float inv_temperature, float* logp_out, float* lse_out, double* logp_fine) {
   if (n_rows == 0) return AIS_OK;
   ScopedTimer timer(ctx, AIS_K_LOGPROB);
   auto launch = [&](const auto* z) {
@@ -479,11 +503,14 @@ int launch_token_logprob(ais_ctx* ctx, const void* logits, ais_dtype dtype, long
     const long long nvec = (long long)vocab / Vec<T>::N;
     auto run = [&](auto threads) {
       constexpr int kThreads = decltype(threads)::value;
-      auto kernel = vec_ok(z, row_stride, sizeof(T)) ? token_logprob_kernel<T, true, kThreads, kUnrollFwd>
-                                                     : token_logprob_kernel<T, false, kThreads, kUnrollFwd>;
+      const bool aligned = vec_ok(z, row_stride, sizeof(T));
+      auto kernel = logp_fine != nullptr ? aligned ? token_logprob_kernel<T, true, kThreads, kUnrollFwd, FineSum>
+                                                   : token_logprob_kernel<T, false, kThreads, kUnrollFwd, FineSum>
+                    : aligned            ? token_logprob_kernel<T, true, kThreads, kUnrollFwd>
+                                         : token_logprob_kernel<T, false, kThreads, kUnrollFwd>;
       kernel<<<dim3((unsigned)n_rows), dim3(kThreads), 0, ctx->stream>>>(
           z, row_stride, vocab, token_ids, valid, inv_temperature, exact_exponents(inv_temperature), logp_out, lse_out,
-          ctx->status_dev);
+          ctx->status_dev, logp_fine);
     };
     const int threads = logprob_threads(ctx, n_rows, nvec, std::is_same_v<T, bf16_t>);
     if (threads == 1024) run(std::integral_constant<int, 1024>{});

@@ -63,7 +63,7 @@ LENGTHS = {
     "one row": [1, 0], "two rows": [1, 1], "nothing": [0, 0], "empty ones between": [0, 3, 0, 0, 5, 0, 0, 0, 7, 2],
     "a tile": [TILE, 0], "a tile and one": [TILE, 1], "borders": [TILE - 1, 1, 1, TILE - 1, TILE, TILE],
     "inside tiles": [700, 900, 1_100, 3_000, 5, 6_001], "long": [50_001, 3], "many short": [1, 2, 0, 3] * 1_500,
-    "mixed": [9_000, 1, 1, 1, 0, 4_096, 2, 2], "ragged": [int(v) for v in np.random.default_rng(5).integers(0, 400, 600)],
+    "mixed": [9_000, 1, 1, 1, 0, 4_096, 2, 2], "one workgroup's": [4_000, 4_192], "one more": [4_000, 4_193], "one workgroup's many": [1, 2, 0] * 2_700 + [1, 1], "ragged": [int(v) for v in np.random.default_rng(5).integers(0, 400, 600)],
 }
 
 
@@ -140,10 +140,12 @@ def test_no_rows(ctx):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("vocab,pitch", [(1, 1), (70, 70), (1_000, 1_003), (4_096, 4_096), (33_001, 33_001)])
+@pytest.mark.parametrize("vocab,pitch", [(1, 1), (70, 70), (1_000, 1_003), (4_096, 4_096), (33_001, 33_001), (140_000, 140_000)])
 def test_through_logits(ctx, dtype, vocab, pitch):
-    """dlogits are the coefficients times softmax less the token's one: a rounding to the type (half a step), and in fp32 the
-    exponential (2^-22 and the shift's 2^-24 times the logit's size, at most 2^-19)."""
+    """Log-probs: each term is off by 2^-22 (an exponential's 2^-23, its exponent's rounding of at most 2^-24 times 40 of a term that is
+    then below e^-20), a batch's sum of 16 by 16 of 2^-25; 2^-20 of min(1, the other tokens' share) covers them, and 2^-24 its own rounding.
+    dlogits are the coefficients times softmax less the token's one: half a step of the type, and in fp32 the exponential and the shift by
+    an lse of up to 20: 2^-19."""
     gen = torch.Generator(device="cuda").manual_seed(7)
     logp0, _, valid, cu, weight = batch([5, 11, 0, 40, 17, 3], seed=4)
     rows = len(logp0)
@@ -151,22 +153,69 @@ def test_through_logits(ctx, dtype, vocab, pitch):
     ids = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
     valid, cu, weight = cuda(valid), cuda(cu), cuda(weight)
     p = B.default_preference_params(beta=0.3, inv_temperature=0.9)
-    logp, lse = ctx.token_logprob(z, ids, valid, 0.9)
-    ref = logp + 0.1 * torch.randn(rows, generator=gen, device="cuda")
-    loss, reward, dz = ctx.preference_loss_grad(z, ids, valid, cu, logp, lse, ref, p, weight=weight)
-    want_loss, want_reward, g = ctx.preference_row_scale(logp, ref, valid, cu, p, weight=weight)
-    assert torch.equal(loss, want_loss) and torch.equal(reward, want_reward)
     temperature = float(np.float32(0.9))
+    exact = torch.log_softmax(z.double() * temperature, dim=1).gather(1, ids.long()[:, None])[:, 0]
+    live = valid != 0
+    ref = (exact + 0.1 * torch.randn(rows, generator=gen, device="cuda")).float()
+    loss, reward, logp, dz = ctx.preference_loss_grad(z, ids, valid, cu, ref, p, weight=weight)
+    others = -torch.expm1(exact)
+    slack = 2.0 ** -20 * others + 1e-300
+    assert (torch.where(live, (logp.double() - exact).abs() <= slack + 2.0 ** -24 * exact.abs(), logp == 0)).all()
+    form = dict(beta=float(p.beta), inv_temperature=temperature)
+    want_loss, want_reward, g = O.preference(exact.cpu().numpy(), ref.cpu().numpy(), valid.cpu().numpy(), cu.cpu().numpy(),
+                                             weight.cpu().numpy(), **form)
+    each = float(p.beta) * float(slack.sum())
+    assert np.allclose(reward.cpu().numpy(), want_reward, rtol=2.0 ** -23, atol=each)
+    assert loss.item() == pytest.approx(want_loss, rel=2.0 ** -22, abs=2 * each * float(weight.sum()))
+    g = torch.tensor(g, device="cuda")
     soft = torch.softmax(z.double() * temperature, dim=1)
-    soft[torch.arange(rows), ids.long()] -= 1.0
-    want = g.double()[:, None] * soft
-    tol = want.abs() * (2.0 ** -9 * 1.01 if dtype == torch.bfloat16 else 0.0) * 2 + want.abs() * 2.0 ** -19 + g.double().abs()[:, None] * 2.0 ** -22
+    soft[torch.arange(rows), ids.long()] = torch.expm1(exact)
+    want = g[:, None] * soft
+    # a slope changes by at most a quarter of what its argument does
+    off = 2.0 ** -19 + each
+    tol = want.abs() * (off + (2.0 ** -8 if dtype == torch.bfloat16 else 0.0)) * 1.01 + g.abs()[:, None] * (slack[:, None] + 2.0 ** -24) \
+        + float(p.beta) * each * weight.max().double() * soft.abs()
     assert ((dz.double() - want).abs() <= tol).all()
-    kept = z.clone()
-    inplace = ctx.preference_loss_grad(z, ids, valid, cu, logp, lse, ref, p, weight=weight, dlogits=z)[2]
+    alone = ctx.preference_loss_grad(z, ids, valid, cu, ref, p, weight=weight, want_grad=False)
+    assert alone[3] is None and all(torch.equal(a, b) for a, b in zip(alone[:3], (loss, reward, logp)))
+    inplace = ctx.preference_loss_grad(z, ids, valid, cu, ref, p, weight=weight, dlogits=z)[3]
     assert inplace.data_ptr() == z.data_ptr() and torch.equal(inplace, dz)
-    _, _, one = ctx.preference_loss_grad(kept, ids, valid, cu, logp, lse, ref, p, weight=weight)
-    assert torch.equal(one, dz)
+
+
+def test_small_terms_of_long_responses_add_up(ctx):
+    """A response's log-ratios, each of which a sum in 32 bits leaves 3e-7 too large, are the sum of exact ones: rows of a large and 60,000
+    small terms, all alike, whose error does not average out.  A term is off by 2^-23 + 2^-24 at most, the same one for all small ones."""
+    rows, vocab = 512, 60_001
+    z = torch.full((rows, vocab), -15.0, device="cuda")
+    z[:, 0] = 0.0
+    ids = torch.ones(rows, dtype=torch.int32, device="cuda")
+    exact = torch.log_softmax(z[:1].double(), dim=1)[0, 1].item()
+    cu = cuda([0, rows, rows], torch.int64)
+    ref = torch.full((rows,), float(np.float32(exact)), device="cuda")
+    _, reward, _, _ = ctx.preference_loss_grad(z, ids, None, cu, ref, B.default_preference_params(beta=1.0), want_grad=False)
+    want = rows * (exact - float(np.float32(exact)))
+    share = 60_000 * np.exp(-15.0) / (1 + 60_000 * np.exp(-15.0))
+    # 15 log2(e) in fp32 is off by 2^-25 times 22, as the terms' common exponent: e^-15's relative error 22 * 2^-25 + 2^-23
+    assert abs(reward[0].item() - want) <= rows * (share * (22 * 2.0 ** -25 + 2.0 ** -23 + 16 * 2.0 ** -25) + 15 * 2.0 ** -50)
+
+
+@pytest.mark.parametrize("shift", [-8_000.0, 8_000.0])
+def test_tokens_far_from_the_rest(ctx, shift):
+    """A sampled token thousands below the row's largest, or above all others."""
+    z = torch.randn(6, 300, device="cuda")
+    z[:, 7] += shift
+    ids = torch.full((6,), 7, dtype=torch.int32, device="cuda")
+    exact = torch.log_softmax(z.double(), dim=1)[:, 7]
+    logp = ctx.preference_loss_grad(z, ids, None, cuda([0, 3, 6], torch.int64), None)[2]
+    assert torch.allclose(logp.double(), exact, rtol=2.0 ** -22, atol=1e-300)
+
+
+def test_faulty_tokens_are_reported(ctx):
+    z = torch.randn(4, 300, device="cuda")
+    ids = cuda(np.array([3, 300, -1, 299], np.int32))
+    _, _, logp, dz = ctx.preference_loss_grad(z, ids, None, cuda([0, 2, 4], torch.int64), None)
+    assert logp[1] == 0 and logp[2] == 0 and logp[0] < 0 and torch.isfinite(dz).all()
+    assert ctx.status() == B.STATUS_BAD_TOKEN and ctx.status() == 0
 
 
 def test_more_rows_than_a_launch_of_tiles_fills(ctx):

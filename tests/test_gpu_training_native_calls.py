@@ -18,9 +18,10 @@ def arguments():
     valid = torch.tensor([1, 1, 0, 1, 1, 1, 0, 1], device="cuda", dtype=torch.uint8)
     cu = torch.tensor([0, 3, 5, 6, 8], device="cuda")
     pair = dict(logp_train=logp, logp_ref=logp - 0.1, valid=valid, cu_rows=cu, weight=torch.rand(2, generator=gen, device="cuda"))
+    through = {k: t for k, t in pair.items() if k != "logp_train"}
     return {
         "preference_row_scale": pair,
-        "preference_loss_grad": dict(pair, logits=z, token_ids=torch.arange(n, device="cuda", dtype=torch.int32), lse=logp.abs() + 4.0),
+        "preference_loss_grad": dict(through, logits=z, token_ids=torch.arange(n, device="cuda", dtype=torch.int32)),
         "norm_rows": dict(x=x, weight=randn(d), bias=randn(d), valid=valid),
         "norm_rows_grad": dict(dy=dy, x=x, weight=randn(d), mean=0.1 * randn(n), rstd=1.0 + logp.abs(), valid=valid),
     }
@@ -33,7 +34,7 @@ def test_same_results(both):  # noqa: F811
             variants += [dict(args, logp_ref=None, weight=None), dict(args, params=B.default_preference_params(kind=2, mean_logp=1))]
         if name == "preference_loss_grad":
             variants += [dict(args, logits=args["logits"].bfloat16()), dict(args, logits=args["logits"][:, 1:]),
-                         dict(args, dlogits=torch.zeros_like(args["logits"]))]
+                         dict(args, dlogits=torch.zeros_like(args["logits"])), dict(args, want_grad=False)]
         if name == "norm_rows":
             x = args["x"]
             variants += [dict(x=x), dict(args, centered=False, bias=None), dict(args, x=x.bfloat16()), dict(args, weight=None),

@@ -45,18 +45,18 @@ def test_preference_row_scale():
 
 
 def test_preference_loss_grad():
-    order = "ctx z dtype n_rows vocab stride ids valid cu n_resp logp lse ref weight params reward loss dz".split()
+    order = "ctx z dtype n_rows vocab stride ids valid cu n_resp ref weight params reward loss logp dz".split()
     call = caller("ais_preference_loss_grad", order,
-                  dict(ctx=None, z=P, dtype=B.AIS_BF16, n_rows=10, vocab=64, stride=64, ids=P, valid=None, cu=P, n_resp=2, logp=P, lse=P,
-                       ref=None, weight=None, params=preference(), reward=Q, loss=Q, dz=Q))
-    assert call() == -1
-    for missing in ("z", "ids", "cu", "logp", "lse", "params", "reward", "loss", "dz"):
+                  dict(ctx=None, z=P, dtype=B.AIS_BF16, n_rows=10, vocab=64, stride=64, ids=P, valid=None, cu=P, n_resp=2, ref=None,
+                       weight=None, params=preference(), reward=Q, loss=Q, logp=Q, dz=Q))
+    assert call() == -1 and call(dz=None) == -1
+    for missing in ("z", "ids", "cu", "logp", "params", "reward", "loss"):
         assert call(**{missing: None}) == -1
     assert call(vocab=0) == -2 and call(n_rows=-1) == -2 and call(stride=63) == -3 and call(dtype=2) == -7 and call(n_resp=5) == -6
     assert call(z=C.c_void_p(0x1001)) == -4 and call(dz=C.c_void_p(0x1001)) == -4
     for bad in BAD_PREFERENCE:
         assert call(params=preference(**bad)) == -5, bad
-    assert call(n_rows=0, z=None, ids=None, logp=None, lse=None, dz=None) == -1
+    assert call(n_rows=0, z=None, ids=None, logp=None, dz=None) == -1
 
 
 def test_norm_rows():
