@@ -470,7 +470,7 @@ void ais_preference_params_default(ais_preference_params* p);
  * The sums are taken in fp64, in a fixed order.  At h_p = 1 the hinge has no slope.
  *   logp_train  [n_rows] fp32, output of ais_token_logprob or ais_lm_head_logprob
  *   logp_ref    [n_rows] fp32, or NULL: no reference (0 everywhere)
- *   valid, cu_rows   as above, n_resp even; neither log-prob is read where valid == 0
+ *   valid, cu_rows   as above, n_resp even; neither log-prob counts where valid == 0, whatever it is
  *   weight      [n_resp / 2] fp32, or NULL: 2 / n_resp each
  *   reward_out  [n_resp] fp32   beta d_i
  *   loss_out    one fp32

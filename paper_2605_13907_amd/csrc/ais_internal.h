@@ -244,7 +244,7 @@ int launch_distill_topk(ais_ctx* ctx, const void* logits, ais_dtype dtype, long 
 
 // Where the arrays of the preference loss lie in the workspace, which begins with the tiles' sums (byte offsets).
 struct PreferenceRoom {
-  size_t counts, loss, coeff;
+  size_t counts, loss, coeff, firsts;
   size_t g, lse, fine;         // of the call through logits
   size_t total;
 };

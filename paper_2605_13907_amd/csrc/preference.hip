@@ -3,10 +3,13 @@
 //   d_i = sum over i's valid rows of logp - ref (or their mean), h = beta (d_2p - d_2p+1) - margin, loss = sum_p w_p l(h_p)
 //   c_t = -d loss / d logp_t = -+ w_p l'(h_p) beta [/ |o_i|]
 //
-// Three launches: partial sums of tiles of rows, pairs, rows.  Bound by launches and, over millions of rows, by reading 9 and
-// writing 4 bytes a row.
+// Three launches: partial sums of tiles of rows, pairs, rows; small batches are one workgroup's.  Reading 9 and writing 4 bytes a row is
+// nothing beside the launches: 1.2 million rows in 4,000 responses take 6.0, 3.6 and 4.9 us, which is how long a workgroup's own chain of
+// loads, scan and stores is, all of them being there at once.  All that a thread needs of its rows is therefore loaded at once, masked rows
+// included, and eight rows lie in registers for the scan and the walk after it (11.2, 4.7 and 11.0 us with loads one after the other).
 #include "ais_internal.h"
 #include "eights.h"
+#include "row_coeff.h"
 
 namespace ais {
 namespace {
@@ -17,6 +20,7 @@ constexpr int kRowsOfThread = 8;
 // A workgroup's tile of rows where there are many; where one workgroup can take them all, it does.
 constexpr int kTileThreads = 256, kOneThreads = 1024;
 constexpr int kTileRows = kRowsOfThread * kTileThreads, kOneRows = kRowsOfThread * kOneThreads;
+constexpr int kOneResponses = 1024;
 
 // The last response that begins at `row` or before it (cu_rows non-decreasing), by a wavefront: each step looks at 64 places.
 __device__ __forceinline__ int response_at(const long long* __restrict__ cu, int n_resp, long long row) {
@@ -61,60 +65,95 @@ struct Preference {
   int* counts;
   double* loss;
   float* coeff;
+  int* firsts;                                   // response that each tile begins in
   float *reward, *loss_out, *g;
   int* status;
 };
 
-// The tile of rows that begins at r0: which response each row belongs to, as marks where responses begin.
+struct Owner {
+  float coeff;
+  long long lo, hi;
+};
+
+// Eight rows of a thread: log-ratios, 0 in rows that do not count, and which of them do.
+struct Rows {
+  double x[kRowsOfThread];
+  unsigned live;
+  __device__ __forceinline__ void load(const Preference& in, long long r, int here) {
+    typedef u32x2 __attribute__((aligned(1))) Bytes;
+    float lp[kRowsOfThread] = {}, rf[kRowsOfThread] = {};
+    live = 0;
+#pragma unroll
+    for (int k = 0; k < kRowsOfThread; ++k) x[k] = 0.0;
+    if (here <= 0) return;
+    // all loads at once: masked rows are loaded and dropped
+    if (here == kRowsOfThread) {
+      u32x2 v = {0x01010101u, 0x01010101u};
+      if (in.valid != nullptr) v = *reinterpret_cast<const Bytes*>(in.valid + r);
+      if (in.ref != nullptr) Eight<float>::unpack(Eight<float>::load_kept(in.ref + r), rf);
+      if (in.fine != nullptr) {
+#pragma unroll
+        for (int k = 0; k < kRowsOfThread; ++k) x[k] = in.fine[r + k];
+      } else {
+        Eight<float>::unpack(Eight<float>::load_kept(in.logp + r), lp);
+      }
+#pragma unroll
+      for (int k = 0; k < kRowsOfThread; ++k) live |= ((v[k >> 2] >> (8 * (k & 3)) & 255u) != 0 ? 1u : 0u) << k;
+    } else {
+#pragma unroll
+      for (int k = 0; k < kRowsOfThread; ++k) {
+        if (k >= here) break;
+        if (in.valid == nullptr || in.valid[r + k] != 0) live |= 1u << k;
+        if (in.fine != nullptr) x[k] = in.fine[r + k];
+        else lp[k] = in.logp[r + k];
+        if (in.ref != nullptr) rf[k] = in.ref[r + k];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kRowsOfThread; ++k)
+      x[k] = live >> k & 1 ? (in.fine != nullptr ? x[k] : (double)lp[k]) - (double)rf[k] : 0.0;
+  }
+};
+
+// A tile of rows from r0 on: which response each row belongs to, as marks where responses begin.
 template <int THREADS>
 struct Tile {
   static constexpr int kRows = kRowsOfThread * THREADS;
-  int begins[kRows];                             // 1 + response, 0
+  alignas(16) int begins[kRows];                 // 1 + response, 0
   Run waves[THREADS / 64];
-  int first;
 
-  __device__ __forceinline__ void mark(const Preference& in, long long r0, long long r1) {
-    for (int k = threadIdx.x; k < kRows; k += THREADS) begins[k] = 0;
-    const int i0 = response_at(in.cu, in.n_resp, r0), i1 = response_at(in.cu, in.n_resp, r1 - 1);
-    if (threadIdx.x == 0) first = i0;
-    __syncthreads();
-    for (int i = i0 + 1 + threadIdx.x; i <= i1; i += THREADS) {
-      const long long at = in.cu[i] - r0;
-      if (at >= 0 && at < r1 - r0) atomicMax(&begins[at], i + 1);      // of several that begin there all but the last are empty
-    }
-    __syncthreads();
+  // The marks of a thread's rows; there are none past the end.
+  __device__ __forceinline__ void marks(int* o) const {
+    const int4 a = reinterpret_cast<const int4*>(begins)[2 * threadIdx.x], b = reinterpret_cast<const int4*>(begins)[2 * threadIdx.x + 1];
+    o[0] = a.x, o[1] = a.y, o[2] = a.z, o[3] = a.w;
+    o[4] = b.x, o[5] = b.y, o[6] = b.z, o[7] = b.w;
   }
 
-  // Partial sums of tile b, between r0 and r1: a segmented scan over the tile's rows, eight to a thread.
-  __device__ __forceinline__ void sum(const Preference& in, int b, long long r0, long long r1) {
+  __device__ __forceinline__ void clear() {
+    reinterpret_cast<int4*>(begins)[threadIdx.x] = int4{0, 0, 0, 0};
+    reinterpret_cast<int4*>(begins)[threadIdx.x + THREADS] = int4{0, 0, 0, 0};
+  }
+  // Response i begins in row `at` of the tile; of several that begin there all but the last are empty.
+  __device__ __forceinline__ void mark(int i, long long at, int rows) {
+    if (at >= 0 && at < rows) atomicMax(&begins[at], i + 1);
+  }
+
+  // Partial sums: a segmented scan over the tile's rows, eight to a thread.  `first`: the response that row 0 belongs to; leave(i,
+  // sum, count) is called once for every response with a row here.
+  template <typename Leave>
+  __device__ __forceinline__ void sum(const Rows& mine, int first, int rows, Leave leave) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int rows = (int)(r1 - r0);
-    const int at = kRowsOfThread * tid, here = min(max(rows - at, 0), kRowsOfThread);
-    double x[kRowsOfThread] = {};
-    unsigned live = 0;
-    if (here > 0) {
-      const long long r = r0 + at;
-#pragma unroll
-      for (int k = 0; k < kRowsOfThread; ++k) live |= (k < here && (in.valid == nullptr || in.valid[r + k] != 0) ? 1u : 0u) << k;
-#pragma unroll
-      for (int k = 0; k < kRowsOfThread; ++k) {
-        if ((live >> k & 1) == 0) continue;
-        x[k] = in.fine != nullptr ? in.fine[r + k] : (double)in.logp[r + k];
-        if (in.ref != nullptr) x[k] -= (double)in.ref[r + k];
-      }
-    }
-    mark(in, r0, r1);
-    Run mine{0.0, 0, 0};
+    const int at = kRowsOfThread * tid;
+    int o[kRowsOfThread];
+    marks(o);
+    Run scan{0.0, 0, 0};
 #pragma unroll
     for (int k = 0; k < kRowsOfThread; ++k) {
-      if (k >= here) break;
-      const int o = begins[at + k];
-      if (o != 0) mine = Run{0.0, 0, o};
-      mine.sum += x[k];
-      mine.count += live >> k & 1;
+      if (o[k] != 0) scan = Run{0.0, 0, o[k]};
+      scan.sum += mine.x[k];
+      scan.count += mine.live >> k & 1;
     }
     // what lies before this thread's rows
-    Run scan = mine;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
       const Run before{__shfl_up(scan.sum, off), __shfl_up(scan.count, off), __shfl_up(scan.owner, off)};
@@ -127,32 +166,29 @@ struct Tile {
     Run ahead{0.0, 0, first + 1};
     for (int w = 0; w < wave; ++w) ahead = join(ahead, waves[w]);
     run = join(ahead, run);
-    auto leave = [&] {
-      const size_t place = (size_t)(run.owner - 1) + b;
-      in.sums[place] = run.sum;
-      in.counts[place] = run.count;
-    };
 #pragma unroll
     for (int k = 0; k < kRowsOfThread; ++k) {
-      if (k >= here) break;
-      const int o = begins[at + k];
-      if (o != 0) {
-        if (at + k > 0) leave();
-        run = Run{0.0, 0, o};
+      if (o[k] != 0) {
+        if (at + k > 0) leave(run.owner - 1, run.sum, run.count);
+        run = Run{0.0, 0, o[k]};
       }
-      run.sum += x[k];
-      run.count += live >> k & 1;
+      run.sum += mine.x[k];
+      run.count += mine.live >> k & 1;
     }
-    if (here > 0 && at + here == rows) leave();
+    if (at < rows && at + kRowsOfThread >= rows) leave(run.owner - 1, run.sum, run.count);
   }
 
-  // Coefficients of the rows between r0 and r1, whose responses have been marked.
-  __device__ __forceinline__ void spread(const Preference& in, long long r0, long long r1) {
+  // Coefficients of the rows from r0 on, whose responses have been marked; of(i): response i's coefficient and rows.
+  template <typename Of>
+  __device__ __forceinline__ void spread(const Preference& in, unsigned live, int first, long long r0, int rows, Of of) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int at = kRowsOfThread * tid, here = min(max((int)(r1 - r0) - at, 0), kRowsOfThread);
+    const int at = kRowsOfThread * tid, here = min(max(rows - at, 0), kRowsOfThread);
+    int o[kRowsOfThread];
+    marks(o);
     // owners grow along the tile where the offsets do: the last mark is the largest so far
     int own = 0;
-    for (int k = 0; k < here; ++k) own = max(own, begins[at + k]);
+#pragma unroll
+    for (int k = 0; k < kRowsOfThread; ++k) own = max(own, o[k]);
     int scan = own;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -165,44 +201,52 @@ struct Tile {
     if (lane == 0) own = 0;
     own = max(own, first + 1);
     for (int w = 0; w < wave; ++w) own = max(own, waves[w].owner);
-    for (int k = 0; k < here; ++k) {
-      own = max(own, begins[at + k]);
+    Owner owner = of(own - 1);
+    float g[kRowsOfThread];
+#pragma unroll
+    for (int k = 0; k < kRowsOfThread; ++k) {
+      if (o[k] > own) {
+        own = o[k];
+        owner = of(own - 1);
+      }
       const long long r = r0 + at + k;
-      const int i = own - 1;
-      const bool mine = (in.valid == nullptr || in.valid[r] != 0) && in.cu[i] <= r && r < in.cu[i + 1];
-      in.g[r] = mine ? in.coeff[i] * in.scale : 0.f;
+      g[k] = (live >> k & 1) != 0 && owner.lo <= r && r < owner.hi ? owner.coeff * in.scale : 0.f;
     }
+    if (here == kRowsOfThread) Eight<float>::store(in.g + r0 + at, g);
+    else if (here > 0) store_some(in.g + r0 + at, here, g);
   }
 };
 
-// A pair's loss, rewards and coefficients from the partial sums of tiles of `tile_rows` rows.
-__device__ __forceinline__ double pair_terms(const Preference& in, int pair, int tile_rows) {
+__device__ __forceinline__ unsigned live_rows(const Preference& in, long long r, int here) {
+  typedef u32x2 __attribute__((aligned(1))) Bytes;
+  if (here <= 0) return 0;
+  if (in.valid == nullptr) return 255u;
+  unsigned live = 0;
+  if (here == kRowsOfThread) {
+    const u32x2 v = *reinterpret_cast<const Bytes*>(in.valid + r);
+#pragma unroll
+    for (int k = 0; k < kRowsOfThread; ++k) live |= ((v[k >> 2] >> (8 * (k & 3)) & 255u) != 0 ? 1u : 0u) << k;
+  } else {
+    for (int k = 0; k < here; ++k) live |= (in.valid[r + k] != 0 ? 1u : 0u) << k;
+  }
+  return live;
+}
+
+// Loss of a pair with log-ratios d, and the coefficients of its two responses' rows.
+__device__ __forceinline__ double pair_terms(const Preference& in, int pair, const double* s, const int* n, float* coeff) {
   const ais_preference_params& p = in.p;
   double d[2], share[2];
-  bool bad = false;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const int i = 2 * pair + j;
-    const long long from = in.cu[i], to = in.cu[i + 1];
-    bad |= from < 0 || to < from || to > in.n_rows || (i == 0 && from != 0) || (i == in.n_resp - 1 && to != in.n_rows);
-    const long long lo = min(max(from, 0LL), in.n_rows), hi = min(max(to, lo), in.n_rows);
-    double s = 0.0;
-    int n = 0;
-    if (hi > lo)
-      for (unsigned b = (unsigned)lo / (unsigned)tile_rows; b <= (unsigned)(hi - 1) / (unsigned)tile_rows; ++b) {
-        s += in.sums[i + (size_t)b];
-        n += in.counts[i + (size_t)b];
-      }
-    share[j] = p.mean_logp ? (n > 0 ? 1.0 / (double)n : 0.0) : 1.0;
-    d[j] = s * share[j];
-    in.reward[i] = (float)((double)p.beta * d[j]);
+    share[j] = p.mean_logp ? (n[j] > 0 ? 1.0 / (double)n[j] : 0.0) : 1.0;
+    d[j] = s[j] * share[j];
+    in.reward[2 * pair + j] = (float)((double)p.beta * d[j]);
   }
-  if (bad) atomicOr(in.status, AIS_STATUS_BAD_CU);
   const double beta = (double)p.beta, h = beta * (d[0] - d[1]) - (double)p.margin;
   const double w = in.weight != nullptr ? (double)in.weight[pair] : 2.0 / (double)in.n_resp;
   double l, slope;
   if (p.kind == 0) {
-    const double e = exp(-fabs(h)), both = log1p(e), wrong = (double)p.label_smoothing;
+    const double e = exp64(-fabs(h)), both = log1p(e), wrong = (double)p.label_smoothing;
     // sigmoid(-h) and sigmoid(h), neither from 1 less the other
     const double small = e / (1.0 + e), large = 1.0 / (1.0 + e);
     const double down = h >= 0.0 ? small : large, up = h >= 0.0 ? large : small;
@@ -219,9 +263,17 @@ __device__ __forceinline__ double pair_terms(const Preference& in, int pair, int
     slope = 2.0 * q / beta;
   }
   const double c = w * slope * beta;
-  in.coeff[2 * pair] = (float)(-c * share[0]);
-  in.coeff[2 * pair + 1] = (float)(c * share[1]);
+  coeff[0] = (float)(-c * share[0]);
+  coeff[1] = (float)(c * share[1]);
   return w * l;
+}
+
+// Rows of response i, whose offsets are from and to, inside the batch; faulty ones are reported.
+__device__ __forceinline__ void rows_of(const Preference& in, int i, long long from, long long to, unsigned* lo, unsigned* hi) {
+  if (from < 0 || to < from || to > in.n_rows || (i == 0 && from != 0) || (i == in.n_resp - 1 && to != in.n_rows))
+    atomicOr(in.status, AIS_STATUS_BAD_CU);
+  *lo = (unsigned)min(max(from, 0LL), in.n_rows);
+  *hi = (unsigned)min(max(to, (long long)*lo), in.n_rows);
 }
 
 // The sum of a workgroup's values, by its first thread, in the order of the wavefronts.
@@ -238,42 +290,110 @@ __device__ __forceinline__ void add_up(double s, float* out) {
 
 __global__ __launch_bounds__(kTileThreads) void preference_sums_kernel(Preference in) {
   __shared__ Tile<kTileThreads> tile;
-  const long long r0 = (long long)blockIdx.x * kTileRows;
-  tile.sum(in, (int)blockIdx.x, r0, min(r0 + kTileRows, in.n_rows));
+  __shared__ int range[2];
+  const int tid = threadIdx.x, b = blockIdx.x;
+  const long long r0 = (long long)b * kTileRows;
+  const int rows = (int)min((long long)kTileRows, in.n_rows - r0);
+  Rows mine;
+  mine.load(in, r0 + kRowsOfThread * tid, min(max(rows - kRowsOfThread * tid, 0), kRowsOfThread));
+  tile.clear();
+  // two wavefronts look for the tile's first and last response
+  if (tid < 128) {
+    const int i = response_at(in.cu, in.n_resp, tid < 64 ? r0 : r0 + rows - 1);
+    if ((tid & 63) == 0) range[tid >> 6] = i;
+    if (tid == 0) in.firsts[b] = i;
+  }
+  __syncthreads();
+  const int first = range[0];
+  for (int i = first + 1 + tid; i <= range[1]; i += kTileThreads) tile.mark(i, in.cu[i] - r0, rows);
+  __syncthreads();
+  tile.sum(mine, first, rows, [&](int i, double sum, int count) {
+    in.sums[(size_t)i + b] = sum;
+    in.counts[(size_t)i + b] = count;
+  });
 }
 
 // A thread to a pair.
 __global__ __launch_bounds__(kTileThreads) void preference_pairs_kernel(Preference in) {
   const int pair = blockIdx.x * kTileThreads + threadIdx.x;
-  if (2 * pair < in.n_resp) in.loss[pair] = pair_terms(in, pair, kTileRows);
+  if (2 * pair >= in.n_resp) return;
+  const long long cu[3] = {in.cu[2 * pair], in.cu[2 * pair + 1], in.cu[2 * pair + 2]};
+  double s[2] = {};
+  int n[2] = {};
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    unsigned lo, hi;
+    rows_of(in, 2 * pair + j, cu[j], cu[j + 1], &lo, &hi);
+    if (hi > lo)
+      for (unsigned b = lo / kTileRows; b <= (hi - 1) / kTileRows; ++b) {
+        s[j] += in.sums[2 * pair + j + (size_t)b];
+        n[j] += in.counts[2 * pair + j + (size_t)b];
+      }
+  }
+  in.loss[pair] = pair_terms(in, pair, s, n, in.coeff + 2 * pair);
 }
 
 // A workgroup to a tile; one more adds up the pairs' losses.
 __global__ __launch_bounds__(kTileThreads) void preference_rows_kernel(Preference in, int tiles) {
   __shared__ Tile<kTileThreads> tile;
-  if ((int)blockIdx.x == tiles) {
+  const int tid = threadIdx.x, b = blockIdx.x;
+  if (b == tiles) {
     double s = 0.0;
-    for (int p = threadIdx.x; p < in.n_resp / 2; p += kTileThreads) s += in.loss[p];
+    for (int p = tid; p < in.n_resp / 2; p += kTileThreads) s += in.loss[p];
     add_up<kTileThreads>(s, in.loss_out);
     return;
   }
-  const long long r0 = (long long)blockIdx.x * kTileRows, r1 = min(r0 + kTileRows, in.n_rows);
-  tile.mark(in, r0, r1);
-  tile.spread(in, r0, r1);
+  const long long r0 = (long long)b * kTileRows;
+  const int rows = (int)min((long long)kTileRows, in.n_rows - r0);
+  const unsigned live = live_rows(in, r0 + kRowsOfThread * tid, min(max(rows - kRowsOfThread * tid, 0), kRowsOfThread));
+  const int first = in.firsts[b], last = b + 1 < tiles ? in.firsts[b + 1] : in.n_resp - 1;
+  tile.clear();
+  __syncthreads();
+  for (int i = first + 1 + tid; i <= last; i += kTileThreads) tile.mark(i, in.cu[i] - r0, rows);
+  __syncthreads();
+  tile.spread(in, live, first, r0, rows, [&](int i) { return Owner{in.coeff[i], in.cu[i], in.cu[i + 1]}; });
 }
 
-// All of it in one workgroup.
-__global__ __launch_bounds__(kOneThreads) void preference_one_kernel(Preference in) {
-  __shared__ Tile<kOneThreads> tile;
-  if (in.n_rows > 0) tile.sum(in, 0, 0, in.n_rows);
-  __threadfence_block();
+// All of it in one workgroup, with the responses' offsets, sums and coefficients in LDS.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void preference_one_kernel(Preference in) {
+  __shared__ Tile<THREADS> tile;
+  __shared__ long long cu[kOneResponses + 1];
+  __shared__ double sums[kOneResponses];
+  __shared__ int counts[kOneResponses];
+  __shared__ float coeff[kOneResponses];
+  __shared__ int first;
+  const int tid = threadIdx.x, rows = (int)in.n_rows;
+  Rows mine;
+  mine.load(in, kRowsOfThread * tid, min(max(rows - kRowsOfThread * tid, 0), kRowsOfThread));
+  for (int i = tid; i <= in.n_resp; i += THREADS) cu[i] = in.cu[i];
+  tile.clear();
+  if (tid == 0) first = 0;
+  __syncthreads();
+  for (int i = tid; i < in.n_resp; i += THREADS) {
+    sums[i] = 0.0;
+    counts[i] = 0;
+    tile.mark(i, cu[i], rows);
+    if (cu[i] <= 0) atomicMax(&first, i);
+  }
+  __syncthreads();
+  tile.sum(mine, first, rows, [&](int i, double sum, int count) {
+    sums[i] = sum;
+    counts[i] = count;
+  });
   __syncthreads();
   double s = 0.0;
-  for (int p = threadIdx.x; p < in.n_resp / 2; p += kOneThreads) s += pair_terms(in, p, kOneRows);
-  __threadfence_block();
+  for (int pair = tid; pair < in.n_resp / 2; pair += THREADS) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      unsigned lo, hi;
+      rows_of(in, 2 * pair + j, cu[2 * pair + j], cu[2 * pair + j + 1], &lo, &hi);
+    }
+    s += pair_terms(in, pair, sums + 2 * pair, counts + 2 * pair, coeff + 2 * pair);
+  }
   __syncthreads();
-  if (in.n_rows > 0) tile.spread(in, 0, in.n_rows);
-  add_up<kOneThreads>(s, in.loss_out);
+  tile.spread(in, mine.live, first, 0, rows, [&](int i) { return Owner{coeff[i], cu[i], cu[i + 1]}; });
+  add_up<THREADS>(s, in.loss_out);
 }
 
 size_t padded(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -286,7 +406,8 @@ PreferenceRoom preference_room(long long n_rows, int n_resp, bool through_logits
   r.counts = padded(8 * places);
   r.loss = r.counts + padded(4 * places);
   r.coeff = r.loss + padded(4 * (size_t)n_resp);
-  r.g = r.coeff + padded(4 * (size_t)n_resp);
+  r.firsts = r.coeff + padded(4 * (size_t)n_resp);
+  r.g = r.firsts + padded(4 * places);
   r.lse = r.g + padded(4 * (size_t)n_rows);
   r.fine = r.lse + padded(4 * (size_t)n_rows);
   r.total = through_logits ? r.fine + padded(8 * (size_t)n_rows) : r.g;
@@ -300,9 +421,11 @@ int launch_preference(ais_ctx* ctx, const float* logp, const double* fine, const
   char* ws = static_cast<char*>(ctx->ws);
   const Preference in{logp, fine, ref, valid, cu_rows, weight, n_resp, n_rows, p, scale, reinterpret_cast<double*>(ws),
                       reinterpret_cast<int*>(ws + room.counts), reinterpret_cast<double*>(ws + room.loss),
-                      reinterpret_cast<float*>(ws + room.coeff), reward, loss_out, g, ctx->status_dev};
-  if (n_rows <= kOneRows && n_resp <= kOneRows) {
-    preference_one_kernel<<<dim3(1), dim3(kOneThreads), 0, ctx->stream>>>(in);
+                      reinterpret_cast<float*>(ws + room.coeff), reinterpret_cast<int*>(ws + room.firsts), reward, loss_out, g, ctx->status_dev};
+  if (n_rows <= kOneRows && n_resp <= kOneResponses) {
+    // 2,048 rows take 9.1 us with 1,024 threads and 6.1 with 256
+    if (n_rows <= kTileRows) preference_one_kernel<kTileThreads><<<dim3(1), dim3(kTileThreads), 0, ctx->stream>>>(in);
+    else preference_one_kernel<kOneThreads><<<dim3(1), dim3(kOneThreads), 0, ctx->stream>>>(in);
     return hip_fail(ctx, hipGetLastError());
   }
   const int tiles = (int)((n_rows + kTileRows - 1) / kTileRows);
