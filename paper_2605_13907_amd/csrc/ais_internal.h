@@ -253,8 +253,13 @@ PreferenceRoom preference_room(long long n_rows, int n_resp, bool through_logits
 int launch_preference(ais_ctx* ctx, const float* logp, const double* fine, const float* ref, const unsigned char* valid,
                       long long n_rows, const long long* cu_rows, int n_resp, const float* weight, const ais_preference_params& p,
                       const PreferenceRoom& room, float scale, float* reward, float* loss_out, float* g);
-int norm_grad_parts(long long n_rows, long long width, int n_cus);
-size_t norm_grad_bytes(long long n_rows, long long width, int sums, int n_cus);
+// How the rows of the normalisation's gradient are shared: threads of a row, rows of a workgroup at a time (0: rows too wide to be held),
+// vectors of a thread, and workgroups, each of which leaves a row of partial sums.
+struct NormGradPlan {
+  int threads, teams, vectors, parts;
+};
+NormGradPlan norm_grad_plan(long long n_rows, long long width, bool bf16, int n_cus);      // bf16: x and dy both
+size_t norm_grad_bytes(long long n_rows, long long width, bool bf16, int sums, int n_cus);
 int launch_norm_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, int width, long long row_stride,
                      const unsigned char* valid, const void* weight, const void* bias, ais_dtype param_dtype, float eps,
                      int centered, void* y, long long y_stride, float* mean, float* rstd);
