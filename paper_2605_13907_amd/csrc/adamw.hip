@@ -19,7 +19,9 @@ namespace {
 using namespace dev;
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 8 * kThreads;             // elements of a workgroup
+constexpr int kVector = 4;                       // elements that a lane loads at once: 16 bytes of fp32
+constexpr int kVectors = 2;                      // of a lane, all on their way together
+constexpr int kChunk = kVector * kVectors * kThreads;        // elements of a workgroup
 constexpr int kTensors = 48;                     // of a launch: their addresses are 3.3 of the 4 KiB of kernel arguments
 
 struct Tensor {
@@ -37,6 +39,7 @@ struct Batch {
 
 struct Rule {
   double b1, b2;
+  double c1, c2;                                 // 1 / (1 - b^step); of no meaning with step_dev
   float lr, eps, decay;
   unsigned seed;
   long long step;
@@ -52,7 +55,7 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
 constexpr uint32_t kPhi = 0x9E3779B1u;
 
 // b^n for n >= 1.
-__device__ __forceinline__ double power(double b, long long n) {
+__host__ __device__ __forceinline__ double power(double b, long long n) {
   double r = 1.0;
   for (; n > 0; n >>= 1) {
     if (n & 1) r *= b;
@@ -60,6 +63,29 @@ __device__ __forceinline__ double power(double b, long long n) {
   }
   return r;
 }
+
+// The rule with what is in device memory.
+struct Now {
+  long long step;
+  double b1, b2, g1, g2;                         // of the moments, of the gradient and its square
+  float c2, decay, rate;                         // v's correction; lr with the decay, and with m's correction
+  __device__ __forceinline__ explicit Now(const Rule& r) : step(r.step), b1(r.b1), b2(r.b2) {
+    double c1d = r.c1, c2d = r.c2, scale = 1.0;
+    float lr = r.lr;
+    if (r.step_dev != nullptr) {                 // uniform, as all of these
+      step = *r.step_dev;
+      c1d = 1.0 / (1.0 - power(b1, step));
+      c2d = 1.0 / (1.0 - power(b2, step));
+    }
+    if (r.lr_dev != nullptr) lr = *r.lr_dev;
+    if (r.grad_scale != nullptr) scale = (double)*r.grad_scale;
+    g1 = (1.0 - b1) * scale;
+    g2 = (1.0 - b2) * (scale * scale);
+    c2 = (float)c2d;
+    decay = (float)((double)lr * (double)r.decay);
+    rate = (float)((double)lr * c1d);
+  }
+};
 
 // The two formats.  kBias: the smallest number with a whole fraction is 2^(1 - kBias) under a scale of 1.  kTop: exponent of the
 // block's largest under its scale, one below the format's own, so that a value rounded up still has a code.
@@ -77,71 +103,155 @@ __device__ __forceinline__ uint32_t scale_byte(float largest) {
   const int e = (int)(__float_as_uint(largest) >> 23) & 255;
   return e == 255 ? 255u : (uint32_t)max(e - F::kTop, F::kTop);
 }
-// 2^(byte - bias) in fp64: what a code's bits, taken as those of an fp32 from bit 20 on, are to be multiplied by.
+// What a code's bits, taken as those of an fp32 from bit 20 on, are to be multiplied by: 2^(byte - bias), in fp64.
 template <typename F>
 __device__ __forceinline__ double decode_factor(uint32_t byte) {
   if (byte == 255) return __longlong_as_double(0x7ff8000000000000LL);
   return __longlong_as_double((long long)((int)byte - F::kBias + 1023) << 52);
 }
 template <typename F>
-__device__ __forceinline__ double decode(uint32_t code, double factor) {
-  const double x = (double)__uint_as_float((code & F::kMagnitude) << 20) * factor;
-  return F::kMagnitude == 127 && (code & 128) ? -x : x;
+__device__ __forceinline__ float code_bits(uint32_t code) {
+  const uint32_t magnitude = (code & F::kMagnitude) << 20;
+  return __uint_as_float(F::kMagnitude == 127 ? magnitude | (code & 128) << 24 : magnitude);
 }
 // The code of a magnitude (bits of an fp32): 20 bits of fraction are dropped after the random number, 16 bits under the
 // code's last, has been added to them.  Below the format's smallest whole exponent the spacing stays that exponent's.
 template <typename F>
 __device__ __forceinline__ uint32_t encode(uint32_t bits, uint32_t byte, uint32_t random16) {
-  const int smallest = (int)byte + 1 - F::kBias;             // its biased fp32 exponent, at least 1
-  const int e = (int)(bits >> 23);
-  const uint32_t whole = (bits & 0x7fffffu) | (e > 0 ? 0x800000u : 0u);
-  const int under = smallest - max(e, 1);
-  const uint32_t fixed = under <= 0 ? bits - ((uint32_t)(smallest - 1) << 23) : whole >> min(under, 31);
+  const uint32_t smallest = byte + 1 - F::kBias;             // its biased fp32 exponent, at least 1
+  // in units of 2^-23 of that exponent; the multiplication is exact where the number is below 2^23 of them, the conversion cuts
+  const uint32_t low = (uint32_t)__builtin_ldexpf(__uint_as_float(bits), 150 - (int)smallest);
+  const uint32_t fixed = bits < smallest << 23 ? low : bits - ((smallest - 1) << 23);
   return (fixed + (random16 << 4)) >> 20;
 }
 
-// Largest of the 32 elements of the four lanes that share a block.
+// Largest of the 32 elements of the eight lanes that share a block; a NaN counts as an infinity, since no maximum drops that.
 __device__ __forceinline__ float block_max(const float* x) {
-  float a = fabsf(x[0]);
-  bool bad = x[0] != x[0];
+  float a = 0.f;
 #pragma unroll
-  for (int k = 1; k < 8; ++k) {
-    a = fmaxf(a, fabsf(x[k]));
-    bad |= x[k] != x[k];
-  }
-  if (bad) a = __builtin_inff();                             // a NaN counts as an infinity: no maximum drops it
+  for (int k = 0; k < kVector; ++k) a = fmaxf(a, x[k] == x[k] ? fabsf(x[k]) : __builtin_inff());
   a = fmaxf(a, dpp_move<kDppQuadXor1>(a));
-  return fmaxf(a, dpp_move<kDppQuadXor2>(a));
+  a = fmaxf(a, dpp_move<kDppQuadXor2>(a));
+  return fmaxf(a, dpp_move<kDppRowHalfMirror>(a));
 }
 
-__device__ __forceinline__ u32x2 load_codes(const unsigned char* p, int n) {
-  if (n == 8) return *reinterpret_cast<const u32x2*>(p);
-  u32x2 q = {0u, 0u};
-#pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (k < n) q[k >> 2] |= (uint32_t)p[k] << (8 * (k & 3));
-  return q;
-}
-__device__ __forceinline__ void store_codes(unsigned char* p, int n, u32x2 q) {
-  if (n == 8) {
-    *reinterpret_cast<u32x2*>(p) = q;
+// Vectors of a lane, the last one of a tensor in part.
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, int n, bool whole, float* x) {
+  typedef Pack<T, kVector> P;
+  if (whole) {
+    P::unpack(__builtin_nontemporal_load(reinterpret_cast<const typename P::Any*>(p)), x);
     return;
   }
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (k < n) p[k] = (unsigned char)(q[k >> 2] >> (8 * (k & 3)));
+  for (int k = 0; k < kVector; ++k) x[k] = k < n ? Vec<T>::load1(p + k) : 0.f;
 }
-__device__ __forceinline__ uint32_t byte_of(u32x2 q, int k) { return (q[k >> 2] >> (8 * (k & 3))) & 255u; }
+template <typename T>
+__device__ __forceinline__ void store4(T* p, int n, bool whole, const float* x) {
+  typedef Pack<T, kVector> P;
+  if (whole) {
+    __builtin_nontemporal_store((typename P::Any)P::pack(x), reinterpret_cast<typename P::Any*>(p));
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kVector; ++k)
+    if (k < n) Vec<T>::store1(p + k, x[k]);
+}
+__device__ __forceinline__ uint32_t load_codes(const unsigned char* p, int n, bool whole) {
+  if (whole) return __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
+  uint32_t q = 0;
+#pragma unroll
+  for (int k = 0; k < kVector; ++k)
+    if (k < n) q |= (uint32_t)p[k] << (8 * k);
+  return q;
+}
+__device__ __forceinline__ void store_codes(unsigned char* p, int n, bool whole, uint32_t q) {
+  if (whole) {
+    __builtin_nontemporal_store(q, reinterpret_cast<uint32_t*>(p));
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kVector; ++k)
+    if (k < n) p[k] = (unsigned char)(q >> (8 * k));
+}
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, float* x) {
-  if (n == 8) Eight<T>::unpack(Eight<T>::load(p), x);
-  else load_some(p, n, x);
-}
-template <typename T>
-__device__ __forceinline__ void store8(T* p, int n, const float* x) {
-  if (n == 8) Eight<T>::store(p, x);
-  else store_some(p, n, x);
+// A lane's part of a chunk.  WHOLE: every element of the chunk is there.
+template <typename P, typename G, bool BYTES, bool WHOLE>
+__device__ __forceinline__ void step_chunk(const Tensor& t, const Rule& rule, size_t base) {
+  size_t at[kVectors];
+  int n[kVectors];
+  float p[kVectors][kVector], g[kVectors][kVector], m[kVectors][kVector], v[kVectors][kVector];
+  uint32_t mc[kVectors], vc[kVectors], ms[kVectors], vs[kVectors];
+#pragma unroll
+  for (int i = 0; i < kVectors; ++i) {
+    at[i] = base + kVector * (i * kThreads + threadIdx.x);
+    n[i] = WHOLE ? kVector : (int)min(max((long long)t.n - (long long)at[i], 0LL), (long long)kVector);
+    const bool whole = WHOLE || n[i] == kVector;
+    load4(static_cast<const P*>(t.p) + at[i], n[i], whole, p[i]);
+    load4(static_cast<const G*>(t.g) + at[i], n[i], whole, g[i]);
+    if constexpr (BYTES) {
+      mc[i] = load_codes(static_cast<const unsigned char*>(t.m) + at[i], n[i], whole);
+      vc[i] = load_codes(static_cast<const unsigned char*>(t.v) + at[i], n[i], whole);
+      ms[i] = WHOLE || n[i] > 0 ? t.ms[at[i] >> 5] : 0;
+      vs[i] = WHOLE || n[i] > 0 ? t.vs[at[i] >> 5] : 0;
+    } else {
+      load4(static_cast<const float*>(t.m) + at[i], n[i], whole, m[i]);
+      load4(static_cast<const float*>(t.v) + at[i], n[i], whole, v[i]);
+    }
+  }
+  const Now now(rule);
+#pragma unroll
+  for (int i = 0; i < kVectors; ++i) {
+    const bool whole = WHOLE || n[i] == kVector;
+    double mb = now.b1, vb = now.b2;                         // what the moments' numbers are multiplied by
+    if constexpr (BYTES) {
+      mb *= decode_factor<First>(ms[i]);
+      vb *= decode_factor<Second>(vs[i]);
+#pragma unroll
+      for (int j = 0; j < kVector; ++j) {
+        m[i][j] = code_bits<First>(mc[i] >> (8 * j) & 255u);
+        v[i][j] = code_bits<Second>(vc[i] >> (8 * j) & 255u);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kVector; ++j) {
+      const double gs = (double)g[i][j];
+      m[i][j] = (float)__builtin_fma(mb, (double)m[i][j], now.g1 * gs);
+      v[i][j] = (float)__builtin_fma(vb, (double)v[i][j], now.g2 * (gs * gs));
+      if (!WHOLE && j >= n[i]) m[i][j] = v[i][j] = 0.f;
+      const float ahead = m[i][j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i][j] * now.c2) + rule.eps);
+      p[i][j] -= __builtin_fmaf(now.decay, p[i][j], now.rate * ahead);
+    }
+    store4(static_cast<P*>(t.p) + at[i], n[i], whole, p[i]);
+    if (t.copy != nullptr) store4(t.copy + at[i], n[i], whole, p[i]);
+    if constexpr (BYTES) {
+      const uint32_t mbyte = scale_byte<First>(block_max(m[i])), vbyte = scale_byte<Second>(block_max(v[i]));
+      const uint32_t key = mix(mix(rule.seed ^ (uint32_t)now.step * kPhi) ^ t.number * kPhi);
+      const uint32_t place = (uint32_t)at[i] * kPhi;
+      uint32_t a = 0, b = 0;
+#pragma unroll
+      for (int j = 0; j < kVector; ++j) {
+        const uint32_t random = mix((place + j * kPhi) ^ key);
+        const uint32_t mbits = __float_as_uint(m[i][j]), vbits = __float_as_uint(v[i][j]);
+        const uint32_t first = encode<First>(mbits & 0x7fffffffu, mbyte, random & 0xffffu) | (mbits >> 24 & 128u);
+        uint32_t second = encode<Second>(vbits, vbyte, random >> 16);
+        if (vbits != 0) second = max(second, 1u);
+        a |= first << (8 * j);
+        b |= second << (8 * j);
+      }
+      if (mbyte == 255) a = 0;
+      if (vbyte == 255) b = 0;
+      store_codes(static_cast<unsigned char*>(t.m) + at[i], n[i], whole, a);
+      store_codes(static_cast<unsigned char*>(t.v) + at[i], n[i], whole, b);
+      if ((threadIdx.x & 7) == 0 && (WHOLE || n[i] > 0)) {
+        t.ms[at[i] >> 5] = (unsigned char)mbyte;
+        t.vs[at[i] >> 5] = (unsigned char)vbyte;
+      }
+    } else {
+      store4(static_cast<float*>(t.m) + at[i], n[i], whole, m[i]);
+      store4(static_cast<float*>(t.v) + at[i], n[i], whole, v[i]);
+    }
+  }
 }
 
 template <typename P, typename G, bool BYTES>
@@ -150,76 +260,9 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Batch batch, Rule rule)
 #pragma unroll
   for (int i = 1; i < kTensors; ++i) k += blockIdx.x >= batch.first[i] ? 1 : 0;
   const Tensor t = batch.t[k];
-  const size_t at = (size_t)(blockIdx.x - batch.first[k]) * kChunk + 8 * threadIdx.x;
-  if (!BYTES && at >= t.n) return;
-  const int n = (int)min((long long)t.n - (long long)min(at, (size_t)t.n), 8LL);    // lanes past the end help with a block's scale
-  const long long step = rule.step_dev != nullptr ? *rule.step_dev : rule.step;
-  const float lr = rule.lr_dev != nullptr ? *rule.lr_dev : rule.lr;
-  const double scale = rule.grad_scale != nullptr ? (double)*rule.grad_scale : 1.0;
-  const float c1 = (float)(1.0 / (1.0 - power(rule.b1, step))), c2 = (float)(1.0 / (1.0 - power(rule.b2, step)));
-  float p[8], g[8];
-  load8(static_cast<const P*>(t.p) + at, n, p);
-  load8(static_cast<const G*>(t.g) + at, n, g);
-  double m[8] = {}, v[8] = {};
-  if constexpr (BYTES) {
-    if (n > 0) {
-      const u32x2 mc = load_codes(static_cast<const unsigned char*>(t.m) + at, n), vc = load_codes(static_cast<const unsigned char*>(t.v) + at, n);
-      const double mf = decode_factor<First>(t.ms[at >> 5]), vf = decode_factor<Second>(t.vs[at >> 5]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        m[j] = decode<First>(byte_of(mc, j), mf);
-        v[j] = decode<Second>(byte_of(vc, j), vf);
-      }
-    }
-  } else {
-    float x[8];
-    load8(static_cast<const float*>(t.m) + at, n, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) m[j] = (double)x[j];
-    load8(static_cast<const float*>(t.v) + at, n, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (double)x[j];
-  }
-  float m1[8], v1[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const double gs = (double)g[j] * scale;
-    m1[j] = j < n ? (float)(rule.b1 * m[j] + (1.0 - rule.b1) * gs) : 0.f;
-    v1[j] = j < n ? (float)(rule.b2 * v[j] + (1.0 - rule.b2) * (gs * gs)) : 0.f;
-    p[j] -= lr * (rule.decay * p[j] + m1[j] * c1 / (sqrtf(v1[j] * c2) + rule.eps));
-  }
-  if (n > 0) {
-    store8(static_cast<P*>(t.p) + at, n, p);
-    if (t.copy != nullptr) store8(t.copy + at, n, p);
-  }
-  if constexpr (BYTES) {
-    const uint32_t mb = scale_byte<First>(block_max(m1)), vb = scale_byte<Second>(block_max(v1));
-    if (n <= 0) return;
-    const uint32_t key = mix(mix(rule.seed ^ (uint32_t)step * kPhi) ^ t.number * kPhi);
-    u32x2 mc = {0u, 0u}, vc = {0u, 0u};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const uint32_t random = mix(((uint32_t)at + j) * kPhi ^ key);
-      const uint32_t mbits = __float_as_uint(m1[j]), vbits = __float_as_uint(v1[j]);
-      uint32_t a = encode<First>(mbits & 0x7fffffffu, mb, random & 0xffffu);
-      uint32_t b = encode<Second>(vbits, vb, random >> 16);
-      if (vbits != 0) b = max(b, 1u);
-      a |= mbits >> 31 << 7;
-      if (mb == 255) a = 0;
-      if (vb == 255) b = 0;
-      mc[j >> 2] |= a << (8 * (j & 3));
-      vc[j >> 2] |= b << (8 * (j & 3));
-    }
-    store_codes(static_cast<unsigned char*>(t.m) + at, n, mc);
-    store_codes(static_cast<unsigned char*>(t.v) + at, n, vc);
-    if ((threadIdx.x & 3) == 0) {
-      t.ms[at >> 5] = (unsigned char)mb;
-      t.vs[at >> 5] = (unsigned char)vb;
-    }
-  } else {
-    store8(static_cast<float*>(t.m) + at, n, m1);
-    store8(static_cast<float*>(t.v) + at, n, v1);
-  }
+  const size_t base = (size_t)(blockIdx.x - batch.first[k]) * kChunk;
+  if (base + kChunk <= t.n) step_chunk<P, G, BYTES, true>(t, rule, base);
+  else step_chunk<P, G, BYTES, false>(t, rule, base);
 }
 
 template <typename F, typename T>
@@ -229,12 +272,15 @@ __global__ __launch_bounds__(kThreads) void adamw_values_kernel(const unsigned c
   const long long at = 8 * ((long long)blockIdx.x * kThreads + threadIdx.x);
   if (at >= n) return;
   const int here = (int)min(n - at, 8LL);
-  const u32x2 q = load_codes(codes + at, here);
   const double factor = decode_factor<F>(scales[at >> 5]);
+  uint32_t q[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) q[k] = load_codes(codes + at + 4 * k, here - 4 * k, here >= 4 * k + 4);
   float x[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = (float)decode<F>(byte_of(q, j), factor);
-  store8(out + at, here, x);
+  for (int j = 0; j < 8; ++j) x[j] = (float)((double)code_bits<F>(q[j >> 2] >> (8 * (j & 3)) & 255u) * factor);
+  if (here == 8) Eight<T>::store(out + at, x);
+  else store_some(out + at, here, x);
 }
 
 }  // namespace
@@ -242,7 +288,8 @@ __global__ __launch_bounds__(kThreads) void adamw_values_kernel(const unsigned c
 int launch_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, int n_tensors, const ais_adamw_params& p,
                       const float* grad_scale, const long long* step_dev, const float* lr_dev) {
   ScopedTimer timer(ctx, AIS_K_ADAMW);
-  const Rule rule{p.beta1, p.beta2, (float)p.lr, (float)p.eps, (float)p.weight_decay, p.seed, p.step, grad_scale, step_dev, lr_dev};
+  auto correction = [&](double b) { return step_dev == nullptr ? 1.0 / (1.0 - power(b, p.step)) : 1.0; };
+  const Rule rule{p.beta1, p.beta2, correction(p.beta1), correction(p.beta2), (float)p.lr, (float)p.eps, (float)p.weight_decay, p.seed, p.step, grad_scale, step_dev, lr_dev};
   hipError_t error = hipSuccess;
   auto run = [&](auto kernel, int param_dtype, int grad_dtype) {
     Batch batch;

@@ -1,5 +1,4 @@
-// Groups of eight consecutive elements of bf16, fp32 or 8-bit arrays that begin at any element: what a lane of the kernels here
-// loads, computes in fp32 and stores.
+// Groups of consecutive elements of bf16 or fp32 arrays that begin at any element: what a lane loads, computes in fp32 and stores.
 #pragma once
 
 #include "device_utils.h"
@@ -41,6 +40,33 @@ template <> struct Eight<float> {
     __builtin_nontemporal_store((Any)Vec<float>::pack(x), reinterpret_cast<Any*>(p));
     __builtin_nontemporal_store((Any)Vec<float>::pack(x + 4), reinterpret_cast<Any*>(p) + 1);
   }
+};
+
+// N elements that a lane loads and stores at once, from any element on: 16 bytes, or 8 of bf16 beside 16 of fp32.
+template <typename T, int N> struct Pack {
+  typedef u32x4 Raw;
+  typedef typename Unaligned<T>::four Any;
+  static __device__ __forceinline__ void unpack(Raw q, float* x) { Vec<T>::unpack(q, x); }
+  static __device__ __forceinline__ Raw pack(const float* x) { return Vec<T>::pack(x); }
+  static __device__ __forceinline__ Raw zero() { return Raw{0u, 0u, 0u, 0u}; }
+};
+template <> struct Pack<bf16_t, 4> {
+  typedef u32x2 Raw;
+  typedef Unaligned<bf16_t>::two Any;
+  static __device__ __forceinline__ void unpack(Raw q, float* x) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      x[2 * k] = __uint_as_float(q[k] << 16);
+      x[2 * k + 1] = __uint_as_float(q[k] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ Raw pack(const float* x) {
+    Raw q;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) q[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * k], x[2 * k + 1]}, bf16x2));
+    return q;
+  }
+  static __device__ __forceinline__ Raw zero() { return Raw{0u, 0u}; }
 };
 
 // The first n (1 to 7) of eight elements, the others 0.

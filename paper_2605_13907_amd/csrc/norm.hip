@@ -118,33 +118,6 @@ __device__ __forceinline__ float sum_of(const float* x) {
   else return a + ((x[4] + x[5]) + (x[6] + x[7]));
 }
 
-// N elements that a lane loads and stores at once, from any element on: 16 bytes, or 8 of bf16 beside 16 of fp32.
-template <typename T, int N> struct Pack {
-  typedef u32x4 Raw;
-  typedef typename Unaligned<T>::four Any;
-  static __device__ __forceinline__ void unpack(Raw q, float* x) { Vec<T>::unpack(q, x); }
-  static __device__ __forceinline__ Raw pack(const float* x) { return Vec<T>::pack(x); }
-  static __device__ __forceinline__ Raw zero() { return Raw{0u, 0u, 0u, 0u}; }
-};
-template <> struct Pack<bf16_t, 4> {
-  typedef u32x2 Raw;
-  typedef Unaligned<bf16_t>::two Any;
-  static __device__ __forceinline__ void unpack(Raw q, float* x) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      x[2 * k] = __uint_as_float(q[k] << 16);
-      x[2 * k + 1] = __uint_as_float(q[k] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ Raw pack(const float* x) {
-    Raw q;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) q[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * k], x[2 * k + 1]}, bf16x2));
-    return q;
-  }
-  static __device__ __forceinline__ Raw zero() { return Raw{0u, 0u}; }
-};
-
 // A row of up to NV vectors of N elements to a thread of the THREADS that share it: those past the row's last repeat it and are left
 // out of the sums.  The elements after the last vector are one each of the first threads.  WHOLE: every thread has all of its vectors.
 template <typename T, int N, int THREADS, int NV, bool WHOLE>

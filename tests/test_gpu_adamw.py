@@ -158,6 +158,15 @@ def test_magnitudes(ctx, size):
             twin.check_step(ctx, grads_of(sizes, [torch.float32], step, size))
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_subnormal_second_moments(ctx, bits):
+    """Squares below fp32's normal numbers are as good as others beside an eps that is smaller still; they are held to 2^-149, which a
+    root takes half of."""
+    twin = Twin([tensor(256, torch.float32, 1)], bits)
+    twin.check_step(ctx, [torch.full((256,), 3e-19, device="cuda")], eps=1e-30)
+    twin.check_step(ctx, [torch.full((256,), -2e-19, device="cuda")], eps=1e-30)
+
+
 def test_blocks_of_zeros_and_of_one_number(ctx):
     g = torch.zeros(160, device="cuda")
     g[40] = 3.0
