@@ -572,22 +572,25 @@ void ais_adamw_params_default(ais_adamw_params* p);
  *   mix(x) = y ^ (y >> 16), y = (x ^ (x >> 15)) 0x6A09E667 mod 2^32;      key = mix(mix(seed ^ step P) ^ tensor P), P = 0x9E3779B1
  *   bits = mix(index P ^ key)
  * v > 0 never becomes 0.  A block with a NaN or infinity has byte 255 and stands for NaN.
- *   tensors     HOST array of n_tensors, read before the call returns; arrays of different tensors must not overlap, but for grads
+ *   tensors     HOST array of n_tensors, read before the call returns; one with grad NULL is left as it is.  Arrays of different tensors
+ *               must not overlap, but for grads
+ *   table       the same array in DEVICE memory, 8-byte aligned, which the caller keeps from step to step; its grad and grad_dtype are not
+ *               looked at
  *   grad_scale  one fp32 in device memory, or NULL (1): a factor from a clipped norm or a loss scale
  *   step_dev, lr_dev   one int64 and one fp32 in device memory that replace params->step and params->lr, or NULL: what a HIP graph
  *               that is replayed needs (the step is read, not counted)
- * One launch for each 48 tensors of the same types; no workspace.
- * Errors: NULL tensors (with n_tensors > 0) / params, n_tensors < 0, n < 0 or >= 2^32 - 4096, NULL or misaligned arrays of a tensor
- * with n > 0, unknown dtypes, parameters outside their ranges, step < 1 without step_dev (AIS_ERR_PARAM). */
-int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, int n_tensors, const ais_adamw_params* params,
-                   const float* grad_scale, const long long* step_dev, const float* lr_dev);
+ * One launch for each 320 tensors; no workspace.
+ * Errors: NULL tensors or table (with n_tensors > 0) / params, n_tensors < 0, n < 0 or >= 2^32 - 4096, more than 2^42 elements in all, NULL
+ * or misaligned arrays of a tensor that is stepped, a misaligned table, unknown dtypes, parameters outside their ranges, step < 1 without step_dev (AIS_ERR_PARAM). */
+int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, const ais_adamw_tensor* table, int n_tensors,
+                   const ais_adamw_params* params, const float* grad_scale, const long long* step_dev, const float* lr_dev);
 
 /* What the codes of 8-bit moments stand for (the other half of the round trip, as in Sec. 2.1), exactly in either type (but where bf16 or fp32 has no number as small).
- *   codes       [n] bytes, 16-byte aligned;  scales  [ceil(n / 32)] bytes;  moment  1 (signed) or 2
- *   values_out  [n] of `dtype`
- * Errors: NULL arrays (with n > 0), n < 0 or above 2^40, moment outside {1, 2} (AIS_ERR_PARAM), misaligned arrays, unknown dtype. */
-int ais_adamw_values(ais_ctx* ctx, const unsigned char* codes, const unsigned char* scales, long long n, int moment,
-                     void* values_out, ais_dtype dtype);
+ *   m, v        [n] bytes, 16-byte aligned;  m_scale, v_scale  [ceil(n / 32)] bytes
+ *   m_out, v_out   [n] of `dtype`, either NULL where it is not wanted, with its arrays
+ * Errors: NULL arrays of a moment that is wanted, neither wanted (with n > 0), n < 0 or above 2^40, misaligned arrays, unknown dtype. */
+int ais_adamw_values(ais_ctx* ctx, const unsigned char* m, const unsigned char* m_scale, const unsigned char* v,
+                     const unsigned char* v_scale, long long n, void* m_out, void* v_out, ais_dtype dtype);
 
 /* ---- measurement helpers -------------------------------------------------------------------- */
 

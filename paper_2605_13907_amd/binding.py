@@ -118,8 +118,8 @@ SYMBOLS = {
     "ais_norm_rows": (_I, [_P, _P, _I, _LL, _LL, _LL, _P, _P, _P, _I, _F, _I, _P, _LL, _P, _P]),
     "ais_norm_rows_grad": (_I, [_P, _P, _I, _LL, _P, _I, _LL, _LL, _LL, _P, _P, _I, _P, _P, _P, _LL, _P, _P]),
     "ais_adamw_params_default": (None, [C.POINTER(AisAdamWParams)]),
-    "ais_adamw_step": (_I, [_P, C.POINTER(AisAdamWTensor), _I, C.POINTER(AisAdamWParams), _P, _P, _P]),
-    "ais_adamw_values": (_I, [_P, _P, _P, _LL, _I, _P, _I]),
+    "ais_adamw_step": (_I, [_P, C.POINTER(AisAdamWTensor), _P, _I, C.POINTER(AisAdamWParams), _P, _P, _P]),
+    "ais_adamw_values": (_I, [_P, _P, _P, _P, _P, _LL, _P, _P, _I]),
     "ais_profile": (_I, [_P, _I]),
     "ais_profile_read": (_I, [_P, _I, C.POINTER(_F), C.POINTER(_I)]),
     "ais_copy": (_I, [_P, _P, _P, _LL]),
@@ -334,6 +334,8 @@ class AdamWState:
             if bits == 8:
                 row.m_scale, row.v_scale = self.m_scale.data_ptr() + at // MOMENT_BLOCK, self.v_scale.data_ptr() + at // MOMENT_BLOCK
             row.n, row.param_dtype = p.numel(), _dtype_code(p)
+        # the same in device memory, for good
+        self._on_gpu = torch.frombuffer(bytearray(self._table), dtype=torch.uint8).to(self.device)
         self._rule = AisAdamWParams()
         _lib().ais_adamw_params_default(C.byref(self._rule))
         self._rule.state_bits, self._rule.seed = bits, self.seed
@@ -878,7 +880,7 @@ class AisContext:
         r.step = 0 if on_gpu else step + 1
         dev = self.device
         if not on_gpu:
-            out = self._native("adamw_step", C.addressof(state._table), C.addressof(r), state.params, state.copies, state.m, state.v,
+            out = self._native("adamw_step", C.addressof(state._table), state._on_gpu, C.addressof(r), state.params, state.copies, state.m, state.v,
                                state.m_scale, state.v_scale, grads, grad_scale, lr_dev)
             if out is not None:
                 state.step = step + 1
@@ -899,19 +901,19 @@ class AisContext:
             if copy is not None and copy.data_ptr() != (row.copy or 0):
                 raise ValueError(f"copies[{i}] is not where it was when the state was made")
             if g is None:
-                row.n = 0
+                row.grad = None
                 continue
             if not isinstance(g, torch.Tensor):
                 raise TypeError(f"grads[{i}] must be a torch.Tensor")
             row.grad_dtype = _dtype_code(g, f"grads[{i}]")
-            row.grad = _ptr(g, None, p.numel(), f"grads[{i}]", dev)
+            row.grad = _ptr(g, None, p.numel(), f"grads[{i}]", dev) or None
         scale_ptr, lr_ptr = _ptr(grad_scale, torch.float32, 1, "grad_scale", dev), _ptr(lr_dev, torch.float32, 1, "lr", dev)
         self._sync_stream()
         step_ptr = None
         if on_gpu:
             step.add_(1)
             step_ptr = step.data_ptr()
-        rc = self._lib.ais_adamw_step(self._h, table, len(grads), C.byref(r), scale_ptr, step_ptr, lr_ptr)
+        rc = self._lib.ais_adamw_step(self._h, table, state._on_gpu.data_ptr(), len(grads), C.byref(r), scale_ptr, step_ptr, lr_ptr)
         if rc != 0:
             if on_gpu:
                 step.sub_(1)                                     # nothing was launched
@@ -931,16 +933,14 @@ class AisContext:
         out = self._native("adamw_values", state.m, state.m_scale, state.v, state.v_scale, 1 if dtype is torch.bfloat16 else 0)
         if out is not None:
             return out
-        out = []
-        for moment, codes, scales in ((1, state.m, state.m_scale), (2, state.v, state.v_scale)):
-            values = torch.empty(codes.numel(), dtype=dtype, device=self.device)
-            self._sync_stream()
-            rc = self._lib.ais_adamw_values(self._h, codes.data_ptr(), scales.data_ptr(), codes.numel(), moment, _ptr(values),
-                                            _dtype_code(values))
-            if rc != 0:
-                raise AisError(rc, "ais_adamw_values")
-            out.append(values)
-        return tuple(out)
+        m, v = (torch.empty(state.m.numel(), dtype=dtype, device=self.device) for _ in range(2))
+        ptrs = [_ptr(t, torch.uint8, None, name, self.device) for name, t in (("m", state.m), ("m_scale", state.m_scale), ("v", state.v),
+                                                                             ("v_scale", state.v_scale))]
+        self._sync_stream()
+        rc = self._lib.ais_adamw_values(self._h, *ptrs, state.m.numel(), _ptr(m), _ptr(v), _dtype_code(m))
+        if rc != 0:
+            raise AisError(rc, "ais_adamw_values")
+        return m, v
 
     # ------------------------------------------------------------------ log-probs without materialised logits
     def lm_head_logprob(self, hidden, weight, token_ids, valid=None, inv_temperature: float = 1.0):

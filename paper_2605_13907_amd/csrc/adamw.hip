@@ -3,8 +3,9 @@
 //   m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,  p <- p - lr (wd p + m / c1 / (sqrt(v / c2) + eps)),  c = 1 - b^step
 //
 // Bound by memory: every array is read once and written once, 28 bytes an element with fp32 arrays and 16.1 with 8-bit moments.
-// The tensors' addresses are kernel arguments, so that a call copies nothing to the GPU and can be recorded.  A lane takes eight
-// consecutive elements; four lanes have a block of 32 whose 8-bit moments share a scale.
+// The gradients' addresses, which change from step to step, are kernel arguments, so that a call copies nothing to the GPU and can be
+// recorded; all else about the tensors lies in a table on the GPU.  A lane takes vectors of four consecutive elements; eight lanes have a
+// block of 32 whose 8-bit moments share a scale.
 //
 // The moments are formed in 64 bits (the GPU's fp64 is as fast as its fp32) and rounded to fp32: which of two 8-bit codes a value
 // goes to depends on its last bits.
@@ -22,20 +23,15 @@ constexpr int kThreads = 256;
 constexpr int kVector = 4;                       // elements that a lane loads at once: 16 bytes of fp32
 constexpr int kVectors = 2;                      // of a lane, all on their way together
 constexpr int kChunk = kVector * kVectors * kThreads;        // elements of a workgroup
-constexpr int kTensors = 48;                     // of a launch: their addresses are 3.3 of the 4 KiB of kernel arguments
+constexpr int kTensors = 320;                    // of a launch: a gradient's address and a number each, of the 4 KiB of kernel arguments
 
-struct Tensor {
-  void* p;
-  const void* g;
-  bf16_t* copy;
-  void *m, *v;
-  unsigned char *ms, *vs;
-  unsigned n, number;
-};
+// What a launch carries: of each tensor where its gradient is, with 1 added if that is bf16, and the workgroup that it begins with.  One that
+// is left out begins where the next one does; past the last tensor: 2^32 - 1.
 struct Batch {
-  Tensor t[kTensors];
-  unsigned first[kTensors];                      // workgroup that a tensor begins with; past the last tensor: 2^32 - 1
+  uintptr_t grad[kTensors];
+  unsigned first[kTensors];
 };
+static_assert(sizeof(Batch) + 128 <= 4096, "");
 
 struct Rule {
   double b1, b2;
@@ -177,7 +173,7 @@ __device__ __forceinline__ void store_codes(unsigned char* p, int n, bool whole,
 
 // A lane's part of a chunk.  WHOLE: every element of the chunk is there.
 template <typename P, typename G, bool BYTES, bool WHOLE>
-__device__ __forceinline__ void step_chunk(const Tensor& t, const Rule& rule, size_t base) {
+__device__ __forceinline__ void step_chunk(const ais_adamw_tensor& t, const G* grad, int number, const Rule& rule, size_t base) {
   size_t at[kVectors];
   int n[kVectors];
   float p[kVectors][kVector], g[kVectors][kVector], m[kVectors][kVector], v[kVectors][kVector];
@@ -187,13 +183,13 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, const Rule& rule, si
     at[i] = base + kVector * (i * kThreads + threadIdx.x);
     n[i] = WHOLE ? kVector : (int)min(max((long long)t.n - (long long)at[i], 0LL), (long long)kVector);
     const bool whole = WHOLE || n[i] == kVector;
-    load4(static_cast<const P*>(t.p) + at[i], n[i], whole, p[i]);
-    load4(static_cast<const G*>(t.g) + at[i], n[i], whole, g[i]);
+    load4(static_cast<const P*>(t.param) + at[i], n[i], whole, p[i]);
+    load4(grad + at[i], n[i], whole, g[i]);
     if constexpr (BYTES) {
       mc[i] = load_codes(static_cast<const unsigned char*>(t.m) + at[i], n[i], whole);
       vc[i] = load_codes(static_cast<const unsigned char*>(t.v) + at[i], n[i], whole);
-      ms[i] = WHOLE || n[i] > 0 ? t.ms[at[i] >> 5] : 0;
-      vs[i] = WHOLE || n[i] > 0 ? t.vs[at[i] >> 5] : 0;
+      ms[i] = WHOLE || n[i] > 0 ? t.m_scale[at[i] >> 5] : 0;
+      vs[i] = WHOLE || n[i] > 0 ? t.v_scale[at[i] >> 5] : 0;
     } else {
       load4(static_cast<const float*>(t.m) + at[i], n[i], whole, m[i]);
       load4(static_cast<const float*>(t.v) + at[i], n[i], whole, v[i]);
@@ -222,11 +218,11 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, const Rule& rule, si
       const float ahead = m[i][j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i][j] * now.c2) + rule.eps);
       p[i][j] -= __builtin_fmaf(now.decay, p[i][j], now.rate * ahead);
     }
-    store4(static_cast<P*>(t.p) + at[i], n[i], whole, p[i]);
-    if (t.copy != nullptr) store4(t.copy + at[i], n[i], whole, p[i]);
+    store4(static_cast<P*>(t.param) + at[i], n[i], whole, p[i]);
+    if (t.copy != nullptr) store4(static_cast<bf16_t*>(t.copy) + at[i], n[i], whole, p[i]);
     if constexpr (BYTES) {
       const uint32_t mbyte = scale_byte<First>(block_max(m[i])), vbyte = scale_byte<Second>(block_max(v[i]));
-      const uint32_t key = mix(mix(rule.seed ^ (uint32_t)now.step * kPhi) ^ t.number * kPhi);
+      const uint32_t key = mix(mix(rule.seed ^ (uint32_t)now.step * kPhi) ^ (uint32_t)number * kPhi);
       const uint32_t place = (uint32_t)at[i] * kPhi;
       uint32_t a = 0, b = 0;
 #pragma unroll
@@ -244,8 +240,8 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, const Rule& rule, si
       store_codes(static_cast<unsigned char*>(t.m) + at[i], n[i], whole, a);
       store_codes(static_cast<unsigned char*>(t.v) + at[i], n[i], whole, b);
       if ((threadIdx.x & 7) == 0 && (WHOLE || n[i] > 0)) {
-        t.ms[at[i] >> 5] = (unsigned char)mbyte;
-        t.vs[at[i] >> 5] = (unsigned char)vbyte;
+        t.m_scale[at[i] >> 5] = (unsigned char)mbyte;
+        t.v_scale[at[i] >> 5] = (unsigned char)vbyte;
       }
     } else {
       store4(static_cast<float*>(t.m) + at[i], n[i], whole, m[i]);
@@ -254,21 +250,34 @@ __device__ __forceinline__ void step_chunk(const Tensor& t, const Rule& rule, si
   }
 }
 
-template <typename P, typename G, bool BYTES>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(Batch batch, Rule rule) {
-  int k = 0;
+// `table`: the tensors from the launch's first on, of which `number` come before.
+template <bool BYTES>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(Batch batch, const ais_adamw_tensor* __restrict__ table, int number, Rule rule) {
+  // every wavefront looks for the workgroup's tensor: the last that begins with it or before it
+  int k = -1;
 #pragma unroll
-  for (int i = 1; i < kTensors; ++i) k += blockIdx.x >= batch.first[i] ? 1 : 0;
-  const Tensor t = batch.t[k];
+  for (int i = 0; i < kTensors; i += 64) k += __popcll(__ballot(batch.first[i + (threadIdx.x & 63)] <= blockIdx.x));
+  k = __builtin_amdgcn_readfirstlane(k);
+  const ais_adamw_tensor t = table[k];
+  const uintptr_t grad = batch.grad[k];
   const size_t base = (size_t)(blockIdx.x - batch.first[k]) * kChunk;
-  if (base + kChunk <= t.n) step_chunk<P, G, BYTES, true>(t, rule, base);
-  else step_chunk<P, G, BYTES, false>(t, rule, base);
+  auto run = [&](auto* param, const auto* g) {
+    typedef std::remove_pointer_t<decltype(param)> P;
+    typedef std::remove_cv_t<std::remove_pointer_t<decltype(g)>> G;
+    if (base + kChunk <= (size_t)t.n) step_chunk<P, G, BYTES, true>(t, g, number + k, rule, base);
+    else step_chunk<P, G, BYTES, false>(t, g, number + k, rule, base);
+  };
+  auto typed = [&](auto* param) {
+    if (grad & 1) run(param, reinterpret_cast<const bf16_t*>(grad - 1));
+    else run(param, reinterpret_cast<const float*>(grad));
+  };
+  if (t.param_dtype == AIS_BF16) typed(static_cast<bf16_t*>(nullptr));
+  else typed(static_cast<float*>(nullptr));
 }
 
 template <typename F, typename T>
-__global__ __launch_bounds__(kThreads) void adamw_values_kernel(const unsigned char* __restrict__ codes,
-                                                                const unsigned char* __restrict__ scales, long long n,
-                                                                T* __restrict__ out) {
+__device__ __forceinline__ void values_of(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
+                                          long long n, T* __restrict__ out) {
   const long long at = 8 * ((long long)blockIdx.x * kThreads + threadIdx.x);
   if (at >= n) return;
   const int here = (int)min(n - at, 8LL);
@@ -282,64 +291,55 @@ __global__ __launch_bounds__(kThreads) void adamw_values_kernel(const unsigned c
   if (here == 8) Eight<T>::store(out + at, x);
   else store_some(out + at, here, x);
 }
+template <typename T>
+__global__ __launch_bounds__(kThreads) void adamw_values_kernel(const unsigned char* m, const unsigned char* m_scale,
+                                                                const unsigned char* v, const unsigned char* v_scale, long long n,
+                                                                T* m_out, T* v_out) {
+  if (blockIdx.y == 0 && m_out != nullptr) values_of<First>(m, m_scale, n, m_out);
+  else values_of<Second>(v, v_scale, n, v_out);
+}
 
 }  // namespace
 
-int launch_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, int n_tensors, const ais_adamw_params& p,
-                      const float* grad_scale, const long long* step_dev, const float* lr_dev) {
+int launch_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, const ais_adamw_tensor* table, int n_tensors,
+                      const ais_adamw_params& p, const float* grad_scale, const long long* step_dev, const float* lr_dev) {
   ScopedTimer timer(ctx, AIS_K_ADAMW);
   auto correction = [&](double b) { return step_dev == nullptr ? 1.0 / (1.0 - power(b, p.step)) : 1.0; };
-  const Rule rule{p.beta1, p.beta2, correction(p.beta1), correction(p.beta2), (float)p.lr, (float)p.eps, (float)p.weight_decay, p.seed, p.step, grad_scale, step_dev, lr_dev};
-  hipError_t error = hipSuccess;
-  auto run = [&](auto kernel, int param_dtype, int grad_dtype) {
+  const Rule rule{p.beta1, p.beta2, correction(p.beta1), correction(p.beta2), (float)p.lr, (float)p.eps, (float)p.weight_decay,
+                  p.seed, p.step, grad_scale, step_dev, lr_dev};
+  for (int from = 0; from < n_tensors; from += kTensors) {
     Batch batch;
-    int held = 0;
     unsigned blocks = 0;
-    auto flush = [&] {
-      if (held == 0) return;
-      for (int k = held; k < kTensors; ++k) batch.first[k] = 0xffffffffu;
-      kernel<<<dim3(blocks), dim3(kThreads), 0, ctx->stream>>>(batch, rule);
-      if (error == hipSuccess) error = hipGetLastError();
-      held = 0;
-      blocks = 0;
-    };
-    for (int i = 0; i < n_tensors; ++i) {
-      const ais_adamw_tensor& t = tensors[i];
-      if (t.n == 0 || t.param_dtype != param_dtype || t.grad_dtype != grad_dtype) continue;
-      batch.t[held] = {t.param, t.grad, static_cast<bf16_t*>(t.copy), t.m, t.v, t.m_scale, t.v_scale, (unsigned)t.n, (unsigned)i};
-      batch.first[held++] = blocks;
+    for (int k = 0; k < kTensors; ++k) {
+      const bool there = from + k < n_tensors;
+      batch.first[k] = there ? blocks : 0xffffffffu;
+      batch.grad[k] = 0;
+      if (!there || tensors[from + k].grad == nullptr) continue;
+      const ais_adamw_tensor& t = tensors[from + k];
+      batch.grad[k] = reinterpret_cast<uintptr_t>(t.grad) + (t.grad_dtype == AIS_BF16 ? 1 : 0);
       blocks += (unsigned)((t.n + kChunk - 1) / kChunk);
-      if (held == kTensors) flush();
     }
-    flush();
-  };
-  auto types = [&](auto bytes) {
-    constexpr bool kBytes = decltype(bytes)::value;
-    run(adamw_kernel<float, float, kBytes>, AIS_F32, AIS_F32);
-    run(adamw_kernel<float, bf16_t, kBytes>, AIS_F32, AIS_BF16);
-    run(adamw_kernel<bf16_t, float, kBytes>, AIS_BF16, AIS_F32);
-    run(adamw_kernel<bf16_t, bf16_t, kBytes>, AIS_BF16, AIS_BF16);
-  };
-  if (p.state_bits == 8) types(std::true_type{});
-  else types(std::false_type{});
-  return hip_fail(ctx, error);
+    if (blocks == 0) continue;
+    auto kernel = p.state_bits == 8 ? adamw_kernel<true> : adamw_kernel<false>;
+    kernel<<<dim3(blocks), dim3(kThreads), 0, ctx->stream>>>(batch, table + from, from, rule);
+    const int rc = hip_fail(ctx, hipGetLastError());
+    if (rc != AIS_OK) return rc;
+  }
+  return AIS_OK;
 }
 
-int launch_adamw_values(ais_ctx* ctx, const unsigned char* codes, const unsigned char* scales, long long n, int moment,
-                        void* out, ais_dtype dtype) {
-  if (n == 0) return AIS_OK;
+int launch_adamw_values(ais_ctx* ctx, const unsigned char* m, const unsigned char* m_scale, const unsigned char* v,
+                        const unsigned char* v_scale, long long n, void* m_out, void* v_out, ais_dtype dtype) {
+  const unsigned moments = (m_out != nullptr) + (v_out != nullptr);
+  if (n == 0 || moments == 0) return AIS_OK;
   ScopedTimer timer(ctx, AIS_K_ADAMW);
-  auto run = [&](auto* to, auto format) {
-    typedef std::remove_pointer_t<decltype(to)> T;
-    adamw_values_kernel<decltype(format), T>
-        <<<dim3((unsigned)((n + kChunk - 1) / kChunk)), dim3(kThreads), 0, ctx->stream>>>(codes, scales, n, to);
-  };
-  auto typed = [&](auto* to) {
-    if (moment == 1) run(to, First{});
-    else run(to, Second{});
-  };
-  if (dtype == AIS_BF16) typed(static_cast<bf16_t*>(out));
-  else typed(static_cast<float*>(out));
+  const dim3 grid((unsigned)((n + 8 * kThreads - 1) / (8 * kThreads)), moments);
+  if (dtype == AIS_BF16)
+    adamw_values_kernel<<<grid, dim3(kThreads), 0, ctx->stream>>>(m, m_scale, v, v_scale, n, static_cast<bf16_t*>(m_out),
+                                                                  static_cast<bf16_t*>(v_out));
+  else
+    adamw_values_kernel<<<grid, dim3(kThreads), 0, ctx->stream>>>(m, m_scale, v, v_scale, n, static_cast<float*>(m_out),
+                                                                  static_cast<float*>(v_out));
   return hip_fail(ctx, hipGetLastError());
 }
 

@@ -267,10 +267,10 @@ int launch_norm_rows_grad(ais_ctx* ctx, const void* dy, ais_dtype dy_dtype, long
                           long long n_rows, int width, long long row_stride, const unsigned char* valid, const void* weight,
                           ais_dtype param_dtype, const float* mean, const float* rstd, void* dx, long long dx_stride,
                           float* dweight, float* dbias);
-int launch_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, int n_tensors, const ais_adamw_params& p,
-                      const float* grad_scale, const long long* step_dev, const float* lr_dev);
-int launch_adamw_values(ais_ctx* ctx, const unsigned char* codes, const unsigned char* scales, long long n, int moment,
-                        void* out, ais_dtype dtype);
+int launch_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, const ais_adamw_tensor* table, int n_tensors,
+                      const ais_adamw_params& p, const float* grad_scale, const long long* step_dev, const float* lr_dev);
+int launch_adamw_values(ais_ctx* ctx, const unsigned char* m, const unsigned char* m_scale, const unsigned char* v,
+                        const unsigned char* v_scale, long long n, void* m_out, void* v_out, ais_dtype dtype);
 
 int launch_lm_head_grad_setup(ais_ctx* ctx, const unsigned char* live_mask, long long n_rows, int n_cap, int width,
                               int width_last, int* row_index, int* row_pos, void* dev_plan);

@@ -187,8 +187,8 @@ int check_adamw_tensor(const ais_adamw_tensor& t, int bits) {
   if (t.n < 0 || t.n >= (1LL << 32) - 4096) return AIS_ERR_SIZE;
   if ((t.param_dtype != AIS_BF16 && t.param_dtype != AIS_F32) || (t.grad_dtype != AIS_BF16 && t.grad_dtype != AIS_F32))
     return AIS_ERR_DTYPE;
-  if (t.n == 0) return AIS_OK;
-  if (t.param == nullptr || t.grad == nullptr || t.m == nullptr || t.v == nullptr) return AIS_ERR_NULL;
+  if (t.n == 0 || t.grad == nullptr) return AIS_OK;
+  if (t.param == nullptr || t.m == nullptr || t.v == nullptr) return AIS_ERR_NULL;
   if (bits == 8 && (t.m_scale == nullptr || t.v_scale == nullptr)) return AIS_ERR_NULL;
   if (!aligned_to(t.param, (ais_dtype)t.param_dtype) || !aligned_to(t.grad, (ais_dtype)t.grad_dtype) || !aligned_to(t.copy, AIS_BF16) ||
       reinterpret_cast<uintptr_t>(t.m) % 16 != 0 || reinterpret_cast<uintptr_t>(t.v) % 16 != 0)
@@ -883,34 +883,41 @@ void ais_adamw_params_default(ais_adamw_params* p) {
   p->step = 1;
 }
 
-int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, int n_tensors, const ais_adamw_params* p,
-                   const float* grad_scale, const long long* step_dev, const float* lr_dev) {
-  if (p == nullptr || (n_tensors > 0 && tensors == nullptr)) return AIS_ERR_NULL;
+int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, const ais_adamw_tensor* table, int n_tensors,
+                   const ais_adamw_params* p, const float* grad_scale, const long long* step_dev, const float* lr_dev) {
+  if (p == nullptr || (n_tensors > 0 && (tensors == nullptr || table == nullptr))) return AIS_ERR_NULL;
   if (n_tensors < 0) return AIS_ERR_SIZE;
+  if (reinterpret_cast<uintptr_t>(table) % 8 != 0) return AIS_ERR_ALIGN;
   auto least = [](double v, double lo) { return std::isfinite(v) && v >= lo; };
   if (!least(p->lr, 0.0) || !least(p->eps, 1e-30) || !least(p->weight_decay, 0.0)) return AIS_ERR_PARAM;
   if (!least(p->beta1, 0.0) || p->beta1 >= 1.0 || !least(p->beta2, 0.0) || p->beta2 >= 1.0) return AIS_ERR_PARAM;
   if (p->state_bits != 32 && p->state_bits != 8) return AIS_ERR_PARAM;
   if (p->step < 1 && step_dev == nullptr) return AIS_ERR_PARAM;
+  long long chunks = 0;
   for (int i = 0; i < n_tensors; ++i) {
     const int rc = check_adamw_tensor(tensors[i], p->state_bits);
     if (rc != AIS_OK) return rc;
+    chunks += (tensors[i].n + 2047) / 2048;
   }
+  if (chunks > 0x7fffffffLL) return AIS_ERR_SIZE;      // workgroups of a launch
   if (ctx == nullptr) return AIS_ERR_NULL;
   DeviceGuard guard(ctx->device);
-  return launch_adamw_step(ctx, tensors, n_tensors, *p, grad_scale, step_dev, lr_dev);
+  return launch_adamw_step(ctx, tensors, table, n_tensors, *p, grad_scale, step_dev, lr_dev);
 }
 
-int ais_adamw_values(ais_ctx* ctx, const unsigned char* codes, const unsigned char* scales, long long n, int moment,
-                     void* values_out, ais_dtype dtype) {
+int ais_adamw_values(ais_ctx* ctx, const unsigned char* m, const unsigned char* m_scale, const unsigned char* v,
+                     const unsigned char* v_scale, long long n, void* m_out, void* v_out, ais_dtype dtype) {
   if (dtype != AIS_BF16 && dtype != AIS_F32) return AIS_ERR_DTYPE;
   if (n < 0 || n > 1LL << 40) return AIS_ERR_SIZE;
-  if (moment != 1 && moment != 2) return AIS_ERR_PARAM;
-  if (n > 0 && (codes == nullptr || scales == nullptr || values_out == nullptr)) return AIS_ERR_NULL;
-  if (reinterpret_cast<uintptr_t>(codes) % 16 != 0 || !aligned_to(values_out, dtype)) return AIS_ERR_ALIGN;
+  if (n > 0 && m_out != nullptr && (m == nullptr || m_scale == nullptr)) return AIS_ERR_NULL;
+  if (n > 0 && v_out != nullptr && (v == nullptr || v_scale == nullptr)) return AIS_ERR_NULL;
+  if (n > 0 && m_out == nullptr && v_out == nullptr) return AIS_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(m) % 16 != 0 || reinterpret_cast<uintptr_t>(v) % 16 != 0 || !aligned_to(m_out, dtype) ||
+      !aligned_to(v_out, dtype))
+    return AIS_ERR_ALIGN;
   if (ctx == nullptr) return AIS_ERR_NULL;
   DeviceGuard guard(ctx->device);
-  return launch_adamw_values(ctx, codes, scales, n, moment, values_out, dtype);
+  return launch_adamw_values(ctx, m, m_scale, v, v_scale, n, m_out, v_out, dtype);
 }
 
 int ais_profile(ais_ctx* ctx, int enable) {

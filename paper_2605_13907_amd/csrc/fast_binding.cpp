@@ -654,9 +654,10 @@ AIS_CALL(norm_rows_grad) {
   return rc != 0 ? PyLong_FromLong(rc) : result(dx, dw, db);
 }
 
-// The state's table and rule, parameters, copies and moments, which have to be where the table says; gradients, grad_scale, lr.
+// The state's table, here and on the GPU, and rule; parameters, copies and moments, which have to be where the table says; gradients, grad_scale, lr.
 AIS_CALL(adamw_step) {
   const ais_adamw_tensor* table = static_cast<const ais_adamw_tensor*>(c.pointer());
+  const at::Tensor* on_gpu = c.tensor();
   const ais_adamw_params* rule = static_cast<const ais_adamw_params*>(c.pointer());
   PyObject *params = c.next(), *copies = c.next();
   if (!c.ok || table == nullptr || rule == nullptr || !PyTuple_CheckExact(params) || !PyTuple_CheckExact(copies) ||
@@ -692,10 +693,8 @@ AIS_CALL(adamw_step) {
     if (!one.ok || p->data_ptr() != t[i].param || p->numel() != t[i].n ||
         p->scalar_type() != (t[i].param_dtype == AIS_BF16 ? at::kBFloat16 : at::kFloat))
       AIS_REFUSE;
-    if (skipped) {
-      t[i].n = 0;
-      continue;
-    }
+    t[i].grad = nullptr;
+    if (skipped) continue;
     const at::Tensor* g = one.tensor();
     if (!one.ok || (g->scalar_type() != at::kBFloat16 && g->scalar_type() != at::kFloat) || !g->is_contiguous() ||
         g->numel() != t[i].n)
@@ -703,7 +702,9 @@ AIS_CALL(adamw_step) {
     t[i].grad = g->data_ptr();
     t[i].grad_dtype = g->scalar_type() == at::kBFloat16 ? AIS_BF16 : AIS_F32;
   }
-  const int rc = c.run([&] { return lib.adamw_step(c.ctx, t.data(), (int)n, rule, scale, nullptr, lr); });
+  if (on_gpu->nbytes() != n * sizeof(ais_adamw_tensor)) AIS_REFUSE;
+  const ais_adamw_tensor* there = static_cast<const ais_adamw_tensor*>(on_gpu->data_ptr());
+  const int rc = c.run([&] { return lib.adamw_step(c.ctx, t.data(), there, (int)n, rule, scale, nullptr, lr); });
   if (rc != 0) return PyLong_FromLong(rc);
   Py_RETURN_TRUE;
 }
@@ -725,10 +726,7 @@ AIS_CALL(adamw_values) {
   const at::Tensor m = empty(c.device, {n}, bf16 ? at::kBFloat16 : at::kFloat), v = at::empty_like(m);
   void* out[2] = {m.data_ptr(), v.data_ptr()};
   const int rc = c.run([&] {
-    int bad = 0;
-    for (int k = 0; k < 2 && bad == 0; ++k)
-      bad = lib.adamw_values(c.ctx, codes[k], scales[k], n, k + 1, out[k], bf16 ? AIS_BF16 : AIS_F32);
-    return bad;
+    return lib.adamw_values(c.ctx, codes[0], scales[0], codes[1], scales[1], n, out[0], out[1], bf16 ? AIS_BF16 : AIS_F32);
   });
   return rc != 0 ? PyLong_FromLong(rc) : result(m, v);
 }

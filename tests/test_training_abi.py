@@ -94,22 +94,24 @@ def test_norm_rows_grad():
     assert call(n_rows=0, dy=None, x=None, rstd=None, dx=None) == -1
 
 
-def adamw(tensors=None, n=1, ctx=None, scale=None, step_dev=None, lr_dev=None, **rule):
+def adamw(tensors=None, n=1, ctx=None, table=P, scale=None, step_dev=None, lr_dev=None, **rule):
     p = B.AisAdamWParams()
     B._lib().ais_adamw_params_default(C.byref(p))
     for k, v in rule.items():
         setattr(p, k, v)
     t = dict(param=0x1000, grad=0x2000, copy=None, m=0x3000, v=0x4000, m_scale=0x5000, v_scale=0x5000, n=100, param_dtype=1, grad_dtype=1)
     t.update(tensors or {})
-    return B._lib().ais_adamw_step(ctx, (B.AisAdamWTensor * 2)(B.AisAdamWTensor(**t), B.AisAdamWTensor(**t)), n, C.byref(p), scale, step_dev,
+    return B._lib().ais_adamw_step(ctx, (B.AisAdamWTensor * 2)(B.AisAdamWTensor(**t), B.AisAdamWTensor(**t)), table, n, C.byref(p), scale, step_dev,
                                    lr_dev)
 
 
 def test_adamw_step():
     assert adamw() == -1 and adamw(state_bits=8) == -1 and adamw(n=2) == -1 and adamw(n=0) == -1
     assert adamw(n=-1) == -2
-    for missing in ("param", "grad", "m", "v"):
+    for missing in ("param", "m", "v"):
         assert adamw({missing: None}) == -1
+    assert adamw(table=None) == -1 and adamw(table=C.c_void_p(0x1004)) == -4
+    assert adamw(dict(grad=None, param=None, m=0x3001)) == -1    # not stepped, so nothing else about it counts
     assert adamw(dict(m_scale=None), state_bits=8) == -1 and adamw(dict(m_scale=None)) == -1
     assert adamw(dict(n=-1)) == -2 and adamw(dict(n=2 ** 32 - 4096)) == -2
     assert adamw(dict(n=0, param=None, grad=None, m=None, v=None)) == -1
@@ -120,18 +122,19 @@ def test_adamw_step():
                 dict(eps=1e-31), dict(weight_decay=-1.0), dict(weight_decay=INF), dict(state_bits=16), dict(step=0), dict(step=-5)):
         assert adamw(**bad) == -5, bad
     lib = B._lib()
-    assert lib.ais_adamw_step(None, None, 1, C.byref(B.AisAdamWParams()), None, None, None) == -1
-    assert lib.ais_adamw_step(None, (B.AisAdamWTensor * 1)(), 1, None, None, None, None) == -1
+    assert lib.ais_adamw_step(None, None, P, 1, C.byref(B.AisAdamWParams()), None, None, None) == -1
+    assert lib.ais_adamw_step(None, (B.AisAdamWTensor * 1)(), P, 1, None, None, None, None) == -1
 
 
 def test_adamw_values():
-    order = "ctx codes scales n moment out dtype".split()
-    call = caller("ais_adamw_values", order, dict(ctx=None, codes=P, scales=P, n=100, moment=1, out=Q, dtype=B.AIS_F32))
-    assert call() == -1 and call(moment=2, dtype=B.AIS_BF16) == -1
-    for missing in ("codes", "scales", "out"):
+    order = "ctx m m_scale v v_scale n m_out v_out dtype".split()
+    call = caller("ais_adamw_values", order, dict(ctx=None, m=P, m_scale=P, v=P, v_scale=P, n=100, m_out=Q, v_out=Q, dtype=B.AIS_F32))
+    assert call() == -1 and call(dtype=B.AIS_BF16) == -1 and call(m=None, m_scale=None, m_out=None) == -1
+    for missing in ("m", "m_scale", "v", "v_scale"):
         assert call(**{missing: None}) == -1
-    assert call(n=-1) == -2 and call(n=2 ** 40 + 1) == -2 and call(moment=0) == -5 and call(moment=3) == -5
-    assert call(codes=C.c_void_p(0x1008)) == -4 and call(out=C.c_void_p(0x1002)) == -4 and call(dtype=7) == -7
+    assert call(m_out=None, v_out=None) == -1 and call(n=-1) == -2 and call(n=2 ** 40 + 1) == -2
+    assert call(m=C.c_void_p(0x1008)) == -4 and call(v=C.c_void_p(0x1008)) == -4 and call(m_out=C.c_void_p(0x1002)) == -4
+    assert call(v_out=C.c_void_p(0x1002)) == -4 and call(dtype=7) == -7
 
 
 def test_descriptors_are_laid_out_as_in_the_header():
