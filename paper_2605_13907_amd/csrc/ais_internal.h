@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "ais.h"
+#include "preference.h"
 #include "row_coeff.h"
 
 namespace ais {
@@ -249,10 +250,15 @@ struct PreferenceRoom {
   size_t total;
 };
 PreferenceRoom preference_room(long long n_rows, int n_resp, bool through_logits);
-// The log-probs in fp32 or, where `fine` is given, in 64 bits.
-int launch_preference(ais_ctx* ctx, const float* logp, const double* fine, const float* ref, const unsigned char* valid,
-                      long long n_rows, const long long* cu_rows, int n_resp, const float* weight, const ais_preference_params& p,
-                      const PreferenceRoom& room, float scale, float* reward, float* loss_out, float* g);
+// The batch with its log-probs in fp32 or, where `fine` is given, in 64 bits.
+Preference preference_batch(ais_ctx* ctx, const float* logp, const double* fine, const float* ref, const unsigned char* valid,
+                            long long n_rows, const long long* cu_rows, int n_resp, const float* weight,
+                            const ais_preference_params& p, const PreferenceRoom& room, float scale, float* reward, float* loss_out,
+                            float* g);
+int launch_preference(ais_ctx* ctx, const Preference& in);
+// Coefficients, loss, rewards and gradient in one launch, for batches small enough; false where this one is not.
+bool try_preference_dlogits_small(ais_ctx* ctx, const Preference& in, const void* logits, ais_dtype dtype, int vocab,
+                                  long long row_stride, const int* token_ids, const float* lse, void* dlogits);
 // How the rows of the normalisation's gradient are shared: threads of a row, rows of a workgroup at a time (0: rows too wide to be held),
 // vectors of a thread, and workgroups, each of which leaves a row of partial sums.
 struct NormGradPlan {

@@ -789,8 +789,8 @@ int ais_preference_row_scale(ais_ctx* ctx, const float* logp_train, const float*
   rc = ensure_workspace(ctx, room.total);
   if (rc != AIS_OK) return rc;
   ctx->plan.valid = false;             // the sums overwrite whatever tiling the workspace held
-  return launch_preference(ctx, logp_train, nullptr, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room,
-                           params->inv_temperature, reward_out, loss_out, g_out);
+  return launch_preference(ctx, preference_batch(ctx, logp_train, nullptr, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room,
+                                                 params->inv_temperature, reward_out, loss_out, g_out));
 }
 
 int ais_preference_loss_grad(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, long long vocab,
@@ -819,8 +819,11 @@ int ais_preference_loss_grad(ais_ctx* ctx, const void* logits, ais_dtype dtype, 
   rc = launch_token_logprob(ctx, logits, dtype, n_rows, (int)vocab, row_stride, token_ids, valid, params->inv_temperature, logp_out,
                             lse, fine);
   if (rc != AIS_OK) return rc;
-  rc = launch_preference(ctx, logp_out, fine, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room, 1.0f, reward_out,
-                         loss_out, g);
+  const Preference in = preference_batch(ctx, logp_out, fine, logp_ref, valid, n_rows, cu_rows, n_resp, weight, *params, room, 1.0f,
+                                         reward_out, loss_out, g);
+  if (dlogits != nullptr && try_preference_dlogits_small(ctx, in, logits, dtype, (int)vocab, row_stride, token_ids, lse, dlogits))
+    return hip_fail(ctx, hipGetLastError());
+  rc = launch_preference(ctx, in);
   if (rc != AIS_OK || dlogits == nullptr) return rc;
   return launch_dlogits(ctx, logits, dtype, n_rows, (int)vocab, row_stride, token_ids, g, nullptr, lse, logp_out,
                         params->inv_temperature, dlogits);

@@ -3,13 +3,14 @@
 //   d_i = sum over i's valid rows of logp - ref (or their mean), h = beta (d_2p - d_2p+1) - margin, loss = sum_p w_p l(h_p)
 //   c_t = -d loss / d logp_t = -+ w_p l'(h_p) beta [/ |o_i|]
 //
-// Three launches: partial sums of tiles of rows, pairs, rows; small batches are one workgroup's.  Reading 9 and writing 4 bytes a row is
+// Three launches: partial sums of tiles of rows, pairs, rows; small batches are one workgroup's, and through logits the gradient sweep's own
+// (512 rows of 1,024 fp32 logits: 4.4 + 6.1 + 3.4 us with a launch for them, 4.4 + 5.8 without).  Reading 9 and writing 4 bytes a row is
 // nothing beside the launches: 1.2 million rows in 4,000 responses take 6.0, 3.6 and 4.9 us, which is how long a workgroup's own chain of
 // loads, scan and stores is, all of them being there at once.  All that a thread needs of its rows is therefore loaded at once, masked rows
 // included, and eight rows lie in registers for the scan and the walk after it (11.2, 4.7 and 11.0 us with loads one after the other).
 #include "ais_internal.h"
 #include "eights.h"
-#include "row_coeff.h"
+#include "preference.h"
 
 namespace ais {
 namespace {
@@ -46,29 +47,6 @@ struct Run {
 __device__ __forceinline__ Run join(Run a, Run b) {
   return b.owner != 0 ? b : Run{a.sum + b.sum, a.count + b.count, a.owner};
 }
-
-// The batch, as the entry points take it.
-struct Preference {
-  const float* logp;
-  const double* fine;                            // the log-probs in 64 bits, or null
-  const float* ref;
-  const unsigned char* valid;
-  const long long* cu;
-  const float* weight;
-  int n_resp;
-  long long n_rows;
-  ais_preference_params p;
-  float scale;                                   // of the rows' coefficients
-  // in the workspace: partial sums and counts (response i in tile b has place i + b, which no other pair of them has), the
-  // pairs' losses, the responses' coefficients
-  double* sums;
-  int* counts;
-  double* loss;
-  float* coeff;
-  int* firsts;                                   // response that each tile begins in
-  float *reward, *loss_out, *g;
-  int* status;
-};
 
 struct Owner {
   float coeff;
@@ -232,50 +210,6 @@ __device__ __forceinline__ unsigned live_rows(const Preference& in, long long r,
   return live;
 }
 
-// Loss of a pair with log-ratios d, and the coefficients of its two responses' rows.
-__device__ __forceinline__ double pair_terms(const Preference& in, int pair, const double* s, const int* n, float* coeff) {
-  const ais_preference_params& p = in.p;
-  double d[2], share[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    share[j] = p.mean_logp ? (n[j] > 0 ? 1.0 / (double)n[j] : 0.0) : 1.0;
-    d[j] = s[j] * share[j];
-    in.reward[2 * pair + j] = (float)((double)p.beta * d[j]);
-  }
-  const double beta = (double)p.beta, h = beta * (d[0] - d[1]) - (double)p.margin;
-  const double w = in.weight != nullptr ? (double)in.weight[pair] : 2.0 / (double)in.n_resp;
-  double l, slope;
-  if (p.kind == 0) {
-    const double e = exp64(-fabs(h)), both = log1p(e), wrong = (double)p.label_smoothing;
-    // sigmoid(-h) and sigmoid(h), neither from 1 less the other
-    const double small = e / (1.0 + e), large = 1.0 / (1.0 + e);
-    const double down = h >= 0.0 ? small : large, up = h >= 0.0 ? large : small;
-    l = (1.0 - wrong) * (both + (h < 0.0 ? -h : 0.0)) + wrong * (both + (h > 0.0 ? h : 0.0));
-    slope = wrong * up - (1.0 - wrong) * down;
-    if (h != h) l = slope = h;
-  } else if (p.kind == 1) {
-    l = h < 1.0 ? 1.0 - h : 0.0;
-    slope = h < 1.0 ? -1.0 : 0.0;
-    if (h != h) l = slope = h;
-  } else {
-    const double q = (h - 0.5) / beta;
-    l = q * q;
-    slope = 2.0 * q / beta;
-  }
-  const double c = w * slope * beta;
-  coeff[0] = (float)(-c * share[0]);
-  coeff[1] = (float)(c * share[1]);
-  return w * l;
-}
-
-// Rows of response i, whose offsets are from and to, inside the batch; faulty ones are reported.
-__device__ __forceinline__ void rows_of(const Preference& in, int i, long long from, long long to, unsigned* lo, unsigned* hi) {
-  if (from < 0 || to < from || to > in.n_rows || (i == 0 && from != 0) || (i == in.n_resp - 1 && to != in.n_rows))
-    atomicOr(in.status, AIS_STATUS_BAD_CU);
-  *lo = (unsigned)min(max(from, 0LL), in.n_rows);
-  *hi = (unsigned)min(max(to, (long long)*lo), in.n_rows);
-}
-
 // The sum of a workgroup's values, by its first thread, in the order of the wavefronts.
 template <int THREADS>
 __device__ __forceinline__ void add_up(double s, float* out) {
@@ -322,15 +256,21 @@ __global__ __launch_bounds__(kTileThreads) void preference_pairs_kernel(Preferen
   int n[2] = {};
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    unsigned lo, hi;
-    rows_of(in, 2 * pair + j, cu[j], cu[j + 1], &lo, &hi);
-    if (hi > lo)
-      for (unsigned b = lo / kTileRows; b <= (hi - 1) / kTileRows; ++b) {
+    const RowRange r = rows_of(in, 2 * pair + j, cu[j], cu[j + 1]);
+    if (!r.sound) atomicOr(in.status, AIS_STATUS_BAD_CU);
+    if (r.hi > r.lo)
+      for (unsigned b = r.lo / kTileRows; b <= (r.hi - 1) / kTileRows; ++b) {
         s[j] += in.sums[2 * pair + j + (size_t)b];
         n[j] += in.counts[2 * pair + j + (size_t)b];
       }
   }
-  in.loss[pair] = pair_terms(in, pair, s, n, in.coeff + 2 * pair);
+  const PairTerm t = pair_term<true>(in, pair, s, n);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    in.reward[2 * pair + j] = t.reward[j];
+    in.coeff[2 * pair + j] = t.coeff[j];
+  }
+  in.loss[pair] = t.loss;
 }
 
 // A workgroup to a tile; one more adds up the pairs' losses.
@@ -384,12 +324,14 @@ __global__ __launch_bounds__(THREADS) void preference_one_kernel(Preference in) 
   __syncthreads();
   double s = 0.0;
   for (int pair = tid; pair < in.n_resp / 2; pair += THREADS) {
+    const PairTerm t = pair_term<true>(in, pair, sums + 2 * pair, counts + 2 * pair);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      unsigned lo, hi;
-      rows_of(in, 2 * pair + j, cu[2 * pair + j], cu[2 * pair + j + 1], &lo, &hi);
+      if (!rows_of(in, 2 * pair + j, cu[2 * pair + j], cu[2 * pair + j + 1]).sound) atomicOr(in.status, AIS_STATUS_BAD_CU);
+      in.reward[2 * pair + j] = t.reward[j];
+      coeff[2 * pair + j] = t.coeff[j];
     }
-    s += pair_terms(in, pair, sums + 2 * pair, counts + 2 * pair, coeff + 2 * pair);
+    s += t.loss;
   }
   __syncthreads();
   tile.spread(in, mine.live, first, 0, rows, [&](int i) { return Owner{coeff[i], cu[i], cu[i + 1]}; });
@@ -414,23 +356,27 @@ PreferenceRoom preference_room(long long n_rows, int n_resp, bool through_logits
   return r;
 }
 
-int launch_preference(ais_ctx* ctx, const float* logp, const double* fine, const float* ref, const unsigned char* valid,
-                      long long n_rows, const long long* cu_rows, int n_resp, const float* weight, const ais_preference_params& p,
-                      const PreferenceRoom& room, float scale, float* reward, float* loss_out, float* g) {
-  ScopedTimer timer(ctx, AIS_K_PREFERENCE);
+Preference preference_batch(ais_ctx* ctx, const float* logp, const double* fine, const float* ref, const unsigned char* valid,
+                            long long n_rows, const long long* cu_rows, int n_resp, const float* weight,
+                            const ais_preference_params& p, const PreferenceRoom& room, float scale, float* reward, float* loss_out,
+                            float* g) {
   char* ws = static_cast<char*>(ctx->ws);
-  const Preference in{logp, fine, ref, valid, cu_rows, weight, n_resp, n_rows, p, scale, reinterpret_cast<double*>(ws),
-                      reinterpret_cast<int*>(ws + room.counts), reinterpret_cast<double*>(ws + room.loss),
-                      reinterpret_cast<float*>(ws + room.coeff), reinterpret_cast<int*>(ws + room.firsts), reward, loss_out, g, ctx->status_dev};
-  if (n_rows <= kOneRows && n_resp <= kOneResponses) {
+  return {logp, fine, ref, valid, cu_rows, weight, n_resp, n_rows, p, scale, reinterpret_cast<double*>(ws),
+          reinterpret_cast<int*>(ws + room.counts), reinterpret_cast<double*>(ws + room.loss), reinterpret_cast<float*>(ws + room.coeff),
+          reinterpret_cast<int*>(ws + room.firsts), reward, loss_out, g, ctx->status_dev};
+}
+
+int launch_preference(ais_ctx* ctx, const Preference& in) {
+  ScopedTimer timer(ctx, AIS_K_PREFERENCE);
+  if (in.n_rows <= kOneRows && in.n_resp <= kOneResponses) {
     // 2,048 rows take 9.1 us with 1,024 threads and 6.1 with 256
-    if (n_rows <= kTileRows) preference_one_kernel<kTileThreads><<<dim3(1), dim3(kTileThreads), 0, ctx->stream>>>(in);
+    if (in.n_rows <= kTileRows) preference_one_kernel<kTileThreads><<<dim3(1), dim3(kTileThreads), 0, ctx->stream>>>(in);
     else preference_one_kernel<kOneThreads><<<dim3(1), dim3(kOneThreads), 0, ctx->stream>>>(in);
     return hip_fail(ctx, hipGetLastError());
   }
-  const int tiles = (int)((n_rows + kTileRows - 1) / kTileRows);
+  const int tiles = (int)((in.n_rows + kTileRows - 1) / kTileRows);
   if (tiles > 0) preference_sums_kernel<<<dim3((unsigned)tiles), dim3(kTileThreads), 0, ctx->stream>>>(in);
-  preference_pairs_kernel<<<dim3((unsigned)((n_resp / 2 - 1) / kTileThreads + 1)), dim3(kTileThreads), 0, ctx->stream>>>(in);
+  preference_pairs_kernel<<<dim3((unsigned)((in.n_resp / 2 - 1) / kTileThreads + 1)), dim3(kTileThreads), 0, ctx->stream>>>(in);
   preference_rows_kernel<<<dim3((unsigned)tiles + 1), dim3(kTileThreads), 0, ctx->stream>>>(in, tiles);
   return hip_fail(ctx, hipGetLastError());
 }

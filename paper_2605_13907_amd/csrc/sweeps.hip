@@ -15,6 +15,7 @@
 // cache between the two sweeps (a temporal load costs the read-only sweep 11 % of its bandwidth).
 #include "ais_internal.h"
 #include "device_utils.h"
+#include "preference.h"
 
 #include <type_traits>
 
@@ -287,6 +288,99 @@ struct OwnCoeff {
   static constexpr int kOwnResponses = 64;       // a lane for each
 };
 
+// ... or of a pair of responses, whose rows the workgroup adds up itself: two of its wavefronts take a response each, the first one
+// forms the coefficient.  The grid's last workgroup forms rewards and loss from the same sums.
+struct PairCoeff {
+  static constexpr bool kOwn = true;
+  static constexpr int kOwnResponses = 64;       // a lane for each
+  Preference in;
+  struct Sum {
+    double s;
+    int n;
+  };
+  // By a whole wavefront, in one order whoever asks.
+  __device__ __forceinline__ Sum response_sum(int i) const {
+    const int lane = threadIdx.x & 63;
+    const RowRange rows = rows_of(in, i, in.cu[i], in.cu[i + 1]);
+    Sum t{0.0, 0};
+    for (unsigned r = rows.lo; r < rows.hi; r += 4 * 64) {
+      double x[4];
+      int live[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const unsigned at = min(r + 64 * k + lane, rows.hi - 1);
+        live[k] = r + 64 * k + lane < rows.hi && (in.valid == nullptr || in.valid[at] != 0);
+        x[k] = in.fine[at] - (in.ref != nullptr ? (double)in.ref[at] : 0.0);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        t.s += live[k] ? x[k] : 0.0;
+        t.n += live[k];
+      }
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      t.s += __shfl_xor(t.s, off);
+      t.n += __shfl_xor(t.n, off);
+    }
+    return t;
+  }
+  // Must be called by the whole workgroup, of two wavefronts or more.
+  __device__ __forceinline__ float of_row(long long row) const {
+    __shared__ double s[2];
+    __shared__ int n[2];
+    __shared__ float c;
+    if (in.valid != nullptr && in.valid[row] == 0) return 0.f;           // uniform
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    bool here = false;
+    if (lane < in.n_resp) here = in.cu[lane] <= row && row < in.cu[lane + 1];
+    const unsigned long long mask = __ballot(here);
+    if (mask == 0) return 0.f;                                           // no response's row: a faulty cu_rows, reported
+    const int i = __builtin_amdgcn_readfirstlane(__builtin_ctzll(mask));
+    if (wave < 2) {
+      const Sum t = response_sum((i & ~1) + wave);
+      if (lane == 0) {
+        s[wave] = t.s;
+        n[wave] = t.n;
+      }
+    }
+    __syncthreads();
+    if (wave == 0) {
+      const PairTerm t = pair_term<false>(in, i >> 1, s, n);
+      if (lane == 0) c = i & 1 ? t.coeff[1] : t.coeff[0];
+    }
+    __syncthreads();
+    return c;
+  }
+  __device__ __forceinline__ float scale(float inv_temperature) const { return inv_temperature; }
+  template <int THREADS>
+  __device__ void loss_of_all() const {
+    __shared__ double sums[kOwnResponses];
+    __shared__ int counts[kOwnResponses];
+    const int tid = threadIdx.x;
+    for (int i = tid >> 6; i < in.n_resp; i += THREADS / 64) {
+      const Sum t = response_sum(i);
+      if ((tid & 63) == 0) {
+        sums[i] = t.s;
+        counts[i] = t.n;
+        if (!rows_of(in, i, in.cu[i], in.cu[i + 1]).sound) atomicOr(in.status, AIS_STATUS_BAD_CU);
+      }
+    }
+    __syncthreads();
+    if (tid >= 64) return;
+    double loss = 0.0;
+    if (2 * tid < in.n_resp) {
+      const PairTerm t = pair_term<true>(in, tid, sums + 2 * tid, counts + 2 * tid);
+      in.reward[2 * tid] = t.reward[0];
+      in.reward[2 * tid + 1] = t.reward[1];
+      loss = t.loss;
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) loss += __shfl_xor(loss, off);
+    if (tid == 0) *in.loss_out = (float)loss;
+  }
+};
+
 // NSEG > 0 promises that the row fits NSEG segments, which are then unrolled: the loop-free form is ~3 %
 // faster than the same code inside a run-time loop.  NSEG = 0: run-time loop over as many segments as needed.
 // KFULL promises that the row has at least KFULL * 1024 vectors: vectors 0 .. KFULL - 1 of every lane exist and
@@ -550,10 +644,11 @@ int launch_dlogits(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long 
 
 // Takes batches whose rows all have a workgroup on the chip at once, in up to 64 responses, with no more than two rows for
 // each thread of the one that forms the loss.
-bool try_loss_dlogits_small(ais_ctx* ctx, const CoeffInputs& in, const void* logits, ais_dtype dtype, long long n_rows,
-                            int vocab, long long row_stride, const int* token_ids, const float* lse, float* wtilde_out,
-                            double* loss_out, void* dlogits) {
-  if (n_rows == 0 || n_rows > 1024 || in.n_resp > OwnCoeff::kOwnResponses) return false;
+template <typename Coeff>
+static bool dlogits_small(ais_ctx* ctx, const Coeff& coeff, int n_resp, const float* logp, float inv_temperature, const void* logits,
+                          ais_dtype dtype, long long n_rows, int vocab, long long row_stride, const int* token_ids, const float* lse,
+                          void* dlogits) {
+  if (n_rows == 0 || n_rows > 1024 || n_resp > Coeff::kOwnResponses) return false;
   auto launch = [&](const auto* z) {
     typedef std::remove_cv_t<std::remove_pointer_t<decltype(z)>> T;
     T* dz = static_cast<T*>(dlogits);
@@ -564,23 +659,35 @@ bool try_loss_dlogits_small(ais_ctx* ctx, const CoeffInputs& in, const void* log
       if (n_rows > 2 * threads || n_rows > ctx->n_cus * (2048LL / threads)) return false;
       ScopedTimer timer(ctx, AIS_K_DLOGITS);
       kernel<<<dim3((unsigned)(((n_rows + 7) / 8) * 8 + 1)), dim3(threads), 0, ctx->stream>>>(
-          z, row_stride, vocab, token_ids, OwnCoeff{in, wtilde_out, loss_out, ctx->status_dev, (int)n_rows}, lse,
-          in.logp_train, in.p.inv_temperature, dz, n_rows);
+          z, row_stride, vocab, token_ids, coeff, lse, logp, inv_temperature, dz, n_rows);
       return true;
     };
     if (aligned) {
-      if (nvec <= 256) return run(dlogits_burst_kernel<T, true, 256, 1, 1, 0, OwnCoeff>, 256);
-      if (nvec <= 512) return run(dlogits_burst_kernel<T, true, 512, 1, 1, 0, OwnCoeff>, 512);
-      if (nvec <= 4096) return run(dlogits_burst_kernel<T, true, 1024, 4, 1, 0, OwnCoeff>, 1024);
-      if (nvec <= 8192) return run(dlogits_burst_kernel<T, true, 1024, 8, 1, 0, OwnCoeff>, 1024);
+      if (nvec <= 256) return run(dlogits_burst_kernel<T, true, 256, 1, 1, 0, Coeff>, 256);
+      if (nvec <= 512) return run(dlogits_burst_kernel<T, true, 512, 1, 1, 0, Coeff>, 512);
+      if (nvec <= 4096) return run(dlogits_burst_kernel<T, true, 1024, 4, 1, 0, Coeff>, 1024);
+      if (nvec <= 8192) return run(dlogits_burst_kernel<T, true, 1024, 8, 1, 0, Coeff>, 1024);
     } else {
-      if (nvec <= 1024) return run(dlogits_burst_kernel<T, false, 256, 4, 1, 0, OwnCoeff>, 256);
-      if (nvec <= 4096) return run(dlogits_burst_kernel<T, false, 1024, 4, 1, 0, OwnCoeff>, 1024);
-      if (nvec <= 8192) return run(dlogits_burst_kernel<T, false, 1024, 8, 1, 0, OwnCoeff>, 1024);
+      if (nvec <= 1024) return run(dlogits_burst_kernel<T, false, 256, 4, 1, 0, Coeff>, 256);
+      if (nvec <= 4096) return run(dlogits_burst_kernel<T, false, 1024, 4, 1, 0, Coeff>, 1024);
+      if (nvec <= 8192) return run(dlogits_burst_kernel<T, false, 1024, 8, 1, 0, Coeff>, 1024);
     }
     return false;
   };
   return dtype == AIS_BF16 ? launch(static_cast<const bf16_t*>(logits)) : launch(static_cast<const float*>(logits));
+}
+
+bool try_loss_dlogits_small(ais_ctx* ctx, const CoeffInputs& in, const void* logits, ais_dtype dtype, long long n_rows,
+                            int vocab, long long row_stride, const int* token_ids, const float* lse, float* wtilde_out,
+                            double* loss_out, void* dlogits) {
+  return dlogits_small(ctx, OwnCoeff{in, wtilde_out, loss_out, ctx->status_dev, (int)n_rows}, in.n_resp, in.logp_train,
+                       in.p.inv_temperature, logits, dtype, n_rows, vocab, row_stride, token_ids, lse, dlogits);
+}
+
+bool try_preference_dlogits_small(ais_ctx* ctx, const Preference& in, const void* logits, ais_dtype dtype, int vocab,
+                                  long long row_stride, const int* token_ids, const float* lse, void* dlogits) {
+  return dlogits_small(ctx, PairCoeff{in}, in.n_resp, in.logp, in.p.inv_temperature, logits, dtype, in.n_rows, vocab, row_stride,
+                       token_ids, lse, dlogits);
 }
 
 int launch_copy(ais_ctx* ctx, void* dst, const void* src, long long bytes) {

@@ -131,6 +131,10 @@ def test_faulty_offsets_are_reported(ctx, cu):
     _, _, g = ctx.preference_row_scale(logp, None, None, cuda(cu, torch.int64))
     assert g.shape == (10,)
     assert ctx.status() == B.STATUS_BAD_CU and ctx.status() == 0
+    z, ids = torch.randn(10, 64, device="cuda"), torch.zeros(10, dtype=torch.int32, device="cuda")
+    dz = ctx.preference_loss_grad(z, ids, None, cuda(cu, torch.int64), None)[3]
+    assert dz.shape == z.shape
+    assert ctx.status() == B.STATUS_BAD_CU and ctx.status() == 0
 
 
 def test_no_rows(ctx):
@@ -146,8 +150,12 @@ def test_through_logits(ctx, dtype, vocab, pitch):
     then below e^-20), a batch's sum of 16 by 16 of 2^-25; 2^-20 of min(1, the other tokens' share) covers them, and 2^-24 its own rounding.
     dlogits are the coefficients times softmax less the token's one: half a step of the type, and in fp32 the exponential and the shift by
     an lse of up to 20: 2^-19."""
+    through_logits(ctx, dtype, vocab, pitch, [5, 11, 0, 40, 17, 3])
+
+
+def through_logits(ctx, dtype, vocab, pitch, lengths):
     gen = torch.Generator(device="cuda").manual_seed(7)
-    logp0, _, valid, cu, weight = batch([5, 11, 0, 40, 17, 3], seed=4)
+    logp0, _, valid, cu, weight = batch(lengths, seed=4)
     rows = len(logp0)
     z = (3 * torch.randn(rows, pitch, generator=gen, device="cuda")).to(dtype)[:, :vocab]
     ids = torch.randint(0, vocab, (rows,), generator=gen, device="cuda", dtype=torch.int32)
@@ -180,6 +188,41 @@ def test_through_logits(ctx, dtype, vocab, pitch):
     assert alone[3] is None and all(torch.equal(a, b) for a, b in zip(alone[:3], (loss, reward, logp)))
     inplace = ctx.preference_loss_grad(z, ids, valid, cu, ref, p, weight=weight, dlogits=z)[3]
     assert inplace.data_ptr() == z.data_ptr() and torch.equal(inplace, dz)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lengths", [[1_000, 24], [1_024, 1], [0, 1_024], [16] * 64, [15] * 66, [0] * 62 + [3, 2], [700, 1, 300, 0], [1_500, 1_000],
+                                     [300] * 10])
+def test_through_logits_of_more_rows(ctx, lengths, dtype):
+    """Batches whose coefficients the gradient's own workgroups form (up to 1,024 rows in 64 responses), and the next larger ones."""
+    through_logits(ctx, dtype, 136, 136, lengths)
+    through_logits(ctx, dtype, 1_501, 1_501, lengths)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("rows", [90, 1_500])
+def test_forms_through_logits(ctx, form, rows):
+    """Either way to the coefficients gives what the log-probs of the same logits give by themselves, up to those log-probs' own
+    rounding: 2^-24 of each, under beta."""
+    logp0, ref, valid, cu, weight = batch([rows // 3, rows // 3, rows // 6, rows // 6], seed=8)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    n, vocab = len(logp0), 200
+    z = torch.randn(n, vocab, generator=gen, device="cuda")
+    ids = torch.randint(0, vocab, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    valid, cu, weight = cuda(valid), cuda(cu), cuda(weight)
+    p = B.default_preference_params(**form)
+    exact = torch.log_softmax(z.double() * p.inv_temperature, dim=1).gather(1, ids.long()[:, None])[:, 0]
+    ref = (exact + 0.05 * torch.randn(n, generator=gen, device="cuda")).float()
+    loss, reward, logp, dz = ctx.preference_loss_grad(z, ids, valid, cu, ref, p, weight=weight)
+    want_loss, want_reward, g = ctx.preference_row_scale(logp, ref, valid, cu, p, weight=weight)
+    off = float(p.beta) * (float(logp.abs().sum()) * 2.0 ** -24 if not p.mean_logp else 8 * 2.0 ** -24) + 2.0 ** -22 * float(want_reward.abs().max())
+    assert torch.allclose(reward, want_reward, rtol=2.0 ** -22, atol=off)
+    scale = 1.0 if p.kind < 2 else 2.0 / p.beta ** 2 * max(1.0, float(want_reward.abs().max()))
+    assert abs(loss.item() - want_loss.item()) <= 2.0 ** -22 * abs(want_loss.item()) + 2 * off * scale * float(weight.sum())
+    want = g.double()[:, None] * torch.softmax(z.double() * p.inv_temperature, dim=1)
+    want[torch.arange(n), ids.long()] = g.double() * torch.expm1(exact)
+    slope = float(p.beta) * float(weight.max()) * (2 * off * scale if p.kind != 1 else 0.0)
+    assert ((dz.double() - want).abs() <= 2.0 ** -19 * want.abs() + slope + 1e-30).all()
 
 
 def test_small_terms_of_long_responses_add_up(ctx):
