@@ -92,13 +92,14 @@ def tensor(n, dtype, seed, size=1.0, offset=0):
 
 
 def grads_of(sizes, dtypes, seed, size=1e-3, offset=0):
-    # gradients of many magnitudes, some of them zero
+    # gradients of many magnitudes, some of them zero (formed in fp32: torch's mixed products leave the device less memory)
     out = []
     for i, n in enumerate(sizes):
         g = tensor(n, dtypes[i % len(dtypes)], seed + i, size, offset)
         gen = torch.Generator(device="cuda").manual_seed(seed + 1_000 + i)
-        g *= torch.exp(3 * torch.randn(n, generator=gen, device="cuda"))
-        g[torch.rand(n, generator=gen, device="cuda") < 0.05] = 0.0
+        wide = g.float() * torch.exp(3 * torch.randn(n, generator=gen, device="cuda"))
+        wide[torch.rand(n, generator=gen, device="cuda") < 0.05] = 0.0
+        g.copy_(wide)
         out.append(g)
     return out
 
