@@ -900,7 +900,7 @@ int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, const ais_adam
   for (int i = 0; i < n_tensors; ++i) {
     const int rc = check_adamw_tensor(tensors[i], p->state_bits);
     if (rc != AIS_OK) return rc;
-    chunks += (tensors[i].n + 2047) / 2048;
+    chunks += (tensors[i].n + 1023) / 1024;
   }
   if (chunks > 0x7fffffffLL) return AIS_ERR_SIZE;      // workgroups of a launch
   if (ctx == nullptr) return AIS_ERR_NULL;

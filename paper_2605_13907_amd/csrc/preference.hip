@@ -371,6 +371,7 @@ int launch_preference(ais_ctx* ctx, const Preference& in) {
   if (in.n_rows <= kOneRows && in.n_resp <= kOneResponses) {
     // 2,048 rows take 9.1 us with 1,024 threads and 6.1 with 256
     if (in.n_rows <= kTileRows) preference_one_kernel<kTileThreads><<<dim3(1), dim3(kTileThreads), 0, ctx->stream>>>(in);
+    else if (in.n_rows <= 2 * kTileRows) preference_one_kernel<2 * kTileThreads><<<dim3(1), dim3(2 * kTileThreads), 0, ctx->stream>>>(in);
     else preference_one_kernel<kOneThreads><<<dim3(1), dim3(kOneThreads), 0, ctx->stream>>>(in);
     return hip_fail(ctx, hipGetLastError());
   }
