@@ -138,6 +138,32 @@ def test_tensors_that_begin_anywhere(ctx, bits):
             twin.check_step(ctx, grads_of(sizes, BOTH, offset, offset=offset))
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_than_32_bits_of_bytes(ctx, bits):
+    """A tensor of 2^31 and some elements: its end is stepped as by itself, in an element's place that the random numbers know."""
+    n, tail = (1 << 31) + 77, 200
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    p[-tail:], g[-tail:] = tensor(tail, torch.bfloat16, 1), tensor(tail, torch.bfloat16, 2, 1e-3)
+    before, grad = numbers(p[-tail:]), numbers(g[-tail:])
+    state = B.AdamWState([p], bits=bits, seed=5)
+    ctx.adamw_step(state, [g], **RULE)
+    want, m, v = O.adamw(before, grad, np.zeros(tail), np.zeros(tail), 1, **RULE)
+    assert (np.abs(numbers(p[-tail:]) - want) <= HALF[torch.bfloat16] * np.abs(want) + 20 * U * (np.abs(want) + RULE["lr"])).all()
+    assert not p[:-tail].any()
+    if bits == 32:
+        assert np.allclose(numbers(state.m[n - tail:n]), m.astype(np.float64), rtol=2.01 * U) and not state.m[:n - tail].any()
+        return
+    first = (n - tail) // 32 * 32                                # the block that the tail begins in
+    pad = n - tail - first
+    key = O.mix(O.mix(5 ^ 0x9E3779B1) ^ 0)
+    at = np.arange(first, n, dtype=np.uint64)
+    bits_of = O.mix((at * np.uint64(0x9E3779B1) & np.uint64(O.M32)) ^ np.uint64(key))
+    for which, x, flat, rnd in ((1, m, state.m, bits_of & np.uint64(65535)), (2, v, state.v, bits_of >> np.uint64(16))):
+        codes, _ = O.encode(np.concatenate((np.zeros(pad, np.float32), x)), rnd, which)
+        assert (flat[first:n].cpu().numpy() == codes).all()
+
+
 def test_a_tensor_without_a_gradient_stays(ctx):
     for bits in (32, 8):
         params = [tensor(n, torch.float32, n) for n in (100, 200, 300)]

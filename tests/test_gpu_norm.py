@@ -16,8 +16,9 @@ pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}          # eps / 2
-WIDTHS = [1, 2, 7, 8, 9, 63, 64, 511, 512, 513, 1_100, 2_047, 2_048, 2_049, 4_095, 4_096, 4_097, 8_191, 8_192, 8_193, 16_384, 16_385,
-          32_768, 32_769, 70_001]
+WIDTHS = [1, 2, 7, 8, 9, 63, 64, 255, 256, 257, 511, 512, 513, 767, 769, 1_023, 1_024, 1_025, 1_100, 1_280, 1_281, 1_536, 1_537, 2_047, 2_048,
+          2_049, 4_095, 4_096, 4_097, 5_120, 5_123, 6_143, 6_145, 8_191, 8_192, 8_193, 10_240, 10_243, 12_288, 12_290, 16_384, 16_385, 32_768,
+          32_769, 70_001]
 
 
 @pytest.fixture(scope="module")
@@ -200,6 +201,22 @@ def test_columns_behind_the_rows_stay(ctx):
     rc = ctx._lib.ais_norm_rows(ctx._h, x.data_ptr(), B.AIS_F32, 5, 100, 104, None, None, None, B.AIS_F32, 1e-5, 0, out.data_ptr(), 104, None,
                                 rstd.data_ptr())
     assert rc == 0 and (out[:, 100:] == 7.0).all() and torch.equal(out[:, :100], ctx.norm_rows(x, centered=False)[0])
+
+
+@pytest.mark.parametrize("width", [100, 4_097, 20_000])
+def test_offsets_beyond_32_bits(ctx, width):
+    """Rows 2^29 + 1 elements apart, the last of them beyond 2^32 elements into its buffer: the same as rows beside one another."""
+    n, pitch = 9, (1 << 29) + 1
+    flat = torch.empty((n - 1) * pitch + width, dtype=torch.bfloat16, device="cuda")
+    far = flat.as_strided((n, width), (pitch, 1))
+    x, dy = rows(n, width, torch.bfloat16, 1), rows(n, width, torch.float32, 2)
+    far.copy_(x)
+    weight, bias = params(width, torch.bfloat16)
+    want = ctx.norm_rows(x, weight, bias)
+    for a, b in zip(want, ctx.norm_rows(far, weight, bias)):
+        assert torch.equal(a, b)
+    for a, b in zip(ctx.norm_rows_grad(dy, x, weight, *want[1:]), ctx.norm_rows_grad(dy, far, weight, *want[1:])):
+        assert torch.equal(a, b)
 
 
 def test_runs_alike(ctx):

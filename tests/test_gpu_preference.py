@@ -265,6 +265,44 @@ def test_more_rows_than_a_launch_of_tiles_fills(ctx):
     compare(ctx, *batch([int(v) for v in np.random.default_rng(9).integers(0, 3_000, 400)], seed=9))
 
 
+@pytest.mark.parametrize("lengths", [[30, 70], [5_000, 4_000, 300, 0]])
+def test_arrays_that_begin_anywhere(ctx, lengths):
+    logp, ref, valid, cu, weight = batch(lengths, seed=11)
+    n = len(logp)
+    p = B.default_preference_params()
+    want = ctx.preference_row_scale(cuda(logp), cuda(ref), cuda(valid), cuda(cu), p, weight=cuda(weight))
+    for shift in (1, 2, 3, 5):
+        moved = []
+        for a in (logp, ref, valid):
+            t = torch.zeros(n + 8, dtype=torch.from_numpy(a).dtype, device="cuda")
+            t[shift:shift + n] = cuda(a)
+            moved.append(t[shift:shift + n])
+        for a, b in zip(want, ctx.preference_row_scale(*moved, cuda(cu), p, weight=cuda(weight))):
+            assert torch.equal(a, b)
+
+
+def test_a_million_responses(ctx):
+    """More responses than rows in most places, and one of half the batch among them."""
+    r = np.random.default_rng(12)
+    lengths = r.integers(0, 2, 1 << 20)
+    lengths[123_457] = 500_000
+    logp, ref, valid, cu, weight = batch([int(v) for v in lengths], seed=12)
+    loss, reward, g = ctx.preference_row_scale(cuda(logp), cuda(ref), cuda(valid), cuda(cu), weight=cuda(weight))
+    delta = np.where(valid != 0, logp.astype(np.float64) - ref, 0.0)
+    d = np.add.reduceat(np.concatenate((delta, [0.0])), cu[:-1]) * (lengths > 0)
+    beta = float(B.default_preference_params().beta)
+    h = beta * (d[0::2] - d[1::2])
+    want = (weight.astype(np.float64) * np.logaddexp(0.0, -h)).sum()
+    c = weight * beta / (1.0 + np.exp(h))
+    rows = np.repeat(np.arange(1 << 20), lengths)
+    want_g = np.where(rows % 2 == 0, 1.0, -1.0) * c[rows // 2] * (valid != 0)
+    noise = beta * np.abs(delta).sum() * 2.0 ** -50
+    assert np.allclose(reward.cpu().numpy(), beta * d, rtol=2.0 ** -23, atol=noise)
+    assert np.allclose(g.cpu().numpy(), want_g, rtol=2.0 ** -22, atol=noise)
+    assert loss.item() == pytest.approx(want, rel=2.0 ** -22)
+    assert ctx.status() == 0
+
+
 def test_runs_alike(ctx):
     logp, ref, valid, cu, weight = (cuda(a) for a in batch([5_000, 7_000, 3, 9_000], seed=6))
     first = ctx.preference_row_scale(logp, ref, valid, cu, weight=weight)
