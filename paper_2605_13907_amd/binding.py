@@ -922,12 +922,12 @@ class AisContext:
             state.step = step + 1
 
     def adamw_values(self, state: AdamWState, dtype=torch.float32):
-        """-> (m, v): what a state's 8-bit moments stand for, flat like state.m and of `dtype` (float32 or bfloat16); fp32 moments
-        of a state of 32 bits are its own buffers."""
+        """-> (m, v): what a state's 8-bit moments stand for, flat like state.m and of `dtype` (float32 or bfloat16).  (Those of a state
+        of 32 bits are state.m and state.v.)  See ais_adamw_values in include/ais.h."""
         if dtype not in (torch.bfloat16, torch.float32):
             raise TypeError(f"moments must be bfloat16 or float32, not {dtype}")
-        if state.bits == 32:
-            return state.m.to(dtype), state.v.to(dtype)
+        if state.bits != 8:
+            raise ValueError("moments of 32 bits are state.m and state.v")
         if state.device != self.device:
             raise ValueError(f"state is on {state.device}, expected {self.device}")
         out = self._native("adamw_values", state.m, state.m_scale, state.v, state.v_scale, 1 if dtype is torch.bfloat16 else 0)

