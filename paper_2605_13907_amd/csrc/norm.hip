@@ -118,8 +118,24 @@ __device__ __forceinline__ float sum_of(const float* x) {
   else return a + ((x[4] + x[5]) + (x[6] + x[7]));
 }
 
+// How rows are cut into vectors of N elements, which begin at whole words: of bf16 rows that begin in the middle of one the first element
+// is left out of them, like those after the last vector.  (The gradient of 28,066 bf16 rows of 2,237 elements, one after the other: 135 us,
+// 164 with vectors from their first element on; 20,000 of 4,097: 114, 137.)  Any cut is sound for any row, whatever it costs; a workgroup has one for all of its rows.
+struct Cut {
+  int head, vectors, left;                       // left: elements outside the vectors, those of the head first
+  template <typename T, int N>
+  __device__ __forceinline__ static Cut of(const T* row, int width) {
+    const int head = sizeof(T) == 2 ? (int)(reinterpret_cast<uintptr_t>(row) >> 1 & 1) : 0;
+    const int vectors = (width - head) / N;
+    return {head, vectors, width - N * vectors};
+  }
+  // Element that the thread-th of the elements outside is.
+  template <int N>
+  __device__ __forceinline__ int rest(int thread) const { return thread < head ? thread : N * vectors + thread; }
+};
+
 // A row of up to NV vectors of N elements to a thread of the THREADS that share it: those past the row's last repeat it and are left
-// out of the sums.  The elements after the last vector are one each of the first threads.  WHOLE: every thread has all of its vectors.
+// out of the sums.  The elements outside are one each of the first threads.  WHOLE: every thread has all of its vectors.
 template <typename T, int N, int THREADS, int NV, bool WHOLE>
 struct HeldRow {
   typedef Pack<T, N> P;
@@ -127,16 +143,18 @@ struct HeldRow {
   float rest;
   static __device__ __forceinline__ int thread() { return THREADS == 64 ? threadIdx.x & 63 : threadIdx.x; }
   static __device__ __forceinline__ bool has(int k, int vectors) { return WHOLE || thread() + k * THREADS < vectors; }
-  static __device__ __forceinline__ int index(int k, int vectors) {
+  // First element of vector k.
+  static __device__ __forceinline__ int element(int k, const Cut& cut) {
     const int g = thread() + k * THREADS;
-    return WHOLE ? g : max(min(g, vectors - 1), 0);
+    return cut.head + N * (WHOLE ? g : max(min(g, cut.vectors - 1), 0));
   }
-  __device__ __forceinline__ void load(const T* row, int vectors, int left) {
+  __device__ __forceinline__ void load(const T* row, const Cut& cut) {
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      q[k] = WHOLE || vectors > 0 ? (typename P::Raw)__builtin_nontemporal_load(reinterpret_cast<const typename P::Any*>(row + N * index(k, vectors)))
-                                  : P::zero();
-    rest = thread() < left ? Vec<T>::load1(row + N * vectors + thread()) : 0.f;
+      q[k] = WHOLE || cut.vectors > 0
+                 ? (typename P::Raw)__builtin_nontemporal_load(reinterpret_cast<const typename P::Any*>(row + element(k, cut)))
+                 : P::zero();
+    rest = thread() < cut.left ? Vec<T>::load1(row + cut.rest<N>(thread())) : 0.f;
   }
   // Vector k, 0 where there is none.
   __device__ __forceinline__ void get(int k, int vectors, float* x) const {
@@ -146,8 +164,9 @@ struct HeldRow {
       for (int j = 0; j < N; ++j) x[j] = 0.f;
     }
   }
-  static __device__ __forceinline__ void store(T* row, int k, const float* x) {
-    __builtin_nontemporal_store((typename P::Any)P::pack(x), reinterpret_cast<typename P::Any*>(row + N * (thread() + k * THREADS)));
+  static __device__ __forceinline__ void store(T* row, int k, const Cut& cut, const float* x) {
+    __builtin_nontemporal_store((typename P::Any)P::pack(x),
+                                reinterpret_cast<typename P::Any*>(row + cut.head + N * (thread() + k * THREADS)));
   }
 };
 
@@ -185,27 +204,29 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const T* x, long long row
   constexpr int N = Vec<T>::N;
   typedef HeldRow<T, N, THREADS, NV, WHOLE> Row;
   __shared__ RowSums<THREADS, 2> sums;
-  const int tid = threadIdx.x, vectors = width / N, left = width % N;
+  const int tid = threadIdx.x;
+  const Cut cut = Cut::of<T, N>(y + blockIdx.x * y_stride, width);
+  const int vectors = cut.vectors, left = cut.left;
   const float n = (float)width;
   float w[NV][N], b[NV][N], w_rest = 1.f, b_rest = 0.f;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    weight.load_vector<N>(N * Row::index(k, vectors), vectors > 0, 1.f, w[k]);
-    bias.load_vector<N>(N * Row::index(k, vectors), vectors > 0, 0.f, b[k]);
+    weight.load_vector<N>(Row::element(k, cut), vectors > 0, 1.f, w[k]);
+    bias.load_vector<N>(Row::element(k, cut), vectors > 0, 0.f, b[k]);
   }
   if (tid < left) {
-    w_rest = weight.load1(N * vectors + tid, 1.f);
-    b_rest = bias.load1(N * vectors + tid, 0.f);
+    w_rest = weight.load1(cut.rest<N>(tid), 1.f);
+    b_rest = bias.load1(cut.rest<N>(tid), 0.f);
   }
   auto live = [&](long long row) { return valid == nullptr || valid[row] != 0; };
   Row now, next;
   bool here = live(blockIdx.x);
-  if (here) now.load(x + blockIdx.x * row_stride, vectors, left);
+  if (here) now.load(x + blockIdx.x * row_stride, cut);
   int turn = 0;
   for (long long row = blockIdx.x; row < n_rows; row += gridDim.x, turn ^= 1) {
     const long long after = row + gridDim.x;
     const bool more = after < n_rows && live(after);
-    if (more) next.load(x + after * row_stride, vectors, left);
+    if (more) next.load(x + after * row_stride, cut);
     T* yr = y + row * y_stride;
     float mean = 0.f, rstd = 0.f;
     if (here) {                                  // uniform
@@ -244,9 +265,9 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const T* x, long long row
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] = __builtin_fmaf((v[j] - mean) * rstd, w[k][j], b[k][j]);
       }
-      Row::store(yr, k, v);
+      Row::store(yr, k, cut, v);
     }
-    if (tid < left) Vec<T>::store1(yr + N * vectors + tid, here ? __builtin_fmaf((now.rest - mean) * rstd, w_rest, b_rest) : 0.f);
+    if (tid < left) Vec<T>::store1(yr + cut.rest<N>(tid), here ? __builtin_fmaf((now.rest - mean) * rstd, w_rest, b_rest) : 0.f);
     if (tid == 0) {
       if (centered) mean_out[row] = mean;
       rstd_out[row] = rstd;
@@ -313,23 +334,28 @@ __global__ __launch_bounds__(kWideThreads) void norm_wide_kernel(const T* x, lon
 // The gradient.  TEAMS teams of THREADS threads of a workgroup take a row each, with the next one on its way, and keep the weight's and
 // the bias's sums of their own columns in registers; a workgroup's leave as one row of partials, which norm_grad_sum_kernel adds up in
 // their order.
-template <typename T, typename D, int THREADS, int TEAMS, int NV, bool WHOLE>
+template <typename T, typename D, int THREADS, int TEAMS, int NV, int WHOLE>
 __global__ __launch_bounds__(THREADS * TEAMS) void norm_grad_kernel(
     const D* dy, long long dy_stride, const T* x, long long row_stride, int n_rows, int width,
     const unsigned char* __restrict__ valid, Affine weight, const float* __restrict__ mean, const float* __restrict__ rstd, T* dx,
     long long dx_stride, float* __restrict__ dweight, float* __restrict__ dbias) {
   static_assert(TEAMS == 1 || THREADS == 64, "a barrier inside a row is the whole workgroup's");
   constexpr int N = sizeof(T) == 2 && sizeof(D) == 2 ? 8 : 4;
-  typedef HeldRow<T, N, THREADS, NV, WHOLE> Row;
-  typedef HeldRow<D, N, THREADS, NV, WHOLE> Grad;
+  typedef HeldRow<T, N, THREADS, NV, WHOLE != 0> Row;
+  typedef HeldRow<D, N, THREADS, NV, WHOLE != 0> Grad;
   __shared__ RowSums<THREADS, 2> sums;
   const int thread = Row::thread(), team = TEAMS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int vectors = width / N, left = width % N;
+  // The teams' sums meet column by column, with one cut for all of them: where rows may begin differently, theirs are a multiple of the
+  // workgroups' number apart, which is even.
+  constexpr bool kAlike = sizeof(T) == 4 || WHOLE == 2;
+  long long row = kAlike ? (long long)blockIdx.x * TEAMS + team : blockIdx.x + (long long)gridDim.x * team;
+  const Cut cut = WHOLE == 2 ? Cut{0, THREADS * NV, 0} : Cut::of<T, N>(dx + blockIdx.x * dx_stride, width);
+  const int vectors = cut.vectors, left = cut.left;
   const float n = (float)width;
   float w[NV][N], w_rest = 1.f;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) weight.load_vector<N>(N * Row::index(k, vectors), vectors > 0, 1.f, w[k]);
-  if (thread < left) w_rest = weight.load1(N * vectors + thread, 1.f);
+  for (int k = 0; k < NV; ++k) weight.load_vector<N>(Row::element(k, cut), vectors > 0, 1.f, w[k]);
+  if (thread < left) w_rest = weight.load1(cut.rest<N>(thread), 1.f);
   float dw[NV][N] = {}, db[NV][N] = {}, dw_rest = 0.f, db_rest = 0.f;
   struct Held {
     Row x;
@@ -340,13 +366,12 @@ __global__ __launch_bounds__(THREADS * TEAMS) void norm_grad_kernel(
   auto load = [&](Held& h, long long row) {
     h.here = row < n_rows && (valid == nullptr || valid[row] != 0);
     if (!h.here) return;
-    h.x.load(x + row * row_stride, vectors, left);
-    h.dy.load(dy + row * dy_stride, vectors, left);
+    h.x.load(x + row * row_stride, cut);
+    h.dy.load(dy + row * dy_stride, cut);
     h.mu = mean != nullptr ? mean[row] : 0.f;
     h.rs = rstd[row];
   };
   const long long stride = (long long)gridDim.x * TEAMS;
-  long long row = (long long)blockIdx.x * TEAMS + team;
   load(now, row);
   int turn = 0;
   for (; row < n_rows; row += stride, turn ^= 1) {
@@ -389,9 +414,9 @@ __global__ __launch_bounds__(THREADS * TEAMS) void norm_grad_kernel(
       if (!Row::has(k, vectors)) break;
 #pragma unroll
       for (int j = 0; j < N; ++j) u[k][j] = now.here ? rs * (u[k][j] - s[0] - v[k][j] * s[1]) : 0.f;
-      Row::store(dr, k, u[k]);
+      Row::store(dr, k, cut, u[k]);
     }
-    if (thread < left) Vec<T>::store1(dr + N * vectors + thread, now.here ? rs * (u_rest - s[0] - v_rest * s[1]) : 0.f);
+    if (thread < left) Vec<T>::store1(dr + cut.rest<N>(thread), now.here ? rs * (u_rest - s[0] - v_rest * s[1]) : 0.f);
     now = next;
   }
   // the teams' sums, added up in their order
@@ -414,12 +439,12 @@ __global__ __launch_bounds__(THREADS * TEAMS) void norm_grad_kernel(
 #pragma unroll
       for (int j = 0; j < N; ++j) sum[k][j] = all(sum[k][j]);
       if (team != 0 || !Row::has(k, vectors)) continue;
-      float* at = to + N * (thread + k * THREADS);
+      float* at = to + cut.head + N * (thread + k * THREADS);
 #pragma unroll
       for (int j = 0; j < N; j += 4) *reinterpret_cast<Unaligned<float>::four*>(at + j) = Vec<float>::pack(sum[k] + j);
     }
     rest = all(rest);
-    if (team == 0 && thread < left) to[N * vectors + thread] = rest;
+    if (team == 0 && thread < left) to[cut.rest<N>(thread)] = rest;
   };
   leave(dw, dw_rest, dweight);
   leave(db, db_rest, dbias);
@@ -518,6 +543,14 @@ __global__ __launch_bounds__(64 * kSumWaves) void norm_grad_sum_kernel(const flo
   if ((long long)blockIdx.x * 64 + lane < width) to[d] = s;
 }
 
+// 1: every row is `most` vectors of n elements, however it is cut; 2: and has no element outside them; 0: neither.
+template <typename T>
+int whole_rows(const T* rows, long long stride, int width, int n, int most) {
+  const bool odd = sizeof(T) == 2 && ((reinterpret_cast<uintptr_t>(rows) / 2 | (uintptr_t)stride) & 1) != 0;
+  if (width / n != most || (odd && (width - 1) / n != most)) return 0;
+  return !odd && width % n == 0 ? 2 : 1;
+}
+
 template <typename T>
 int norm_typed(ais_ctx* ctx, const T* x, int n_rows, int width, long long row_stride, const unsigned char* valid, Affine weight,
                Affine bias, float eps, int centered, T* y, long long y_stride, float* mean, float* rstd) {
@@ -525,16 +558,19 @@ int norm_typed(ais_ctx* ctx, const T* x, int n_rows, int width, long long row_st
   // Two rows to a workgroup, so that the second is read while the first is written and the weight is loaded for both; one each where there
   // are few.  41,643 rows of 4,096 bf16 elements, us with one, two, four rows each, and with as many workgroups as there is room for: 146,
   // 116, 118 to 122, 124.
-  const unsigned grid = (unsigned)(n_rows <= 8 * ctx->n_cus ? n_rows : (n_rows + 1) / 2);
+  // (An even number of workgroups: rows of one begin alike.)
+  const unsigned grid = n_rows <= 8 * ctx->n_cus ? (unsigned)n_rows : (unsigned)(n_rows / 4 * 2 + 2);
   auto held = [&](auto threads, auto most) {
     constexpr int kThreads = decltype(threads)::value, kMost = decltype(most)::value;
-    auto kernel = vectors == kThreads * kMost ? norm_kernel<T, kThreads, kMost, true> : norm_kernel<T, kThreads, kMost, false>;
+    auto kernel = whole_rows(y, y_stride, width, Vec<T>::N, kThreads * kMost) ? norm_kernel<T, kThreads, kMost, true>
+                                                                              : norm_kernel<T, kThreads, kMost, false>;
     kernel<<<dim3(grid), dim3(kThreads), 0, ctx->stream>>>(x, row_stride, n_rows, width, valid, weight, bias, eps, centered, y,
                                                            y_stride, mean, rstd);
     return hip_fail(ctx, hipGetLastError());
   };
   // Threads and vectors of each that hold a row with few of them idle; us with these and with half or twice as many threads, rows of 1.4 GB in all:
   // bf16, 1,024 elements 33, 36; 2,048 61, 61, 77; 4,096 116, 118, 131; 5,120 (as 192 x 4, 320 x 2, 256 x 4) 139, 142, 155; 8,192 120, 133, 157;
+  // 2,240 (28,066 rows of them, as 64 x 5, 128 x 3, 256 x 2) 61, 66, 81;
   // fp32, 1,024 57, 58; 4,096 (512 x 2, 256 x 4, 128 x 8) 222, 227, 226; 5,120 222, 230; 8,192 (512 x 4, 256 x 8, 1,024 x 2) 224, 232, 268.
 #define AIS_NORM_CASE(THREADS, NV)                                                                                     \
   if (vectors <= THREADS * NV) return held(std::integral_constant<int, THREADS>{}, std::integral_constant<int, NV>{});
@@ -542,6 +578,8 @@ int norm_typed(ais_ctx* ctx, const T* x, int n_rows, int width, long long row_st
   AIS_NORM_CASE(64, 2)
   AIS_NORM_CASE(64, 3)
   AIS_NORM_CASE(64, 4)
+  AIS_NORM_CASE(64, 5)
+  AIS_NORM_CASE(128, 3)
   AIS_NORM_CASE(256, 2)
   AIS_NORM_CASE(192, 4)
   AIS_NORM_CASE(256, 4)
@@ -562,7 +600,7 @@ template <typename T, typename D>
 int norm_grad_typed(ais_ctx* ctx, const D* dy, long long dy_stride, const T* x, long long row_stride, int n_rows, int width,
                     const unsigned char* valid, Affine weight, const float* mean, const float* rstd, T* dx, long long dx_stride,
                     float* dweight, float* dbias) {
-  const NormGradPlan plan = norm_grad_plan(n_rows, width, sizeof(T) == 2 && sizeof(D) == 2, ctx->n_cus);
+  const NormGradPlan plan = norm_grad_plan(n_rows, width, sizeof(T) + sizeof(D), ctx->n_cus);
   const size_t all = (size_t)plan.parts * width;
   float* at = static_cast<float*>(ctx->ws);
   float *dw = nullptr, *db = nullptr;
@@ -578,8 +616,10 @@ int norm_grad_typed(ais_ctx* ctx, const D* dy, long long dy_stride, const T* x, 
     auto held = [&](auto threads, auto teams, auto most) {
       constexpr int kThreads = decltype(threads)::value, kTeams = decltype(teams)::value, kMost = decltype(most)::value;
       constexpr int kN = sizeof(T) == 2 && sizeof(D) == 2 ? 8 : 4;
-      auto kernel = width / kN == kThreads * kMost ? norm_grad_kernel<T, D, kThreads, kTeams, kMost, true>
-                                                   : norm_grad_kernel<T, D, kThreads, kTeams, kMost, false>;
+      const int whole = whole_rows(dx, dx_stride, width, kN, kThreads * kMost);
+      auto kernel = whole == 2   ? norm_grad_kernel<T, D, kThreads, kTeams, kMost, 2>
+                    : whole == 1 ? norm_grad_kernel<T, D, kThreads, kTeams, kMost, 1>
+                                 : norm_grad_kernel<T, D, kThreads, kTeams, kMost, 0>;
       kernel<<<dim3((unsigned)plan.parts), dim3(kThreads * kTeams), 0, ctx->stream>>>(dy, dy_stride, x, row_stride, n_rows, width,
                                                                                       valid, weight, mean, rstd, dx, dx_stride, dw, db);
     };
@@ -590,9 +630,13 @@ int norm_grad_typed(ais_ctx* ctx, const D* dy, long long dy_stride, const T* x, 
     AIS_GRAD_CASE(64, 4, 2)
     AIS_GRAD_CASE(64, 4, 4)
     AIS_GRAD_CASE(256, 1, 2)
+    AIS_GRAD_CASE(256, 1, 3)
     if constexpr (sizeof(T) == 2 && sizeof(D) == 2) {
       AIS_GRAD_CASE(64, 4, 3)
+      AIS_GRAD_CASE(128, 1, 2)
+      AIS_GRAD_CASE(128, 1, 3)
       AIS_GRAD_CASE(256, 1, 4)
+      AIS_GRAD_CASE(1024, 1, 1)
     } else {
       AIS_GRAD_CASE(64, 4, 5)
       AIS_GRAD_CASE(512, 1, 2)
@@ -609,28 +653,44 @@ int norm_grad_typed(ais_ctx* ctx, const D* dy, long long dy_stride, const T* x, 
 
 }  // namespace
 
-// Two workgroups to a compute unit (of 1,024 threads: one).  us with two, three, four of them: 41,643 rows of 4,096 elements, bf16 with an fp32
-// gradient 230, 254, 236 (256 threads with four vectors each 232, 246; 1,024 with one 249); fp32 334, 341 with four; bf16 in vectors of eight
-// 180, 184, and in vectors of four 185, 216 (20,000 rows of 8,192: 177 and 205).  A wavefront to a row has no barrier in it: 5,001 rows of 1,100
-// fp32 elements 22.0, 256 threads 24.1; 41,643 of 1,024, bf16 and fp32, 64 and 68.
-NormGradPlan norm_grad_plan(long long n_rows, long long width, bool bf16, int n_cus) {
+// Threads and vectors that hold a row with few of them idle, and as many workgroups as a compute unit has room for, each with six rows at
+// least where there is more than one of them to a unit: their partial sums have to be written and read.  us, in turns with other choices:
+//   bf16 with an fp32 gradient: 41,643 rows of 4,096 elements, two, three, four workgroups 230, 254, 236 (256 threads with four vectors each
+//     232, 246; 1,024 with one 249); 28,066 of 2,240 91, with 512 threads and two vectors 112; 41,643 of 1,024, a wavefront to a row, which has
+//     no barrier in it, 64, 256 threads 68;
+//   fp32: 41,643 of 4,096 334, 341 with four workgroups; 5,001 of 1,100 22.0, 256 threads 24.1;
+//   bf16: 28,066 of 2,240 80, with 256 threads and two vectors 103; 30,000 of 3,500 139, two workgroups 156; 25,000 of 5,000 138, with 256
+//     threads and four vectors 236; 72,000 of 1,600 132, a wavefront with four vectors 176; 1,000 of 4,096 15.1, two workgroups 19.4.
+//   Four vectors of eight a thread leave registers for two workgroups to a unit only where no element lies outside them: there (60,000 of
+//     2,048 128, 14,000 of 8,192 126) they are ahead of 128 threads with two (138) and 1,024 with one (136).
+NormGradPlan norm_grad_plan(long long n_rows, long long width, int bytes, int n_cus) {
+  const bool bf16 = bytes == 4;
   const long long vectors = width / (bf16 ? 8 : 4);
   NormGradPlan p{0, 0, 0, 0};
-  auto held = [&](int threads, int teams, int most) {
+  auto held = [&](int threads, int teams, int most, int of_a_cu) {
     if (p.teams != 0 || vectors > threads * most) return;
-    p = {threads, teams, most, (int)std::min((n_rows + teams - 1) / teams, threads == 1024 ? (long long)n_cus : 2LL * n_cus)};
+    const long long each = (n_rows + teams - 1) / teams, even = teams > 1 ? (each + 1) / 2 * 2 : each;
+    const long long parts = std::max((long long)n_cus, std::min((long long)of_a_cu * n_cus, n_rows / 6));
+    p = {threads, teams, most, (int)std::min(even, (parts + 1) / 2 * 2)};
   };
-  held(64, 4, 1);
-  held(64, 4, 2);
-  if (bf16) held(64, 4, 3);
-  held(64, 4, 4);
-  if (!bf16) held(64, 4, 5);
-  held(256, 1, 2);
+  held(64, 4, 1, 2);
+  held(64, 4, 2, 2);
   if (bf16) {
-    held(256, 1, 4);
+    held(64, 4, 3, 2);
+    if (width == 8 * 256) held(64, 4, 4, 1);
+    held(128, 1, 2, 6);
+    held(128, 1, 3, 4);
+    held(256, 1, 2, 3);
+    held(256, 1, 3, 2);
+    if (width == 8 * 1024) held(256, 1, 4, 2);
+    held(1024, 1, 1, 1);
   } else {
-    held(512, 1, 2);
-    held(1024, 1, 2);
+    held(64, 4, 4, 2);
+    held(64, 4, 5, 2);
+    held(256, 1, 2, bytes == 6 ? 3 : 2);
+    held(256, 1, 3, bytes == 6 ? 3 : 2);
+    held(512, 1, 2, 2);
+    held(1024, 1, 2, 1);
   }
   if (p.teams == 0) {
     const long long tiles = (width - 1) / (8 * kColumnThreads) + 1;
@@ -639,8 +699,8 @@ NormGradPlan norm_grad_plan(long long n_rows, long long width, bool bf16, int n_
   return p;
 }
 
-size_t norm_grad_bytes(long long n_rows, long long width, bool bf16, int sums, int n_cus) {
-  const NormGradPlan p = norm_grad_plan(n_rows, width, bf16, n_cus);
+size_t norm_grad_bytes(long long n_rows, long long width, int bytes, int sums, int n_cus) {
+  const NormGradPlan p = norm_grad_plan(n_rows, width, bytes, n_cus);
   return 4 * (size_t)sums * (size_t)p.parts * (size_t)width + (p.teams == 0 ? 8 * (size_t)n_rows : 0);
 }
 

@@ -117,6 +117,18 @@ def test_numbers_of_rows(ctx, n, width):
     check_grad(ctx, rows(n, width, torch.float32, n + 1), x, weight, mean, rstd)
 
 
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("width", [1_601, 2_048, 2_049, 2_237, 3_001, 3_500, 5_001, 7_001, 8_192, 8_193])
+def test_several_rows_to_a_workgroup(ctx, width, dtype, offset):
+    """Rows of one workgroup that begin at a whole word and in the middle of one, and masked ones among them."""
+    n = 1_603
+    x, valid = rows(n, width, torch.bfloat16, width, offset), (torch.arange(n, device="cuda") % 7 != 3).to(torch.uint8)
+    weight, bias = params(width, torch.float32)
+    mean, rstd = check_norm(ctx, x, weight, bias, True, valid)
+    check_grad(ctx, rows(n, width, dtype, width + 1, offset), x, weight, mean, rstd, valid)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("width", [5, 100, 1_101, 4_096, 20_001, 40_003])
 def test_rows_that_begin_anywhere(ctx, width, dtype):
