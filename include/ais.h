@@ -522,7 +522,7 @@ int ais_norm_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows
  *   x, weight   as above;  mean, rstd  outputs of ais_norm_rows; mean NULL: root-mean-square norm
  *   dx          [n_rows, dx_stride] of `dtype`, 0 where valid == 0.  May be dy itself (same type and stride), or x.
  *   dweight_out, dbias_out   [width] fp32, each NULL where it is not wanted; summed in a fixed order, without atomics
- * Uses 4 * width bytes of the context workspace for each sum that is wanted and each of up to two workgroups a compute unit; for rows of more
+ * Uses 4 * width bytes of the context workspace for each sum that is wanted and each of up to six workgroups a compute unit; for rows of more
  * than 8,192 elements up to 8 workgroups, divided by width / 2,048, and 8 * n_rows bytes beside.
  * Errors: NULL dy / x / rstd / dx (with n_rows > 0), otherwise as ais_norm_rows. */
 int ais_norm_rows_grad(ais_ctx* ctx, const void* dy, ais_dtype dy_dtype, long long dy_stride, const void* x, ais_dtype dtype,
