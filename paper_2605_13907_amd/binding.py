@@ -271,7 +271,7 @@ class AdamWState:
                  tensor i begins at offsets[i], a multiple of 32; of() gives the part of one tensor.  A state that goes on from
                  stored moments is made with them, or has them copied into its buffers; the buffers stay the same ones.
     step         number of steps made; an int, or an int64 tensor of one element on the GPU, which a HIP graph counts on when it
-                 is replayed
+                 is replayed (with an int a call is not recorded: every replay would be the same step)
     seed         of the random numbers that 8-bit moments are rounded with
     """
 
@@ -880,6 +880,8 @@ class AisContext:
         r.step = 0 if on_gpu else step + 1
         dev = self.device
         if not on_gpu:
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError("step: a call that is recorded needs a tensor on the GPU")
             out = self._native("adamw_step", C.addressof(state._table), state._on_gpu, C.addressof(r), state.params, state.copies, state.m, state.v,
                                state.m_scale, state.v_scale, grads, grad_scale, lr_dev)
             if out is not None:

@@ -123,6 +123,24 @@ def test_recorded_steps_match_eager_ones(bits):
     ctx.close()
 
 
+def test_a_count_on_the_host_is_not_recorded():
+    ctx = B.AisContext()
+    state, grad = B.AdamWState([torch.ones(100, device="cuda")]), [torch.ones(100, device="cuda")]
+    ctx.adamw_step(state, grad)
+    want = state.params[0].clone()
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            other = grad[0] * 2
+            with pytest.raises(ValueError, match="step"):
+                ctx.adamw_step(state, grad)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(state.params[0], want) and state.step == 1 and bool((other == 2).all())
+    ctx.close()
+
+
 def test_two_graphs_share_a_workspace():
     """Two recorded calls of different sizes, replayed one after the other in either order."""
     ctx = B.AisContext()
