@@ -14,7 +14,7 @@ import importlib.util
 import os
 import sysconfig
 import warnings
-from typing import Optional
+from typing import Optional, overload
 
 import torch
 
@@ -772,11 +772,42 @@ class AisContext:
             raise AisError(rc, "ais_preference_row_scale")
         return loss, reward, g
 
+    @overload
     def preference_loss_grad(self, logits, token_ids, valid, cu_rows, logp_ref, params: Optional[AisPreferenceParams] = None,
-                             weight=None, want_grad: bool = True, dlogits=None):
-        """-> (loss [1] fp32, reward [B] fp32, logp [R] fp32, dlogits like logits or None): the loss through logits, whose tokens'
-        log-probs are formed in the call.  Pass dlogits=logits to overwrite the logits in place.  See ais_preference_loss_grad in
-        include/ais.h."""
+                             weight=None, want_grad: bool = True, dlogits=None): ...
+
+    @overload
+    def preference_loss_grad(self, logits, token_ids, valid, cu_rows, logp_train, lse, logp_ref,
+                             params: Optional[AisPreferenceParams] = None, weight=None, dlogits=None): ...
+
+    def preference_loss_grad(self, logits, token_ids, valid, cu_rows, *args, **kwargs):
+        """preference_loss_grad(logits, token_ids, valid, cu_rows, logp_ref, params=None, weight=None, want_grad=True, dlogits=None)
+        -> (loss [1] fp32, reward [B] fp32, logp [R] fp32, dlogits like logits or None): the loss through logits, whose tokens'
+        log-probs are formed in the call.  Pass dlogits=logits to overwrite the logits in place.
+
+        preference_loss_grad(logits, token_ids, valid, cu_rows, logp_train, lse, logp_ref, params=None, weight=None, dlogits=None)
+        -> (loss, reward, dlogits), the same ones: for programs that hold logp_train and lse, token_logprob's outputs for these
+        logits.  A response's log-ratios nearly cancel, and log-probs that were summed and rounded in 32 bits leave rewards 2e-5 off:
+        the call forms its own in 64 bits all the same, at the price of another pass over the logits, and looks at the given ones'
+        form alone.
+
+        See ais_preference_loss_grad in include/ais.h."""
+        if "lse" in kwargs or "logp_train" in kwargs or (len(args) > 1 and isinstance(args[1], torch.Tensor)):
+            return self._preference_with_logprobs(logits, token_ids, valid, cu_rows, *args, **kwargs)
+        return self._preference_through_logits(logits, token_ids, valid, cu_rows, *args, **kwargs)
+
+    def _preference_with_logprobs(self, logits, token_ids, valid, cu_rows, logp_train, lse, logp_ref, params=None, weight=None,
+                                  dlogits=None):
+        n_rows = _logits_geometry(logits, self.device)[0]
+        for name, t in (("logp_train", logp_train), ("lse", lse)):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name} must be a torch.Tensor")
+            _ptr(t, torch.float32, n_rows, name, self.device)
+        out = self._preference_through_logits(logits, token_ids, valid, cu_rows, logp_ref, params, weight, True, dlogits)
+        return out[0], out[1], out[3]
+
+    def _preference_through_logits(self, logits, token_ids, valid, cu_rows, logp_ref, params=None, weight=None, want_grad=True,
+                                   dlogits=None):
         p = params or default_preference_params()
         if p.__class__ is AisPreferenceParams:
             out = self._native("preference_loss_grad", logits, token_ids, logp_ref, valid, cu_rows, weight, C.addressof(p),
