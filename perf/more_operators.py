@@ -388,8 +388,9 @@ def run(state):
         return dict(pairs=plain_pairs, norm=plain_norm, norm_grad=plain_norm_grad, adamw=plain_adamw)[kind](s)
     ctx = context()
     if kind == "pairs":
-        loss, reward, _, dlogits = ctx.preference_loss_grad(s["logits"], s["ids"], s["valid"], s["cu"], s["ref"], loss_params(case),
-                                                            weight=s["weight"])
+        logp, lse = ctx.token_logprob(s["logits"], s["ids"], s["valid"])
+        loss, reward, dlogits = ctx.preference_loss_grad(s["logits"], s["ids"], s["valid"], s["cu"], logp, lse, s["ref"],
+                                                         loss_params(case), weight=s["weight"])
         return dict(loss=loss, reward=reward, dlogits=dlogits)
     if kind == "scores":
         loss, reward, g = ctx.preference_row_scale(s["logp"], s["ref"], s["valid"], s["cu"], loss_params(case), weight=s["weight"])
