@@ -170,8 +170,9 @@ struct HeldRow {
   }
 };
 
-// Sums of a row's parts over the THREADS threads that share it.  Rows take turns with two places in LDS, so that one barrier a sum is enough:
-// whoever writes a place again has passed the next row's barrier, which nobody reaches before having read this one.
+// Sums of a row's parts over the THREADS threads that share it.  The rows that are summed take turns with two places in LDS, so that one
+// barrier a sum is enough: whoever writes a place again has passed the barrier of the row summed in between, which nobody reaches before
+// having read this one.  (Masked rows have no barrier: they take no turn.)
 template <int THREADS, int SUMS>
 struct RowSums {
   float part[2][SUMS][THREADS == 64 ? 1 : THREADS / 64];
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const T* x, long long row
   bool here = live(blockIdx.x);
   if (here) now.load(x + blockIdx.x * row_stride, cut);
   int turn = 0;
-  for (long long row = blockIdx.x; row < n_rows; row += gridDim.x, turn ^= 1) {
+  for (long long row = blockIdx.x; row < n_rows; row += gridDim.x) {
     const long long after = row + gridDim.x;
     const bool more = after < n_rows && live(after);
     if (more) next.load(x + after * row_stride, cut);
@@ -255,6 +256,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const T* x, long long row
       }
       sums.add(turn, 1, 1, &q);
       rstd = 1.f / sqrtf(q / n + eps);
+      turn ^= 1;
     }
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -374,7 +376,7 @@ __global__ __launch_bounds__(THREADS * TEAMS) void norm_grad_kernel(
   const long long stride = (long long)gridDim.x * TEAMS;
   load(now, row);
   int turn = 0;
-  for (; row < n_rows; row += stride, turn ^= 1) {
+  for (; row < n_rows; row += stride) {
     load(next, row + stride);
     T* dr = dx + row * dx_stride;
     float v[NV][N], u[NV][N], v_rest = 0.f, u_rest = 0.f, s[2] = {0.f, 0.f};
@@ -406,6 +408,7 @@ __global__ __launch_bounds__(THREADS * TEAMS) void norm_grad_kernel(
         s[1] += u_rest * v_rest;
       }
       sums.add(turn, 0, 2, s);
+      turn ^= 1;
       s[0] = mean != nullptr ? s[0] / n : 0.f;
       s[1] /= n;
     }
