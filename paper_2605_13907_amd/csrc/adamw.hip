@@ -66,7 +66,7 @@ __host__ __device__ __forceinline__ double power(double b, long long n) {
 struct Now {
   long long step;
   double b1, b2, g1, g2;                         // of the moments, of the gradient and its square
-  float c2, decay, rate;                         // v's correction; lr with the decay, and with m's correction
+  float c2, c2_small, decay, rate;               // v's correction, and times 2^64; lr with the decay, and with m's correction
   __device__ __forceinline__ explicit Now(const Rule& r) : step(r.step), b1(r.b1), b2(r.b2) {
     double c1d = r.c1, c2d = r.c2, scale = 1.0;
     float lr = r.lr;
@@ -80,6 +80,7 @@ struct Now {
     g1 = (1.0 - b1) * scale;
     g2 = (1.0 - b2) * (scale * scale);
     c2 = (float)c2d;
+    c2_small = c2 * 0x1p64f;                     // at most 2^53 times that: 1 - b2 is at least 2^-53
     decay = (float)((double)lr * (double)r.decay);
     rate = (float)((double)lr * c1d);
   }
@@ -121,6 +122,13 @@ __device__ __forceinline__ uint32_t encode(uint32_t bits, uint32_t byte, uint32_
   const uint32_t low = (uint32_t)__builtin_ldexpf(__uint_as_float(bits), 150 - (int)smallest);
   const uint32_t fixed = bits < smallest << 23 ? low : bits - ((smallest - 1) << 23);
   return (fixed + (random16 << 4)) >> 20;
+}
+
+// sqrt(v c2) + eps.  The root is the hardware's, which takes subnormal numbers for 0: small squares are scaled before and behind it.
+constexpr float kSmall = 0x1p-100f;
+__device__ __forceinline__ float root_of(float v, const Now& now, float eps) {
+  const bool small = v < kSmall;
+  return __builtin_fmaf(__builtin_amdgcn_sqrtf(v * (small ? now.c2_small : now.c2)), small ? 0x1p-32f : 1.f, eps);
 }
 
 // Largest of the 32 elements of the eight lanes that share a block; a NaN counts as an infinity, since no maximum drops that.
@@ -218,7 +226,7 @@ __device__ __forceinline__ void step_chunk(const ais_adamw_tensor& t, const G* g
       m[i][j] = (float)__builtin_fma(mb, (double)m[i][j], now.g1 * gs);
       v[i][j] = (float)__builtin_fma(vb, (double)v[i][j], now.g2 * (gs * gs));
       if (!WHOLE && j >= n[i]) m[i][j] = v[i][j] = 0.f;
-      const float ahead = m[i][j] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[i][j] * now.c2) + rule.eps);
+      const float ahead = m[i][j] * __builtin_amdgcn_rcpf(root_of(v[i][j], now, rule.eps));
       p[i][j] -= __builtin_fmaf(now.decay, p[i][j], now.rate * ahead);
     }
     store4(static_cast<P*>(t.param) + at[i], n[i], whole, p[i]);
