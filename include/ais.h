@@ -579,9 +579,9 @@ void ais_adamw_params_default(ais_adamw_params* p);
  *   grad_scale  one fp32 in device memory, or NULL (1): a factor from a clipped norm or a loss scale
  *   step_dev, lr_dev   one int64 and one fp32 in device memory that replace params->step and params->lr, or NULL: what a HIP graph
  *               that is replayed needs (the step is read, not counted)
- * One launch for each 320 tensors; no workspace.
- * Errors: NULL tensors or table (with n_tensors > 0) / params, n_tensors < 0, n < 0 or >= 2^32 - 4096, more than 2^41 elements in all, NULL
- * or misaligned arrays of a tensor that is stepped, a misaligned table, unknown dtypes, parameters outside their ranges, step < 1 without step_dev (AIS_ERR_PARAM). */
+ * One launch for each 320 tensors, or for each 2^33 elements (2^34 with moments of 32 bits) where there are more; no workspace.
+ * Errors: NULL tensors or table (with n_tensors > 0) / params, n_tensors < 0, n < 0 or >= 2^32 - 4096, NULL or misaligned arrays of a
+ * tensor that is stepped, a misaligned table, unknown dtypes, parameters outside their ranges, step < 1 without step_dev (AIS_ERR_PARAM). */
 int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, const ais_adamw_tensor* table, int n_tensors,
                    const ais_adamw_params* params, const float* grad_scale, const long long* step_dev, const float* lr_dev);
 

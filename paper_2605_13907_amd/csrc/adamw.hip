@@ -9,6 +9,7 @@
 //
 // The moments are formed in 64 bits (the GPU's fp64 is as fast as its fp32) and rounded to fp32: which of two 8-bit codes a value
 // goes to depends on its last bits.
+#include <algorithm>
 #include <type_traits>
 
 #include "ais_internal.h"
@@ -34,6 +35,10 @@ struct Batch {
   unsigned first[kTensors];
 };
 static_assert(sizeof(Batch) + 128 <= 4096, "");
+// Workgroups of a launch, which may have no more than 2^32 - 1 threads: 2^31 here.  A tensor has 2^22 at most.
+constexpr long long kMostBlocks = (1LL << 31) / kThreads;
+// Of the launch that gives out moments' values, whose workgroups go on behind the others where there are more elements (2^31).
+constexpr long long kMostValueBlocks = 1 << 20;
 
 struct Rule {
   double b1, b2;
@@ -289,18 +294,18 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Batch batch, const ais_
 template <typename F, typename T>
 __device__ __forceinline__ void values_of(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
                                           long long n, T* __restrict__ out) {
-  const long long at = 8 * ((long long)blockIdx.x * kThreads + threadIdx.x);
-  if (at >= n) return;
-  const int here = (int)min(n - at, 8LL);
-  const double factor = decode_factor<F>(scales[at >> 5]);
-  uint32_t q[2];
+  for (long long at = 8 * ((long long)blockIdx.x * kThreads + threadIdx.x); at < n; at += 8LL * gridDim.x * kThreads) {
+    const int here = (int)min(n - at, 8LL);
+    const double factor = decode_factor<F>(scales[at >> 5]);
+    uint32_t q[2];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) q[k] = load_codes(codes + at + 4 * k, here - 4 * k, here >= 4 * k + 4);
-  float x[8];
+    for (int k = 0; k < 2; ++k) q[k] = load_codes(codes + at + 4 * k, here - 4 * k, here >= 4 * k + 4);
+    float x[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = (float)((double)code_bits<F>(q[j >> 2] >> (8 * (j & 3)) & 255u) * factor);
-  if (here == 8) Eight<T>::store(out + at, x);
-  else store_some(out + at, here, x);
+    for (int j = 0; j < 8; ++j) x[j] = (float)((double)code_bits<F>(q[j >> 2] >> (8 * (j & 3)) & 255u) * factor);
+    if (here == 8) Eight<T>::store(out + at, x);
+    else store_some(out + at, here, x);
+  }
 }
 template <typename T>
 __global__ __launch_bounds__(kThreads) void adamw_values_kernel(const unsigned char* m, const unsigned char* m_scale,
@@ -319,21 +324,29 @@ int launch_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, const ais_a
   const Rule rule{p.beta1, p.beta2, correction(p.beta1), correction(p.beta2), (float)p.lr, (float)p.eps, (float)p.weight_decay,
                   p.seed, p.step, grad_scale, step_dev, lr_dev};
   const int chunk = chunk_of(p.state_bits == 8);
-  for (int from = 0; from < n_tensors; from += kTensors) {
+  for (int from = 0, behind; from < n_tensors; from = behind) {
+    // the tensors before `behind`: as many as a launch has arguments for, whose workgroups it can have
     Batch batch;
-    unsigned blocks = 0;
+    long long blocks = 0;
+    behind = n_tensors;
     for (int k = 0; k < kTensors; ++k) {
-      const bool there = from + k < n_tensors;
-      batch.first[k] = there ? blocks : 0xffffffffu;
+      batch.first[k] = 0xffffffffu;
       batch.grad[k] = 0;
-      if (!there || tensors[from + k].grad == nullptr) continue;
+      if (from + k >= behind) continue;
       const ais_adamw_tensor& t = tensors[from + k];
-      batch.grad[k] = reinterpret_cast<uintptr_t>(t.grad) + (t.grad_dtype == AIS_BF16 ? 1 : 0);
-      blocks += (unsigned)((t.n + chunk - 1) / chunk);
+      const long long here = t.grad != nullptr ? (t.n + chunk - 1) / chunk : 0;
+      if (blocks + here > kMostBlocks) {
+        behind = from + k;
+        continue;
+      }
+      batch.first[k] = (unsigned)blocks;
+      blocks += here;
+      if (here > 0) batch.grad[k] = reinterpret_cast<uintptr_t>(t.grad) + (t.grad_dtype == AIS_BF16 ? 1 : 0);
     }
+    behind = std::min(behind, from + kTensors);
     if (blocks == 0) continue;
     auto kernel = p.state_bits == 8 ? adamw_kernel<true> : adamw_kernel<false>;
-    kernel<<<dim3(blocks), dim3(kThreads), 0, ctx->stream>>>(batch, table + from, from, rule);
+    kernel<<<dim3((unsigned)blocks), dim3(kThreads), 0, ctx->stream>>>(batch, table + from, from, rule);
     const int rc = hip_fail(ctx, hipGetLastError());
     if (rc != AIS_OK) return rc;
   }
@@ -345,7 +358,7 @@ int launch_adamw_values(ais_ctx* ctx, const unsigned char* m, const unsigned cha
   const unsigned moments = (m_out != nullptr) + (v_out != nullptr);
   if (n == 0 || moments == 0) return AIS_OK;
   ScopedTimer timer(ctx, AIS_K_ADAMW);
-  const dim3 grid((unsigned)((n + 8 * kThreads - 1) / (8 * kThreads)), moments);
+  const dim3 grid((unsigned)std::min((n + 8 * kThreads - 1) / (8 * kThreads), kMostValueBlocks), moments);
   if (dtype == AIS_BF16)
     adamw_values_kernel<<<grid, dim3(kThreads), 0, ctx->stream>>>(m, m_scale, v, v_scale, n, static_cast<bf16_t*>(m_out),
                                                                   static_cast<bf16_t*>(v_out));

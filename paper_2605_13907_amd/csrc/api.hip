@@ -896,13 +896,10 @@ int ais_adamw_step(ais_ctx* ctx, const ais_adamw_tensor* tensors, const ais_adam
   if (!least(p->beta1, 0.0) || p->beta1 >= 1.0 || !least(p->beta2, 0.0) || p->beta2 >= 1.0) return AIS_ERR_PARAM;
   if (p->state_bits != 32 && p->state_bits != 8) return AIS_ERR_PARAM;
   if (p->step < 1 && step_dev == nullptr) return AIS_ERR_PARAM;
-  long long chunks = 0;
   for (int i = 0; i < n_tensors; ++i) {
     const int rc = check_adamw_tensor(tensors[i], p->state_bits);
     if (rc != AIS_OK) return rc;
-    chunks += (tensors[i].n + 1023) / 1024;
   }
-  if (chunks > 0x7fffffffLL) return AIS_ERR_SIZE;      // workgroups of a launch
   if (ctx == nullptr) return AIS_ERR_NULL;
   DeviceGuard guard(ctx->device);
   return launch_adamw_step(ctx, tensors, table, n_tensors, *p, grad_scale, step_dev, lr_dev);

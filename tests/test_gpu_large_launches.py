@@ -1,0 +1,78 @@
+"""Calls with more elements or rows than one launch has threads for (no launch has 2^32): what lies behind the first launch's share, or what a
+workgroup comes to after its first share, is what it is in a call by itself."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.training_oracle as O
+from paper_2605_13907_amd import binding as B
+from tests.test_gpu_adamw import HALF, RULE, U, numbers, tensor
+
+pytestmark = pytest.mark.gpu
+
+GIB = 1 << 30
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.AisContext()
+    yield c
+    c.close()
+    torch.cuda.empty_cache()
+
+
+def room(gib):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gib * GIB:
+        pytest.skip(f"needs {gib} GiB")
+
+
+def test_a_step_of_many_billions(ctx):
+    """Six tensors of 2.9 billion elements, 16,992,192 workgroups of 256 threads in all: each one's end is stepped as by itself."""
+    room(80)
+    n, count, tail = 2_900_000_011, 6, 200
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[-tail:] = tensor(tail, torch.bfloat16, 2, 1e-3)
+    params = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(count)]
+    for i, p in enumerate(params):
+        p[-tail:] = tensor(tail, torch.bfloat16, 10 + i)
+    before, grad = [numbers(p[-tail:]) for p in params], numbers(g[-tail:])
+    state = B.AdamWState(params, bits=8, seed=5)
+    ctx.adamw_step(state, [g] * count, **RULE)
+    assert state.step == 1
+    first = (n - tail) // 32 * 32                                # the block that the tail begins in
+    at = np.arange(first, n, dtype=np.uint64)
+    for i, p in enumerate(params):
+        want, m, v = O.adamw(before[i], grad, np.zeros(tail), np.zeros(tail), 1, **RULE)
+        assert (np.abs(numbers(p[-tail:]) - want) <= HALF[torch.bfloat16] * np.abs(want) + 20 * U * (np.abs(want) + RULE["lr"])).all(), i
+        assert not p[:-tail].any()
+        key = O.mix(O.mix(5 ^ 0x9E3779B1) ^ (i * 0x9E3779B1 & O.M32))
+        bits = O.mix((at * np.uint64(0x9E3779B1) & np.uint64(O.M32)) ^ np.uint64(key))
+        for which, x, flat, rnd in ((1, m, state.m, bits & np.uint64(65535)), (2, v, state.v, bits >> np.uint64(16))):
+            codes, _ = O.encode(np.concatenate((np.zeros(n - tail - first, np.float32), x)), rnd, which)
+            assert (flat[state.offsets[i] + first:state.offsets[i] + n].cpu().numpy() == codes).all(), (i, which)
+
+
+@pytest.mark.parametrize("moment", [0, 1])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_values_of_billions(ctx, dtype, moment):
+    """2^31 elements are a workgroup's eight by 256 of the most that a launch has."""
+    room(16)
+    n, part = (1 << 31) + 2_077, 1 << 20
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    codes = torch.randint(0, 256, (n,), generator=gen, device="cuda", dtype=torch.uint8)
+    scales = torch.randint(90, 160, (-(-n // 32),), generator=gen, device="cuda", dtype=torch.uint8)
+
+    def values(at, count):
+        out = torch.full((count + 8,), 7.0, dtype=dtype, device="cuda")
+        arrays = [codes.data_ptr() + at, scales.data_ptr() + at // 32]
+        arrays = [*arrays, None, None, count, out.data_ptr(), None] if moment == 0 else [None, None, *arrays, count, None, out.data_ptr()]
+        assert ctx._lib.ais_adamw_values(ctx._h, *arrays, B.AIS_BF16 if dtype == torch.bfloat16 else B.AIS_F32) == 0
+        assert (out[count:] == 7.0).all()
+        return out[:count]
+
+    got = values(0, n)
+    for at in (0, (1 << 30) + 32, (1 << 31) - part, n // 32 * 32 - part):
+        assert torch.equal(got[at:at + part], values(at, part))
+    end = n // 32 * 32
+    assert torch.equal(got[end:], values(end, n - end))
