@@ -20,6 +20,9 @@ namespace {
 using namespace dev;
 
 constexpr int kWideThreads = 1024;
+// Workgroups of a launch, which may have no more than 2^32 - 1 threads; where there are more rows (columns, of the sums), each goes on
+// behind the others.  Of more than two million rows a workgroup that holds them has more than two.
+constexpr int kMostBlocks = 1 << 20, kMostWideBlocks = 1 << 16;
 
 // Weight or bias of either type; null: the value it stands for.
 struct Affine {
@@ -281,55 +284,56 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const T* x, long long row
 
 // Rows of any width, read three times.
 template <typename T>
-__global__ __launch_bounds__(kWideThreads) void norm_wide_kernel(const T* x, long long row_stride, int width,
+__global__ __launch_bounds__(kWideThreads) void norm_wide_kernel(const T* x, long long row_stride, int n_rows, int width,
                                                                  const unsigned char* __restrict__ valid, Affine weight,
                                                                  Affine bias, float eps, int centered, T* y, long long y_stride,
                                                                  float* __restrict__ mean_out, float* __restrict__ rstd_out) {
   __shared__ float lds[kWideThreads / 64];
-  const long long row = blockIdx.x;
   const int tid = threadIdx.x, groups = (width - 1) / 8 + 1;
-  const T* xr = x + row * row_stride;
-  T* yr = y + row * y_stride;
-  const bool here = valid == nullptr || valid[row] != 0;
-  float mean = 0.f, rstd = 0.f;
-  if (here) {
-    const float n = (float)width;
-    if (centered) {
-      float s = 0.f;
+  for (long long row = blockIdx.x; row < n_rows; row += gridDim.x) {
+    const T* xr = x + row * row_stride;
+    T* yr = y + row * y_stride;
+    const bool here = valid == nullptr || valid[row] != 0;
+    float mean = 0.f, rstd = 0.f;
+    if (here) {
+      const float n = (float)width;
+      if (centered) {
+        float s = 0.f;
+        for (int g = tid; g < groups; g += kWideThreads) {
+          float v[8];
+          load_group(xr, g, width, v);
+          s += sum8(v);
+        }
+        mean = row_sum<kWideThreads>(s, lds) / n;
+      }
+      float q = 0.f;
       for (int g = tid; g < groups; g += kWideThreads) {
         float v[8];
         load_group(xr, g, width, v);
-        s += sum8(v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float d = 8 * (long long)g + j < width ? v[j] - mean : 0.f;
+          v[j] = d * d;
+        }
+        q += sum8(v);
       }
-      mean = row_sum<kWideThreads>(s, lds) / n;
+      rstd = 1.f / sqrtf(row_sum<kWideThreads>(q, lds) / n + eps);
     }
-    float q = 0.f;
     for (int g = tid; g < groups; g += kWideThreads) {
-      float v[8];
-      load_group(xr, g, width, v);
+      float v[8] = {}, w[8] = {}, b[8] = {};
+      if (here) {
+        load_group(xr, g, width, v);
+        load_group(weight, g, width, 1.f, w);
+        load_group(bias, g, width, 0.f, b);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float d = 8 * (long long)g + j < width ? v[j] - mean : 0.f;
-        v[j] = d * d;
+        for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf((v[j] - mean) * rstd, w[j], b[j]);
       }
-      q += sum8(v);
+      store_group(yr, g, width, v);
     }
-    rstd = 1.f / sqrtf(row_sum<kWideThreads>(q, lds) / n + eps);
-  }
-  for (int g = tid; g < groups; g += kWideThreads) {
-    float v[8] = {}, w[8] = {}, b[8] = {};
-    if (here) {
-      load_group(xr, g, width, v);
-      load_group(weight, g, width, 1.f, w);
-      load_group(bias, g, width, 0.f, b);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __builtin_fmaf((v[j] - mean) * rstd, w[j], b[j]);
+    if (tid == 0) {
+      if (centered) mean_out[row] = mean;
+      rstd_out[row] = rstd;
     }
-    store_group(yr, g, width, v);
-  }
-  if (tid == 0) {
-    if (centered) mean_out[row] = mean;
-    rstd_out[row] = rstd;
   }
 }
 
@@ -456,34 +460,35 @@ __global__ __launch_bounds__(THREADS * TEAMS) void norm_grad_kernel(
 // Rows too wide for that, in two kernels: <u> and <u n> of every row ...
 template <typename T, typename D>
 __global__ __launch_bounds__(kWideThreads) void norm_grad_rows_kernel(const D* __restrict__ dy, long long dy_stride,
-                                                                      const T* __restrict__ x, long long row_stride, int width,
+                                                                      const T* __restrict__ x, long long row_stride, int n_rows, int width,
                                                                       const unsigned char* __restrict__ valid, Affine weight,
                                                                       const float* __restrict__ mean,
                                                                       const float* __restrict__ rstd, float* __restrict__ sums) {
   __shared__ float lds[2][kWideThreads / 64];
-  const long long row = blockIdx.x;
-  if (valid != nullptr && valid[row] == 0) return;
   const int tid = threadIdx.x, groups = (width - 1) / 8 + 1;
-  const float mu = mean != nullptr ? mean[row] : 0.f, rs = rstd[row];
-  float s1 = 0.f, s2 = 0.f;
-  for (int g = tid; g < groups; g += kWideThreads) {
-    float v[8], u[8], w[8] = {};
-    load_group(x + row * row_stride, g, width, v);
-    load_group(dy + row * dy_stride, g, width, u);
-    load_group(weight, g, width, 1.f, w);
+  for (long long row = blockIdx.x; row < n_rows; row += gridDim.x) {
+    if (valid != nullptr && valid[row] == 0) continue;             // uniform
+    const float mu = mean != nullptr ? mean[row] : 0.f, rs = rstd[row];
+    float s1 = 0.f, s2 = 0.f;
+    for (int g = tid; g < groups; g += kWideThreads) {
+      float v[8], u[8], w[8] = {};
+      load_group(x + row * row_stride, g, width, v);
+      load_group(dy + row * dy_stride, g, width, u);
+      load_group(weight, g, width, 1.f, w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      u[j] = 8 * (long long)g + j < width ? u[j] * w[j] : 0.f;
-      v[j] = u[j] * ((v[j] - mu) * rs);
+      for (int j = 0; j < 8; ++j) {
+        u[j] = 8 * (long long)g + j < width ? u[j] * w[j] : 0.f;
+        v[j] = u[j] * ((v[j] - mu) * rs);
+      }
+      s1 += sum8(u);
+      s2 += sum8(v);
     }
-    s1 += sum8(u);
-    s2 += sum8(v);
-  }
-  s1 = row_sum<kWideThreads>(s1, lds[0]);
-  s2 = row_sum<kWideThreads>(s2, lds[1]);
-  if (tid == 0) {
-    sums[2 * row] = mean != nullptr ? s1 / (float)width : 0.f;
-    sums[2 * row + 1] = s2 / (float)width;
+    s1 = row_sum<kWideThreads>(s1, lds[0]);
+    s2 = row_sum<kWideThreads>(s2, lds[1]);
+    if (tid == 0) {
+      sums[2 * row] = mean != nullptr ? s1 / (float)width : 0.f;
+      sums[2 * row + 1] = s2 / (float)width;
+    }
   }
 }
 // ... and a workgroup for 256 groups of columns and every gridDim.y-th row.
@@ -529,21 +534,25 @@ __global__ __launch_bounds__(64 * kSumWaves) void norm_grad_sum_kernel(const flo
   const float* from = first ? dweight_parts : dbias_parts;
   float* to = first ? dweight : dbias;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long d = min((long long)blockIdx.x * 64 + lane, (long long)width - 1);
-  float s = 0.f;
-  for (int k = wave; k < parts; k += 8 * kSumWaves) {
-    float v[8];
+  for (long long at = 64LL * blockIdx.x; at < width; at += 64LL * gridDim.x) {
+    const long long d = min(at + lane, (long long)width - 1);
+    float s = 0.f;
+    for (int k = wave; k < parts; k += 8 * kSumWaves) {
+      float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = from[(size_t)min(k + i * kSumWaves, parts - 1) * width + d];
+      for (int i = 0; i < 8; ++i) v[i] = from[(size_t)min(k + i * kSumWaves, parts - 1) * width + d];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += k + i * kSumWaves < parts ? v[i] : 0.f;
+      for (int i = 0; i < 8; ++i) s += k + i * kSumWaves < parts ? v[i] : 0.f;
+    }
+    if (at != 64LL * blockIdx.x) __syncthreads();            // the first wavefront has read the columns before
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int k = 1; k < kSumWaves; ++k) s += lds[k][lane];
+      if (at + lane < width) to[d] = s;
+    }
   }
-  lds[wave][lane] = s;
-  __syncthreads();
-  if (wave != 0) return;
-#pragma unroll
-  for (int k = 1; k < kSumWaves; ++k) s += lds[k][lane];
-  if ((long long)blockIdx.x * 64 + lane < width) to[d] = s;
 }
 
 // 1: every row is `most` vectors of n elements, however it is cut; 2: and has no element outside them; 0: neither.
@@ -562,7 +571,7 @@ int norm_typed(ais_ctx* ctx, const T* x, int n_rows, int width, long long row_st
   // are few.  41,643 rows of 4,096 bf16 elements, us with one, two, four rows each, and with as many workgroups as there is room for: 146,
   // 116, 118 to 122, 124.
   // (An even number of workgroups: rows of one begin alike.)
-  const unsigned grid = n_rows <= 8 * ctx->n_cus ? (unsigned)n_rows : (unsigned)(n_rows / 4 * 2 + 2);
+  const unsigned grid = (unsigned)(n_rows <= 8 * ctx->n_cus ? n_rows : std::min(n_rows / 4 * 2 + 2, kMostBlocks));
   auto held = [&](auto threads, auto most) {
     constexpr int kThreads = decltype(threads)::value, kMost = decltype(most)::value;
     auto kernel = whole_rows(y, y_stride, width, Vec<T>::N, kThreads * kMost) ? norm_kernel<T, kThreads, kMost, true>
@@ -594,8 +603,8 @@ int norm_typed(ais_ctx* ctx, const T* x, int n_rows, int width, long long row_st
     AIS_NORM_CASE(512, 8)
   }
 #undef AIS_NORM_CASE
-  norm_wide_kernel<T><<<dim3((unsigned)n_rows), dim3(kWideThreads), 0, ctx->stream>>>(x, row_stride, width, valid, weight, bias, eps,
-                                                                                   centered, y, y_stride, mean, rstd);
+  norm_wide_kernel<T><<<dim3((unsigned)std::min(n_rows, kMostWideBlocks)), dim3(kWideThreads), 0, ctx->stream>>>(
+      x, row_stride, n_rows, width, valid, weight, bias, eps, centered, y, y_stride, mean, rstd);
   return hip_fail(ctx, hipGetLastError());
 }
 
@@ -610,8 +619,8 @@ int norm_grad_typed(ais_ctx* ctx, const D* dy, long long dy_stride, const T* x, 
   if (dweight != nullptr) dw = at, at += all;
   if (dbias != nullptr) db = at, at += all;
   if (plan.teams == 0) {
-    norm_grad_rows_kernel<T, D><<<dim3((unsigned)n_rows), dim3(kWideThreads), 0, ctx->stream>>>(dy, dy_stride, x, row_stride, width,
-                                                                                             valid, weight, mean, rstd, at);
+    norm_grad_rows_kernel<T, D><<<dim3((unsigned)std::min(n_rows, kMostWideBlocks)), dim3(kWideThreads), 0, ctx->stream>>>(
+        dy, dy_stride, x, row_stride, n_rows, width, valid, weight, mean, rstd, at);
     norm_grad_columns_kernel<T, D><<<dim3((unsigned)((width - 1) / (8 * kColumnThreads) + 1), (unsigned)plan.parts), dim3(kColumnThreads),
                                      0, ctx->stream>>>(dy, dy_stride, x, row_stride, n_rows, width, valid, weight, mean, rstd, at, dx,
                                                        dx_stride, dw, db);
@@ -649,8 +658,8 @@ int norm_grad_typed(ais_ctx* ctx, const D* dy, long long dy_stride, const T* x, 
   }
   const unsigned sums = (dweight != nullptr) + (dbias != nullptr);
   if (sums > 0)
-    norm_grad_sum_kernel<<<dim3((unsigned)((width - 1) / 64 + 1), sums), dim3(64 * kSumWaves), 0, ctx->stream>>>(dw, db, plan.parts, width,
-                                                                                                           dweight, dbias);
+    norm_grad_sum_kernel<<<dim3((unsigned)std::min((width - 1) / 64 + 1, kMostBlocks), sums), dim3(64 * kSumWaves), 0, ctx->stream>>>(
+        dw, db, plan.parts, width, dweight, dbias);
   return hip_fail(ctx, hipGetLastError());
 }
 

@@ -76,3 +76,63 @@ def test_values_of_billions(ctx, dtype, moment):
         assert torch.equal(got[at:at + part], values(at, part))
     end = n // 32 * 32
     assert torch.equal(got[end:], values(end, n - end))
+
+
+def same_rows(got, want, at, live):
+    """Rows from `at` on of a call's outputs against those rows' own, zero where they are masked."""
+    for a, b in zip(got, want):
+        if a is None:
+            assert b is None
+            continue
+        part = a[at:at + len(b)]
+        assert torch.equal(part, b if live is None else torch.where(live.view(-1, *[1] * (b.dim() - 1)), b, torch.zeros_like(b)))
+
+
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("centered", [True, False])
+@pytest.mark.parametrize("width,n,gib", [(64, (1 << 21) + 70_001, 4), (2_568, (1 << 21) + 3_001, 40), (16_392, (1 << 16) + 301, 12)])
+def test_rows_of_large_batches(ctx, width, n, gib, centered, masked):
+    """A million workgroups have more than two rows each; of rows that are not held, 65,536 workgroups more than one."""
+    room(gib)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.empty(n, width, dtype=torch.bfloat16, device="cuda")
+    for part in x.split(1 << 18):
+        part.copy_(torch.randn(part.shape, generator=gen, device="cuda"))
+    weight, bias = (torch.randn(width, generator=gen, device="cuda") for _ in range(2))
+    # live, masked, live at the distance that a workgroup's rows have
+    valid = ((torch.arange(n, device="cuda") // (1 << 16)) % 16 % 3 != 1).to(torch.uint8) if masked else None
+    got = ctx.norm_rows(x, weight, bias, centered=centered, valid=valid)
+    for at in range(0, n, 4_000 if width == 64 else 300_000 if width < 10_000 else 2_000):
+        some = x[at:at + 2_000]
+        same_rows(got, ctx.norm_rows(some, weight, bias, centered=centered), at, None if valid is None else valid[at:at + 2_000] != 0)
+    at = n - 2_000
+    same_rows(got, ctx.norm_rows(x[at:], weight, bias, centered=centered), at, None if valid is None else valid[at:] != 0)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_gradient_of_many_wide_rows(ctx, masked):
+    room(12)
+    n, width = (1 << 16) + 301, 8_200
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    x, dy = (torch.empty(n, width, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (x, dy):
+        for part in t.split(1 << 15):
+            part.copy_(torch.randn(part.shape, generator=gen, device="cuda"))
+    weight, mean, rstd = torch.randn(width, generator=gen, device="cuda"), torch.randn(n, generator=gen, device="cuda"), torch.ones(n, device="cuda")
+    valid = (torch.arange(n, device="cuda") % 3 != 1).to(torch.uint8) if masked else None
+    dx = ctx.norm_rows_grad(dy, x, weight, mean, rstd, valid=valid)[0]
+    for at in (*range(0, n, 8_000), n - 2_000):
+        here = slice(at, at + 2_000)
+        want = ctx.norm_rows_grad(dy[here], x[here], weight, mean[here], rstd[here])[0]
+        same_rows([dx], [want], at, None if valid is None else valid[here] != 0)
+
+
+def test_sums_of_very_wide_rows(ctx):
+    """More than 2^26 columns, of one row: each one's sum is its one term."""
+    room(8)
+    width = (1 << 26) + 1_003
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    x, dy = (torch.randn(1, width, generator=gen, device="cuda") for _ in range(2))
+    rstd = torch.full((1,), 0.75, device="cuda")
+    _, dw, db = ctx.norm_rows_grad(dy, x, torch.ones(width, device="cuda"), None, rstd)
+    assert torch.equal(dw, dy[0] * (x[0] * 0.75)) and torch.equal(db, dy[0])
