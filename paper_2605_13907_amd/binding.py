@@ -903,7 +903,8 @@ class AisContext:
                    weight_decay: float = 0.01, grad_scale=None):
         """One AdamW step of state.params, in place, with a gradient (bf16 or fp32, contiguous) for each, or None for those that
         stay as they are.  lr: a number, or an fp32 tensor of one element on the GPU; grad_scale: such a tensor that the gradients
-        are multiplied by, or None.  See ais_adamw_step in include/ais.h."""
+        are multiplied by, or None.  Like torch's in-place operations it makes a backward pass raise that needs the stepped tensors as
+        they were (a replayed graph does not).  See ais_adamw_step in include/ais.h."""
         r, step = state._rule, state.step
         on_gpu = isinstance(step, torch.Tensor)
         lr_dev = lr if isinstance(lr, torch.Tensor) else None
@@ -951,6 +952,9 @@ class AisContext:
             if on_gpu:
                 step.sub_(1)                                     # nothing was launched
             raise AisError(rc, "ais_adamw_step")
+        # written in place: a backward pass through what they were has to notice
+        torch.autograd.graph.increment_version([t for p, c, g in zip(state.params, state.copies, grads) if g is not None
+                                                for t in (p, c) if t is not None])
         if not on_gpu:
             state.step = step + 1
 

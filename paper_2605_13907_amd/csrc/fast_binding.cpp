@@ -706,6 +706,12 @@ AIS_CALL(adamw_step) {
   const ais_adamw_tensor* there = static_cast<const ais_adamw_tensor*>(on_gpu->data_ptr());
   const int rc = c.run([&] { return lib.adamw_step(c.ctx, t.data(), there, (int)n, rule, scale, nullptr, lr); });
   if (rc != 0) return PyLong_FromLong(rc);
+  // written in place: a backward pass through what they were has to notice
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (t[i].grad == nullptr) continue;
+    for (PyObject* o : {PyTuple_GET_ITEM(params, i), PyTuple_GET_ITEM(copies, i)})
+      if (o != Py_None && !THPVariable_Unpack(o).is_inference()) THPVariable_Unpack(o).unsafeGetTensorImpl()->bump_version();
+  }
   Py_RETURN_TRUE;
 }
 
