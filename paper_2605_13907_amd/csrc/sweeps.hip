@@ -17,6 +17,7 @@
 #include "device_utils.h"
 #include "preference.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace ais {
@@ -585,6 +586,13 @@ int logprob_threads(const ais_ctx* ctx, long long n_rows, long long nvec, bool b
   return nvec >= 512 ? 128 : 64;
 }
 
+// Rows of a launch, which may have no more than 2^32 - 1 threads, up to 1,024 of them a row; others have their own.
+constexpr long long kMostRows = 1 << 21;
+template <typename P>
+P* behind(P* p, long long rows) {
+  return p != nullptr ? p + rows : nullptr;
+}
+
 }  // namespace
 
 int launch_token_logprob(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long n_rows, int vocab,
@@ -592,19 +600,20 @@ int launch_token_logprob(ais_ctx* ctx, const void* logits, ais_dtype dtype, long
                          float inv_temperature, float* logp_out, float* lse_out, double* logp_fine) {
   if (n_rows == 0) return AIS_OK;
   ScopedTimer timer(ctx, AIS_K_LOGPROB);
-  auto launch = [&](const auto* z) {
-    typedef std::remove_cv_t<std::remove_pointer_t<decltype(z)>> T;
+  auto launch = [&](const auto* logits) {
+    typedef std::remove_cv_t<std::remove_pointer_t<decltype(logits)>> T;
     const long long nvec = (long long)vocab / Vec<T>::N;
     auto run = [&](auto threads) {
       constexpr int kThreads = decltype(threads)::value;
-      const bool aligned = vec_ok(z, row_stride, sizeof(T));
+      const bool aligned = vec_ok(logits, row_stride, sizeof(T));
       auto kernel = logp_fine != nullptr ? aligned ? token_logprob_kernel<T, true, kThreads, kUnrollFwd, FineSum>
                                                    : token_logprob_kernel<T, false, kThreads, kUnrollFwd, FineSum>
                     : aligned            ? token_logprob_kernel<T, true, kThreads, kUnrollFwd>
                                          : token_logprob_kernel<T, false, kThreads, kUnrollFwd>;
-      kernel<<<dim3((unsigned)n_rows), dim3(kThreads), 0, ctx->stream>>>(
-          z, row_stride, vocab, token_ids, valid, inv_temperature, exact_exponents(inv_temperature), logp_out, lse_out,
-          ctx->status_dev, logp_fine);
+      for (long long r = 0; r < n_rows; r += kMostRows)
+        kernel<<<dim3((unsigned)std::min(n_rows - r, kMostRows)), dim3(kThreads), 0, ctx->stream>>>(
+            logits + r * row_stride, row_stride, vocab, token_ids + r, behind(valid, r), inv_temperature,
+            exact_exponents(inv_temperature), logp_out + r, lse_out + r, ctx->status_dev, behind(logp_fine, r));
     };
     const int threads = logprob_threads(ctx, n_rows, nvec, std::is_same_v<T, bf16_t>);
     if (threads == 1024) run(std::integral_constant<int, 1024>{});
@@ -622,23 +631,25 @@ int launch_dlogits(ais_ctx* ctx, const void* logits, ais_dtype dtype, long long 
                    long long row_stride, const int* token_ids, const float* g, const unsigned char* valid,
                    const float* lse, const float* logp, float inv_temperature, void* dlogits) {
   if (n_rows == 0) return AIS_OK;
-  dim3 grid((unsigned)n_rows), block(kSweepThreads);
   ScopedTimer timer(ctx, AIS_K_DLOGITS);
-  auto launch = [&](const auto* z) {
-    typedef std::remove_cv_t<std::remove_pointer_t<decltype(z)>> T;
-    T* dz = static_cast<T*>(dlogits);
+  auto some = [&](const auto* z, auto* dz, long long rows, const int* token_ids, const float* g, const unsigned char* valid,
+                  const float* lse, const float* logp) {
+    typedef std::remove_pointer_t<decltype(dz)> T;
     if (vec_ok(z, row_stride, sizeof(T)) && vec_ok(dz, row_stride, sizeof(T)))
-      launch_dlogits_burst<T, true>(ctx, z, n_rows, vocab, row_stride, token_ids, g, valid, lse, logp, inv_temperature,
-                                    dz);
+      launch_dlogits_burst<T, true>(ctx, z, rows, vocab, row_stride, token_ids, g, valid, lse, logp, inv_temperature, dz);
     else if (same_lines(z, dz) && vocab * sizeof(T) >= kElementwiseBytes)
-      launch_dlogits_burst<T, false>(ctx, z, n_rows, vocab, row_stride, token_ids, g, valid, lse, logp, inv_temperature,
-                                     dz);
+      launch_dlogits_burst<T, false>(ctx, z, rows, vocab, row_stride, token_ids, g, valid, lse, logp, inv_temperature, dz);
     else
-      dlogits_elementwise_kernel<T><<<grid, block, 0, ctx->stream>>>(z, row_stride, vocab, token_ids, g, valid, lse,
-                                                                     logp, inv_temperature, dz);
+      dlogits_elementwise_kernel<T><<<dim3((unsigned)rows), dim3(kSweepThreads), 0, ctx->stream>>>(
+          z, row_stride, vocab, token_ids, g, valid, lse, logp, inv_temperature, dz);
   };
-  if (dtype == AIS_BF16) launch(static_cast<const bf16_t*>(logits));
-  else launch(static_cast<const float*>(logits));
+  auto launch = [&](const auto* z, auto* dz) {
+    for (long long r = 0; r < n_rows; r += kMostRows)
+      some(z + r * row_stride, dz + r * row_stride, std::min(n_rows - r, kMostRows), token_ids + r, behind(g, r), behind(valid, r),
+           lse + r, logp + r);
+  };
+  if (dtype == AIS_BF16) launch(static_cast<const bf16_t*>(logits), static_cast<bf16_t*>(dlogits));
+  else launch(static_cast<const float*>(logits), static_cast<float*>(dlogits));
   return hip_fail(ctx, hipGetLastError());
 }
 

@@ -136,3 +136,35 @@ def test_sums_of_very_wide_rows(ctx):
     rstd = torch.full((1,), 0.75, device="cuda")
     _, dw, db = ctx.norm_rows_grad(dy, x, torch.ones(width, device="cuda"), None, rstd)
     assert torch.equal(dw, dy[0] * (x[0] * 0.75)) and torch.equal(db, dy[0])
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("masked", [False, True])
+def test_sweeps_over_many_rows(ctx, masked, offset):
+    """More rows than 2^32 threads of 256 to a row.  The hinge's slope is -1 behind a margin that no response reaches, so that a row's
+    gradient is its own."""
+    room(24)
+    n, vocab, part = (1 << 24) + 1_003, 64, 4_096
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    flat = torch.empty(n * vocab + offset, dtype=torch.bfloat16, device="cuda")
+    z = flat[offset:].view(n, vocab)
+    for some in z.split(1 << 22):
+        some.copy_(torch.randn(some.shape, generator=gen, device="cuda"))
+    ids = torch.randint(0, vocab, (n,), generator=gen, device="cuda", dtype=torch.int32)
+    valid = (torch.rand(n, generator=gen, device="cuda") < 0.7).to(torch.uint8) if masked else None
+    p = B.default_preference_params(kind=1, margin=1e6, beta=1e-3)
+    cu = lambda rows: torch.tensor([0, rows, rows], device="cuda")
+
+    def calls(at, rows):
+        rows = min(rows, n - at)
+        some = slice(at, at + rows)
+        mask = None if valid is None else valid[some]
+        logp, lse = ctx.token_logprob(z[some], ids[some], mask)
+        loss = ctx.preference_loss_grad(z[some], ids[some], mask, cu(rows), None, p, weight=torch.ones(1, device="cuda"))
+        return logp, lse, loss[2], loss[3], *ctx.token_logprob_softmax_grad(z[some], ids[some], mask)
+
+    got = calls(0, n)
+    for at in (0, (1 << 21) - 2_000, 3 << 21, (1 << 22) - 1, (1 << 24) - 2_000, n - part):
+        for a, b in zip(got, calls(at, part)):
+            assert torch.equal(a[at:at + part], b)
+    assert ctx.status() == 0
