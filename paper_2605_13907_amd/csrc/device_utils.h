@@ -180,35 +180,53 @@ __device__ __forceinline__ void accumulate(const float* x, float scale, MaxSum& 
 }
 
 
-// The same state for log-probabilities that are added up over whole responses, where what every row has too little adds up, too: a
-// thread that has met the row's largest logits drops what is small beside them, 3e-7 of the row's sum on the average of 151,936
-// logits.  Here a batch of terms is summed by itself and then added with what the addition drops.
+// The same state for log-probabilities that are added up over whole responses, where what every row has too little or too much adds up,
+// too.  A thread that has met the row's largest logits drops what is small beside them, 3e-7 of the row's sum on the average of 151,936
+// logits: here a batch of terms is summed by itself and then added with what the addition drops.  The scale is rounded to fp32, 1.3e-8 of
+// it without a temperature and up to 7e-8 with one, which is a log-prob's error times the mean distance of the others from the largest: the
+// terms are also summed times their exponents, which says what the sum would be with the scale as it is.  (Half of the probability 12
+// below the largest, 151,936 fp32 logits: 7e-8 and, at 1 / 0.9, 3e-7 off in every row without, 1e-8 with; 8,192 x 151,936 bf16
+// 1,047 us a loss with its gradient without, 1,056 with, 3,001 x 50,257 130.6 and 134.4.)
 struct FineSum {
   float m;
   double s;
+  float d;                                       // sum of the terms times their exponents less m
+  // The sum with every exponent times `exact`, which is 1 but for the scale's rounding: to first order.
+  __device__ __forceinline__ double sum(double exact) const { return s + (exact - 1.0) * 0.6931471805599453 * (double)d; }
 };
+// An exponent whose term is 0, in the place of those below it, infinite ones too.
+constexpr float kNoTerm = -200.f;
 template <int n>
 __device__ __forceinline__ void accumulate(const float* x, float scale, FineSum& st) {
   float cm = x[0];
 #pragma unroll
   for (int k = 1; k < n; ++k) cm = fmaxf(cm, x[k]);
   const float mn = fmaxf(st.m, cm * scale);
-  float acc0 = 0.f, acc1 = 0.f;
+  float acc0 = 0.f, acc1 = 0.f, dev0 = 0.f, dev1 = 0.f;
 #pragma unroll
   for (int k = 0; k < n; k += 2) {
-    acc0 += exp2_fast(__builtin_fmaf(x[k], scale, -mn));
-    if (k + 1 < n) acc1 += exp2_fast(__builtin_fmaf(x[k + 1], scale, -mn));
+    const float e0 = __builtin_fmaf(x[k], scale, -mn), p0 = exp2_fast(e0);
+    acc0 += p0;
+    dev0 = __builtin_fmaf(p0, fmaxf(e0, kNoTerm), dev0);
+    if (k + 1 < n) {
+      const float e1 = __builtin_fmaf(x[k + 1], scale, -mn), p1 = exp2_fast(e1);
+      acc1 += p1;
+      dev1 = __builtin_fmaf(p1, fmaxf(e1, kNoTerm), dev1);
+    }
   }
-  st.s = st.s * (double)exp2_fast(st.m - mn) + (double)(acc0 + acc1);
+  const float factor = exp2_fast(st.m - mn);
+  st.d = __builtin_fmaf(factor, __builtin_fmaf(fmaxf(st.m - mn, kNoTerm), (float)st.s, st.d), dev0 + dev1);
+  st.s = st.s * (double)factor + (double)(acc0 + acc1);
   st.m = mn;
 }
 __device__ __forceinline__ FineSum merge(FineSum a, FineSum b) {
-  const float m = fmaxf(a.m, b.m);
-  return {m, a.s * (double)exp2_fast(a.m - m) + b.s * (double)exp2_fast(b.m - m)};
+  const float m = fmaxf(a.m, b.m), fa = exp2_fast(a.m - m), fb = exp2_fast(b.m - m);
+  const float da = __builtin_fmaf(fmaxf(a.m - m, kNoTerm), (float)a.s, a.d), db = __builtin_fmaf(fmaxf(b.m - m, kNoTerm), (float)b.s, b.d);
+  return {m, a.s * (double)fa + b.s * (double)fb, fa * da + fb * db};
 }
 __device__ __forceinline__ FineSum wave_merge(FineSum a) {
 #pragma unroll
-  for (int off = 1; off < 64; off <<= 1) a = merge(a, FineSum{__shfl_xor(a.m, off), __shfl_xor(a.s, off)});
+  for (int off = 1; off < 64; off <<= 1) a = merge(a, FineSum{__shfl_xor(a.m, off), __shfl_xor(a.s, off), __shfl_xor(a.d, off)});
   return a;
 }
 

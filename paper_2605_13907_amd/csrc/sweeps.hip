@@ -127,8 +127,8 @@ __global__ __launch_bounds__(THREADS) void token_logprob_kernel(
 #pragma unroll
     for (int w = 1; w < THREADS / 64; ++w) st = merge(st, lds[w]);
     double l1p = 0.0, lse;
+    st.s = st.sum(exact);
     if (y_ok) {
-      // the terms' exponents are those of a `scale` that is off by `exact`: what that does to the sum is below 2e-8 of a log-prob
       const double e = ((double)st.m - (double)zy * (double)scale) * exact;
       l1p = st.s > 0.0 ? e > 64.0 ? e * 0.6931471805599453 + log(st.s) : log1p(st.s * exp2(e)) : st.s;
       lse = (double)zy * (double)inv_temperature + l1p;
