@@ -37,8 +37,8 @@ struct Batch {
 static_assert(sizeof(Batch) + 128 <= 4096, "");
 // Workgroups of a launch, which may have no more than 2^32 - 1 threads: 2^31 here.  A tensor has 2^22 at most.
 constexpr long long kMostBlocks = (1LL << 31) / kThreads;
-// Of the launch that gives out moments' values, whose workgroups go on behind the others where there are more elements (2^31).
-constexpr long long kMostValueBlocks = 1 << 20;
+// Elements whose values a launch gives out.  (Workgroups that go on behind the others take 700 instead of 670 us for 622 million elements.)
+constexpr long long kMostValues = 1LL << 31;
 
 struct Rule {
   double b1, b2;
@@ -294,18 +294,18 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Batch batch, const ais_
 template <typename F, typename T>
 __device__ __forceinline__ void values_of(const unsigned char* __restrict__ codes, const unsigned char* __restrict__ scales,
                                           long long n, T* __restrict__ out) {
-  for (long long at = 8 * ((long long)blockIdx.x * kThreads + threadIdx.x); at < n; at += 8LL * gridDim.x * kThreads) {
-    const int here = (int)min(n - at, 8LL);
-    const double factor = decode_factor<F>(scales[at >> 5]);
-    uint32_t q[2];
+  const long long at = 8 * ((long long)blockIdx.x * kThreads + threadIdx.x);
+  if (at >= n) return;
+  const int here = (int)min(n - at, 8LL);
+  const double factor = decode_factor<F>(scales[at >> 5]);
+  uint32_t q[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) q[k] = load_codes(codes + at + 4 * k, here - 4 * k, here >= 4 * k + 4);
-    float x[8];
+  for (int k = 0; k < 2; ++k) q[k] = load_codes(codes + at + 4 * k, here - 4 * k, here >= 4 * k + 4);
+  float x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = (float)((double)code_bits<F>(q[j >> 2] >> (8 * (j & 3)) & 255u) * factor);
-    if (here == 8) Eight<T>::store(out + at, x);
-    else store_some(out + at, here, x);
-  }
+  for (int j = 0; j < 8; ++j) x[j] = (float)((double)code_bits<F>(q[j >> 2] >> (8 * (j & 3)) & 255u) * factor);
+  if (here == 8) Eight<T>::store(out + at, x);
+  else store_some(out + at, here, x);
 }
 template <typename T>
 __global__ __launch_bounds__(kThreads) void adamw_values_kernel(const unsigned char* m, const unsigned char* m_scale,
@@ -358,13 +358,16 @@ int launch_adamw_values(ais_ctx* ctx, const unsigned char* m, const unsigned cha
   const unsigned moments = (m_out != nullptr) + (v_out != nullptr);
   if (n == 0 || moments == 0) return AIS_OK;
   ScopedTimer timer(ctx, AIS_K_ADAMW);
-  const dim3 grid((unsigned)std::min((n + 8 * kThreads - 1) / (8 * kThreads), kMostValueBlocks), moments);
-  if (dtype == AIS_BF16)
-    adamw_values_kernel<<<grid, dim3(kThreads), 0, ctx->stream>>>(m, m_scale, v, v_scale, n, static_cast<bf16_t*>(m_out),
-                                                                  static_cast<bf16_t*>(v_out));
-  else
-    adamw_values_kernel<<<grid, dim3(kThreads), 0, ctx->stream>>>(m, m_scale, v, v_scale, n, static_cast<float*>(m_out),
-                                                                  static_cast<float*>(v_out));
+  auto run = [&](auto* m_to, auto* v_to) {
+    for (long long at = 0; at < n; at += kMostValues) {
+      const long long here = std::min(n - at, kMostValues);
+      auto from = [&](auto* p, long long behind) { return p != nullptr ? p + behind : p; };
+      adamw_values_kernel<<<dim3((unsigned)((here + 8 * kThreads - 1) / (8 * kThreads)), moments), dim3(kThreads), 0, ctx->stream>>>(
+          from(m, at), from(m_scale, at / 32), from(v, at), from(v_scale, at / 32), here, from(m_to, at), from(v_to, at));
+    }
+  };
+  if (dtype == AIS_BF16) run(static_cast<bf16_t*>(m_out), static_cast<bf16_t*>(v_out));
+  else run(static_cast<float*>(m_out), static_cast<float*>(v_out));
   return hip_fail(ctx, hipGetLastError());
 }
 
