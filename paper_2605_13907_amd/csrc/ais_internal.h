@@ -264,8 +264,9 @@ bool try_preference_dlogits_small(ais_ctx* ctx, const Preference& in, const void
 struct NormGradPlan {
   int threads, teams, vectors, parts;
 };
-NormGradPlan norm_grad_plan(long long n_rows, long long width, int bytes, int n_cus);      // bytes: of an element of x and one of dy
-size_t norm_grad_bytes(long long n_rows, long long width, int bytes, int sums, int n_cus);
+// bytes: of an element of x and one of dy; dx: the rows' gradient, whose place the choice goes by.
+NormGradPlan norm_grad_plan(long long n_rows, long long width, int bytes, const void* dx, long long dx_stride, int n_cus);
+size_t norm_grad_bytes(long long n_rows, long long width, int bytes, const void* dx, long long dx_stride, int sums, int n_cus);
 int launch_norm_rows(ais_ctx* ctx, const void* x, ais_dtype dtype, long long n_rows, int width, long long row_stride,
                      const unsigned char* valid, const void* weight, const void* bias, ais_dtype param_dtype, float eps,
                      int centered, void* y, long long y_stride, float* mean, float* rstd);

@@ -867,7 +867,8 @@ int ais_norm_rows_grad(ais_ctx* ctx, const void* dy, ais_dtype dy_dtype, long lo
             out, (size_t)width);
     return hip_fail(ctx, hipGetLastError());
   }
-  rc = ensure_workspace(ctx, norm_grad_bytes(n_rows, width, (dtype == AIS_BF16 ? 2 : 4) + (dy_dtype == AIS_BF16 ? 2 : 4), (dweight_out != nullptr) + (dbias_out != nullptr), ctx->n_cus));
+  const int bytes = (dtype == AIS_BF16 ? 2 : 4) + (dy_dtype == AIS_BF16 ? 2 : 4), sums = (dweight_out != nullptr) + (dbias_out != nullptr);
+  rc = ensure_workspace(ctx, norm_grad_bytes(n_rows, width, bytes, dx, dx_stride, sums, ctx->n_cus));
   if (rc != AIS_OK) return rc;
   ctx->plan.valid = false;             // the partial sums overwrite whatever tiling the workspace held
   return launch_norm_rows_grad(ctx, dy, dy_dtype, dy_stride, x, dtype, n_rows, (int)width, row_stride, valid, weight, param_dtype,

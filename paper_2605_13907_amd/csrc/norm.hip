@@ -123,7 +123,8 @@ __device__ __forceinline__ float sum_of(const float* x) {
 
 // How rows are cut into vectors of N elements, which begin at whole words: of bf16 rows that begin in the middle of one the first element
 // is left out of them, like those after the last vector.  (The gradient of 28,066 bf16 rows of 2,237 elements, one after the other: 135 us,
-// 164 with vectors from their first element on; 20,000 of 4,097: 114, 137.)  Any cut is sound for any row, whatever it costs; a workgroup has one for all of its rows.
+// 164 with vectors from their first element on; 20,000 of 4,097: 114, 137.)  Any cut is sound for any row, whatever it costs; a workgroup
+// has one for all of its rows.
 struct Cut {
   int head, vectors, left;                       // left: elements outside the vectors, those of the head first
   template <typename T, int N>
@@ -555,10 +556,13 @@ __global__ __launch_bounds__(64 * kSumWaves) void norm_grad_sum_kernel(const flo
   }
 }
 
+// Whether bf16 rows all begin at whole words.
+bool at_words(const void* rows, long long stride) { return ((reinterpret_cast<uintptr_t>(rows) / 2 | (uintptr_t)stride) & 1) == 0; }
+
 // 1: every row is `most` vectors of n elements, however it is cut; 2: and has no element outside them; 0: neither.
 template <typename T>
 int whole_rows(const T* rows, long long stride, int width, int n, int most) {
-  const bool odd = sizeof(T) == 2 && ((reinterpret_cast<uintptr_t>(rows) / 2 | (uintptr_t)stride) & 1) != 0;
+  const bool odd = sizeof(T) == 2 && !at_words(rows, stride);
   if (width / n != most || (odd && (width - 1) / n != most)) return 0;
   return !odd && width % n == 0 ? 2 : 1;
 }
@@ -612,7 +616,7 @@ template <typename T, typename D>
 int norm_grad_typed(ais_ctx* ctx, const D* dy, long long dy_stride, const T* x, long long row_stride, int n_rows, int width,
                     const unsigned char* valid, Affine weight, const float* mean, const float* rstd, T* dx, long long dx_stride,
                     float* dweight, float* dbias) {
-  const NormGradPlan plan = norm_grad_plan(n_rows, width, sizeof(T) + sizeof(D), ctx->n_cus);
+  const NormGradPlan plan = norm_grad_plan(n_rows, width, sizeof(T) + sizeof(D), dx, dx_stride, ctx->n_cus);
   const size_t all = (size_t)plan.parts * width;
   float* at = static_cast<float*>(ctx->ws);
   float *dw = nullptr, *db = nullptr;
@@ -674,9 +678,10 @@ int norm_grad_typed(ais_ctx* ctx, const D* dy, long long dy_stride, const T* x, 
 //   bf16: 28,066 of 2,240 80, with 256 threads and two vectors 103; 30,000 of 3,500 139, two workgroups 156; 25,000 of 5,000 138, with 256
 //     threads and four vectors 236; 72,000 of 1,600 132, a wavefront with four vectors 176; 1,000 of 4,096 15.1, two workgroups 19.4.
 //   Four vectors of eight a thread leave registers for two workgroups to a unit only where no element lies outside them: there (60,000 of
-//     2,048 128, 14,000 of 8,192 126) they are ahead of 128 threads with two (138) and 1,024 with one (136).
-NormGradPlan norm_grad_plan(long long n_rows, long long width, int bytes, int n_cus) {
-  const bool bf16 = bytes == 4;
+//     2,048 128, 14,000 of 8,192 126) they are ahead of 128 threads with two (138) and 1,024 with one (136), elsewhere (the same rows,
+//     beginning in the middle of a word) behind them: 203 and 200, 147 and 157 with those.
+NormGradPlan norm_grad_plan(long long n_rows, long long width, int bytes, const void* dx, long long dx_stride, int n_cus) {
+  const bool bf16 = bytes == 4, words = at_words(dx, dx_stride);
   const long long vectors = width / (bf16 ? 8 : 4);
   NormGradPlan p{0, 0, 0, 0};
   auto held = [&](int threads, int teams, int most, int of_a_cu) {
@@ -689,12 +694,12 @@ NormGradPlan norm_grad_plan(long long n_rows, long long width, int bytes, int n_
   held(64, 4, 2, 2);
   if (bf16) {
     held(64, 4, 3, 2);
-    if (width == 8 * 256) held(64, 4, 4, 1);
+    if (words && width == 8 * 256) held(64, 4, 4, 1);
     held(128, 1, 2, 6);
     held(128, 1, 3, 4);
     held(256, 1, 2, 3);
     held(256, 1, 3, 2);
-    if (width == 8 * 1024) held(256, 1, 4, 2);
+    if (words && width == 8 * 1024) held(256, 1, 4, 2);
     held(1024, 1, 1, 1);
   } else {
     held(64, 4, 4, 2);
@@ -711,8 +716,8 @@ NormGradPlan norm_grad_plan(long long n_rows, long long width, int bytes, int n_
   return p;
 }
 
-size_t norm_grad_bytes(long long n_rows, long long width, int bytes, int sums, int n_cus) {
-  const NormGradPlan p = norm_grad_plan(n_rows, width, bytes, n_cus);
+size_t norm_grad_bytes(long long n_rows, long long width, int bytes, const void* dx, long long dx_stride, int sums, int n_cus) {
+  const NormGradPlan p = norm_grad_plan(n_rows, width, bytes, dx, dx_stride, n_cus);
   return 4 * (size_t)sums * (size_t)p.parts * (size_t)width + (p.teams == 0 ? 8 * (size_t)n_rows : 0);
 }
 
