@@ -478,7 +478,8 @@ void ais_preference_params_default(ais_preference_params* p);
  *   g_out       [n_rows] fp32: c_t times inv_temperature, 0 where valid == 0: the `coeff` of ais_lm_head_grad, and the
  *               scale of what ais_token_logprob_softmax_grad writes
  * ais_preference_loss_grad forms the log-probs itself, from logits and token_ids as ais_token_logprob takes them.  A response's
- * log-ratios nearly cancel, so a row's sum is kept in 64 bits there, and its log-prob until it has been added up; it writes
+ * log-ratios nearly cancel, so a row's sum is kept in 64 bits there, and its log-prob until it has been added up (with ais_token_logprob's,
+ * summed and rounded in 32 bits, rewards come out 2e-5 off); it writes
  *   logp_out    [n_rows] fp32: the log-probs, 0 where valid == 0
  *   dlogits     [n_rows, row_stride] of `dtype`, or NULL (loss alone): c_t inv_temperature (softmax(inv_temperature z_t) - 1[v =
  *               y_t]); 0 in rows with c_t = 0, which are not read again.  May be `logits` itself.
